@@ -65,7 +65,8 @@ enum {
   LM_DEVERR_NOT_FOUND = 2,  /* a source id that the destination id list lacks */
   LM_DEVERR_CAPACITY = 4,   /* a device-side count above its buffer's capacity */
   LM_DEVERR_SPIN = 8,       /* a bounded inter-workgroup wait gave up */
-  LM_DEVERR_NONFINITE = 16  /* a compressed (binary16) value is infinite or NaN */
+  LM_DEVERR_NONFINITE = 16  /* a compressed (binary16) value is infinite or NaN, or a second
+                               moment that AdamW would write */
 };
 
 /* Index dtypes: word indices are int32 or int64; every position, count and
@@ -408,6 +409,161 @@ int lm_sparse_apply_f16(float* table, int64_t V, int64_t D, int64_t ld_table,
                         float inv_scale, int32_t opt, float lr, float beta1, float beta2,
                         float eps, float weight_decay, int64_t step, float* m, float* v,
                         int32_t* dev_err, void* stream);
+
+/* ------------------------------------------------------------------------
+ * AdamW over many tensors — the step-7 update for the parameters that are
+ * not named by word: one launch steps every tensor of a list, with the
+ * arithmetic of lm_sparse_apply's LM_OPT_ADAM on every value:
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *     p -= lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
+ *              + weight_decay p),
+ * p fp32, g = grad * grad_scale. With moments in fp32 the results are those
+ * of lm_sparse_apply with every row named, bit for bit. A value whose new v
+ * is not finite (its gradient is not, or its square overflows) keeps p, m
+ * and v and sets LM_DEVERR_NONFINITE.
+ *
+ * Moments in 8 bits. LM_MOMENT_BLOCK consecutive values of one tensor share
+ * a scale 2^k, k the smallest integer >= -127 with max|x| <= 448 * 2^k, kept
+ * as the byte k + 127 (0 where all are zero); a value is its OCP e4m3 code
+ * times the scale. m is kept as it is, v as its square root. The step
+ * computes in fp32 on the decoded values and rounds stochastically: with s
+ * the step of the e4m3 numbers at |x| 2^-k, the code is
+ *     floor(|x| 2^-k / s + R / 2^20) * s,  with x's sign,
+ * R the high (m) or low (v) 20 bits of the value's random word; a nonzero
+ * root of v never gets the code zero. The words are a function of `seed` and
+ * the value's number: the values of a list count through, each tensor from
+ * the next multiple of LM_MOMENT_BLOCK (of a table: id * D + column). Give
+ * every step and every list its own seed; the same seed repeats a call bit
+ * for bit. State that starts from zero starts from zero bytes.
+ *
+ * The plan is a table that names the list's memory. lm_adamw_plan writes it
+ * into host memory, the caller copies it to the device (256-byte aligned, as
+ * device allocations are) and may use it for every step while the list's
+ * memory stays where it is.
+ *
+ * p, g, m, v host arrays of `tensors` device pointers, at the alignment of
+ *            their elements: fp32; dtype `gtype`; fp32 or, with `states` 8,
+ *            bytes (both).
+ * m_scale, v_scale  the same, ceil(size / LM_MOMENT_BLOCK) bytes per tensor,
+ *            with `states` 8; NULL with 32.
+ * copies     the same or NULL: bf16 copies of the parameters, written with
+ *            every step (rounded to nearest even).
+ * sizes      host array: each tensor's values (0 allowed; its pointers are
+ *            not looked at). Tensors are contiguous.
+ * decay      host array or NULL: nonzero where weight_decay applies (NULL:
+ *            to all).
+ * states     32 or 8.
+ * plan       host, plan_bytes >= lm_adamw_plan_bytes(sizes, tensors), 8-byte
+ *            aligned, written.
+ * chunks     host, written: what lm_adamw takes.
+ * Pieces of memory that a step writes and that meet each other or a
+ * gradient return LM_E_INVAL. lm_adamw_plan_bytes returns 0 for sizes that
+ * the library does not handle (negative, or more than LM_ADAMW_MAX_VALUES
+ * together).
+ *
+ * lm_adamw: plan is the device copy; tensors, chunks, gtype, states and
+ * copies (0 or 1) are those it was made with (another plan's set
+ * LM_DEVERR_CAPACITY and nothing is stepped).
+ * grad_scale device fp32 or NULL (1): multiplies every gradient (gradient
+ *            clipping, loss scales).
+ * dev_err    device int32 or NULL.
+ * step       >= 1; beta1, beta2 in [0, 1).
+ * ------------------------------------------------------------------------ */
+#define LM_MOMENT_BLOCK 32
+#define LM_ADAMW_MAX_VALUES ((int64_t)1 << 42)
+size_t lm_adamw_plan_bytes(const int64_t* sizes, int64_t tensors);
+int lm_adamw_plan(void* const* p, const void* const* g, void* const* m, void* const* v,
+                  void* const* m_scale, void* const* v_scale, void* const* copies,
+                  const int64_t* sizes, const int32_t* decay, int64_t tensors, int32_t gtype,
+                  int32_t states, void* plan, size_t plan_bytes, int64_t* chunks);
+int lm_adamw(const void* plan, int64_t tensors, int64_t chunks, int32_t gtype, int32_t states,
+             int32_t copies, float lr, float beta1, float beta2, float eps, float weight_decay,
+             int64_t step, const float* grad_scale, uint64_t seed, int32_t* dev_err,
+             void* stream);
+
+/* lm_sparse_apply_q8: lm_sparse_apply with LM_OPT_ADAM and moments in 8 bits
+ * as above, the blocks along each row.
+ * m, v       device, V x D bytes (codes), row stride ld_codes >= D.
+ * m_scale, v_scale  device, V x ceil(D / LM_MOMENT_BLOCK) bytes, row stride
+ *            ld_scale.
+ * The other arguments and their errors are those of lm_sparse_apply; rows
+ * that are not named are untouched in all five arrays. A value whose new v
+ * is not finite keeps its parameter and moments and sets
+ * LM_DEVERR_NONFINITE (its moments are rounded again where its block's scale
+ * changes). */
+int lm_sparse_apply_q8(float* table, int64_t V, int64_t D, int64_t ld_table, const void* rows,
+                       int32_t idtype, const int64_t* n_rows, int64_t rows_cap, const float* vals,
+                       int64_t ld_vals, float lr, float beta1, float beta2, float eps,
+                       float weight_decay, int64_t step, uint8_t* m, uint8_t* v,
+                       int64_t ld_codes, uint8_t* m_scale, uint8_t* v_scale, int64_t ld_scale,
+                       uint64_t seed, int32_t* dev_err, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Relative position bias — a learned table that attention looks up by the
+ * distance of a key from its query, for every pair and head:
+ *     out[b, h, i, j] = add[b, h, i, j] + table[bucket(j - (q_start + i)), h]
+ * and its gradient, a Seg-Sum (Sec. III-A step 2) whose ids need no sort:
+ *     dtable[n, h] = sum of dout[b, h, i, j] over b, i, j in bucket n.
+ *
+ * Buckets are segments of the distance axis: segment s holds the distances
+ * from starts[s] up to starts[s + 1] - 1 (the last one: all above), and
+ * ids[s] is its table row, or -1: those places are masked (out is -infinity
+ * whatever add holds, which is not read; dout there is left out of every
+ * sum). starts ascend from INT32_MIN.
+ *
+ * lm_rel_buckets writes the segments of logarithmic buckets. A side of n
+ * buckets gives the distances d below n / 2 one bucket each and puts the
+ * others in bucket n / 2 + floor(N log(d / (n / 2)) / log(max_distance / (n /
+ * 2))), N = n - n / 2, at most n - 1 (borders are found in whole numbers: a
+ * distance on one is in the upper bucket).
+ *   LM_REL_BOTH    half of the buckets for keys up to the query, half (the
+ *                  upper rows) for keys after it; num_buckets even.
+ *   LM_REL_PAST    all buckets for keys up to the query; keys after it are
+ *                  in bucket 0.
+ *   LM_REL_CAUSAL  the same, keys after the query masked.
+ * num_buckets    4 or more (LM_REL_BOTH), 2 or more, at most
+ *                LM_REL_MAX_BUCKETS; max_distance above n / 2, below 2^24.
+ * starts, ids    host, LM_REL_MAX_SEGMENTS entries; n_seg: host, how many
+ *                were written.
+ *
+ * lm_rel_bias and lm_rel_bias_grad take starts and ids from host memory (read
+ * during the call).
+ * table      device, num_buckets x H fp32, row stride ld_table.
+ * add        device, B x H x Lq x Lk of dtype `dtype` (LM_F32 / LM_BF16) with
+ *            unit stride along Lk and add_strides (host: b, h, i) in elements
+ *            (0 repeats a dimension), or NULL: the bias alone.
+ * out        device, the same shape and dtype, out_strides; sums in fp32,
+ *            rounded once. It may be add itself, with the same strides;
+ *            otherwise the two must not meet.
+ * q_start    the position of query 0 where key 0 is at 0 (one new token
+ *            against a cache of Lk: Lk - 1); within +-LM_REL_MAX_START.
+ *
+ * lm_rel_bias_grad: dout like add. dtable fp32, row stride ld_table, every
+ * row written (accumulate 0) or added to (1); sums in fp32 in a fixed order,
+ * which depends on the sizes only: repeated calls give the same bits.
+ * ws         device workspace of lm_rel_bias_grad_workspace_bytes(...), no
+ *            initial contents required.
+ * Lengths, heads and batch up to LM_REL_MAX_LENGTH, 2^40 elements together;
+ * a length of 0 is valid (the gradient is then zero).
+ * ------------------------------------------------------------------------ */
+enum { LM_REL_BOTH = 0, LM_REL_PAST = 1, LM_REL_CAUSAL = 2 };
+#define LM_REL_MAX_BUCKETS 256
+#define LM_REL_MAX_SEGMENTS 257
+#define LM_REL_MAX_LENGTH ((int64_t)1 << 24)
+#define LM_REL_MAX_START ((int64_t)1 << 30)
+int lm_rel_buckets(int32_t num_buckets, int32_t max_distance, int32_t mode, int32_t* starts,
+                   int32_t* ids, int32_t* n_seg);
+int lm_rel_bias(const float* table, int64_t ld_table, int32_t num_buckets, const int32_t* starts,
+                const int32_t* ids, int32_t n_seg, int64_t B, int64_t H, int64_t Lq, int64_t Lk,
+                int64_t q_start, const void* add, const int64_t* add_strides, void* out,
+                const int64_t* out_strides, int32_t dtype, void* stream);
+size_t lm_rel_bias_grad_workspace_bytes(int64_t B, int64_t H, int64_t Lq, int64_t Lk,
+                                        int32_t dtype, int32_t n_seg);
+int lm_rel_bias_grad(const void* dout, int32_t dtype, int64_t B, int64_t H, int64_t Lq, int64_t Lk,
+                     const int64_t* dout_strides, int64_t q_start, const int32_t* starts,
+                     const int32_t* ids, int32_t n_seg, int32_t num_buckets, float* dtable,
+                     int64_t ld_table, int32_t accumulate, void* ws, size_t ws_bytes,
+                     void* stream);
 
 /* ------------------------------------------------------------------------
  * Candidate sampler — Sec. II-A (sampled softmax) and Sec. III-B

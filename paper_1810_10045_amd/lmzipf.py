@@ -10,6 +10,11 @@ Entry points have the C names without the ``lm_`` prefix: ``unique``,
 payload forms ``fill_values_f16`` and ``sparse_apply_f16``, and
 ``sample_ids``; ``unique_workspace_bytes`` is the workspace query that
 ``unique`` makes itself, for callers that size a workspace up front.
+
+Beside the embedding's path: ``adamw_plan`` and ``adamw`` (the AdamW step over
+many tensors, moments in fp32 or 8 bits), ``sparse_apply_q8`` (the lazy step on
+table rows with 8-bit moments), ``rel_buckets``, ``rel_bias`` and
+``rel_bias_grad`` (a learned relative position bias and its gradient).
 """
 from __future__ import annotations
 
@@ -32,12 +37,17 @@ I32, I64 = 0, 1
 F32, BF16 = 0, 1
 FILL_EXPAND, FILL_SCATTER, FILL_SCATTER_ADD = 0, 1, 2
 OPT_SGD, OPT_ADAM = 0, 1
+REL_BOTH, REL_PAST, REL_CAUSAL = 0, 1, 2
+MOMENT_BLOCK, REL_MAX_SEGMENTS = 32, 257
 MAX_K = 1 << 30
 
 EXPORTS = ("lm_status_string", "lm_abi_version", "lm_workspace_clear",
            "lm_unique_workspace_bytes", "lm_unique", "lm_segsum_workspace_bytes",
            "lm_segsum", "lm_map_ids", "lm_fill_values", "lm_sparse_apply",
-           "lm_fill_values_f16", "lm_sparse_apply_f16", "lm_sample_ids")
+           "lm_fill_values_f16", "lm_sparse_apply_f16", "lm_sample_ids",
+           "lm_adamw_plan_bytes", "lm_adamw_plan", "lm_adamw", "lm_sparse_apply_q8",
+           "lm_rel_buckets", "lm_rel_bias", "lm_rel_bias_grad_workspace_bytes",
+           "lm_rel_bias_grad")
 
 
 class LmError(RuntimeError):
@@ -82,12 +92,28 @@ def _load():
     L.lm_sparse_apply_f16.argtypes = [P, I64_, I64_, I64_, P, I32_, P, I64_, P, I64_, F, I32_,
                                       F, F, F, F, F, I64_, P, P, P, P]
     L.lm_sample_ids.argtypes = [P, I64_, I64_, P, I32_, P]
+    U64 = ctypes.c_uint64
+    L.lm_adamw_plan_bytes.argtypes = [P, I64_]
+    L.lm_adamw_plan_bytes.restype = SZ
+    L.lm_adamw_plan.argtypes = [P, P, P, P, P, P, P, P, P, I64_, I32_, I32_, P, SZ, P]
+    L.lm_adamw.argtypes = [P, I64_, I64_, I32_, I32_, I32_, F, F, F, F, F, I64_, P, U64, P, P]
+    L.lm_sparse_apply_q8.argtypes = [P, I64_, I64_, I64_, P, I32_, P, I64_, P, I64_, F, F, F, F, F,
+                                     I64_, P, P, I64_, P, P, I64_, U64, P, P]
+    L.lm_rel_buckets.argtypes = [I32_, I32_, I32_, P, P, P]
+    L.lm_rel_bias.argtypes = [P, I64_, I32_, P, P, I32_, I64_, I64_, I64_, I64_, I64_, P, P, P, P,
+                              I32_, P]
+    L.lm_rel_bias_grad_workspace_bytes.argtypes = [I64_, I64_, I64_, I64_, I32_, I32_]
+    L.lm_rel_bias_grad_workspace_bytes.restype = SZ
+    L.lm_rel_bias_grad.argtypes = [P, I32_, I64_, I64_, I64_, I64_, P, I64_, P, P, I32_, I32_, P,
+                                   I64_, I32_, P, SZ, P]
     L.lm_segsum_set_two_launches.argtypes = [I32_]
     L.lm_test_force_wait_failure.argtypes = [I32_, ctypes.c_uint32]
     for f in ("lm_abi_version", "lm_workspace_clear", "lm_unique", "lm_unique_noalloc",
               "lm_segsum", "lm_segsum_rows", "lm_segsum_sgd", "lm_segsum_adam", "lm_map_ids",
               "lm_fill_values", "lm_sparse_apply", "lm_fill_values_f16", "lm_sparse_apply_f16",
-              "lm_sample_ids", "lm_segsum_set_two_launches", "lm_test_force_wait_failure"):
+              "lm_sample_ids", "lm_segsum_set_two_launches", "lm_test_force_wait_failure",
+              "lm_adamw_plan", "lm_adamw", "lm_sparse_apply_q8", "lm_rel_buckets", "lm_rel_bias",
+              "lm_rel_bias_grad"):
         getattr(L, f).restype = ctypes.c_int
     return L
 
@@ -186,7 +212,7 @@ def check(dev_err: torch.Tensor):
                                 (DEVERR_NOT_FOUND, "id not found"),
                                 (DEVERR_CAPACITY, "capacity exceeded"),
                                 (DEVERR_SPIN, "inter-workgroup wait gave up"),
-                                (DEVERR_NONFINITE, "compressed value not finite")) if v & b]
+                                (DEVERR_NONFINITE, "compressed value or second moment not finite")) if v & b]
         raise DeviceError(f"device error 0x{v:x}: {', '.join(names)}")
 
 
@@ -550,3 +576,302 @@ def sample_ids(r: torch.Tensor, V: int, out: Optional[torch.Tensor] = None,
     _call(_lib.lm_sample_ids(_ptr(r), r.numel(), V, _ptr(out), _idtype(out), _stream(stream)),
           "lm_sample_ids")
     return out
+
+
+# ---------------------------------------------------------------------------
+# AdamW over many tensors, and on table rows with 8-bit moments
+# ---------------------------------------------------------------------------
+class _On:
+    """The device of a call's tensors, made current where it is not, and the
+    stream the call goes to (a stream of another device is refused)."""
+
+    def __init__(self, device: torch.device, stream=None):
+        index = device.index
+        if stream is not None and stream.device.index != index:
+            raise LmError(f"stream is on {stream.device}, the tensors are on {device}")
+        self.other = None if torch.cuda.current_device() == index else torch.cuda.device(device)
+        self.stream = stream
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+        return _stream(self.stream)
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise LmError(f"{name} is on {t.device}, not on {device}")
+
+
+def _one_of(t: Optional[torch.Tensor], dtype, what: str):
+    if t is not None and (t.dtype != dtype or t.numel() < 1):
+        raise LmError(f"{what} must be a {dtype} tensor of one element")
+
+
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _codes(t: torch.Tensor, what: str):
+    if t.dtype not in _CODES:
+        raise LmError(f"{what} must hold e4m3 codes (float8_e4m3fn, or its bits as uint8)")
+
+
+def _scales(t: torch.Tensor, what: str):
+    if t.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+        raise LmError(f"{what} must hold scale bytes (uint8 or float8_e8m0fnu)")
+
+
+class AdamwPlan(NamedTuple):
+    """A list of tensors as ``adamw`` steps it: the table that names their
+    memory on the device, and the tensors themselves, which it keeps alive.
+    It stands for the memory the tensors had when it was made."""
+    table: torch.Tensor
+    tensors: tuple
+    count: int
+    chunks: int
+    gtype: int
+    states: int
+    copies: bool
+
+
+def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
+               decay=None) -> AdamwPlan:
+    """lm_adamw_plan: lists of contiguous tensors of equal sizes on one device.
+    params fp32, grads all fp32 or all bf16, m and v fp32; or 8-bit moments: m
+    and v e4m3 codes (v of its square root), m_scale and v_scale one byte per
+    MOMENT_BLOCK values. copies: bf16 copies of the parameters, written with
+    every step. decay: one truth value per tensor, whether weight_decay
+    applies. Copies the table to the device; make a new plan when a tensor
+    (say, a gradient) gets other memory."""
+    params, grads, m, v = (list(x) for x in (params, grads, m, v))
+    lists = {"grads": grads, "m": m, "v": v}
+    for name, x in (("m_scale", m_scale), ("v_scale", v_scale), ("copies", copies)):
+        if x is not None:
+            lists[name] = list(x)
+    n = len(params)
+    decay = None if decay is None else [int(bool(d)) for d in decay]
+    for name, x in list(lists.items()) + ([] if decay is None else [("decay", decay)]):
+        if len(x) != n:
+            raise LmError(f"{name} has {len(x)} entries, params has {n}")
+    eight = "m_scale" in lists
+    if eight != ("v_scale" in lists):
+        raise LmError("8-bit moments need m_scale and v_scale")
+    if not n:
+        raise LmError("params is empty")
+    device = params[0].device
+    _dev(params[0], "params")
+    gtype = _gtype(grads[0])
+    for i, p in enumerate(params):
+        k = p.numel()
+        if p.dtype != torch.float32:
+            raise LmError("params must be float32")
+        blocks = -(-k // MOMENT_BLOCK)
+        for name, t, want in ([("params", p, k)] + [(a, x[i], blocks if a.endswith("_scale") else k)
+                                                    for a, x in lists.items()]):
+            if t.device != device or not t.is_contiguous() or t.numel() != want:
+                raise LmError(f"{name}[{i}] must be contiguous on {device} with {want} elements")
+        if _gtype(grads[i]) != gtype:
+            raise LmError("grads must share a dtype")
+        for a in ("m", "v"):
+            if eight:
+                _codes(lists[a][i], a)
+                _scales(lists[a + "_scale"][i], a + "_scale")
+            elif lists[a][i].dtype != torch.float32:
+                raise LmError(f"{a} must be float32 (8-bit moments come with scales)")
+        if "copies" in lists and lists["copies"][i].dtype != torch.bfloat16:
+            raise LmError("copies must be bfloat16")
+
+    def pointers(x):
+        return None if x is None else (ctypes.c_void_p * n)(*[t.data_ptr() for t in x])
+    sizes = (ctypes.c_int64 * n)(*[p.numel() for p in params])
+    need = _lib.lm_adamw_plan_bytes(sizes, n)
+    if need == 0:
+        raise LmError("lm_adamw_plan_bytes rejected the sizes")
+    host = torch.empty(need, dtype=torch.uint8)
+    chunks = ctypes.c_int64()
+    _call(_lib.lm_adamw_plan(
+        pointers(params), pointers(grads), pointers(m), pointers(v), pointers(lists.get("m_scale")),
+        pointers(lists.get("v_scale")), pointers(lists.get("copies")), sizes,
+        None if decay is None else (ctypes.c_int32 * n)(*decay), n, gtype, 8 if eight else 32,
+        _ptr(host), need, ctypes.byref(chunks)), "lm_adamw_plan")
+    keep = tuple(tuple(x) for x in [params] + list(lists.values()))
+    return AdamwPlan(host.to(device), keep, n, chunks.value, gtype, 8 if eight else 32,
+                     "copies" in lists)
+
+
+def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
+          eps: float = 1e-8, weight_decay: float = 0.0, step: int = 1,
+          grad_scale: Optional[torch.Tensor] = None, seed: int = 0,
+          dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
+    """lm_adamw: one AdamW step of every tensor of the plan, in place, in one
+    launch. grad_scale: a device fp32 number that multiplies every gradient.
+    seed: of the 8-bit moments' rounding; give every step its own."""
+    table = plan.table
+    _same_device(table.device, grad_scale=grad_scale, dev_err=dev_err)
+    _one_of(grad_scale, torch.float32, "grad_scale")
+    _one_of(dev_err, torch.int32, "dev_err")
+    with _On(table.device, stream) as st:
+        _call(_lib.lm_adamw(_ptr(table), plan.count, plan.chunks, plan.gtype, plan.states,
+                            plan.copies, lr, beta1, beta2, eps, weight_decay, step,
+                            _ptr(grad_scale), seed, _ptr(dev_err), st), "lm_adamw")
+
+
+def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tensor,
+                    vals: torch.Tensor, m: torch.Tensor, v: torch.Tensor, m_scale: torch.Tensor,
+                    v_scale: torch.Tensor, lr: float = 1e-3, beta1: float = 0.9,
+                    beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
+                    step: int = 1, seed: int = 0, dev_err: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """lm_sparse_apply_q8: the lazy AdamW step of ``sparse_apply(opt="adam")``
+    with 8-bit moments, in place: m and v V x D codes (v of its square root),
+    m_scale and v_scale V x ceil(D / MOMENT_BLOCK) bytes."""
+    _dev(table, "table")
+    V, D = table.shape
+    if table.dtype != torch.float32 or vals.dtype != torch.float32:
+        raise LmError("table and vals must be float32")
+    if vals.dim() != 2 or vals.shape[1] != D:
+        raise LmError("vals and table widths differ")
+    blocks = -(-D // MOMENT_BLOCK)
+    for name, t, want, kind in (("m", m, D, _codes), ("v", v, D, _codes),
+                                ("m_scale", m_scale, blocks, _scales),
+                                ("v_scale", v_scale, blocks, _scales)):
+        kind(t, name)
+        if t.shape != (V, want):
+            raise LmError(f"{name} must be {V} x {want}")
+    if m.stride() != v.stride() or m_scale.stride() != v_scale.stride():
+        raise LmError("m and v, and their scales, must share their strides")
+    if not rows.is_contiguous():
+        raise LmError("rows must be contiguous")
+    _one_of(n_rows, torch.int64, "n_rows")
+    _one_of(dev_err, torch.int32, "dev_err")
+    _same_device(table.device, rows=rows, n_rows=n_rows, vals=vals, m=m, v=v, m_scale=m_scale,
+                 v_scale=v_scale, dev_err=dev_err)
+    with _On(table.device, stream) as st:
+        if dev_err is None:
+            dev_err = _own_err(table.device, stream)
+        _call(_lib.lm_sparse_apply_q8(
+            _ptr(table), V, D, _rows(table, "table"), _ptr(rows), _idtype(rows), _ptr(n_rows),
+            min(rows.numel(), vals.shape[0]), _ptr(vals), _rows(vals, "vals"), lr, beta1, beta2,
+            eps, weight_decay, step, _ptr(m), _ptr(v), _rows(m, "m"), _ptr(m_scale), _ptr(v_scale),
+            _rows(m_scale, "m_scale"), seed, _ptr(dev_err), st), "lm_sparse_apply_q8")
+    return table
+
+
+# ---------------------------------------------------------------------------
+# Relative position bias
+# ---------------------------------------------------------------------------
+class RelBuckets(NamedTuple):
+    """Segments of the distance axis and their table rows (host memory)."""
+    starts: ctypes.Array
+    ids: ctypes.Array
+    n_seg: int
+    num_buckets: int
+
+
+_REL_MODES = {"both": REL_BOTH, "past": REL_PAST, "causal": REL_CAUSAL}
+
+
+def rel_buckets(num_buckets: int, max_distance: int, mode: str = "both") -> RelBuckets:
+    """lm_rel_buckets: logarithmic buckets. mode "both": half for keys up to
+    the query and half for those after it; "past": keys after the query are in
+    bucket 0; "causal": they are masked. Computed once, for every later call."""
+    starts = (ctypes.c_int32 * REL_MAX_SEGMENTS)()
+    ids = (ctypes.c_int32 * REL_MAX_SEGMENTS)()
+    n = ctypes.c_int32()
+    if mode not in _REL_MODES:
+        raise LmError(f"mode must be one of {sorted(_REL_MODES)}, got {mode!r}")
+    _call(_lib.lm_rel_buckets(num_buckets, max_distance, _REL_MODES[mode], starts, ids,
+                              ctypes.byref(n)), "lm_rel_buckets")
+    return RelBuckets(starts, ids, n.value, num_buckets)
+
+
+def _scores(t: torch.Tensor, what: str):
+    """Strides (b, h, i) of a B x H x Lq x Lk tensor with unit column stride."""
+    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
+        raise LmError(f"{what} must be a 4-D tensor with unit stride along the keys")
+    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+
+
+def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start: int = 0,
+             add: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+             dtype=torch.float32, stream=None) -> torch.Tensor:
+    """lm_rel_bias: table[bucket(j - (q_start + i)), h] for every head, query i
+    and key j, as an H x Lq x Lk tensor of `dtype`; with `add` (B x H x Lq x Lk
+    attention scores) the scores plus the bias, of their shape and dtype. `out`
+    may be `add` itself."""
+    _dev(table, "table")
+    if table.dim() != 2 or table.dtype != torch.float32 or table.shape[0] != buckets.num_buckets:
+        raise LmError(f"table must be float32 with {buckets.num_buckets} rows")
+    H = table.shape[1]
+    device = table.device
+    if add is not None:
+        dtype = add.dtype
+        if add.dim() != 4 or tuple(add.shape[1:]) != (H, Lq, Lk):
+            raise LmError(f"add must be B x {H} x {Lq} x {Lk}")
+    shape = (H, Lq, Lk) if add is None else tuple(add.shape)
+    _same_device(device, add=add, out=out)
+    with _On(device, stream) as st:
+        if out is None:
+            out = _on_stream(stream, lambda: torch.empty(shape, dtype=dtype, device=device))
+        if tuple(out.shape) != shape or out.dtype != dtype:
+            raise LmError(f"out must be {' x '.join(map(str, shape))} of {dtype}")
+        full = out if add is not None else out.unsqueeze(0)
+        _call(_lib.lm_rel_bias(
+            _ptr(table), _rows(table, "table"), buckets.num_buckets, buckets.starts, buckets.ids,
+            buckets.n_seg, full.shape[0], H, Lq, Lk, q_start, _ptr(add),
+            None if add is None else _scores(add, "add"), _ptr(out), _scores(full, "out"),
+            _gtype(out), st), "lm_rel_bias")
+    return out
+
+
+def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
+                  out: Optional[torch.Tensor] = None, accumulate: bool = False,
+                  ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
+    """lm_rel_bias_grad: the table's gradient, num_buckets x H fp32, from that
+    of the scores (B x H x Lq x Lk, or H x Lq x Lk). accumulate: add to `out`.
+    Without `ws` the call takes its workspace from torch's allocator."""
+    _dev(dout, "dout")
+    if dout.dim() == 3:
+        dout = dout.unsqueeze(0)
+    strides = _scores(dout, "dout")
+    B, H, Lq, Lk = dout.shape
+    gtype = _gtype(dout)
+    device = dout.device
+    if accumulate and out is None:
+        raise LmError("accumulate needs out")
+    if out is not None and (out.dtype != torch.float32 or
+                            tuple(out.shape) != (buckets.num_buckets, H)):
+        raise LmError(f"out must be float32, {buckets.num_buckets} x {H}")
+    _same_device(device, out=out)
+    if ws is not None and ws.buf.device != device:
+        raise LmError(f"ws is on {ws.buf.device}, not on {device}")
+    need = _lib.lm_rel_bias_grad_workspace_bytes(B, H, Lq, Lk, gtype, buckets.n_seg)
+    with _On(device, stream) as st:
+        if out is None:
+            out = _on_stream(stream, lambda: torch.empty((buckets.num_buckets, H),
+                                                         dtype=torch.float32, device=device))
+        buf = ws.get(need) if ws is not None else _on_stream(
+            stream, lambda: torch.empty(need, dtype=torch.uint8, device=device))
+        _call(_lib.lm_rel_bias_grad(
+            _ptr(dout), gtype, B, H, Lq, Lk, strides, q_start, buckets.starts, buckets.ids,
+            buckets.n_seg, buckets.num_buckets, _ptr(out), _rows(out, "out"), bool(accumulate),
+            _ptr(buf), buf.numel(), st), "lm_rel_bias_grad")
+    return out
+
+
+def _on_stream(stream, make):
+    """`make()` with `stream` current, so that torch's allocator gives the
+    memory to that stream and takes it back in its order."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
+def _own_err(device, stream):
+    return _on_stream(stream, lambda: torch.zeros(1, dtype=torch.int32, device=device))
