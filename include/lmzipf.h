@@ -429,8 +429,10 @@ int lm_sparse_apply_f16(float* table, int64_t V, int64_t D, int64_t ld_table,
  * computes in fp32 on the decoded values and rounds stochastically: with s
  * the step of the e4m3 numbers at |x| 2^-k, the code is
  *     floor(|x| 2^-k / s + R / 2^20) * s,  with x's sign,
- * R the high (m) or low (v) 20 bits of the value's random word; a nonzero
- * root of v never gets the code zero. The words are a function of `seed` and
+ * R the high (m) or low (v) 20 bits of the value's random word and 2^-k the
+ * fp32 power that the device's math library gives (for some k half a unit in
+ * the last place low: torch.ldexp's, so torch operations give the same
+ * codes); a nonzero root of v never gets the code zero. The words are a function of `seed` and
  * the value's number: the values of a list count through, each tensor from
  * the next multiple of LM_MOMENT_BLOCK (of a table: id * D + column). Give
  * every step and every list its own seed; the same seed repeats a call bit

@@ -122,6 +122,8 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw(
     if (threadIdx.x == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
     return;
   }
+  __shared__ float inverse[EIGHT ? kScales : 1];
+  if constexpr (EIGHT) fill_scales(inverse, kAdamwThreads);
   const PlanTensor* tensors = reinterpret_cast<const PlanTensor*>(head + 1);
   const PlanChunk chunk = reinterpret_cast<const PlanChunk*>(tensors + want.tensors)[blockIdx.x];
   const PlanTensor t = tensors[chunk.tensor];
@@ -184,8 +186,8 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw(
       }
     }
     if constexpr (EIGHT) {
-      mc[j] = encode4<false>(m[j], word, ms[j]);
-      vc[j] = encode4<true>(v[j], low, vs[j]);
+      mc[j] = encode4<false>(m[j], word, inverse, ms[j]);
+      vc[j] = encode4<true>(v[j], low, inverse, vs[j]);
     }
     if (have <= 0) continue;
     store4(t.p + at + i, have, p[j]);
@@ -216,6 +218,8 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
     uint8_t* __restrict__ v, int64_t ld_codes, uint8_t* __restrict__ m_scale,
     uint8_t* __restrict__ v_scale, int64_t ld_scale, int64_t nwaves,
     int32_t* __restrict__ dev_err) {
+  __shared__ float inverse[kScales];
+  fill_scales(inverse, kAdamwThreads);
   const int lane = lane_id();
   const int64_t w = first_lane(static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) +
                                (threadIdx.x >> 6));
@@ -269,8 +273,8 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
           word[e] = value_word(static_cast<uint64_t>(id * D + c + e), keys);
           low[e] = word[e] << 12;
         }
-        mc[j] = encode4<false>(mx, word, ms[j]);
-        vc[j] = encode4<true>(vx, low, vs[j]);
+        mc[j] = encode4<false>(mx, word, inverse, ms[j]);
+        vc[j] = encode4<true>(vx, low, inverse, vs[j]);
         if (have <= 0) continue;
         store4(prow + c, have, p[j]);
         store_codes(mrow + c, have, mc[j]);

@@ -77,10 +77,26 @@ __device__ __forceinline__ void decode4(uint32_t codes, int scale, float* x) {
   x[3] = __builtin_amdgcn_ldexpf(__builtin_amdgcn_cvt_f32_fp8(codes, 3), k);
 }
 
+// 2^-k by scale byte, in LDS: what a value is multiplied by before it is rounded.
+// powf gives some of these powers half a unit in the last place low. They are
+// taken as it gives them, since torch's ldexp multiplies by the same numbers: a
+// program that computes codes with torch operations gets the kernels', bit for
+// bit. A rounding's threshold moves by 2^-20 of a step at most, the resolution of
+// its random part; none is high, so no value passes 448. A thread's call of powf
+// serves 16 values and more.
+constexpr int kScales = 256;
+
+__device__ __forceinline__ void fill_scales(float* inverse, int threads) {
+  for (int b = threadIdx.x; b < kScales; b += threads)
+    inverse[b] = powf(2.f, static_cast<float>(127 - b));
+  __syncthreads();
+}
+
 // The codes of 4 values of this lane's block (8 lanes) and the block's scale byte.
 // FLOOR: values above zero round to no code below 1.
 template <bool FLOOR>
-__device__ __forceinline__ uint32_t encode4(const float* x, const uint32_t* word, int& scale) {
+__device__ __forceinline__ uint32_t encode4(const float* x, const uint32_t* word,
+                                            const float* inverse, int& scale) {
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -88,10 +104,11 @@ __device__ __forceinline__ uint32_t encode4(const float* x, const uint32_t* word
     top = a > top ? a : top;
   }
   scale = scale_byte(block_max8(top));
+  const float by = inverse[scale];
   float y[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    y[e] = __builtin_amdgcn_ldexpf(x[e], 127 - scale);
+    y[e] = x[e] * by;
     if (FLOOR) y[e] = x[e] > 0.f ? fmaxf(y[e], 0x1p-9f) : 0.f;
   }
   int c = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], word[0], 0, 0);

@@ -156,13 +156,22 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
       T* o = out + b * so.b + h * so.h + static_cast<int64_t>(row) * so.q + col;
       const T* a = ADD ? add + b * sa.b + h * sa.h + static_cast<int64_t>(row) * sa.q + col
                        : nullptr;
+      // Every load of the patch before its first store: out may be add, so the
+      // compiler keeps a load behind the stores before it.
+      typename Patch<T>::raw_t raw[P];
+      if (ADD && !masked) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const T* ai = a + (i < nr ? i : 0) * sa.q;
+          raw[i] = have >= P ? Patch<T>::load(ai) : Patch<T>::part(ai, have);
+        }
+      }
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         if (i >= nr) break;
         float x[P];
         if (ADD && !masked) {
-          const T* ai = a + i * sa.q;
-          Patch<T>::widen(have >= P ? Patch<T>::load(ai) : Patch<T>::part(ai, have), x);
+          Patch<T>::widen(raw[i], x);
 #pragma unroll
           for (int e = 0; e < P; ++e) {
             const float y = d[P - 1 - i + e];
@@ -262,32 +271,41 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
   }
 }
 
-// dtable[n, h] (+)= the sums of the segments with id n over a head's waves.
-__global__ __launch_bounds__(kRelThreads) void k_rel_join(
+// dtable[n, h] (+)= the sums of the segments with id n over a head's waves. One
+// workgroup per head: a thread adds one segment (a column of the workspace) over
+// every kJoinThreads / width-th wave, so neighbouring threads read neighbouring
+// words, and the threads of a segment are added in their order.
+constexpr int kJoinThreads = 1024;
+
+__global__ __launch_bounds__(kJoinThreads) void k_rel_join(
     const float* __restrict__ ws, Segments seg, int waves, int num_buckets,
     float* __restrict__ dtable, int64_t ld_table, int accumulate) {
-  __shared__ float part[kRelThreads];
+  __shared__ float part[kJoinThreads];
   __shared__ float sums[LM_REL_MAX_SEGMENTS];
-  const int h = blockIdx.x;
-  const float* mine = ws + static_cast<int64_t>(h) * waves * seg.n;
-  for (int s = 0; s < seg.n; ++s) {
-    float x = 0.f;
-    for (int w = threadIdx.x; w < waves; w += kRelThreads) x += mine[static_cast<int64_t>(w) * seg.n + s];
-    part[threadIdx.x] = x;
-    __syncthreads();
-    for (int off = kRelThreads / 2; off > 0; off >>= 1) {
-      if (static_cast<int>(threadIdx.x) < off) part[threadIdx.x] += part[threadIdx.x + off];
-      __syncthreads();
-    }
-    if (threadIdx.x == 0) sums[s] = part[0];
-    __syncthreads();
+  const int h = blockIdx.x, n = seg.n;
+  int width = 32;  // segments of one turn
+  while (width < n && width < kJoinThreads) width *= 2;
+  const int column = threadIdx.x % width, first = threadIdx.x / width, step = kJoinThreads / width;
+  const float* mine = ws + static_cast<int64_t>(h) * waves * n;
+  float x = 0.f;
+  if (column < n) {
+#pragma unroll 8
+    for (int w = first; w < waves; w += step) x += mine[static_cast<int64_t>(w) * n + column];
   }
-  for (int n = threadIdx.x; n < num_buckets; n += kRelThreads) {
-    float x = 0.f;
-    for (int s = 0; s < seg.n; ++s)
-      if (seg.ids[s] == n) x += sums[s];
-    float* d = dtable + n * ld_table + h;
-    *d = accumulate ? *d + x : x;
+  part[threadIdx.x] = x;
+  __syncthreads();
+  if (threadIdx.x < n) {
+    float y = 0.f;
+    for (int g = 0; g < step; ++g) y += part[g * width + threadIdx.x];
+    sums[threadIdx.x] = y;
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < num_buckets; b += kJoinThreads) {
+    float y = 0.f;
+    for (int s = 0; s < n; ++s)
+      if (seg.ids[s] == b) y += sums[s];
+    float* d = dtable + b * ld_table + h;
+    *d = accumulate ? *d + y : y;
   }
 }
 
@@ -394,7 +412,7 @@ int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, 
     const int rc = launch_status(hipGetLastError());
     if (rc != LM_OK) return rc;
   }
-  k_rel_join<<<static_cast<uint32_t>(H), kRelThreads, 0, st>>>(
+  k_rel_join<<<static_cast<uint32_t>(H), kJoinThreads, 0, st>>>(
       static_cast<const float*>(ws), seg, static_cast<int>(waves), num_buckets, dtable, ld_table,
       accumulate);
   return launch_status(hipGetLastError());

@@ -1,6 +1,11 @@
 """The AdamW step with 8-bit moments in numpy (no test functions here): every
 product, sum and root of the moments in IEEE fp32, so codes and scale bytes are
-the kernels' bit for bit; the parameter in 64 bits."""
+the kernels' bit for bit; the parameter in 64 bits.
+
+A value is multiplied by INVERSE[byte], 2^-k, before it is rounded. On the device
+these are the math library's powers, some half a unit in the last place low:
+the GPU tests put them here (device_powers), after they are checked to be within
+that of the powers themselves."""
 from __future__ import annotations
 
 import numpy as np
@@ -16,6 +21,19 @@ _e, _f = (_b >> 3) & 15, _b & 7
 E4M3 = np.where(_e == 0, _f / 8.0 * 2.0 ** -6, (1 + _f / 8.0) * 2.0 ** (_e - 7.0))
 E4M3[(_b & 0x7F) == 0x7F] = np.nan
 E4M3 = np.where(_b & 0x80, -E4M3, E4M3)
+
+
+INVERSE = np.exp2(127.0 - np.arange(256)).astype(np.float32)
+
+
+def device_powers(torch):
+    """INVERSE as torch.ldexp has it on the device: within half a unit in the last
+    place of 2^-k, never above it."""
+    k = 127 - torch.arange(255, dtype=torch.int32, device="cuda")
+    got = torch.ldexp(torch.ones(255, device="cuda"), k).cpu().numpy()
+    want = np.exp2(127.0 - np.arange(255))
+    assert (got <= want).all() and (got >= want * (1 - 2.0 ** -24)).all()
+    INVERSE[:255] = got
 
 
 def words(number, seed):
@@ -56,7 +74,9 @@ def encode(x, part, keep):
     f, e = np.frexp(top)  # top = f 2^e, f in [1/2, 1): at most 448 2^k = 7/8 2^(k + 9)
     k = np.where(top == 0, -127, np.maximum(e - 9 + (f > 0.875), -127))
     byte = (k + 127).astype(np.uint8)
-    y = a / scale_of(byte, n)
+    with np.errstate(under="ignore"):
+        y = np.abs(x) * np.repeat(INVERSE[byte], BLOCK, -1)[..., :n]
+    y = y.astype(np.float64)
     exp = np.maximum(np.frexp(y)[1] - 1, -6)
     step = np.exp2(exp - 3.0)
     q = np.floor(y / step + part) * step

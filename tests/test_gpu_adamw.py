@@ -24,6 +24,7 @@ SIZES = [0, 1, 2, 3, 4, 5, 31, 32, 33, 63, 64, 65, 255, 256, 257, 1023, 1024, 10
 def lz():
     from paper_1810_10045_amd import lmzipf
     assert torch.cuda.is_available(), "GPU tests need a GPU"
+    R.device_powers(torch)
     return lmzipf
 
 
