@@ -463,8 +463,8 @@ int lm_sparse_apply_f16(float* table, int64_t V, int64_t D, int64_t ld_table,
  * the library does not handle (negative, or more than LM_ADAMW_MAX_VALUES
  * together).
  *
- * lm_adamw: plan is the device copy; tensors, chunks, gtype, states and
- * copies (0 or 1) are those it was made with (another plan's set
+ * lm_adamw: plan is the device copy of plan_bytes bytes; chunks, gtype,
+ * states and copies (0 or 1) are those it was made with (others set
  * LM_DEVERR_CAPACITY and nothing is stepped).
  * grad_scale device fp32 or NULL (1): multiplies every gradient (gradient
  *            clipping, loss scales).
@@ -478,7 +478,7 @@ int lm_adamw_plan(void* const* p, const void* const* g, void* const* m, void* co
                   void* const* m_scale, void* const* v_scale, void* const* copies,
                   const int64_t* sizes, const int32_t* decay, int64_t tensors, int32_t gtype,
                   int32_t states, void* plan, size_t plan_bytes, int64_t* chunks);
-int lm_adamw(const void* plan, int64_t tensors, int64_t chunks, int32_t gtype, int32_t states,
+int lm_adamw(const void* plan, size_t plan_bytes, int64_t chunks, int32_t gtype, int32_t states,
              int32_t copies, float lr, float beta1, float beta2, float eps, float weight_decay,
              int64_t step, const float* grad_scale, uint64_t seed, int32_t* dev_err,
              void* stream);
@@ -488,8 +488,8 @@ int lm_adamw(const void* plan, int64_t tensors, int64_t chunks, int32_t gtype, i
  * m, v       device, V x D bytes (codes), row stride ld_codes >= D.
  * m_scale, v_scale  device, V x ceil(D / LM_MOMENT_BLOCK) bytes, row stride
  *            ld_scale.
- * The other arguments and their errors are those of lm_sparse_apply; rows
- * that are not named are untouched in all five arrays. A value whose new v
+ * The other arguments and their errors are those of lm_sparse_apply, but
+ * dev_err may be NULL and a V of 0 is no error; rows that are not named are untouched in all five arrays. A value whose new v
  * is not finite keeps its parameter and moments and sets
  * LM_DEVERR_NONFINITE (its moments are rounded again where its block's scale
  * changes). */

@@ -16,16 +16,9 @@ constexpr int kVectors = 4;   // vectors a lane holds at once
 constexpr int kChunk = kAdamwThreads * kVec * kVectors;
 static_assert(kChunk % kMomentBlock == 0, "chunks start on whole blocks");
 
-// The plan: a header, one entry per tensor, one word pair per chunk.
-struct PlanHead {
-  uint64_t magic;
-  int64_t tensors, chunks;
-  int32_t gtype, states;
-  int32_t copies, pad[7];
-};
-static_assert(sizeof(PlanHead) == 64);
-
-struct PlanTensor {
+// The plan: one record per chunk, with everything its workgroup needs, so that
+// the data's addresses are one load away from the launch.
+struct PlanChunk {
   float* p;
   const void* g;
   void* m;
@@ -33,55 +26,68 @@ struct PlanTensor {
   uint8_t* m_scale;
   uint8_t* v_scale;
   uint16_t* copy;
-  int64_t n;
-  int64_t first;  // the number of the tensor's first value: whole blocks before it
-  float decay;    // 1 or 0: whether the weight decay applies
-  int32_t pad;
+  int64_t first;  // the number of the chunk's first value: whole blocks before it
+  int32_t n;      // values, 1 to kChunk
+  int32_t decay;  // 1 or 0: whether the weight decay applies
+  uint64_t kind;  // of the list: plan_kind
 };
-static_assert(sizeof(PlanTensor) == 80);
+static_assert(sizeof(PlanChunk) == 80);
 
-struct PlanChunk {
-  uint32_t tensor, index;
-};
+static uint64_t plan_kind(int64_t chunks, int gtype, int states, bool copies) {
+  return 0x6c6d5a41ull << 32 ^ static_cast<uint64_t>(chunks) << 8 ^ gtype << 7 ^ copies << 6 ^ states;
+}
 
-constexpr uint64_t kPlanMagic = 0x6c6d5a61646d7731ull;
-
-// VEC values at p of which `have` (1 to VEC) exist.
-__device__ __forceinline__ void load4(const float* p, int have, float* x) {
-  if (have >= 4) {
-    const f32x4e t = *reinterpret_cast<const f32x4e*>(p);
+// ---------------------------------------------------------------------------
+// A lane's vectors. Whole vectors are one load; the last ones of a tensor load
+// each value by itself, those past its end from its last value's place (and
+// count as zero): no load stands under a condition, so all of a lane's loads
+// are under way at once.
+// ---------------------------------------------------------------------------
+template <bool WHOLE>
+__device__ __forceinline__ void load4(const float* p, int i, int n, float* x) {
+  if constexpr (WHOLE) {
+    const f32x4e t = *reinterpret_cast<const f32x4e*>(p + i);
     x[0] = t.x; x[1] = t.y; x[2] = t.z; x[3] = t.w;
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = e < have ? p[e] : 0.f;
+    for (int e = 0; e < 4; ++e) x[e] = p[i + e < n ? i + e : n - 1];
   }
 }
 
-__device__ __forceinline__ void load4(const bf16_t* p, int have, float* x) {
-  if (have >= 4) {
-    const u32x2e t = *reinterpret_cast<const u32x2e*>(p);
+template <bool WHOLE>
+__device__ __forceinline__ void load4(const bf16_t* p, int i, int n, float* x) {
+  if constexpr (WHOLE) {
+    const u32x2e t = *reinterpret_cast<const u32x2e*>(p + i);
     x[0] = __uint_as_float(t.x << 16); x[1] = __uint_as_float(t.x & 0xffff0000u);
     x[2] = __uint_as_float(t.y << 16); x[3] = __uint_as_float(t.y & 0xffff0000u);
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = e < have ? bf16_to_f32(p[e].bits) : 0.f;
+    for (int e = 0; e < 4; ++e) x[e] = bf16_to_f32(p[i + e < n ? i + e : n - 1].bits);
   }
 }
 
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int have) {
-  if (have >= 4) return *reinterpret_cast<const u32e*>(p);
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int i, int n) {
+  if constexpr (WHOLE) return *reinterpret_cast<const u32e*>(p + i);
   uint32_t w = 0;
-  for (int e = 0; e < have; ++e) w |= uint32_t(p[e]) << (8 * e);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w |= uint32_t(p[i + e < n ? i + e : n - 1]) << (8 * e);
   return w;
 }
 
-__device__ __forceinline__ void store4(float* p, int have, const float* x) {
-  if (have >= 4) {
-    *reinterpret_cast<f32x4e*>(p) = f32x4e{x[0], x[1], x[2], x[3]};
+__device__ __forceinline__ void zero_past(int i, int n, float* x) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = i + e < n ? x[e] : 0.f;
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ void store4(float* p, int i, int n, const float* x) {
+  if constexpr (WHOLE) {
+    *reinterpret_cast<f32x4e*>(p + i) = f32x4e{x[0], x[1], x[2], x[3]};
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (e < have) p[e] = x[e];
+      if (i + e < n) p[i + e] = x[e];
   }
 }
 
@@ -89,22 +95,26 @@ __device__ __forceinline__ uint32_t bf16_bits(float x) {
   return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
 }
 
-__device__ __forceinline__ void store4(uint16_t* p, int have, const float* x) {
-  if (have >= 4) {
-    *reinterpret_cast<u32x2e*>(p) = u32x2e{bf16_bits(x[0]) | bf16_bits(x[1]) << 16,
-                                           bf16_bits(x[2]) | bf16_bits(x[3]) << 16};
+template <bool WHOLE>
+__device__ __forceinline__ void store4(uint16_t* p, int i, int n, const float* x) {
+  if constexpr (WHOLE) {
+    *reinterpret_cast<u32x2e*>(p + i) = u32x2e{bf16_bits(x[0]) | bf16_bits(x[1]) << 16,
+                                               bf16_bits(x[2]) | bf16_bits(x[3]) << 16};
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (e < have) p[e] = static_cast<uint16_t>(bf16_bits(x[e]));
+      if (i + e < n) p[i + e] = static_cast<uint16_t>(bf16_bits(x[e]));
   }
 }
 
-__device__ __forceinline__ void store_codes(uint8_t* p, int have, uint32_t w) {
-  if (have >= 4) {
-    *reinterpret_cast<u32e*>(p) = w;
+template <bool WHOLE>
+__device__ __forceinline__ void store_codes(uint8_t* p, int i, int n, uint32_t w) {
+  if constexpr (WHOLE) {
+    *reinterpret_cast<u32e*>(p + i) = w;
   } else {
-    for (int e = 0; e < have; ++e) p[e] = static_cast<uint8_t>(w >> (8 * e));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e < n) p[i + e] = static_cast<uint8_t>(w >> (8 * e));
   }
 }
 
@@ -113,65 +123,55 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int have, uint32_t w) {
 // are a workgroup's width apart, so every load and store of a wave is one
 // contiguous piece.
 // ---------------------------------------------------------------------------
-template <typename GT, bool EIGHT, bool COPY>
-__global__ __launch_bounds__(kAdamwThreads) void k_adamw(
-    const PlanHead* __restrict__ head, PlanHead want, OptParams o, MomentParams q, StepKeys keys,
-    const float* __restrict__ grad_scale, int32_t* __restrict__ dev_err) {
-  if (head->magic != want.magic || head->tensors != want.tensors || head->chunks != want.chunks ||
-      head->gtype != want.gtype || head->states != want.states || head->copies != want.copies) {
-    if (threadIdx.x == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
-    return;
-  }
-  __shared__ float inverse[EIGHT ? kScales : 1];
-  if constexpr (EIGHT) fill_scales(inverse, kAdamwThreads);
-  const PlanTensor* tensors = reinterpret_cast<const PlanTensor*>(head + 1);
-  const PlanChunk chunk = reinterpret_cast<const PlanChunk*>(tensors + want.tensors)[blockIdx.x];
-  const PlanTensor t = tensors[chunk.tensor];
-  const int64_t at = static_cast<int64_t>(chunk.index) * kChunk;
-  const int n = t.n - at < kChunk ? static_cast<int>(t.n - at) : kChunk;
-  const float gs = grad_scale ? *grad_scale : 1.f;
-  const float wd = t.decay * o.wd;
+template <typename GT, bool EIGHT, bool COPY, bool WHOLE>
+__device__ __forceinline__ bool step_chunk(const PlanChunk& t, float gs, const OptParams& o,
+                                           const MomentParams& q, const StepKeys& keys,
+                                           const float* inverse) {
+  const int n = WHOLE ? kChunk : t.n;
+  constexpr int kStride = kAdamwThreads * kVec;
   const int i0 = threadIdx.x * kVec;
   float p[kVectors][kVec], g[kVectors][kVec], m[kVectors][kVec], v[kVectors][kVec];
   uint32_t mc[kVectors], vc[kVectors];
   int ms[kVectors], vs[kVectors];
 #pragma unroll
   for (int j = 0; j < kVectors; ++j) {
-    const int i = i0 + j * kAdamwThreads * kVec, have = n - i;
-    mc[j] = vc[j] = 0;
-    ms[j] = vs[j] = 0;
-    if (have <= 0) {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) p[j][e] = g[j][e] = m[j][e] = v[j][e] = 0.f;
-      continue;
-    }
-    load4(t.p + at + i, have, p[j]);
-    load4(static_cast<const GT*>(t.g) + at + i, have, g[j]);
+    if (!WHOLE && j * kStride >= n) break;
+    const int i = i0 + j * kStride;
+    load4<WHOLE>(t.p, i, n, p[j]);
+    load4<WHOLE>(static_cast<const GT*>(t.g), i, n, g[j]);
     if constexpr (EIGHT) {
-      mc[j] = load_codes(static_cast<const uint8_t*>(t.m) + at + i, have);
-      vc[j] = load_codes(static_cast<const uint8_t*>(t.v) + at + i, have);
-      ms[j] = t.m_scale[(at + i) / kMomentBlock];
-      vs[j] = t.v_scale[(at + i) / kMomentBlock];
+      const int b = (WHOLE || i < n ? i : n - 1) / kMomentBlock;
+      mc[j] = load_codes<WHOLE>(static_cast<const uint8_t*>(t.m), i, n);
+      vc[j] = load_codes<WHOLE>(static_cast<const uint8_t*>(t.v), i, n);
+      ms[j] = t.m_scale[b];
+      vs[j] = t.v_scale[b];
     } else {
-      load4(static_cast<const float*>(t.m) + at + i, have, m[j]);
-      load4(static_cast<const float*>(t.v) + at + i, have, v[j]);
+      load4<WHOLE>(static_cast<const float*>(t.m), i, n, m[j]);
+      load4<WHOLE>(static_cast<const float*>(t.v), i, n, v[j]);
     }
   }
+  const float wd = t.decay ? o.wd : 0.f;
   bool ok = true;
 #pragma unroll
   for (int j = 0; j < kVectors; ++j) {
-    const int i = i0 + j * kAdamwThreads * kVec, have = n - i;
+    if (!WHOLE && j * kStride >= n) break;
+    const int i = i0 + j * kStride;
     if constexpr (EIGHT) {
       decode4(mc[j], ms[j], m[j]);
       decode4(vc[j], vs[j], v[j]);
+      if constexpr (!WHOLE) {
+        zero_past(i, n, m[j]);
+        zero_past(i, n, v[j]);
+      }
     }
+    if constexpr (!WHOLE) zero_past(i, n, g[j]);
     uint32_t word[kVec], low[kVec];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       const float x = g[j][e] * gs;
       if constexpr (EIGHT) {
         ok &= adamw_value8(p[j][e], m[j][e], v[j][e], x, wd, q);
-        word[e] = value_word(static_cast<uint64_t>(t.first + at + i + e), keys);
+        word[e] = value_word(static_cast<uint64_t>(t.first + i + e), keys);
         low[e] = word[e] << 12;
       } else {
         float p1 = p[j][e], m1 = m[j][e], v1 = v[j][e];
@@ -182,110 +182,149 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw(
         p[j][e] = fine ? p1 : p[j][e];
         m[j][e] = fine ? m1 : m[j][e];
         v[j][e] = fine ? v1 : v[j][e];
-        ok &= fine;
+        ok &= fine || (!WHOLE && i + e >= n);
       }
     }
     if constexpr (EIGHT) {
       mc[j] = encode4<false>(m[j], word, inverse, ms[j]);
       vc[j] = encode4<true>(v[j], low, inverse, vs[j]);
     }
-    if (have <= 0) continue;
-    store4(t.p + at + i, have, p[j]);
-    if constexpr (COPY) store4(t.copy + at + i, have, p[j]);
+    store4<WHOLE>(t.p, i, n, p[j]);
+    if constexpr (COPY) store4<WHOLE>(t.copy, i, n, p[j]);
     if constexpr (EIGHT) {
-      store_codes(static_cast<uint8_t*>(t.m) + at + i, have, mc[j]);
-      store_codes(static_cast<uint8_t*>(t.v) + at + i, have, vc[j]);
-      if ((threadIdx.x & 7) == 0) {
-        t.m_scale[(at + i) / kMomentBlock] = static_cast<uint8_t>(ms[j]);
-        t.v_scale[(at + i) / kMomentBlock] = static_cast<uint8_t>(vs[j]);
+      store_codes<WHOLE>(static_cast<uint8_t*>(t.m), i, n, mc[j]);
+      store_codes<WHOLE>(static_cast<uint8_t*>(t.v), i, n, vc[j]);
+      if ((threadIdx.x & 7) == 0 && (WHOLE || i < n)) {
+        t.m_scale[i / kMomentBlock] = static_cast<uint8_t>(ms[j]);
+        t.v_scale[i / kMomentBlock] = static_cast<uint8_t>(vs[j]);
       }
     } else {
-      store4(static_cast<float*>(t.m) + at + i, have, m[j]);
-      store4(static_cast<float*>(t.v) + at + i, have, v[j]);
+      store4<WHOLE>(static_cast<float*>(t.m), i, n, m[j]);
+      store4<WHOLE>(static_cast<float*>(t.v), i, n, v[j]);
     }
+  }
+  return ok;
+}
+
+template <typename GT, bool EIGHT, bool COPY>
+__global__ __launch_bounds__(kAdamwThreads) void k_adamw(
+    const PlanChunk* __restrict__ plan, int chunks, uint64_t kind, OptParams o, MomentParams q,
+    StepKeys keys, const float* __restrict__ grad_scale, int32_t* __restrict__ dev_err) {
+  __shared__ float inverse[EIGHT ? kScales : 1];
+  const float gs = grad_scale ? *grad_scale : 1.f;
+  if constexpr (EIGHT) fill_scales(inverse, kAdamwThreads);
+  bool ok = true;
+  for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+    const PlanChunk t = plan[c];
+    if (t.kind != kind) {
+      if (threadIdx.x == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
+      return;
+    }
+    ok &= t.n == kChunk ? step_chunk<GT, EIGHT, COPY, true>(t, gs, o, q, keys, inverse)
+                        : step_chunk<GT, EIGHT, COPY, false>(t, gs, o, q, keys, inverse);
   }
   if (ballot(!ok) && lane_id() == 0) raise_err(dev_err, LM_DEVERR_NONFINITE);
 }
 
 // ---------------------------------------------------------------------------
-// The lazy step on the rows of a table: one wave per row (grid-stride).
+// The lazy step on the rows of a table. LANES lanes hold a row (all 64 of a wave
+// where it has more than 128 columns, else as few as cover it, a block of 32
+// values being 8 lanes), NV vectors of it at a time, and kSlots / NV rows, so that
+// a wave has kSlots vectors of every operand under way. Rows of whole vectors
+// (WHOLE) load past their end from their last vector.
 // ---------------------------------------------------------------------------
-template <typename KeyT>
+constexpr int kSlots = 4;
+
+template <typename KeyT, int LANES, int NV, bool WHOLE>
 __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
     float* __restrict__ table, int64_t V, int D, int64_t ld_table, const KeyT* __restrict__ rows,
     const int64_t* __restrict__ n_rows, int64_t rows_cap, const float* __restrict__ vals,
     int64_t ld_vals, MomentParams q, StepKeys keys, uint8_t* __restrict__ m,
     uint8_t* __restrict__ v, int64_t ld_codes, uint8_t* __restrict__ m_scale,
-    uint8_t* __restrict__ v_scale, int64_t ld_scale, int64_t nwaves,
-    int32_t* __restrict__ dev_err) {
+    uint8_t* __restrict__ v_scale, int64_t ld_scale, int32_t* __restrict__ dev_err) {
+  constexpr int kRows = kSlots / NV;              // rows a lane holds at once
+  constexpr int kPerWave = kWave / LANES * kRows;  // rows of a wave's turn
   __shared__ float inverse[kScales];
   fill_scales(inverse, kAdamwThreads);
-  const int lane = lane_id();
-  const int64_t w = first_lane(static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) +
-                               (threadIdx.x >> 6));
+  const int lane = lane_id(), part = lane % LANES, group = lane / LANES;
+  const int64_t wave = first_lane(static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) +
+                                  (threadIdx.x >> 6));
+  const int64_t waves = static_cast<int64_t>(gridDim.x) * (kAdamwThreads / kWave);
   int64_t count = first_lane(*n_rows);
   if (count > rows_cap) {
-    if (w == 0 && lane == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
+    if (wave == 0 && lane == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
     count = rows_cap;
   }
-  bool ok = true;
-  for (int64_t u = w; u < count; u += nwaves) {
-    const int64_t id = first_lane(static_cast<int64_t>(rows[u]));
-    if (!(id >= 0 && id < V)) {
-      if (lane == 0) raise_err(dev_err, LM_DEVERR_ID_RANGE);
-      continue;
+  bool ok = true, range = true;
+  for (int64_t u0 = wave * kPerWave; u0 < count; u0 += waves * kPerWave) {
+    int64_t id[kRows];
+    bool live[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const int64_t u = u0 + r * (kWave / LANES) + group;
+      id[r] = static_cast<int64_t>(rows[u < count ? u : count - 1]);
+      if constexpr (LANES == kWave) id[r] = first_lane(id[r]);
+      live[r] = u < count;
     }
-    float* prow = table + id * ld_table;
-    const float* grow = vals + u * ld_vals;
-    uint8_t *mrow = m + id * ld_codes, *vrow = v + id * ld_codes;
-    uint8_t *msrow = m_scale + id * ld_scale, *vsrow = v_scale + id * ld_scale;
-    for (int cb = 0; cb < D; cb += kVectors * kWave * kVec) {
-      float p[kVectors][kVec], g[kVectors][kVec];
-      uint32_t mc[kVectors], vc[kVectors];
-      int ms[kVectors], vs[kVectors];
 #pragma unroll
-      for (int j = 0; j < kVectors; ++j) {
-        const int c = cb + (j * kWave + lane) * kVec, have = D - c;
-        mc[j] = vc[j] = 0;
-        ms[j] = vs[j] = 0;
-        if (have <= 0) {
+    for (int r = 0; r < kRows; ++r) {
+      const bool in = id[r] >= 0 && id[r] < V;
+      range &= in || !live[r];
+      live[r] = live[r] && in;
+      id[r] = in ? id[r] : 0;  // any row of the table: loaded, not stored
+    }
+    for (int cb = 0; cb < D; cb += NV * LANES * kVec) {
+      float p[kSlots][kVec], g[kSlots][kVec];
+      uint32_t mc[kSlots], vc[kSlots];
+      int ms[kSlots], vs[kSlots];
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) p[j][e] = g[j][e] = 0.f;
-          continue;
-        }
-        load4(prow + c, have, p[j]);
-        load4(grow + c, have, g[j]);
-        mc[j] = load_codes(mrow + c, have);
-        vc[j] = load_codes(vrow + c, have);
-        ms[j] = msrow[c / kMomentBlock];
-        vs[j] = vsrow[c / kMomentBlock];
+      for (int s = 0; s < kSlots; ++s) {
+        const int r = s / NV, c = cb + (s % NV * LANES + part) * kVec;
+        const int64_t u = u0 + r * (kWave / LANES) + group;
+        const int cl = WHOLE ? (c < D ? c : D - kVec) : c;
+        const int b = (c < D ? c : D - 1) / kMomentBlock;
+        load4<WHOLE>(table + id[r] * ld_table, cl, D, p[s]);
+        load4<WHOLE>(vals + (u < count ? u : count - 1) * ld_vals, cl, D, g[s]);
+        mc[s] = load_codes<WHOLE>(m + id[r] * ld_codes, cl, D);
+        vc[s] = load_codes<WHOLE>(v + id[r] * ld_codes, cl, D);
+        ms[s] = m_scale[id[r] * ld_scale + b];
+        vs[s] = v_scale[id[r] * ld_scale + b];
       }
 #pragma unroll
-      for (int j = 0; j < kVectors; ++j) {
-        const int c = cb + (j * kWave + lane) * kVec, have = D - c;
+      for (int s = 0; s < kSlots; ++s) {
+        const int r = s / NV, c = cb + (s % NV * LANES + part) * kVec;
         float mx[kVec], vx[kVec];
         uint32_t word[kVec], low[kVec];
-        decode4(mc[j], ms[j], mx);
-        decode4(vc[j], vs[j], vx);
+        decode4(mc[s], ms[s], mx);
+        decode4(vc[s], vs[s], vx);
+        if constexpr (!WHOLE) {
+          zero_past(c, D, mx);
+          zero_past(c, D, vx);
+          zero_past(c, D, g[s]);
+        }
+        const uint64_t number = static_cast<uint64_t>(id[r]) * D + c;
+        bool fine = true;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-          ok &= adamw_value8(p[j][e], mx[e], vx[e], g[j][e], q.wd, q);
-          word[e] = value_word(static_cast<uint64_t>(id * D + c + e), keys);
+          fine &= adamw_value8(p[s][e], mx[e], vx[e], g[s][e], q.wd, q);
+          word[e] = value_word(number + e, keys);
           low[e] = word[e] << 12;
         }
-        mc[j] = encode4<false>(mx, word, inverse, ms[j]);
-        vc[j] = encode4<true>(vx, low, inverse, vs[j]);
-        if (have <= 0) continue;
-        store4(prow + c, have, p[j]);
-        store_codes(mrow + c, have, mc[j]);
-        store_codes(vrow + c, have, vc[j]);
+        mc[s] = encode4<false>(mx, word, inverse, ms[s]);
+        vc[s] = encode4<true>(vx, low, inverse, vs[s]);
+        if (!live[r] || c >= D) continue;
+        ok &= fine;
+        store4<WHOLE>(table + id[r] * ld_table, c, D, p[s]);
+        store_codes<WHOLE>(m + id[r] * ld_codes, c, D, mc[s]);
+        store_codes<WHOLE>(v + id[r] * ld_codes, c, D, vc[s]);
         if ((lane & 7) == 0) {
-          msrow[c / kMomentBlock] = static_cast<uint8_t>(ms[j]);
-          vsrow[c / kMomentBlock] = static_cast<uint8_t>(vs[j]);
+          m_scale[id[r] * ld_scale + c / kMomentBlock] = static_cast<uint8_t>(ms[s]);
+          v_scale[id[r] * ld_scale + c / kMomentBlock] = static_cast<uint8_t>(vs[s]);
         }
       }
     }
   }
+  if (ballot(!range) && lane == 0) raise_err(dev_err, LM_DEVERR_ID_RANGE);
   if (ballot(!ok) && lane == 0) raise_err(dev_err, LM_DEVERR_NONFINITE);
 }
 
@@ -300,75 +339,113 @@ int64_t adamw_plan_chunks(const int64_t* sizes, int64_t tensors) {
   return c;
 }
 
-size_t adamw_plan_bytes(const int64_t* sizes, int64_t tensors) {
-  return sizeof(PlanHead) + static_cast<size_t>(tensors) * sizeof(PlanTensor) +
-         static_cast<size_t>(adamw_plan_chunks(sizes, tensors)) * sizeof(PlanChunk);
-}
-
-static PlanHead plan_head(int64_t tensors, int64_t chunks, int gtype, int states, bool copies) {
-  PlanHead h{};
-  h.magic = kPlanMagic;
-  h.tensors = tensors;
-  h.chunks = chunks;
-  h.gtype = gtype;
-  h.states = states;
-  h.copies = copies ? 1 : 0;
-  return h;
+size_t adamw_plan_bytes(int64_t chunks) {
+  return static_cast<size_t>(chunks > 0 ? chunks : 1) * sizeof(PlanChunk);
 }
 
 void adamw_plan_write(void* const* p, const void* const* g, void* const* m, void* const* v,
                       void* const* m_scale, void* const* v_scale, void* const* copies,
                       const int64_t* sizes, const int32_t* decay, int64_t tensors, int gtype,
                       int states, void* plan) {
-  PlanHead* head = static_cast<PlanHead*>(plan);
-  *head = plan_head(tensors, adamw_plan_chunks(sizes, tensors), gtype, states, copies != nullptr);
-  PlanTensor* t = reinterpret_cast<PlanTensor*>(head + 1);
-  PlanChunk* c = reinterpret_cast<PlanChunk*>(t + tensors);
+  PlanChunk* c = static_cast<PlanChunk*>(plan);
+  const int64_t chunks = adamw_plan_chunks(sizes, tensors);
+  const uint64_t kind = plan_kind(chunks, gtype, states, copies != nullptr);
+  const int64_t state = states == 8 ? 1 : 4, grad = gtype == LM_BF16 ? 2 : 4;
+  auto at = [](const void* base, int64_t bytes) {
+    return const_cast<char*>(static_cast<const char*>(base)) + bytes;
+  };
   int64_t first = 0;
   for (int64_t i = 0; i < tensors; ++i) {
-    t[i] = PlanTensor{static_cast<float*>(p[i]), g[i], m[i], v[i],
-                      m_scale ? static_cast<uint8_t*>(m_scale[i]) : nullptr,
-                      v_scale ? static_cast<uint8_t*>(v_scale[i]) : nullptr,
-                      copies ? static_cast<uint16_t*>(copies[i]) : nullptr, sizes[i], first,
-                      !decay || decay[i] ? 1.f : 0.f, 0};
+    for (int64_t k = 0; k < sizes[i]; k += kChunk) {
+      PlanChunk x{};
+      x.p = static_cast<float*>(p[i]) + k;
+      x.g = at(g[i], k * grad);
+      x.m = at(m[i], k * state);
+      x.v = at(v[i], k * state);
+      if (states == 8) {
+        x.m_scale = static_cast<uint8_t*>(m_scale[i]) + k / kMomentBlock;
+        x.v_scale = static_cast<uint8_t*>(v_scale[i]) + k / kMomentBlock;
+      }
+      if (copies) x.copy = static_cast<uint16_t*>(copies[i]) + k;
+      x.first = first + k;
+      x.n = static_cast<int32_t>(sizes[i] - k < kChunk ? sizes[i] - k : kChunk);
+      x.decay = !decay || decay[i] ? 1 : 0;
+      x.kind = kind;
+      *c++ = x;
+    }
     first += (sizes[i] + kMomentBlock - 1) / kMomentBlock * kMomentBlock;
-    for (int64_t k = 0; k < chunks_of(sizes[i]); ++k)
-      *c++ = PlanChunk{static_cast<uint32_t>(i), static_cast<uint32_t>(k)};
   }
 }
 
 template <typename GT, bool EIGHT>
-static void adamw_launch(const PlanHead& want, const void* plan, const OptParams& o,
-                         const MomentParams& q, const StepKeys& keys, const float* grad_scale,
-                         int32_t* dev_err, hipStream_t st) {
-  const PlanHead* head = static_cast<const PlanHead*>(plan);
-  const dim3 grid(static_cast<uint32_t>(want.chunks));
-  if (want.copies)
-    k_adamw<GT, EIGHT, true><<<grid, kAdamwThreads, 0, st>>>(head, want, o, q, keys, grad_scale,
-                                                             dev_err);
+static void adamw_launch(const void* plan, int64_t chunks, uint64_t kind, bool copies,
+                         const OptParams& o, const MomentParams& q, const StepKeys& keys,
+                         const float* grad_scale, int32_t* dev_err, hipStream_t st) {
+  const PlanChunk* c = static_cast<const PlanChunk*>(plan);
+  const int64_t most = EIGHT ? 256 * 16 : INT32_MAX;
+  const dim3 grid(static_cast<uint32_t>(chunks < most ? chunks : most));
+  if (copies)
+    k_adamw<GT, EIGHT, true><<<grid, kAdamwThreads, 0, st>>>(
+        c, static_cast<int>(chunks), kind, o, q, keys, grad_scale, dev_err);
   else
-    k_adamw<GT, EIGHT, false><<<grid, kAdamwThreads, 0, st>>>(head, want, o, q, keys, grad_scale,
-                                                              dev_err);
+    k_adamw<GT, EIGHT, false><<<grid, kAdamwThreads, 0, st>>>(
+        c, static_cast<int>(chunks), kind, o, q, keys, grad_scale, dev_err);
 }
 
-int adamw_run(const void* plan, int64_t tensors, int64_t chunks, int gtype, int states,
-              bool copies, float lr, float beta1, float beta2, float eps, float weight_decay,
-              int64_t step, const float* grad_scale, uint64_t seed, int32_t* dev_err,
-              hipStream_t st) {
+int adamw_run(const void* plan, int64_t chunks, int gtype, int states, bool copies, float lr,
+              float beta1, float beta2, float eps, float weight_decay, int64_t step,
+              const float* grad_scale, uint64_t seed, int32_t* dev_err, hipStream_t st) {
   if (chunks == 0) return LM_OK;
   const OptParams o = make_opt_params(true, lr, beta1, beta2, eps, weight_decay, step, 1.f);
   const MomentParams q = make_moment_params(o, beta2, step);
-  const PlanHead want = plan_head(tensors, chunks, gtype, states, copies);
+  const uint64_t kind = plan_kind(chunks, gtype, states, copies);
   const StepKeys keys = step_keys(seed);
   const bool eight = states == 8;
-  if (gtype == LM_BF16) {
-    if (eight) adamw_launch<bf16_t, true>(want, plan, o, q, keys, grad_scale, dev_err, st);
-    else adamw_launch<bf16_t, false>(want, plan, o, q, keys, grad_scale, dev_err, st);
-  } else {
-    if (eight) adamw_launch<float, true>(want, plan, o, q, keys, grad_scale, dev_err, st);
-    else adamw_launch<float, false>(want, plan, o, q, keys, grad_scale, dev_err, st);
-  }
+  auto launch = gtype == LM_BF16 ? (eight ? adamw_launch<bf16_t, true> : adamw_launch<bf16_t, false>)
+                                 : (eight ? adamw_launch<float, true> : adamw_launch<float, false>);
+  launch(plan, chunks, kind, copies, o, q, keys, grad_scale, dev_err, st);
   return launch_status(hipGetLastError());
+}
+
+struct Rows8 {
+  float* table;
+  int64_t V;
+  int D;
+  int64_t ld_table;
+  const void* rows;
+  const int64_t* n_rows;
+  int64_t rows_cap;
+  const float* vals;
+  int64_t ld_vals;
+  MomentParams q;
+  StepKeys keys;
+  uint8_t *m, *v;
+  int64_t ld_codes;
+  uint8_t *m_scale, *v_scale;
+  int64_t ld_scale;
+  int32_t* dev_err;
+};
+
+template <typename KeyT, int LANES, int NV, bool WHOLE>
+static void rows8_launch(const Rows8& a, hipStream_t st) {
+  constexpr int kPerBlock = kAdamwThreads / LANES * (kSlots / NV);
+  const int64_t turns = (a.rows_cap + kPerBlock - 1) / kPerBlock, most = 256 * 16;
+  const dim3 grid(static_cast<uint32_t>(turns < most ? turns : most));
+  k_rows8<KeyT, LANES, NV, WHOLE><<<grid, kAdamwThreads, 0, st>>>(
+      a.table, a.V, a.D, a.ld_table, static_cast<const KeyT*>(a.rows), a.n_rows, a.rows_cap,
+      a.vals, a.ld_vals, a.q, a.keys, a.m, a.v, a.ld_codes, a.m_scale, a.v_scale, a.ld_scale,
+      a.dev_err);
+}
+
+template <typename KeyT, bool WHOLE>
+static void rows8_shape(const Rows8& a, hipStream_t st) {
+  const int vectors = (a.D + kVec - 1) / kVec;
+  if (vectors <= 8) rows8_launch<KeyT, 8, 1, WHOLE>(a, st);
+  else if (vectors <= 16) rows8_launch<KeyT, 16, 1, WHOLE>(a, st);
+  else if (vectors <= 32) rows8_launch<KeyT, 32, 1, WHOLE>(a, st);
+  else if (vectors <= 64) rows8_launch<KeyT, 64, 1, WHOLE>(a, st);
+  else if (vectors <= 128) rows8_launch<KeyT, 64, 2, WHOLE>(a, st);
+  else rows8_launch<KeyT, 64, 4, WHOLE>(a, st);
 }
 
 int rows8_run(float* table, int64_t V, int64_t D, int64_t ld_table, const void* rows, int idtype,
@@ -376,23 +453,16 @@ int rows8_run(float* table, int64_t V, int64_t D, int64_t ld_table, const void* 
               float lr, float beta1, float beta2, float eps, float weight_decay, int64_t step,
               uint8_t* m, uint8_t* v, int64_t ld_codes, uint8_t* m_scale, uint8_t* v_scale,
               int64_t ld_scale, uint64_t seed, int32_t* dev_err, hipStream_t st) {
-  if (D == 0 || rows_cap == 0) return LM_OK;
+  if (D == 0 || rows_cap == 0 || V == 0) return LM_OK;
   const OptParams o = make_opt_params(true, lr, beta1, beta2, eps, weight_decay, step, 1.f);
-  const MomentParams q = make_moment_params(o, beta2, step);
-  const StepKeys keys = step_keys(seed);
-  constexpr int kWaves = kAdamwThreads / kWave;
-  const int64_t waves = rows_cap < (int64_t(1) << 20) ? rows_cap : int64_t(1) << 20;
-  const uint32_t blocks = static_cast<uint32_t>((waves + kWaves - 1) / kWaves);
+  const Rows8 a{table, V, static_cast<int>(D), ld_table, rows, n_rows, rows_cap, vals, ld_vals,
+                make_moment_params(o, beta2, step), step_keys(seed), m, v, ld_codes, m_scale,
+                v_scale, ld_scale, dev_err};
+  const bool whole = D % kVec == 0;
   if (idtype == LM_I64)
-    k_rows8<int64_t><<<blocks, kAdamwThreads, 0, st>>>(
-        table, V, static_cast<int>(D), ld_table, static_cast<const int64_t*>(rows), n_rows,
-        rows_cap, vals, ld_vals, q, keys, m, v, ld_codes, m_scale, v_scale, ld_scale,
-        int64_t(blocks) * kWaves, dev_err);
+    whole ? rows8_shape<int64_t, true>(a, st) : rows8_shape<int64_t, false>(a, st);
   else
-    k_rows8<int32_t><<<blocks, kAdamwThreads, 0, st>>>(
-        table, V, static_cast<int>(D), ld_table, static_cast<const int32_t*>(rows), n_rows,
-        rows_cap, vals, ld_vals, q, keys, m, v, ld_codes, m_scale, v_scale, ld_scale,
-        int64_t(blocks) * kWaves, dev_err);
+    whole ? rows8_shape<int32_t, true>(a, st) : rows8_shape<int32_t, false>(a, st);
   return launch_status(hipGetLastError());
 }
 

@@ -42,16 +42,15 @@ int apply_run_f16(float* table, int64_t V, int64_t D, int64_t ld_table, const vo
                   float eps, float weight_decay, int64_t step, float* m, float* v,
                   int32_t* dev_err, hipStream_t st);
 
-size_t adamw_plan_bytes(const int64_t* sizes, int64_t tensors);
+size_t adamw_plan_bytes(int64_t chunks);
 int64_t adamw_plan_chunks(const int64_t* sizes, int64_t tensors);
 void adamw_plan_write(void* const* p, const void* const* g, void* const* m, void* const* v,
                       void* const* m_scale, void* const* v_scale, void* const* copies,
                       const int64_t* sizes, const int32_t* decay, int64_t tensors, int gtype,
                       int states, void* plan);
-int adamw_run(const void* plan, int64_t tensors, int64_t chunks, int gtype, int states,
-              bool copies, float lr, float beta1, float beta2, float eps, float weight_decay,
-              int64_t step, const float* grad_scale, uint64_t seed, int32_t* dev_err,
-              hipStream_t st);
+int adamw_run(const void* plan, int64_t chunks, int gtype, int states, bool copies, float lr,
+              float beta1, float beta2, float eps, float weight_decay, int64_t step,
+              const float* grad_scale, uint64_t seed, int32_t* dev_err, hipStream_t st);
 int rows8_run(float* table, int64_t V, int64_t D, int64_t ld_table, const void* rows, int idtype,
               const int64_t* n_rows, int64_t rows_cap, const float* vals, int64_t ld_vals,
               float lr, float beta1, float beta2, float eps, float weight_decay, int64_t step,
@@ -402,7 +401,7 @@ size_t lm_adamw_plan_bytes(const int64_t* sizes, int64_t tensors) {
     if (sizes[i] < 0 || sizes[i] > LM_ADAMW_MAX_VALUES - total) return 0;
     total += sizes[i];
   }
-  return adamw_plan_bytes(sizes, tensors);
+  return adamw_plan_bytes(adamw_plan_chunks(sizes, tensors));
 }
 
 int lm_adamw_plan(void* const* p, const void* const* g, void* const* m, void* const* v,
@@ -450,15 +449,16 @@ int lm_adamw_plan(void* const* p, const void* const* g, void* const* m, void* co
   return LM_OK;
 }
 
-int lm_adamw(const void* plan, int64_t tensors, int64_t chunks, int32_t gtype, int32_t states,
+int lm_adamw(const void* plan, size_t plan_bytes, int64_t chunks, int32_t gtype, int32_t states,
              int32_t copies, float lr, float beta1, float beta2, float eps, float weight_decay,
              int64_t step, const float* grad_scale, uint64_t seed, int32_t* dev_err,
              void* stream) {
   if (!valid_dtype(gtype) || (states != 32 && states != 8)) return LM_E_UNSUPPORTED;
-  if (tensors < 0 || chunks < 0 || chunks > INT32_MAX) return LM_E_INVAL;
+  if (chunks < 0 || chunks > INT32_MAX) return LM_E_INVAL;
   if (step < 1 || !valid_betas(beta1, beta2)) return LM_E_INVAL;
   if (chunks > 0 && (!plan || (reinterpret_cast<uintptr_t>(plan) & 7))) return LM_E_INVAL;
-  return adamw_run(plan, tensors, chunks, gtype, states, copies != 0, lr, beta1, beta2, eps,
+  if (plan_bytes < adamw_plan_bytes(chunks)) return LM_E_WORKSPACE;
+  return adamw_run(plan, chunks, gtype, states, copies != 0, lr, beta1, beta2, eps,
                    weight_decay, step, grad_scale, seed, dev_err,
                    static_cast<hipStream_t>(stream));
 }
@@ -476,7 +476,7 @@ int lm_sparse_apply_q8(float* table, int64_t V, int64_t D, int64_t ld_table, con
   if (D > (int64_t(1) << 24)) return LM_E_UNSUPPORTED;
   if (step < 1 || !valid_betas(beta1, beta2)) return LM_E_INVAL;
   if (rows_cap > 0 && D > 0 &&
-      (!table || !rows || !n_rows || !vals || !m || !v || !m_scale || !v_scale || !dev_err))
+      (!table || !rows || !n_rows || !vals || !m || !v || !m_scale || !v_scale))
     return LM_E_INVAL;
   return rows8_run(table, V, D, ld_table, rows, idtype, n_rows, rows_cap, vals, ld_vals, lr, beta1,
                    beta2, eps, weight_decay, step, m, v, ld_codes, m_scale, v_scale, ld_scale,

@@ -96,7 +96,7 @@ def _load():
     L.lm_adamw_plan_bytes.argtypes = [P, I64_]
     L.lm_adamw_plan_bytes.restype = SZ
     L.lm_adamw_plan.argtypes = [P, P, P, P, P, P, P, P, P, I64_, I32_, I32_, P, SZ, P]
-    L.lm_adamw.argtypes = [P, I64_, I64_, I32_, I32_, I32_, F, F, F, F, F, I64_, P, U64, P, P]
+    L.lm_adamw.argtypes = [P, SZ, I64_, I32_, I32_, I32_, F, F, F, F, F, I64_, P, U64, P, P]
     L.lm_sparse_apply_q8.argtypes = [P, I64_, I64_, I64_, P, I32_, P, I64_, P, I64_, F, F, F, F, F,
                                      I64_, P, P, I64_, P, P, I64_, U64, P, P]
     L.lm_rel_buckets.argtypes = [I32_, I32_, I32_, P, P, P]
@@ -632,7 +632,6 @@ class AdamwPlan(NamedTuple):
     It stands for the memory the tensors had when it was made."""
     table: torch.Tensor
     tensors: tuple
-    count: int
     chunks: int
     gtype: int
     states: int
@@ -700,7 +699,7 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
         None if decay is None else (ctypes.c_int32 * n)(*decay), n, gtype, 8 if eight else 32,
         _ptr(host), need, ctypes.byref(chunks)), "lm_adamw_plan")
     keep = tuple(tuple(x) for x in [params] + list(lists.values()))
-    return AdamwPlan(host.to(device), keep, n, chunks.value, gtype, 8 if eight else 32,
+    return AdamwPlan(host.to(device), keep, chunks.value, gtype, 8 if eight else 32,
                      "copies" in lists)
 
 
@@ -716,7 +715,7 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
     _one_of(grad_scale, torch.float32, "grad_scale")
     _one_of(dev_err, torch.int32, "dev_err")
     with _On(table.device, stream) as st:
-        _call(_lib.lm_adamw(_ptr(table), plan.count, plan.chunks, plan.gtype, plan.states,
+        _call(_lib.lm_adamw(_ptr(table), table.numel(), plan.chunks, plan.gtype, plan.states,
                             plan.copies, lr, beta1, beta2, eps, weight_decay, step,
                             _ptr(grad_scale), seed, _ptr(dev_err), st), "lm_adamw")
 
@@ -752,8 +751,6 @@ def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tenso
     _same_device(table.device, rows=rows, n_rows=n_rows, vals=vals, m=m, v=v, m_scale=m_scale,
                  v_scale=v_scale, dev_err=dev_err)
     with _On(table.device, stream) as st:
-        if dev_err is None:
-            dev_err = _own_err(table.device, stream)
         _call(_lib.lm_sparse_apply_q8(
             _ptr(table), V, D, _rows(table, "table"), _ptr(rows), _idtype(rows), _ptr(n_rows),
             min(rows.numel(), vals.shape[0]), _ptr(vals), _rows(vals, "vals"), lr, beta1, beta2,
@@ -872,6 +869,3 @@ def _on_stream(stream, make):
     with torch.cuda.stream(stream):
         return make()
 
-
-def _own_err(device, stream):
-    return _on_stream(stream, lambda: torch.zeros(1, dtype=torch.int32, device=device))

@@ -317,12 +317,14 @@ def test_adamw_refuses_another_list_with_the_plan(lz):
     p, g, m, v = (torch.ones(5000, device=DEV) for _ in range(4))
     plan = lz.adamw_plan([p], [g], [m], [v])
     err = torch.zeros(1, dtype=torch.int32, device=DEV)
-    for bad in (plan._replace(chunks=1), plan._replace(count=2), plan._replace(gtype=lz.BF16),
+    for bad in (plan._replace(chunks=1), plan._replace(gtype=lz.BF16),
                 plan._replace(states=8), plan._replace(copies=True)):
         err.zero_()
         lz.adamw(bad, dev_err=err)
         assert int(err.item()) == lz.DEVERR_CAPACITY
     assert all(bool((x == 1).all()) for x in (p, g, m, v))
+    with pytest.raises(lz.LmError):  # more chunks than the plan holds
+        lz.adamw(plan._replace(chunks=3), dev_err=err)
 
 
 def test_adamw_in_a_graph_and_on_another_stream(lz):

@@ -37,7 +37,7 @@ def lib():
     L.lm_adamw_plan_bytes.argtypes = [P, I64]
     L.lm_adamw_plan_bytes.restype = SZ
     L.lm_adamw_plan.argtypes = [P, P, P, P, P, P, P, P, P, I64, I32, I32, P, SZ, P]
-    L.lm_adamw.argtypes = [P, I64, I64, I32, I32, I32, F, F, F, F, F, I64, P, U64, P, P]
+    L.lm_adamw.argtypes = [P, SZ, I64, I32, I32, I32, F, F, F, F, F, I64, P, U64, P, P]
     L.lm_sparse_apply_q8.argtypes = [P, I64, I64, I64, P, I32, P, I64, P, I64, F, F, F, F, F, I64,
                                      P, P, I64, P, P, I64, U64, P, P]
     return L
@@ -213,7 +213,7 @@ def test_adamw_plan_refuses_memory_that_meets(lib):
 
 def test_adamw_plan_bytes(lib):
     q = lambda *s: lib.lm_adamw_plan_bytes((I64 * len(s))(*s), len(s))  # noqa: E731
-    assert q() > 0 and q(0) > 0 and q(5) > q(0)
+    assert q() > 0 and q(0) > 0 and q(5) > 0 and q(5, 5) > q(5) and q(4097) > q(4096)
     assert q(-1) == 0 and q((1 << 42) + 1) == 0 and q(1 << 41, (1 << 41) + 1) == 0
     assert lib.lm_adamw_plan_bytes(None, 1) == 0 and lib.lm_adamw_plan_bytes(None, -1) == 0
 
@@ -221,27 +221,27 @@ def test_adamw_plan_bytes(lib):
 def test_adamw_refusals(lib):
     v = P(0x1000)
 
-    def step(plan=v, tensors=1, chunks=1, gtype=0, states=32, b1=0.9, b2=0.999, t=1):
-        return lib.lm_adamw(plan, tensors, chunks, gtype, states, 0, 1e-3, b1, b2, 1e-8, 0.0, t,
+    def step(plan=v, nbytes=1 << 20, chunks=1, gtype=0, states=32, b1=0.9, b2=0.999, t=1):
+        return lib.lm_adamw(plan, nbytes, chunks, gtype, states, 0, 1e-3, b1, b2, 1e-8, 0.0, t,
                             None, 0, None, None)
     assert step(gtype=2) == UNSUPPORTED and step(states=4) == UNSUPPORTED
-    assert step(tensors=-1) == INVAL and step(chunks=-1) == INVAL and step(chunks=1 << 31) == INVAL
+    assert step(nbytes=79) == WORKSPACE and step(chunks=-1) == INVAL and step(chunks=1 << 31) == INVAL
     assert step(plan=None) == INVAL and step(plan=P(0x1004)) == INVAL
     assert step(b1=1.0) == INVAL and step(b2=-1.0) == INVAL and step(b1=float("nan")) == INVAL
     assert step(t=0) == INVAL and step(chunks=0, plan=None) == 0
 
     def rows(table=v, V=10, D=40, ld=40, ids=v, idt=0, n=v, cap=3, vals=v, ldv=40, b1=0.9, t=1,
-             m=v, mv=v, ldc=40, ms=v, vs=v, lds=2, err=v):
+             m=v, mv=v, ldc=40, ms=v, vs=v, lds=2):
         return lib.lm_sparse_apply_q8(table, V, D, ld, ids, idt, n, cap, vals, ldv, 1e-3, b1, 0.999,
-                                      1e-8, 0.0, t, m, mv, ldc, ms, vs, lds, 0, err, None)
+                                      1e-8, 0.0, t, m, mv, ldc, ms, vs, lds, 0, None, None)
     assert rows(idt=2) == UNSUPPORTED and rows(D=(1 << 24) + 1, ld=1 << 25, ldv=1 << 25,
                                                ldc=1 << 25, lds=1 << 25) == UNSUPPORTED
     for bad in (dict(V=-1), dict(D=-1), dict(cap=-1), dict(ld=39), dict(ldv=39), dict(ldc=39),
                 dict(lds=1), dict(b1=1.0), dict(t=0), dict(table=None), dict(ids=None),
                 dict(n=None), dict(vals=None), dict(m=None), dict(mv=None), dict(ms=None),
-                dict(vs=None), dict(err=None)):
+                dict(vs=None)):
         assert rows(**bad) == INVAL, bad
-    assert rows(cap=0) == 0 and rows(D=0) == 0
+    assert rows(cap=0) == 0 and rows(D=0) == 0 and rows(V=0) == 0
 
 
 def test_reference_moments():
