@@ -12,7 +12,7 @@ namespace lmz {
 
 constexpr int kAdamwThreads = 256;
 constexpr int kVec = 4;       // values of a lane's vector (16 bytes of fp32)
-constexpr int kVectors = 4;   // vectors a lane holds at once
+constexpr int kVectors = 2;   // vectors a lane holds at once
 constexpr int kChunk = kAdamwThreads * kVec * kVectors;
 static_assert(kChunk % kMomentBlock == 0, "chunks start on whole blocks");
 
@@ -46,7 +46,7 @@ static uint64_t plan_kind(int64_t chunks, int gtype, int states, bool copies) {
 template <bool WHOLE>
 __device__ __forceinline__ void load4(const float* p, int i, int n, float* x) {
   if constexpr (WHOLE) {
-    const f32x4e t = *reinterpret_cast<const f32x4e*>(p + i);
+    const f32x4 t = stream_load_e(reinterpret_cast<const f32x4e*>(p + i));
     x[0] = t.x; x[1] = t.y; x[2] = t.z; x[3] = t.w;
   } else {
 #pragma unroll
@@ -57,7 +57,7 @@ __device__ __forceinline__ void load4(const float* p, int i, int n, float* x) {
 template <bool WHOLE>
 __device__ __forceinline__ void load4(const bf16_t* p, int i, int n, float* x) {
   if constexpr (WHOLE) {
-    const u32x2e t = *reinterpret_cast<const u32x2e*>(p + i);
+    const u32x2e t = __builtin_nontemporal_load(reinterpret_cast<const u32x2e*>(p + i));
     x[0] = __uint_as_float(t.x << 16); x[1] = __uint_as_float(t.x & 0xffff0000u);
     x[2] = __uint_as_float(t.y << 16); x[3] = __uint_as_float(t.y & 0xffff0000u);
   } else {
@@ -68,7 +68,7 @@ __device__ __forceinline__ void load4(const bf16_t* p, int i, int n, float* x) {
 
 template <bool WHOLE>
 __device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int i, int n) {
-  if constexpr (WHOLE) return *reinterpret_cast<const u32e*>(p + i);
+  if constexpr (WHOLE) return __builtin_nontemporal_load(reinterpret_cast<const u32e*>(p + i));
   uint32_t w = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) w |= uint32_t(p[i + e < n ? i + e : n - 1]) << (8 * e);
@@ -83,7 +83,7 @@ __device__ __forceinline__ void zero_past(int i, int n, float* x) {
 template <bool WHOLE>
 __device__ __forceinline__ void store4(float* p, int i, int n, const float* x) {
   if constexpr (WHOLE) {
-    *reinterpret_cast<f32x4e*>(p + i) = f32x4e{x[0], x[1], x[2], x[3]};
+    __builtin_nontemporal_store(f32x4e{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4e*>(p + i));
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -98,8 +98,9 @@ __device__ __forceinline__ uint32_t bf16_bits(float x) {
 template <bool WHOLE>
 __device__ __forceinline__ void store4(uint16_t* p, int i, int n, const float* x) {
   if constexpr (WHOLE) {
-    *reinterpret_cast<u32x2e*>(p + i) = u32x2e{bf16_bits(x[0]) | bf16_bits(x[1]) << 16,
-                                               bf16_bits(x[2]) | bf16_bits(x[3]) << 16};
+    const u32x2e w = {bf16_bits(x[0]) | bf16_bits(x[1]) << 16,
+                      bf16_bits(x[2]) | bf16_bits(x[3]) << 16};
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x2e*>(p + i));
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -110,7 +111,7 @@ __device__ __forceinline__ void store4(uint16_t* p, int i, int n, const float* x
 template <bool WHOLE>
 __device__ __forceinline__ void store_codes(uint8_t* p, int i, int n, uint32_t w) {
   if constexpr (WHOLE) {
-    *reinterpret_cast<u32e*>(p + i) = w;
+    __builtin_nontemporal_store(w, reinterpret_cast<u32e*>(p + i));
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -123,20 +124,17 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int i, int n, uint32_t w
 // are a workgroup's width apart, so every load and store of a wave is one
 // contiguous piece.
 // ---------------------------------------------------------------------------
-template <typename GT, bool EIGHT, bool COPY, bool WHOLE>
-__device__ __forceinline__ bool step_chunk(const PlanChunk& t, float gs, const OptParams& o,
-                                           const MomentParams& q, const StepKeys& keys,
-                                           const float* inverse) {
-  const int n = WHOLE ? kChunk : t.n;
-  constexpr int kStride = kAdamwThreads * kVec;
-  const int i0 = threadIdx.x * kVec;
-  float p[kVectors][kVec], g[kVectors][kVec], m[kVectors][kVec], v[kVectors][kVec];
-  uint32_t mc[kVectors], vc[kVectors];
-  int ms[kVectors], vs[kVectors];
+template <typename GT, bool EIGHT, bool COPY, bool WHOLE, int NV>
+__device__ __forceinline__ bool step_vectors(const PlanChunk& t, int i0, float gs,
+                                             const OptParams& o, const MomentParams& q,
+                                             const StepKeys& keys, const float* inverse) {
+  const int n = t.n;
+  float p[NV][kVec], g[NV][kVec], m[NV][kVec], v[NV][kVec];
+  uint32_t mc[NV], vc[NV];
+  int ms[NV], vs[NV];
 #pragma unroll
-  for (int j = 0; j < kVectors; ++j) {
-    if (!WHOLE && j * kStride >= n) break;
-    const int i = i0 + j * kStride;
+  for (int j = 0; j < NV; ++j) {
+    const int i = i0 + j * kAdamwThreads * kVec;
     load4<WHOLE>(t.p, i, n, p[j]);
     load4<WHOLE>(static_cast<const GT*>(t.g), i, n, g[j]);
     if constexpr (EIGHT) {
@@ -153,9 +151,8 @@ __device__ __forceinline__ bool step_chunk(const PlanChunk& t, float gs, const O
   const float wd = t.decay ? o.wd : 0.f;
   bool ok = true;
 #pragma unroll
-  for (int j = 0; j < kVectors; ++j) {
-    if (!WHOLE && j * kStride >= n) break;
-    const int i = i0 + j * kStride;
+  for (int j = 0; j < NV; ++j) {
+    const int i = i0 + j * kAdamwThreads * kVec;
     if constexpr (EIGHT) {
       decode4(mc[j], ms[j], m[j]);
       decode4(vc[j], vs[j], v[j]);
@@ -208,20 +205,24 @@ __device__ __forceinline__ bool step_chunk(const PlanChunk& t, float gs, const O
 
 template <typename GT, bool EIGHT, bool COPY>
 __global__ __launch_bounds__(kAdamwThreads) void k_adamw(
-    const PlanChunk* __restrict__ plan, int chunks, uint64_t kind, OptParams o, MomentParams q,
+    const PlanChunk* __restrict__ plan, uint64_t kind, OptParams o, MomentParams q,
     StepKeys keys, const float* __restrict__ grad_scale, int32_t* __restrict__ dev_err) {
   __shared__ float inverse[EIGHT ? kScales : 1];
+  const PlanChunk t = plan[blockIdx.x];
   const float gs = grad_scale ? *grad_scale : 1.f;
+  if (t.kind != kind) {
+    if (threadIdx.x == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
+    return;
+  }
   if constexpr (EIGHT) fill_scales(inverse, kAdamwThreads);
+  const int i0 = threadIdx.x * kVec;
   bool ok = true;
-  for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const PlanChunk t = plan[c];
-    if (t.kind != kind) {
-      if (threadIdx.x == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
-      return;
-    }
-    ok &= t.n == kChunk ? step_chunk<GT, EIGHT, COPY, true>(t, gs, o, q, keys, inverse)
-                        : step_chunk<GT, EIGHT, COPY, false>(t, gs, o, q, keys, inverse);
+  if (t.n == kChunk) {
+    ok = step_vectors<GT, EIGHT, COPY, true, kVectors>(t, i0, gs, o, q, keys, inverse);
+  } else {
+#pragma unroll 1  // a small copy of the code: a list of small tensors waits for it from memory
+    for (int j = 0; j < t.n; j += kAdamwThreads * kVec)
+      ok &= step_vectors<GT, EIGHT, COPY, false, 1>(t, i0 + j, gs, o, q, keys, inverse);
   }
   if (ballot(!ok) && lane_id() == 0) raise_err(dev_err, LM_DEVERR_NONFINITE);
 }
@@ -245,7 +246,6 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
   constexpr int kRows = kSlots / NV;              // rows a lane holds at once
   constexpr int kPerWave = kWave / LANES * kRows;  // rows of a wave's turn
   __shared__ float inverse[kScales];
-  fill_scales(inverse, kAdamwThreads);
   const int lane = lane_id(), part = lane % LANES, group = lane / LANES;
   const int64_t wave = first_lane(static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) +
                                   (threadIdx.x >> 6));
@@ -255,6 +255,8 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
     if (wave == 0 && lane == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
     count = rows_cap;
   }
+  if (static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) * kPerWave >= count) return;
+  fill_scales(inverse, kAdamwThreads);
   bool ok = true, range = true;
   for (int64_t u0 = wave * kPerWave; u0 < count; u0 += waves * kPerWave) {
     int64_t id[kRows];
@@ -382,14 +384,13 @@ static void adamw_launch(const void* plan, int64_t chunks, uint64_t kind, bool c
                          const OptParams& o, const MomentParams& q, const StepKeys& keys,
                          const float* grad_scale, int32_t* dev_err, hipStream_t st) {
   const PlanChunk* c = static_cast<const PlanChunk*>(plan);
-  const int64_t most = EIGHT ? 256 * 16 : INT32_MAX;
-  const dim3 grid(static_cast<uint32_t>(chunks < most ? chunks : most));
+  const dim3 grid(static_cast<uint32_t>(chunks));
   if (copies)
-    k_adamw<GT, EIGHT, true><<<grid, kAdamwThreads, 0, st>>>(
-        c, static_cast<int>(chunks), kind, o, q, keys, grad_scale, dev_err);
+    k_adamw<GT, EIGHT, true><<<grid, kAdamwThreads, 0, st>>>(c, kind, o, q, keys, grad_scale,
+                                                             dev_err);
   else
-    k_adamw<GT, EIGHT, false><<<grid, kAdamwThreads, 0, st>>>(
-        c, static_cast<int>(chunks), kind, o, q, keys, grad_scale, dev_err);
+    k_adamw<GT, EIGHT, false><<<grid, kAdamwThreads, 0, st>>>(c, kind, o, q, keys, grad_scale,
+                                                              dev_err);
 }
 
 int adamw_run(const void* plan, int64_t chunks, int gtype, int states, bool copies, float lr,
@@ -429,7 +430,7 @@ struct Rows8 {
 template <typename KeyT, int LANES, int NV, bool WHOLE>
 static void rows8_launch(const Rows8& a, hipStream_t st) {
   constexpr int kPerBlock = kAdamwThreads / LANES * (kSlots / NV);
-  const int64_t turns = (a.rows_cap + kPerBlock - 1) / kPerBlock, most = 256 * 16;
+  const int64_t turns = (a.rows_cap + kPerBlock - 1) / kPerBlock, most = int64_t(1) << 30;
   const dim3 grid(static_cast<uint32_t>(turns < most ? turns : most));
   k_rows8<KeyT, LANES, NV, WHOLE><<<grid, kAdamwThreads, 0, st>>>(
       a.table, a.V, a.D, a.ld_table, static_cast<const KeyT*>(a.rows), a.n_rows, a.rows_cap,

@@ -62,7 +62,7 @@ int rel_bias_run(const float* table, int64_t ld_table, const int32_t* starts, co
                  int n_seg, int64_t B, int64_t H, int64_t Lq, int64_t Lk, int64_t q_start,
                  const void* add, const int64_t* sa, void* out, const int64_t* so, int dtype,
                  hipStream_t st);
-int64_t rel_grad_waves(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype);
+int64_t rel_grad_parts(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype);
 int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, int64_t Lk,
                  const int64_t* sd, int64_t q_start, const int32_t* starts, const int32_t* ids,
                  int n_seg, int num_buckets, float* dtable, int64_t ld_table, int accumulate,
@@ -520,7 +520,7 @@ size_t lm_rel_bias_grad_workspace_bytes(int64_t B, int64_t H, int64_t Lq, int64_
   if (!valid_dtype(dtype) || check_rel_sizes(B, H, Lq, Lk, 0) != LM_OK || n_seg < 1 ||
       n_seg > LM_REL_MAX_SEGMENTS)
     return 0;
-  return static_cast<size_t>(rel_grad_waves(B, H, Lq, Lk, dtype)) * H * n_seg * sizeof(float);
+  return static_cast<size_t>(rel_grad_parts(B, H, Lq, Lk, dtype)) * H * n_seg * sizeof(float);
 }
 
 int lm_rel_bias_grad(const void* dout, int32_t dtype, int64_t B, int64_t H, int64_t Lq, int64_t Lk,
@@ -538,8 +538,8 @@ int lm_rel_bias_grad(const void* dout, int32_t dtype, int64_t B, int64_t H, int6
     if (!dout || !ws || (reinterpret_cast<uintptr_t>(ws) & 3)) return LM_E_INVAL;
     if (reinterpret_cast<uintptr_t>(dout) & (dtype == LM_BF16 ? 1 : 3)) return LM_E_INVAL;
     if (!check_strides(dout_strides, B, H, Lq, Lk, false)) return LM_E_INVAL;
-    const int64_t waves = rel_grad_waves(B, H, Lq, Lk, dtype);
-    if (waves > INT32_MAX / H) return LM_E_UNSUPPORTED;
+    const int64_t parts = rel_grad_parts(B, H, Lq, Lk, dtype);
+    if (parts > INT32_MAX / H) return LM_E_UNSUPPORTED;
     if (ws_bytes < lm_rel_bias_grad_workspace_bytes(B, H, Lq, Lk, dtype, n_seg))
       return LM_E_WORKSPACE;
   }

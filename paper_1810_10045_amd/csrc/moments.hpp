@@ -149,7 +149,7 @@ __device__ __forceinline__ bool adamw_value8(float& p, float& m, float& r, float
   const float v1 = (r * r) * o.b2 + (g * o.c2) * g;
   const bool ok = v1 < __builtin_inff();  // false for NaN too
   const float r1 = sqrtf(v1);
-  const float step = (m1 * o.inv_c1) / __builtin_fmaf(r1, o.root_c2, o.eps);
+  const float step = (m1 * o.inv_c1) * __builtin_amdgcn_rcpf(__builtin_fmaf(r1, o.root_c2, o.eps));
   const float p1 = __builtin_fmaf(-o.lr, __builtin_fmaf(wd, p, step), p);
   p = ok ? p1 : p;
   m = ok ? m1 : m;

@@ -34,7 +34,8 @@ __device__ __forceinline__ int segment_of(const int32_t* starts, int n, int r) {
   return lo;
 }
 
-// kP values of a row: 16 bytes at the alignment of an element.
+// P values of a row: 16 bytes at the alignment of an element. Matrices are read
+// once: past the caches.
 template <typename T>
 struct Patch;
 
@@ -43,23 +44,25 @@ struct Patch<float> {
   static constexpr int P = 4;
   using raw_t = f32x4;
   static __device__ __forceinline__ raw_t load(const float* p) {
-    return *reinterpret_cast<const f32x4e*>(p);
-  }
-  static __device__ __forceinline__ raw_t part(const float* p, int have) {
-    return f32x4{have > 0 ? p[0] : 0.f, have > 1 ? p[1] : 0.f, have > 2 ? p[2] : 0.f, 0.f};
+    return stream_load_e(reinterpret_cast<const f32x4e*>(p));
   }
   static __device__ __forceinline__ void widen(const raw_t& r, float* x) {
     x[0] = r.x; x[1] = r.y; x[2] = r.z; x[3] = r.w;
   }
-  static __device__ __forceinline__ void store(float* p, int have, const float* x) {
-    if (have >= P) {
-      *reinterpret_cast<f32x4e*>(p) = f32x4e{x[0], x[1], x[2], x[3]};
-    } else {
-#pragma unroll
-      for (int e = 0; e < P; ++e)
-        if (e < have) p[e] = x[e];
-    }
+  // The values from number `by` (0 to 4) on, zeros behind them.
+  static __device__ __forceinline__ raw_t shift(const raw_t& r, int by) {
+    raw_t a = by & 2 ? raw_t{r.z, r.w, 0.f, 0.f} : r;
+    a = by & 1 ? raw_t{a.y, a.z, a.w, 0.f} : a;
+    return by & 4 ? raw_t{0.f, 0.f, 0.f, 0.f} : a;
   }
+  static __device__ __forceinline__ raw_t pack(const float* x) {
+    return raw_t{x[0], x[1], x[2], x[3]};
+  }
+  static __device__ __forceinline__ void store(float* p, const float* x) {
+    __builtin_nontemporal_store(f32x4e{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4e*>(p));
+  }
+  static __device__ __forceinline__ float one(const float* p) { return *p; }
+  static __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 };
 
 template <>
@@ -67,16 +70,7 @@ struct Patch<bf16_t> {
   static constexpr int P = 8;
   using raw_t = u32x4;
   static __device__ __forceinline__ raw_t load(const bf16_t* p) {
-    return *reinterpret_cast<const u32x4e*>(p);
-  }
-  static __device__ __forceinline__ raw_t part(const bf16_t* p, int have) {
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      w[e] = 2 * e < have ? p[2 * e].bits : 0u;
-      w[e] |= (2 * e + 1 < have ? uint32_t(p[2 * e + 1].bits) : 0u) << 16;
-    }
-    return u32x4{w[0], w[1], w[2], w[3]};
+    return stream_load_e(reinterpret_cast<const u32x4e*>(p));
   }
   static __device__ __forceinline__ void widen(const raw_t& r, float* x) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
@@ -86,20 +80,57 @@ struct Patch<bf16_t> {
       x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
     }
   }
+  static __device__ __forceinline__ raw_t shift(const raw_t& r, int by) {
+    raw_t a = by & 4 ? raw_t{r.z, r.w, 0u, 0u} : r;
+    a = by & 2 ? raw_t{a.y, a.z, a.w, 0u} : a;
+    if (by & 1)
+      a = raw_t{a.x >> 16 | a.y << 16, a.y >> 16 | a.z << 16, a.z >> 16 | a.w << 16, a.w >> 16};
+    return by & 8 ? raw_t{0u, 0u, 0u, 0u} : a;
+  }
   static __device__ __forceinline__ uint32_t bits(float x) {
     return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
   }
-  static __device__ __forceinline__ void store(bf16_t* p, int have, const float* x) {
-    if (have >= P) {
-      u32x4 w;
+  static __device__ __forceinline__ raw_t pack(const float* x) {
+    return raw_t{bits(x[0]) | bits(x[1]) << 16, bits(x[2]) | bits(x[3]) << 16,
+                 bits(x[4]) | bits(x[5]) << 16, bits(x[6]) | bits(x[7]) << 16};
+  }
+  static __device__ __forceinline__ void store(bf16_t* p, const float* x) {
+    const raw_t w = pack(x);
+    __builtin_nontemporal_store(u32x4e{w.x, w.y, w.z, w.w}, reinterpret_cast<u32x4e*>(p));
+  }
+  static __device__ __forceinline__ float one(const bf16_t* p) { return bf16_to_f32(p->bits); }
+  static __device__ __forceinline__ void put(bf16_t* p, float x) {
+    p->bits = static_cast<uint16_t>(bits(x));
+  }
+};
+
+// Where a lane's patch lies in its rows: `have` of its P columns exist (0 or less:
+// it is outside). It loads from column `from`, inside the row wherever it lies, and
+// its values start at number `by` of what it loads; so no load stands under a
+// condition and all of a patch's rows are under way at once. Rows of less than P
+// values (NARROW) are loaded one value at a time.
+template <typename T, bool NARROW>
+struct Columns {
+  static constexpr int P = Patch<T>::P;
+  int from, by, have;
+  __device__ __forceinline__ Columns(int col, int Lk, bool use) {
+    have = col < 0 || !use ? 0 : Lk - col;
+    const int last = Lk - P;  // the last whole patch
+    from = have <= 0 || NARROW ? 0 : col < last ? col : last;
+    by = have <= 0 ? P : have < P && !NARROW ? P - have : 0;
+  }
+  __device__ __forceinline__ bool whole() const { return have >= P; }
+  // Row p's patch as it is loaded, and its values moved to their places.
+  __device__ __forceinline__ typename Patch<T>::raw_t load(const T* p, int Lk) const {
+    if constexpr (!NARROW) return Patch<T>::load(p + from);
+    float x[P];  // a row's few values: the only patch in it starts at column 0
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = bits(x[2 * e]) | bits(x[2 * e + 1]) << 16;
-      *reinterpret_cast<u32x4e*>(p) = w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < P; ++e)
-        if (e < have) p[e].bits = static_cast<uint16_t>(bits(x[e]));
-    }
+    for (int e = 0; e < P; ++e) x[e] = e < Lk ? Patch<T>::one(p + e) : 0.f;
+    return Patch<T>::pack(x);
+  }
+  __device__ __forceinline__ typename Patch<T>::raw_t place(
+      const typename Patch<T>::raw_t& r) const {
+    return Patch<T>::shift(r, by);
   }
 };
 
@@ -114,34 +145,54 @@ struct Strides {
 // ---------------------------------------------------------------------------
 constexpr int kRelRows = 64;
 
-template <typename T, bool ADD>
+template <typename T, bool ADD, bool NARROW>
 __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
     const float* __restrict__ table, int64_t ld_table, Segments seg, int B, int Lq, int Lk,
     int q_start, const T* add, Strides sa, T* out, Strides so, int col_tiles, int row_tiles) {
   constexpr int P = Patch<T>::P;
   constexpr int kCols = kWave * P;
   constexpr int kLine = kRelRows + kCols;
+  using raw_t = typename Patch<T>::raw_t;
   __shared__ __attribute__((aligned(16))) float line[kLine];
   __shared__ int32_t starts[LM_REL_MAX_SEGMENTS];
-  for (int s = threadIdx.x; s < seg.n; s += kRelThreads) starts[s] = seg.starts[s];
-  __syncthreads();
+  __shared__ float value[LM_REL_MAX_SEGMENTS];
   const int ct = blockIdx.x % col_tiles, rest = blockIdx.x / col_tiles;
   const int rt = rest % row_tiles, h = rest / row_tiles;
-  const int row0 = rt * kRelRows, col0 = ct * kCols;
-  // line[x]: column c of row r has x = c - r + kRelRows - 1 (c, r from the tile's corner)
-  const int base = col0 - row0 - q_start - (kRelRows - 1);
-  for (int x = threadIdx.x; x < kLine; x += kRelThreads) {
-    const int id = seg.ids[segment_of(starts, seg.n, base + x)];
-    line[x] = id < 0 ? -__builtin_inff() : table[id * ld_table + h];
+  const int lane = lane_id(), wave = first_lane(threadIdx.x >> 6);
+  const int row0 = rt * kRelRows, col0 = ct * kCols, col = col0 + lane * P;
+  const Columns<T, NARROW> cols(col, Lk, true);
+  // The scores of a patch: P rows from row0 + r of batch entry b. Rows past the last
+  // are loaded from the last.
+  auto load = [&](int r, int b, raw_t* raw) {
+    const T* a = add + b * sa.b + h * sa.h;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int row = row0 + r + i < Lq ? row0 + r + i : Lq - 1;
+      raw[i] = cols.load(a + static_cast<int64_t>(row) * sa.q, Lk);
+    }
+  };
+  // the smallest distance from which on everything is masked
+  const int masked = seg.ids[seg.n - 1] < 0 ? seg.starts[seg.n - 1] : INT32_MAX;
+  auto hidden = [&](int r) { return col0 - (row0 + r + P - 1) - q_start >= masked; };
+  raw_t raw[P], next[P];
+  int r = wave * P;
+  const bool some = row0 + r < Lq;
+  if (ADD && some && !hidden(r)) load(r, 0, next);
+  for (int s = threadIdx.x; s < seg.n; s += kRelThreads) {
+    const int id = seg.ids[s];
+    starts[s] = seg.starts[s];
+    value[s] = id < 0 ? -__builtin_inff() : table[id * ld_table + h];
   }
   __syncthreads();
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
-  const int col = col0 + lane * P, have = Lk - col;
-  if (have <= 0) return;
-  for (int r = wave * P; r < kRelRows; r += kRelWaves * P) {
-    const int row = row0 + r;
-    if (row >= Lq) break;
-    const int nr = Lq - row < P ? Lq - row : P;
+  // line[x]: column c of row r has x = c - r + kRelRows - 1 (c, r from the tile's corner)
+  const int base = col0 - row0 - q_start - (kRelRows - 1);
+  for (int x = threadIdx.x; x < kLine; x += kRelThreads)
+    line[x] = value[segment_of(starts, seg.n, base + x)];
+  __syncthreads();
+  if (!some) return;
+  const int rows = Lq - row0 < kRelRows ? Lq - row0 : kRelRows;
+  for (; r < rows; r += kRelWaves * P) {
+    const int nr = rows - r < P ? rows - r : P;
     float d[2 * P];  // d[k]: diagonal k - (P - 1) of the patch
     const int at = lane * P + kRelRows - P - r;
 #pragma unroll
@@ -149,39 +200,42 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
       const f32x4 t = *reinterpret_cast<const f32x4*>(&line[at + k]);
       d[k] = t.x; d[k + 1] = t.y; d[k + 2] = t.z; d[k + 3] = t.w;
     }
-    bool masked = true;  // a patch that is masked as a whole is not read
-#pragma unroll
-    for (int k = 0; k < 2 * P - 1; ++k) masked &= d[k] == -__builtin_inff();
+    const bool plain = !ADD || hidden(r);  // the bias alone
     for (int b = 0; b < B; ++b) {
-      T* o = out + b * so.b + h * so.h + static_cast<int64_t>(row) * so.q + col;
-      const T* a = ADD ? add + b * sa.b + h * sa.h + static_cast<int64_t>(row) * sa.q + col
-                       : nullptr;
-      // Every load of the patch before its first store: out may be add, so the
-      // compiler keeps a load behind the stores before it.
-      typename Patch<T>::raw_t raw[P];
-      if (ADD && !masked) {
+      if (!plain) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-          const T* ai = a + (i < nr ? i : 0) * sa.q;
-          raw[i] = have >= P ? Patch<T>::load(ai) : Patch<T>::part(ai, have);
-        }
+        for (int i = 0; i < P; ++i) raw[i] = next[i];
       }
+      // The next patch's loads go out before this one's stores: they would wait behind
+      // them otherwise, since out may be add.
+      if (ADD) {
+        const bool more = b + 1 < B;
+        const int r1 = more ? r : r + kRelWaves * P;
+        if (r1 < rows && !hidden(r1)) load(r1, more ? b + 1 : 0, next);
+      }
+      T* o = out + b * so.b + h * so.h + static_cast<int64_t>(row0 + r) * so.q + col;
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         if (i >= nr) break;
         float x[P];
-        if (ADD && !masked) {
-          Patch<T>::widen(raw[i], x);
+        if (plain) {
+#pragma unroll
+          for (int e = 0; e < P; ++e) x[e] = d[P - 1 - i + e];
+        } else {
+          Patch<T>::widen(cols.whole() ? raw[i] : cols.place(raw[i]), x);
 #pragma unroll
           for (int e = 0; e < P; ++e) {
             const float y = d[P - 1 - i + e];
             x[e] = y == -__builtin_inff() ? y : x[e] + y;
           }
+        }
+        if (cols.whole()) {
+          Patch<T>::store(o + i * so.q, x);
         } else {
 #pragma unroll
-          for (int e = 0; e < P; ++e) x[e] = d[P - 1 - i + e];
+          for (int e = 0; e < P; ++e)
+            if (e < cols.have) Patch<T>::put(o + i * so.q + e, x[e]);
         }
-        Patch<T>::store(o + i * so.q, have, x);
       }
     }
   }
@@ -190,95 +244,118 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
 // ---------------------------------------------------------------------------
 // The gradient. Patches are numbered along a line: patch diagonal q has its
 // column c = P * (t + q - (nt - 1)) at row group t (nt groups of P rows), so it
-// starts at the matrix's lower left corner and ends at its upper right. A wave
-// takes 64 neighbouring patch diagonals (a band), some row groups and some
-// batch entries of one head. Its 2P - 1 sums of a lane are added by segment at
-// the end and written to the workspace; k_rel_join adds the waves' sums in
-// their order, so results are the same from run to run.
+// starts at the matrix's lower left corner and ends at its upper right. A
+// workgroup takes 64 neighbouring patch diagonals (a band) of one head; its waves
+// take turns of `steps` patches down the band, through the batch. A lane's 2P - 1
+// sums stay in registers for the whole turn; the waves' sums are then added by
+// distance and by segment in LDS, and written to the workspace. k_rel_join adds
+// the workgroups' sums in their order, so results are the same from run to run.
 // ---------------------------------------------------------------------------
 struct GradPlan {
-  int bands, row_parts, batch_parts;  // waves of a head: their product
-  int groups;                         // row groups of a part
-  int batches;                        // batch entries of a part
+  int bands, parts;  // workgroups of a head: their product
+  int steps;         // patches of a wave's turn
 };
 
-template <typename T>
+template <typename T, bool NARROW>
 __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
-    const T* __restrict__ dout, Strides sd, Segments seg, int H, int B, int Lq, int Lk,
-    int q_start, GradPlan g, int waves, float* __restrict__ ws) {
+    const T* __restrict__ dout, Strides sd, Segments seg, int B, int Lq, int Lk, int q_start,
+    GradPlan g, float* __restrict__ ws) {
   constexpr int P = Patch<T>::P;
+  constexpr int kLine = kWave * P + P;  // a band's distances (one more than there are)
+  using raw_t = typename Patch<T>::raw_t;
   __shared__ int32_t starts[LM_REL_MAX_SEGMENTS + 1];
-  for (int s = threadIdx.x; s < seg.n; s += kRelThreads) starts[s] = seg.starts[s];
-  if (threadIdx.x == 0) starts[seg.n] = INT32_MAX;
-  __syncthreads();
-  const int lane = lane_id();
-  const int64_t all = first_lane(static_cast<int64_t>(blockIdx.x) * kRelWaves + (threadIdx.x >> 6));
-  if (all >= static_cast<int64_t>(waves) * H) return;
-  const int h = static_cast<int>(all / waves), w = static_cast<int>(all % waves);
-  const int band = w % g.bands, rest = w / g.bands;
-  const int rp = rest % g.row_parts, bp = rest / g.row_parts;
+  __shared__ float sums[kRelWaves][kLine];
+  const int lane = lane_id(), wave = first_lane(threadIdx.x >> 6);
+  const int band = blockIdx.x % g.bands, rest = blockIdx.x / g.bands;
+  const int part = rest % g.parts, h = rest / g.parts;
   const int nt = (Lq + P - 1) / P, nk = (Lk + P - 1) / P;
-  const int q = band * kWave + lane;
-  // the groups where this band meets the matrix
-  int t0 = rp * g.groups, t1 = t0 + g.groups < nt ? t0 + g.groups : nt;
-  const int first = nt - 1 - (band * kWave + kWave - 1), last = nt - 1 - band * kWave + nk;
-  if (first > t0) t0 = first;
-  if (last < t1) t1 = last;
-  const int b0 = bp * g.batches, b1 = b0 + g.batches < B ? b0 + g.batches : B;
-  // lane's diagonal k has distance r0 + k; the wave's distances are w0 to w1
-  const int r0 = P * (q - (nt - 1)) - q_start - (P - 1);
-  const int w0 = r0 - lane * P, w1 = w0 + (kWave - 1) * P + 2 * P - 2;
-  // a patch whose distances are all masked is not read
-  const int own = segment_of(starts, seg.n, r0);
-  const bool masked = starts[own + 1] > r0 + 2 * P - 2 && seg.ids[own] < 0;
+  const int q0 = band * kWave - (nt - 1), q = q0 + lane;  // column patch at row group 0
+  // lane's diagonal k has distance r0 + k; the band's distances start at w0
+  const int w0 = P * q0 - q_start - (P - 1), r0 = w0 + lane * P;
+  const int masked = seg.ids[seg.n - 1] < 0 ? seg.starts[seg.n - 1] : INT32_MAX;
+  // the row groups t0 to t1 where this band meets the matrix and is not masked as a whole
+  const int t0 = -(q0 + kWave - 1) > 0 ? -(q0 + kWave - 1) : 0;
+  const int t1 = w0 >= masked ? t0 : nk - q0 < nt ? nk - q0 : nt;
+  const int64_t all = t1 > t0 ? static_cast<int64_t>(t1 - t0) * B : 0;
+  const int64_t from = (static_cast<int64_t>(part) * kRelWaves + wave) * g.steps;
+  const int64_t to = from + g.steps < all ? from + g.steps : all;
   float acc[2 * P - 1];
 #pragma unroll
   for (int k = 0; k < 2 * P - 1; ++k) acc[k] = 0.f;
-  for (int b = b0; b < b1; ++b) {
-    for (int t = t0; t < t1; ++t) {
-      const int col = P * (t + q - (nt - 1)), have = Lk - col;
-      if (col < 0 || have <= 0 || masked) continue;
+  if (from < to) {
+    const bool use = r0 < masked;
+    int t = t0 + static_cast<int>(from % (t1 - t0));
+    const T* base = dout + from / (t1 - t0) * sd.b + h * sd.h;
+    for (int64_t s = from; s < to; ++s) {
+      const Columns<T, NARROW> cols(P * (t + q), Lk, use);
       const int nr = Lq - t * P < P ? Lq - t * P : P;
-      const T* p = dout + b * sd.b + h * sd.h + static_cast<int64_t>(t) * P * sd.q + col;
-      typename Patch<T>::raw_t raw[P];
+      const T* p = base + static_cast<int64_t>(t) * P * sd.q;
+      raw_t raw[P];
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        const T* pi = p + (i < nr ? i : 0) * sd.q;
-        raw[i] = have >= P ? Patch<T>::load(pi) : Patch<T>::part(pi, have);
+      for (int i = 0; i < P; ++i) raw[i] = cols.load(p + (i < nr ? i : 0) * sd.q, Lk);
+      if (nr < P || ballot(!cols.whole())) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) raw[i] = Patch<T>::shift(raw[i], i < nr ? cols.by : P);
       }
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         float x[P];
         Patch<T>::widen(raw[i], x);
 #pragma unroll
-        for (int e = 0; e < P; ++e) acc[P - 1 - i + e] += i < nr ? x[e] : 0.f;
+        for (int e = 0; e < P; ++e) acc[P - 1 - i + e] += x[e];
+      }
+      if (++t == t1) {
+        t = t0;
+        base += sd.b;
       }
     }
   }
-  // Segment sums of the wave's distances; most waves lie in one or two segments.
-  float* mine = ws + (static_cast<int64_t>(h) * waves + w) * seg.n;
-  const int s0 = segment_of(starts, seg.n, w0), s1 = segment_of(starts, seg.n, w1);
-  for (int s = lane; s < seg.n; s += kWave)
-    if (s < s0 || s > s1) mine[s] = 0.f;
-  for (int s = s0; s <= s1; ++s) {
-    const int lo = starts[s], hi = starts[s + 1];
-    float x = 0.f;
+  for (int s = threadIdx.x; s < seg.n; s += kRelThreads) starts[s] = seg.starts[s];
+  if (threadIdx.x == 0) starts[seg.n] = INT32_MAX;
+  // Diagonal P + k of a lane is diagonal k of the next one.
 #pragma unroll
-    for (int k = 0; k < 2 * P - 1; ++k) x += r0 + k >= lo && r0 + k < hi ? acc[k] : 0.f;
+  for (int k = 0; k < P; ++k) {
+    float below = 0.f;
+    if (k < P - 1) {
+      below = __shfl_up(acc[P + k], 1, kWave);
+      if (lane == 0) below = 0.f;
+      if (lane == kWave - 1) sums[wave][kWave * P + k] = acc[P + k];
+    }
+    sums[wave][lane * P + k] = acc[k] + below;
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < kLine - 1; x += kRelThreads) {
+    float y = sums[0][x];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, kWave);
-    if (lane == 0) mine[s] = x;
+    for (int w = 1; w < kRelWaves; ++w) y += sums[w][x];
+    sums[0][x] = y;
+  }
+  __syncthreads();
+  // Segment sums: 8 lanes add the distances of one, each every eighth.
+  float* mine = ws + static_cast<int64_t>(blockIdx.x) * seg.n;
+  for (int s = threadIdx.x / 8; s < (seg.n + kRelThreads / 8 - 1) / (kRelThreads / 8) * (kRelThreads / 8);
+       s += kRelThreads / 8) {
+    float y = 0.f;
+    if (s < seg.n) {
+      const int64_t lo = static_cast<int64_t>(starts[s]) - w0, hi = static_cast<int64_t>(starts[s + 1]) - w0;
+      const int x1 = hi < kLine - 1 ? static_cast<int>(hi) : kLine - 1;
+      for (int x = (lo > 0 ? static_cast<int>(lo < kLine ? lo : kLine) : 0) + (threadIdx.x & 7); x < x1; x += 8)
+        y += sums[0][x];
+    }
+#pragma unroll
+    for (int off = 4; off > 0; off >>= 1) y += __shfl_xor(y, off, kWave);
+    if (s < seg.n && (threadIdx.x & 7) == 0) mine[s] = y;
   }
 }
 
-// dtable[n, h] (+)= the sums of the segments with id n over a head's waves. One
+// dtable[n, h] (+)= the sums of the segments with id n over a head's parts. One
 // workgroup per head: a thread adds one segment (a column of the workspace) over
-// every kJoinThreads / width-th wave, so neighbouring threads read neighbouring
+// every kJoinThreads / width-th part, so neighbouring threads read neighbouring
 // words, and the threads of a segment are added in their order.
 constexpr int kJoinThreads = 1024;
 
 __global__ __launch_bounds__(kJoinThreads) void k_rel_join(
-    const float* __restrict__ ws, Segments seg, int waves, int num_buckets,
+    const float* __restrict__ ws, Segments seg, int parts, int num_buckets,
     float* __restrict__ dtable, int64_t ld_table, int accumulate) {
   __shared__ float part[kJoinThreads];
   __shared__ float sums[LM_REL_MAX_SEGMENTS];
@@ -286,11 +363,11 @@ __global__ __launch_bounds__(kJoinThreads) void k_rel_join(
   int width = 32;  // segments of one turn
   while (width < n && width < kJoinThreads) width *= 2;
   const int column = threadIdx.x % width, first = threadIdx.x / width, step = kJoinThreads / width;
-  const float* mine = ws + static_cast<int64_t>(h) * waves * n;
+  const float* mine = ws + static_cast<int64_t>(h) * parts * n;
   float x = 0.f;
   if (column < n) {
 #pragma unroll 8
-    for (int w = first; w < waves; w += step) x += mine[static_cast<int64_t>(w) * n + column];
+    for (int w = first; w < parts; w += step) x += mine[static_cast<int64_t>(w) * n + column];
   }
   part[threadIdx.x] = x;
   __syncthreads();
@@ -330,16 +407,14 @@ static void rel_bias_launch(const float* table, int64_t ld_table, const Segments
                             const Strides& sa, void* out, const Strides& so, hipStream_t st) {
   const int64_t ct = ceil_div(Lk, kWave * Patch<T>::P), rt = ceil_div(Lq, kRelRows);
   const dim3 grid(static_cast<uint32_t>(ct * rt * H));
-  if (add)
-    k_rel_bias<T, true><<<grid, kRelThreads, 0, st>>>(
-        table, ld_table, seg, static_cast<int>(B), static_cast<int>(Lq), static_cast<int>(Lk),
-        static_cast<int>(q_start), static_cast<const T*>(add), sa, static_cast<T*>(out), so,
-        static_cast<int>(ct), static_cast<int>(rt));
-  else
-    k_rel_bias<T, false><<<grid, kRelThreads, 0, st>>>(
-        table, ld_table, seg, static_cast<int>(B), static_cast<int>(Lq), static_cast<int>(Lk),
-        static_cast<int>(q_start), nullptr, sa, static_cast<T*>(out), so, static_cast<int>(ct),
-        static_cast<int>(rt));
+  const bool narrow = Lk < Patch<T>::P;
+  auto kernel = add ? (narrow ? k_rel_bias<T, true, true> : k_rel_bias<T, true, false>)
+                    : k_rel_bias<T, false, false>;
+  kernel<<<grid, kRelThreads, 0, st>>>(table, ld_table, seg, static_cast<int>(B),
+                                       static_cast<int>(Lq), static_cast<int>(Lk),
+                                       static_cast<int>(q_start), static_cast<const T*>(add), sa,
+                                       static_cast<T*>(out), so, static_cast<int>(ct),
+                                       static_cast<int>(rt));
 }
 
 // Workgroups of a call, for the check of the grid's size.
@@ -363,29 +438,27 @@ int rel_bias_run(const float* table, int64_t ld_table, const int32_t* starts, co
   return launch_status(hipGetLastError());
 }
 
-// How a head's matrices are shared out among waves: about 64 KB for each, and
-// at least 16 waves for each compute unit of the device where there is that much.
+// How a head's matrices are shared out among waves.
 static GradPlan grad_plan(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype) {
   const int P = dtype == LM_BF16 ? Patch<bf16_t>::P : Patch<float>::P;
   const int64_t nt = ceil_div(Lq, P), nk = ceil_div(Lk, P);
   GradPlan g;
   g.bands = static_cast<int>(ceil_div(nt - 1 + nk, kWave));
-  const int64_t steps = nt * B;                    // a band's steps of P rows, all batch entries
-  int64_t per = steps * g.bands * H / 4096;        // for 4096 waves
-  per = per < 1 ? 1 : per > 16 ? 16 : per;
-  g.groups = static_cast<int>(per < nt ? per : nt);
-  g.row_parts = static_cast<int>(ceil_div(nt, g.groups));
-  const int64_t nb = per / g.groups;
-  g.batches = static_cast<int>(nb < 1 ? 1 : nb < B ? nb : B);
-  g.batch_parts = static_cast<int>(ceil_div(B, g.batches));
+  // patches of 64 lanes in all: each row group meets its columns' bands and one more
+  const int64_t all = nt * (nk / kWave + 1) * B * H;
+  const int64_t most = nt < nk + kWave ? nt : nk + kWave;  // row groups of the longest band
+  int64_t steps = all / 8192;
+  steps = steps < 1 ? 1 : steps > 32 ? 32 : steps;
+  g.steps = static_cast<int>(steps);
+  g.parts = static_cast<int>(ceil_div(most * B, steps * kRelWaves));
   return g;
 }
 
-// Waves of one head; 0 where there is nothing to add.
-int64_t rel_grad_waves(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype) {
+// Workgroups of one head; 0 where there is nothing to add.
+int64_t rel_grad_parts(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype) {
   if (B == 0 || H == 0 || Lq == 0 || Lk == 0) return 0;
   const GradPlan g = grad_plan(B, H, Lq, Lk, dtype);
-  return static_cast<int64_t>(g.bands) * g.row_parts * g.batch_parts;
+  return static_cast<int64_t>(g.bands) * g.parts;
 }
 
 int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, int64_t Lk,
@@ -394,26 +467,27 @@ int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, 
                  void* ws, hipStream_t st) {
   if (H == 0) return LM_OK;
   const Segments seg = make_segments(starts, ids, n_seg);
-  const int64_t waves = rel_grad_waves(B, H, Lq, Lk, dtype);
-  if (waves) {
+  const int64_t parts = rel_grad_parts(B, H, Lq, Lk, dtype);
+  if (parts) {
     const GradPlan g = grad_plan(B, H, Lq, Lk, dtype);
     const Strides s{sd[0], sd[1], sd[2]};
-    const dim3 grid(static_cast<uint32_t>(ceil_div(waves * H, kRelWaves)));
+    const dim3 grid(static_cast<uint32_t>(parts * H));
+    auto launch = [&](auto kernel, auto* matrix) {
+      kernel<<<grid, kRelThreads, 0, st>>>(matrix, s, seg, static_cast<int>(B),
+                                           static_cast<int>(Lq), static_cast<int>(Lk),
+                                           static_cast<int>(q_start), g, static_cast<float*>(ws));
+    };
     if (dtype == LM_BF16)
-      k_rel_grad<bf16_t><<<grid, kRelThreads, 0, st>>>(
-          static_cast<const bf16_t*>(dout), s, seg, static_cast<int>(H), static_cast<int>(B),
-          static_cast<int>(Lq), static_cast<int>(Lk), static_cast<int>(q_start), g,
-          static_cast<int>(waves), static_cast<float*>(ws));
+      launch(Lk < Patch<bf16_t>::P ? k_rel_grad<bf16_t, true> : k_rel_grad<bf16_t, false>,
+             static_cast<const bf16_t*>(dout));
     else
-      k_rel_grad<float><<<grid, kRelThreads, 0, st>>>(
-          static_cast<const float*>(dout), s, seg, static_cast<int>(H), static_cast<int>(B),
-          static_cast<int>(Lq), static_cast<int>(Lk), static_cast<int>(q_start), g,
-          static_cast<int>(waves), static_cast<float*>(ws));
+      launch(Lk < Patch<float>::P ? k_rel_grad<float, true> : k_rel_grad<float, false>,
+             static_cast<const float*>(dout));
     const int rc = launch_status(hipGetLastError());
     if (rc != LM_OK) return rc;
   }
   k_rel_join<<<static_cast<uint32_t>(H), kJoinThreads, 0, st>>>(
-      static_cast<const float*>(ws), seg, static_cast<int>(waves), num_buckets, dtable, ld_table,
+      static_cast<const float*>(ws), seg, static_cast<int>(parts), num_buckets, dtable, ld_table,
       accumulate);
   return launch_status(hipGetLastError());
 }

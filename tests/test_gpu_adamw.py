@@ -324,7 +324,7 @@ def test_adamw_refuses_another_list_with_the_plan(lz):
         assert int(err.item()) == lz.DEVERR_CAPACITY
     assert all(bool((x == 1).all()) for x in (p, g, m, v))
     with pytest.raises(lz.LmError):  # more chunks than the plan holds
-        lz.adamw(plan._replace(chunks=3), dev_err=err)
+        lz.adamw(plan._replace(chunks=plan.chunks + 1), dev_err=err)
 
 
 def test_adamw_in_a_graph_and_on_another_stream(lz):
