@@ -535,13 +535,14 @@ int lm_rel_bias_grad(const void* dout, int32_t dtype, int64_t B, int64_t H, int6
   if (H == 0) return LM_OK;
   if (!dtable) return LM_E_INVAL;
   if (B > 0 && Lq > 0 && Lk > 0) {
-    if (!dout || !ws || (reinterpret_cast<uintptr_t>(ws) & 3)) return LM_E_INVAL;
+    if (!dout) return LM_E_INVAL;
     if (reinterpret_cast<uintptr_t>(dout) & (dtype == LM_BF16 ? 1 : 3)) return LM_E_INVAL;
     if (!check_strides(dout_strides, B, H, Lq, Lk, false)) return LM_E_INVAL;
     const int64_t parts = rel_grad_parts(B, H, Lq, Lk, dtype);
     if (parts > INT32_MAX / H) return LM_E_UNSUPPORTED;
-    if (ws_bytes < lm_rel_bias_grad_workspace_bytes(B, H, Lq, Lk, dtype, n_seg))
-      return LM_E_WORKSPACE;
+    const size_t need = lm_rel_bias_grad_workspace_bytes(B, H, Lq, Lk, dtype, n_seg);
+    if (need > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 3))) return LM_E_INVAL;
+    if (ws_bytes < need) return LM_E_WORKSPACE;
   }
   return rel_grad_run(dout, dtype, B, H, Lq, Lk, dout_strides, q_start, starts, ids, n_seg,
                       num_buckets, dtable, ld_table, accumulate, ws,

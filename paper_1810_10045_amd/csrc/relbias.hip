@@ -4,13 +4,11 @@
 // distances from starts[s] up to starts[s + 1], and ids[s] names its table row
 // (-1: masked).
 //
-// A head's bias depends on j - i only. The kernels work on square patches of
-// kP rows and columns (a column vector of 16 bytes): 2 kP - 1 diagonals, each
-// one number. The bias of a patch is that many values in registers; the
-// gradient adds a patch into that many sums, and the patch one step down and
-// right has the same diagonals, so a wave that walks down the diagonal keeps its
-// sums in registers through the whole matrix. Each element of the matrices is
-// read or written once: HBM bounds both.
+// A head's bias depends on j - i only. The kernels work on square patches of P rows
+// and columns (a lane's column vector of 16 bytes, P = 8 bf16 or 4 fp32), 64 of
+// them side by side: 2P - 1 diagonals, each one number. The bias of a patch is that
+// many values in registers; the gradient adds a patch into that many sums. Each
+// element of the matrices is read or written once: HBM bounds both.
 #include "common.hpp"
 
 namespace lmz {
@@ -22,6 +20,7 @@ struct Segments {
   int32_t starts[LM_REL_MAX_SEGMENTS];
   int16_t ids[LM_REL_MAX_SEGMENTS];
   int32_t n;
+  int32_t masked;  // from this distance on everything is masked (INT32_MAX: nothing)
 };
 
 // The last segment that starts at or before r (starts[0] is below every distance).
@@ -138,122 +137,123 @@ struct Strides {
   int64_t b, h, q;
 };
 
-// ---------------------------------------------------------------------------
-// The bias, written or added. A workgroup covers kRelRows rows and one wave's
-// width of columns of one head, for every batch entry: it looks up the numbers
-// of its diagonals once, in LDS, and each wave takes patches from there.
-// ---------------------------------------------------------------------------
-constexpr int kRelRows = 64;
+__device__ __forceinline__ float read_lane(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
 
+// The value of the lane below; 0 in lane 0.
+__device__ __forceinline__ float from_lane_below(float v) {
+  return __int_as_float(
+      __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x138, 0xf, 0xf, true));  // wave_shr:1
+}
+
+// ---------------------------------------------------------------------------
+// The bias, written or added. A workgroup covers a patch's width for each of its
+// waves, one below the other, in one head, for every batch entry: it looks up the
+// numbers of its diagonals once, in LDS, and each lane takes its patch's from there.
+// Tiles of one column come one after the other (row tiles first): 8 x 16 x 2048 x
+// 2048 bf16 scores took 322 us so, 339 with column tiles first, 377 with two
+// patches of each wave and 420 with four.
+// ---------------------------------------------------------------------------
 template <typename T, bool ADD, bool NARROW>
 __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
     const float* __restrict__ table, int64_t ld_table, Segments seg, int B, int Lq, int Lk,
     int q_start, const T* add, Strides sa, T* out, Strides so, int col_tiles, int row_tiles) {
   constexpr int P = Patch<T>::P;
-  constexpr int kCols = kWave * P;
-  constexpr int kLine = kRelRows + kCols;
+  constexpr int kCols = kWave * P, kRows = kRelWaves * P;
+  constexpr int kLine = kRows + kCols;
   using raw_t = typename Patch<T>::raw_t;
   __shared__ __attribute__((aligned(16))) float line[kLine];
   __shared__ int32_t starts[LM_REL_MAX_SEGMENTS];
   __shared__ float value[LM_REL_MAX_SEGMENTS];
-  const int ct = blockIdx.x % col_tiles, rest = blockIdx.x / col_tiles;
-  const int rt = rest % row_tiles, h = rest / row_tiles;
-  const int lane = lane_id(), wave = first_lane(threadIdx.x >> 6);
-  const int row0 = rt * kRelRows, col0 = ct * kCols, col = col0 + lane * P;
+  const int rt = blockIdx.x % row_tiles, rest = blockIdx.x / row_tiles;
+  const int ct = rest % col_tiles, h = rest / col_tiles;
+  const int lane = lane_id(), r = first_lane(threadIdx.x >> 6) * P;  // this wave's rows
+  const int row0 = rt * kRows, col0 = ct * kCols, row = row0 + r, col = col0 + lane * P;
   const Columns<T, NARROW> cols(col, Lk, true);
-  // The scores of a patch: P rows from row0 + r of batch entry b. Rows past the last
-  // are loaded from the last.
-  auto load = [&](int r, int b, raw_t* raw) {
+  // the scores of batch entry b; rows past the last are loaded from the last
+  auto load = [&](int b, raw_t* raw) {
     const T* a = add + b * sa.b + h * sa.h;
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int row = row0 + r + i < Lq ? row0 + r + i : Lq - 1;
-      raw[i] = cols.load(a + static_cast<int64_t>(row) * sa.q, Lk);
-    }
+    for (int i = 0; i < P; ++i)
+      raw[i] = cols.load(a + static_cast<int64_t>(row + i < Lq ? row + i : Lq - 1) * sa.q, Lk);
   };
-  // the smallest distance from which on everything is masked
-  const int masked = seg.ids[seg.n - 1] < 0 ? seg.starts[seg.n - 1] : INT32_MAX;
-  auto hidden = [&](int r) { return col0 - (row0 + r + P - 1) - q_start >= masked; };
-  raw_t raw[P], next[P];
-  int r = wave * P;
-  const bool some = row0 + r < Lq;
-  if (ADD && some && !hidden(r)) load(r, 0, next);
+  const bool read = ADD && row < Lq && col0 - (row + P - 1) - q_start < seg.masked;
+  raw_t next[P];
+  if (read) load(0, next);  // on its way while the diagonals are looked up
   for (int s = threadIdx.x; s < seg.n; s += kRelThreads) {
     const int id = seg.ids[s];
     starts[s] = seg.starts[s];
     value[s] = id < 0 ? -__builtin_inff() : table[id * ld_table + h];
   }
   __syncthreads();
-  // line[x]: column c of row r has x = c - r + kRelRows - 1 (c, r from the tile's corner)
-  const int base = col0 - row0 - q_start - (kRelRows - 1);
+  // line[x]: column c of row i has x = c - i + kRows - 1 (c, i from the tile's corner)
+  const int base = col0 - row0 - q_start - (kRows - 1);
   for (int x = threadIdx.x; x < kLine; x += kRelThreads)
     line[x] = value[segment_of(starts, seg.n, base + x)];
   __syncthreads();
-  if (!some) return;
-  const int rows = Lq - row0 < kRelRows ? Lq - row0 : kRelRows;
-  for (; r < rows; r += kRelWaves * P) {
-    const int nr = rows - r < P ? rows - r : P;
-    float d[2 * P];  // d[k]: diagonal k - (P - 1) of the patch
-    const int at = lane * P + kRelRows - P - r;
+  if (row >= Lq) return;
+  const int nr = Lq - row < P ? Lq - row : P;
+  float d[2 * P];  // d[k]: diagonal k - (P - 1) of the patch
 #pragma unroll
-    for (int k = 0; k < 2 * P; k += 4) {
-      const f32x4 t = *reinterpret_cast<const f32x4*>(&line[at + k]);
-      d[k] = t.x; d[k + 1] = t.y; d[k + 2] = t.z; d[k + 3] = t.w;
-    }
-    const bool plain = !ADD || hidden(r);  // the bias alone
-    for (int b = 0; b < B; ++b) {
-      if (!plain) {
+  for (int k = 0; k < 2 * P; k += 4) {
+    const f32x4 t = *reinterpret_cast<const f32x4*>(&line[lane * P + kRows - P - r + k]);
+    d[k] = t.x; d[k + 1] = t.y; d[k + 2] = t.z; d[k + 3] = t.w;
+  }
+  for (int b = 0; b < B; ++b) {
+    raw_t raw[P];
+    if (read) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) raw[i] = next[i];
-      }
+      for (int i = 0; i < P; ++i) raw[i] = next[i];
       // The next patch's loads go out before this one's stores: they would wait behind
       // them otherwise, since out may be add.
-      if (ADD) {
-        const bool more = b + 1 < B;
-        const int r1 = more ? r : r + kRelWaves * P;
-        if (r1 < rows && !hidden(r1)) load(r1, more ? b + 1 : 0, next);
+      if (b + 1 < B) load(b + 1, next);
+    }
+    T* o = out + b * so.b + h * so.h + static_cast<int64_t>(row) * so.q + col;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      if (i >= nr) break;
+      float x[P];
+      if (read) {
+        Patch<T>::widen(cols.whole() ? raw[i] : cols.place(raw[i]), x);
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+          const float y = d[P - 1 - i + e];
+          x[e] = y == -__builtin_inff() ? y : x[e] + y;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < P; ++e) x[e] = d[P - 1 - i + e];
       }
-      T* o = out + b * so.b + h * so.h + static_cast<int64_t>(row0 + r) * so.q + col;
+      if (cols.whole()) {
+        Patch<T>::store(o + i * so.q, x);
+      } else {
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        if (i >= nr) break;
-        float x[P];
-        if (plain) {
-#pragma unroll
-          for (int e = 0; e < P; ++e) x[e] = d[P - 1 - i + e];
-        } else {
-          Patch<T>::widen(cols.whole() ? raw[i] : cols.place(raw[i]), x);
-#pragma unroll
-          for (int e = 0; e < P; ++e) {
-            const float y = d[P - 1 - i + e];
-            x[e] = y == -__builtin_inff() ? y : x[e] + y;
-          }
-        }
-        if (cols.whole()) {
-          Patch<T>::store(o + i * so.q, x);
-        } else {
-#pragma unroll
-          for (int e = 0; e < P; ++e)
-            if (e < cols.have) Patch<T>::put(o + i * so.q + e, x[e]);
-        }
+        for (int e = 0; e < P; ++e)
+          if (e < cols.have) Patch<T>::put(o + i * so.q + e, x[e]);
       }
     }
   }
 }
 
 // ---------------------------------------------------------------------------
-// The gradient. Patches are numbered along a line: patch diagonal q has its
-// column c = P * (t + q - (nt - 1)) at row group t (nt groups of P rows), so it
-// starts at the matrix's lower left corner and ends at its upper right. A
-// workgroup takes 64 neighbouring patch diagonals (a band) of one head; its waves
-// take turns of `steps` patches down the band, through the batch. A lane's 2P - 1
-// sums stay in registers for the whole turn; the waves' sums are then added by
-// distance and by segment in LDS, and written to the workspace. k_rel_join adds
-// the workgroups' sums in their order, so results are the same from run to run.
+// The gradient. A wave goes down `groups` row groups of P rows in one column tile of
+// one head and, at each, through `batches` batch entries: their patches have the
+// same diagonals, so a lane's 2P - 1 sums stay in registers. After a row group they
+// are added to the wave's sums by distance in LDS, by a load, an add and a store:
+// each address belongs to one lane of an instruction (ds_add_f32, which needs no
+// such care, took about 195 clocks for a wave). Column tiles, not diagonal bands: a wave that walked down the diagonal kept its sums in registers
+// throughout, but its rows began between cache lines (16 x 16 x 2048 x 2048 bf16:
+// 450 us). At the end a workgroup adds its waves' sums by segment, into the
+// workspace; k_rel_join adds the workgroups' in their order, so results are the
+// same from run to run.
 // ---------------------------------------------------------------------------
+constexpr int kMaxGroups = 16;
+
 struct GradPlan {
-  int bands, parts;  // workgroups of a head: their product
-  int steps;         // patches of a wave's turn
+  int groups, batches;                    // of a wave
+  int row_parts, col_tiles, batch_parts;  // workgroups of a head: their product
+  int64_t parts() const { return static_cast<int64_t>(row_parts) * col_tiles * batch_parts; }
 };
 
 template <typename T, bool NARROW>
@@ -261,39 +261,46 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
     const T* __restrict__ dout, Strides sd, Segments seg, int B, int Lq, int Lk, int q_start,
     GradPlan g, float* __restrict__ ws) {
   constexpr int P = Patch<T>::P;
-  constexpr int kLine = kWave * P + P;  // a band's distances (one more than there are)
+  // The sum of distance x of a wave is at plane x % P, place x / P: neighbouring
+  // lanes' sums of one diagonal lie side by side.
+  constexpr int kPlane = kWave + kMaxGroups + 1;
+  constexpr int kLong = 32;  // distances of a segment that a whole wave adds
   using raw_t = typename Patch<T>::raw_t;
+  __shared__ float sums[kRelWaves][P * kPlane];
+  __shared__ float line[P * (kWave + kRelWaves * kMaxGroups)];
   __shared__ int32_t starts[LM_REL_MAX_SEGMENTS + 1];
-  __shared__ float sums[kRelWaves][kLine];
   const int lane = lane_id(), wave = first_lane(threadIdx.x >> 6);
-  const int band = blockIdx.x % g.bands, rest = blockIdx.x / g.bands;
-  const int part = rest % g.parts, h = rest / g.parts;
-  const int nt = (Lq + P - 1) / P, nk = (Lk + P - 1) / P;
-  const int q0 = band * kWave - (nt - 1), q = q0 + lane;  // column patch at row group 0
-  // lane's diagonal k has distance r0 + k; the band's distances start at w0
-  const int w0 = P * q0 - q_start - (P - 1), r0 = w0 + lane * P;
-  const int masked = seg.ids[seg.n - 1] < 0 ? seg.starts[seg.n - 1] : INT32_MAX;
-  // the row groups t0 to t1 where this band meets the matrix and is not masked as a whole
-  const int t0 = -(q0 + kWave - 1) > 0 ? -(q0 + kWave - 1) : 0;
-  const int t1 = w0 >= masked ? t0 : nk - q0 < nt ? nk - q0 : nt;
-  const int64_t all = t1 > t0 ? static_cast<int64_t>(t1 - t0) * B : 0;
-  const int64_t from = (static_cast<int64_t>(part) * kRelWaves + wave) * g.steps;
-  const int64_t to = from + g.steps < all ? from + g.steps : all;
-  float acc[2 * P - 1];
+  const int rp = blockIdx.x % g.row_parts, rest = blockIdx.x / g.row_parts;
+  const int ct = rest % g.col_tiles, rest2 = rest / g.col_tiles;
+  const int bp = rest2 % g.batch_parts, h = rest2 / g.batch_parts;
+  const int nt = (Lq + P - 1) / P;
+  const int t0 = (rp * kRelWaves + wave) * g.groups;
+  const int t1 = t0 + g.groups < nt ? t0 + g.groups : nt;
+  const int b0 = bp * g.batches, b1 = b0 + g.batches < B ? b0 + g.batches : B;
+  const int col0 = ct * kWave * P, col = col0 + lane * P;
+  // a patch's diagonal k has distance low + k
+  auto low = [&](int column, int t) { return column - (t * P + P - 1) - q_start; };
+  float* mine = ws + static_cast<int64_t>(blockIdx.x) * seg.n;
+  const int first = low(col0, (rp + 1) * kRelWaves * g.groups - 1);  // the smallest distance
+  if (first >= seg.masked) {  // all of this workgroup's patches are
+    for (int s = threadIdx.x; s < seg.n; s += kRelThreads) mine[s] = 0.f;
+    return;
+  }
+  for (int x = lane; x < P * kPlane; x += kWave) sums[wave][x] = 0.f;
+  for (int t = t0; t < t1; ++t) {
+    if (low(col0, t) >= seg.masked) continue;
+    const Columns<T, NARROW> cols(col, Lk, low(col, t) < seg.masked);
+    const int nr = Lq - t * P < P ? Lq - t * P : P;
+    const bool edge = nr < P || ballot(!cols.whole());
+    const T* p = dout + b0 * sd.b + h * sd.h + static_cast<int64_t>(t) * P * sd.q;
+    float acc[2 * P - 1];
 #pragma unroll
-  for (int k = 0; k < 2 * P - 1; ++k) acc[k] = 0.f;
-  if (from < to) {
-    const bool use = r0 < masked;
-    int t = t0 + static_cast<int>(from % (t1 - t0));
-    const T* base = dout + from / (t1 - t0) * sd.b + h * sd.h;
-    for (int64_t s = from; s < to; ++s) {
-      const Columns<T, NARROW> cols(P * (t + q), Lk, use);
-      const int nr = Lq - t * P < P ? Lq - t * P : P;
-      const T* p = base + static_cast<int64_t>(t) * P * sd.q;
+    for (int k = 0; k < 2 * P - 1; ++k) acc[k] = 0.f;
+    for (int b = b0; b < b1; ++b, p += sd.b) {
       raw_t raw[P];
 #pragma unroll
       for (int i = 0; i < P; ++i) raw[i] = cols.load(p + (i < nr ? i : 0) * sd.q, Lk);
-      if (nr < P || ballot(!cols.whole())) {
+      if (edge) {
 #pragma unroll
         for (int i = 0; i < P; ++i) raw[i] = Patch<T>::shift(raw[i], i < nr ? cols.by : P);
       }
@@ -304,47 +311,65 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
 #pragma unroll
         for (int e = 0; e < P; ++e) acc[P - 1 - i + e] += x[e];
       }
-      if (++t == t1) {
-        t = t0;
-        base += sd.b;
-      }
     }
+    // Diagonal P + k of a lane is diagonal k of the next one; the last lane's go one
+    // place further, each by a lane of its own.
+    const int place = lane + (g.groups - 1 - (t - t0));
+    float over = 0.f;
+#pragma unroll
+    for (int k = 0; k < P - 1; ++k) {
+      over = lane == k ? read_lane(acc[P + k], kWave - 1) : over;
+      acc[k] += from_lane_below(acc[P + k]);
+    }
+    float* at = &sums[wave][place];
+#pragma unroll
+    for (int k = 0; k < P; ++k) at[k * kPlane] += acc[k];
+    if (lane < P - 1) sums[wave][lane * kPlane + place - lane + kWave] += over;
+    // The next group's places are its neighbour lanes' of this one: in LDS a wave's
+    // instructions take effect in their order, which the compiler has to keep.
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
   for (int s = threadIdx.x; s < seg.n; s += kRelThreads) starts[s] = seg.starts[s];
   if (threadIdx.x == 0) starts[seg.n] = INT32_MAX;
-  // Diagonal P + k of a lane is diagonal k of the next one.
-#pragma unroll
-  for (int k = 0; k < P; ++k) {
-    float below = 0.f;
-    if (k < P - 1) {
-      below = __shfl_up(acc[P + k], 1, kWave);
-      if (lane == 0) below = 0.f;
-      if (lane == kWave - 1) sums[wave][kWave * P + k] = acc[P + k];
-    }
-    sums[wave][lane * P + k] = acc[k] + below;
-  }
   __syncthreads();
-  for (int x = threadIdx.x; x < kLine - 1; x += kRelThreads) {
-    float y = sums[0][x];
-#pragma unroll
-    for (int w = 1; w < kRelWaves; ++w) y += sums[w][x];
-    sums[0][x] = y;
-  }
-  __syncthreads();
-  // Segment sums: 8 lanes add the distances of one, each every eighth.
-  float* mine = ws + static_cast<int64_t>(blockIdx.x) * seg.n;
-  for (int s = threadIdx.x / 8; s < (seg.n + kRelThreads / 8 - 1) / (kRelThreads / 8) * (kRelThreads / 8);
-       s += kRelThreads / 8) {
+  // The waves' sums by distance: line[x] is that of distance first + x, sum x of wave
+  // w that of first + (kRelWaves - 1 - w) * below + x.
+  const int below = g.groups * P, length = P * kWave + kRelWaves * below - 1;
+  for (int x = threadIdx.x; x < length; x += kRelThreads) {
     float y = 0.f;
-    if (s < seg.n) {
-      const int64_t lo = static_cast<int64_t>(starts[s]) - w0, hi = static_cast<int64_t>(starts[s + 1]) - w0;
-      const int x1 = hi < kLine - 1 ? static_cast<int>(hi) : kLine - 1;
-      for (int x = (lo > 0 ? static_cast<int>(lo < kLine ? lo : kLine) : 0) + (threadIdx.x & 7); x < x1; x += 8)
-        y += sums[0][x];
+#pragma unroll
+    for (int w = 0; w < kRelWaves; ++w) {
+      const int at = x - (kRelWaves - 1 - w) * below;
+      if (at >= 0 && at < P * kWave + below - 1) y += sums[w][at % P * kPlane + at / P];
     }
+    line[x] = y;
+  }
+  __syncthreads();
+  // Segment sums: a wave for each of the long ones, 8 lanes for each of the others.
+  auto begin = [&](int s) { return starts[s] > first ? starts[s] - first : 0; };
+  auto end = [&](int s) {
+    return starts[s + 1] < first + length ? starts[s + 1] - first : length;
+  };
+  for (int s = wave; s < seg.n; s += kRelWaves) {
+    const int x0 = begin(s), x1 = end(s);
+    if (x1 - x0 <= kLong) continue;
+    float y = 0.f;
+    for (int x = x0 + lane; x < x1; x += kWave) y += line[x];
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) y += __shfl_xor(y, off, kWave);
+    if (lane == 0) mine[s] = y;
+  }
+  for (int s0 = 0; s0 < seg.n; s0 += kRelThreads / 8) {
+    const int s = s0 + static_cast<int>(threadIdx.x) / 8;
+    const int x0 = s < seg.n ? begin(s) : 0, x1 = s < seg.n ? end(s) : 0;
+    const bool brief = x1 - x0 <= kLong;
+    float y = 0.f;
+    for (int x = x0 + static_cast<int>(threadIdx.x) % 8; x < (brief ? x1 : x0); x += 8)
+      y += line[x];
 #pragma unroll
     for (int off = 4; off > 0; off >>= 1) y += __shfl_xor(y, off, kWave);
-    if (s < seg.n && (threadIdx.x & 7) == 0) mine[s] = y;
+    if (s < seg.n && brief && threadIdx.x % 8 == 0) mine[s] = y;
   }
 }
 
@@ -359,29 +384,32 @@ __global__ __launch_bounds__(kJoinThreads) void k_rel_join(
     float* __restrict__ dtable, int64_t ld_table, int accumulate) {
   __shared__ float part[kJoinThreads];
   __shared__ float sums[LM_REL_MAX_SEGMENTS];
+  __shared__ int ids[LM_REL_MAX_SEGMENTS];
   const int h = blockIdx.x, n = seg.n;
   int width = 32;  // segments of one turn
-  while (width < n && width < kJoinThreads) width *= 2;
+  while (width < n) width *= 2;
   const int column = threadIdx.x % width, first = threadIdx.x / width, step = kJoinThreads / width;
   const float* mine = ws + static_cast<int64_t>(h) * parts * n;
   float x = 0.f;
   if (column < n) {
-#pragma unroll 8
+    if (first == 0) ids[column] = seg.ids[column];
+#pragma unroll 4
     for (int w = first; w < parts; w += step) x += mine[static_cast<int64_t>(w) * n + column];
   }
   part[threadIdx.x] = x;
   __syncthreads();
   if (threadIdx.x < n) {
     float y = 0.f;
+#pragma unroll 4
     for (int g = 0; g < step; ++g) y += part[g * width + threadIdx.x];
     sums[threadIdx.x] = y;
   }
   __syncthreads();
-  for (int b = threadIdx.x; b < num_buckets; b += kJoinThreads) {
+  // A row may have several segments, or none.
+  for (int row = threadIdx.x; row < num_buckets; row += kJoinThreads) {
     float y = 0.f;
-    for (int s = 0; s < n; ++s)
-      if (seg.ids[s] == b) y += sums[s];
-    float* d = dtable + b * ld_table + h;
+    for (int s = 0; s < n; ++s) y += ids[s] == row ? sums[s] : 0.f;
+    float* d = dtable + row * ld_table + h;
     *d = accumulate ? *d + y : y;
   }
 }
@@ -396,6 +424,7 @@ static Segments make_segments(const int32_t* starts, const int32_t* ids, int n) 
     s.starts[i] = starts[i];
     s.ids[i] = static_cast<int16_t>(ids[i]);
   }
+  s.masked = ids[n - 1] < 0 ? starts[n - 1] : INT32_MAX;
   return s;
 }
 
@@ -405,7 +434,8 @@ template <typename T>
 static void rel_bias_launch(const float* table, int64_t ld_table, const Segments& seg, int64_t B,
                             int64_t H, int64_t Lq, int64_t Lk, int64_t q_start, const void* add,
                             const Strides& sa, void* out, const Strides& so, hipStream_t st) {
-  const int64_t ct = ceil_div(Lk, kWave * Patch<T>::P), rt = ceil_div(Lq, kRelRows);
+  constexpr int P = Patch<T>::P;
+  const int64_t ct = ceil_div(Lk, kWave * P), rt = ceil_div(Lq, kRelWaves * P);
   const dim3 grid(static_cast<uint32_t>(ct * rt * H));
   const bool narrow = Lk < Patch<T>::P;
   auto kernel = add ? (narrow ? k_rel_bias<T, true, true> : k_rel_bias<T, true, false>)
@@ -420,7 +450,7 @@ static void rel_bias_launch(const float* table, int64_t ld_table, const Segments
 // Workgroups of a call, for the check of the grid's size.
 int64_t rel_bias_blocks(int64_t H, int64_t Lq, int64_t Lk, int dtype) {
   const int P = dtype == LM_BF16 ? Patch<bf16_t>::P : Patch<float>::P;
-  return ceil_div(Lk, kWave * P) * ceil_div(Lq, kRelRows) * H;
+  return ceil_div(Lk, kWave * P) * ceil_div(Lq, kRelWaves * P) * H;
 }
 
 int rel_bias_run(const float* table, int64_t ld_table, const int32_t* starts, const int32_t* ids,
@@ -441,24 +471,32 @@ int rel_bias_run(const float* table, int64_t ld_table, const int32_t* starts, co
 // How a head's matrices are shared out among waves.
 static GradPlan grad_plan(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype) {
   const int P = dtype == LM_BF16 ? Patch<bf16_t>::P : Patch<float>::P;
-  const int64_t nt = ceil_div(Lq, P), nk = ceil_div(Lk, P);
+  const int64_t nt = ceil_div(Lq, P), ct = ceil_div(Lk, kWave * P);
   GradPlan g;
-  g.bands = static_cast<int>(ceil_div(nt - 1 + nk, kWave));
-  // patches of 64 lanes in all: each row group meets its columns' bands and one more
-  const int64_t all = nt * (nk / kWave + 1) * B * H;
-  const int64_t most = nt < nk + kWave ? nt : nk + kWave;  // row groups of the longest band
-  int64_t steps = all / 8192;
-  steps = steps < 1 ? 1 : steps > 32 ? 32 : steps;
-  g.steps = static_cast<int>(steps);
-  g.parts = static_cast<int>(ceil_div(most * B, steps * kRelWaves));
+  int64_t patches = nt * ct * B * H / 2048;  // of a wave (64 lanes')
+  patches = patches < 1 ? 1 : patches > kMaxGroups ? kMaxGroups : patches;
+  g.batches = static_cast<int>(B < patches ? B : patches);
+  g.groups = static_cast<int>(patches / g.batches);
+  g.row_parts = static_cast<int>(ceil_div(nt, static_cast<int64_t>(g.groups) * kRelWaves));
+  g.col_tiles = static_cast<int>(ct);
+  g.batch_parts = static_cast<int>(ceil_div(B, g.batches));
   return g;
 }
 
-// Workgroups of one head; 0 where there is nothing to add.
+// Workgroups of one head that write to the workspace.
 int64_t rel_grad_parts(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype) {
   if (B == 0 || H == 0 || Lq == 0 || Lk == 0) return 0;
-  const GradPlan g = grad_plan(B, H, Lq, Lk, dtype);
-  return static_cast<int64_t>(g.bands) * g.parts;
+  return grad_plan(B, H, Lq, Lk, dtype).parts();
+}
+
+template <typename T>
+static void rel_grad_launch(const void* dout, const Strides& s, const Segments& seg, int64_t B,
+                            int64_t H, int64_t Lq, int64_t Lk, int64_t q_start, const GradPlan& g,
+                            float* ws, hipStream_t st) {
+  auto kernel = Lk < Patch<T>::P ? k_rel_grad<T, true> : k_rel_grad<T, false>;
+  kernel<<<static_cast<uint32_t>(g.parts() * H), kRelThreads, 0, st>>>(
+      static_cast<const T*>(dout), s, seg, static_cast<int>(B), static_cast<int>(Lq),
+      static_cast<int>(Lk), static_cast<int>(q_start), g, ws);
 }
 
 int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, int64_t Lk,
@@ -467,28 +505,19 @@ int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, 
                  void* ws, hipStream_t st) {
   if (H == 0) return LM_OK;
   const Segments seg = make_segments(starts, ids, n_seg);
-  const int64_t parts = rel_grad_parts(B, H, Lq, Lk, dtype);
-  if (parts) {
+  float* sums = static_cast<float*>(ws);
+  int64_t parts = 0;
+  if (B > 0 && Lq > 0 && Lk > 0) {
     const GradPlan g = grad_plan(B, H, Lq, Lk, dtype);
     const Strides s{sd[0], sd[1], sd[2]};
-    const dim3 grid(static_cast<uint32_t>(parts * H));
-    auto launch = [&](auto kernel, auto* matrix) {
-      kernel<<<grid, kRelThreads, 0, st>>>(matrix, s, seg, static_cast<int>(B),
-                                           static_cast<int>(Lq), static_cast<int>(Lk),
-                                           static_cast<int>(q_start), g, static_cast<float*>(ws));
-    };
-    if (dtype == LM_BF16)
-      launch(Lk < Patch<bf16_t>::P ? k_rel_grad<bf16_t, true> : k_rel_grad<bf16_t, false>,
-             static_cast<const bf16_t*>(dout));
-    else
-      launch(Lk < Patch<float>::P ? k_rel_grad<float, true> : k_rel_grad<float, false>,
-             static_cast<const float*>(dout));
+    if (dtype == LM_BF16) rel_grad_launch<bf16_t>(dout, s, seg, B, H, Lq, Lk, q_start, g, sums, st);
+    else rel_grad_launch<float>(dout, s, seg, B, H, Lq, Lk, q_start, g, sums, st);
     const int rc = launch_status(hipGetLastError());
     if (rc != LM_OK) return rc;
+    parts = g.parts();
   }
   k_rel_join<<<static_cast<uint32_t>(H), kJoinThreads, 0, st>>>(
-      static_cast<const float*>(ws), seg, static_cast<int>(parts), num_buckets, dtable, ld_table,
-      accumulate);
+      sums, seg, static_cast<int>(parts), num_buckets, dtable, ld_table, accumulate);
   return launch_status(hipGetLastError());
 }
 

@@ -852,12 +852,14 @@ def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
         if out is None:
             out = _on_stream(stream, lambda: torch.empty((buckets.num_buckets, H),
                                                          dtype=torch.float32, device=device))
-        buf = ws.get(need) if ws is not None else _on_stream(
-            stream, lambda: torch.empty(need, dtype=torch.uint8, device=device))
+        buf = None
+        if need:
+            buf = ws.get(need) if ws is not None else _on_stream(
+                stream, lambda: torch.empty(need, dtype=torch.uint8, device=device))
         _call(_lib.lm_rel_bias_grad(
             _ptr(dout), gtype, B, H, Lq, Lk, strides, q_start, buckets.starts, buckets.ids,
             buckets.n_seg, buckets.num_buckets, _ptr(out), _rows(out, "out"), bool(accumulate),
-            _ptr(buf), buf.numel(), st), "lm_rel_bias_grad")
+            _ptr(buf), need, st), "lm_rel_bias_grad")
     return out
 
 
