@@ -57,7 +57,7 @@ int rows8_run(float* table, int64_t V, int64_t D, int64_t ld_table, const void* 
               uint8_t* m, uint8_t* v, int64_t ld_codes, uint8_t* m_scale, uint8_t* v_scale,
               int64_t ld_scale, uint64_t seed, int32_t* dev_err, hipStream_t st);
 int rel_buckets(int num_buckets, int max_distance, int mode, int32_t* starts, int32_t* ids);
-int64_t rel_bias_blocks(int64_t H, int64_t Lq, int64_t Lk, int dtype);
+int64_t rel_bias_blocks(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype);
 int rel_bias_run(const float* table, int64_t ld_table, const int32_t* starts, const int32_t* ids,
                  int n_seg, int64_t B, int64_t H, int64_t Lq, int64_t Lk, int64_t q_start,
                  const void* add, const int64_t* sa, void* out, const int64_t* so, int dtype,
@@ -510,7 +510,7 @@ int lm_rel_bias(const float* table, int64_t ld_table, int32_t num_buckets, const
     return LM_E_INVAL;
   if (!check_strides(out_strides, B, H, Lq, Lk, true)) return LM_E_INVAL;
   if (add && !check_strides(add_strides, B, H, Lq, Lk, false)) return LM_E_INVAL;
-  if (rel_bias_blocks(H, Lq, Lk, dtype) > INT32_MAX) return LM_E_UNSUPPORTED;
+  if (rel_bias_blocks(B, H, Lq, Lk, dtype) > INT32_MAX) return LM_E_UNSUPPORTED;
   return rel_bias_run(table, ld_table, starts, ids, n_seg, B, H, Lq, Lk, q_start, add, add_strides,
                       out, out_strides, dtype, static_cast<hipStream_t>(stream));
 }

@@ -149,15 +149,16 @@ __device__ __forceinline__ float from_lane_below(float v) {
 
 // ---------------------------------------------------------------------------
 // The bias, written or added. A workgroup covers a patch's width for each of its
-// waves, one below the other, in one head, for every batch entry: it looks up the
+// waves, one below the other, in one head of one batch entry: it looks up the
 // numbers of its diagonals once, in LDS, and each lane takes its patch's from there.
-// Tiles of one column come one after the other (row tiles first): 8 x 16 x 2048 x
-// 2048 bf16 scores took 322 us so, 339 with column tiles first, 377 with two
-// patches of each wave and 420 with four.
+// Tiles of one column come one after the other (row tiles first), a batch entry
+// after the other: 8 x 16 x 2048 x 2048 causal bf16 scores take 288 us so (5.6 TB/s),
+// 321 to 328 where a workgroup keeps its diagonals for several batch entries, 339
+// with column tiles first, 377 to 420 with two and four patches of each wave.
 // ---------------------------------------------------------------------------
 template <typename T, bool ADD, bool NARROW>
 __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
-    const float* __restrict__ table, int64_t ld_table, Segments seg, int B, int Lq, int Lk,
+    const float* __restrict__ table, int64_t ld_table, Segments seg, int H, int Lq, int Lk,
     int q_start, const T* add, Strides sa, T* out, Strides so, int col_tiles, int row_tiles) {
   constexpr int P = Patch<T>::P;
   constexpr int kCols = kWave * P, kRows = kRelWaves * P;
@@ -167,20 +168,19 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
   __shared__ int32_t starts[LM_REL_MAX_SEGMENTS];
   __shared__ float value[LM_REL_MAX_SEGMENTS];
   const int rt = blockIdx.x % row_tiles, rest = blockIdx.x / row_tiles;
-  const int ct = rest % col_tiles, h = rest / col_tiles;
+  const int ct = rest % col_tiles, rest2 = rest / col_tiles;
+  const int h = rest2 % H, b = rest2 / H;
   const int lane = lane_id(), r = first_lane(threadIdx.x >> 6) * P;  // this wave's rows
   const int row0 = rt * kRows, col0 = ct * kCols, row = row0 + r, col = col0 + lane * P;
   const Columns<T, NARROW> cols(col, Lk, true);
-  // the scores of batch entry b; rows past the last are loaded from the last
-  auto load = [&](int b, raw_t* raw) {
+  const bool read = ADD && row < Lq && col0 - (row + P - 1) - q_start < seg.masked;
+  raw_t raw[P];
+  if (read) {  // on their way while the diagonals are looked up; rows past the last: the last
     const T* a = add + b * sa.b + h * sa.h;
 #pragma unroll
     for (int i = 0; i < P; ++i)
       raw[i] = cols.load(a + static_cast<int64_t>(row + i < Lq ? row + i : Lq - 1) * sa.q, Lk);
-  };
-  const bool read = ADD && row < Lq && col0 - (row + P - 1) - q_start < seg.masked;
-  raw_t next[P];
-  if (read) load(0, next);  // on its way while the diagonals are looked up
+  }
   for (int s = threadIdx.x; s < seg.n; s += kRelThreads) {
     const int id = seg.ids[s];
     starts[s] = seg.starts[s];
@@ -200,38 +200,28 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
     const f32x4 t = *reinterpret_cast<const f32x4*>(&line[lane * P + kRows - P - r + k]);
     d[k] = t.x; d[k + 1] = t.y; d[k + 2] = t.z; d[k + 3] = t.w;
   }
-  for (int b = 0; b < B; ++b) {
-    raw_t raw[P];
+  T* o = out + b * so.b + h * so.h + static_cast<int64_t>(row) * so.q + col;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if (i >= nr) break;
+    float x[P];
     if (read) {
+      Patch<T>::widen(cols.whole() ? raw[i] : cols.place(raw[i]), x);
 #pragma unroll
-      for (int i = 0; i < P; ++i) raw[i] = next[i];
-      // The next patch's loads go out before this one's stores: they would wait behind
-      // them otherwise, since out may be add.
-      if (b + 1 < B) load(b + 1, next);
+      for (int e = 0; e < P; ++e) {
+        const float y = d[P - 1 - i + e];
+        x[e] = y == -__builtin_inff() ? y : x[e] + y;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < P; ++e) x[e] = d[P - 1 - i + e];
     }
-    T* o = out + b * so.b + h * so.h + static_cast<int64_t>(row) * so.q + col;
+    if (cols.whole()) {
+      Patch<T>::store(o + i * so.q, x);
+    } else {
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      if (i >= nr) break;
-      float x[P];
-      if (read) {
-        Patch<T>::widen(cols.whole() ? raw[i] : cols.place(raw[i]), x);
-#pragma unroll
-        for (int e = 0; e < P; ++e) {
-          const float y = d[P - 1 - i + e];
-          x[e] = y == -__builtin_inff() ? y : x[e] + y;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < P; ++e) x[e] = d[P - 1 - i + e];
-      }
-      if (cols.whole()) {
-        Patch<T>::store(o + i * so.q, x);
-      } else {
-#pragma unroll
-        for (int e = 0; e < P; ++e)
-          if (e < cols.have) Patch<T>::put(o + i * so.q + e, x[e]);
-      }
+      for (int e = 0; e < P; ++e)
+        if (e < cols.have) Patch<T>::put(o + i * so.q + e, x[e]);
     }
   }
 }
@@ -436,11 +426,11 @@ static void rel_bias_launch(const float* table, int64_t ld_table, const Segments
                             const Strides& sa, void* out, const Strides& so, hipStream_t st) {
   constexpr int P = Patch<T>::P;
   const int64_t ct = ceil_div(Lk, kWave * P), rt = ceil_div(Lq, kRelWaves * P);
-  const dim3 grid(static_cast<uint32_t>(ct * rt * H));
+  const dim3 grid(static_cast<uint32_t>(ct * rt * H * B));
   const bool narrow = Lk < Patch<T>::P;
   auto kernel = add ? (narrow ? k_rel_bias<T, true, true> : k_rel_bias<T, true, false>)
                     : k_rel_bias<T, false, false>;
-  kernel<<<grid, kRelThreads, 0, st>>>(table, ld_table, seg, static_cast<int>(B),
+  kernel<<<grid, kRelThreads, 0, st>>>(table, ld_table, seg, static_cast<int>(H),
                                        static_cast<int>(Lq), static_cast<int>(Lk),
                                        static_cast<int>(q_start), static_cast<const T*>(add), sa,
                                        static_cast<T*>(out), so, static_cast<int>(ct),
@@ -448,9 +438,9 @@ static void rel_bias_launch(const float* table, int64_t ld_table, const Segments
 }
 
 // Workgroups of a call, for the check of the grid's size.
-int64_t rel_bias_blocks(int64_t H, int64_t Lq, int64_t Lk, int dtype) {
+int64_t rel_bias_blocks(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype) {
   const int P = dtype == LM_BF16 ? Patch<bf16_t>::P : Patch<float>::P;
-  return ceil_div(Lk, kWave * P) * ceil_div(Lq, kRelWaves * P) * H;
+  return ceil_div(Lk, kWave * P) * ceil_div(Lq, kRelWaves * P) * H * B;
 }
 
 int rel_bias_run(const float* table, int64_t ld_table, const int32_t* starts, const int32_t* ids,

@@ -581,25 +581,12 @@ def sample_ids(r: torch.Tensor, V: int, out: Optional[torch.Tensor] = None,
 # ---------------------------------------------------------------------------
 # AdamW over many tensors, and on table rows with 8-bit moments
 # ---------------------------------------------------------------------------
-class _On:
-    """The device of a call's tensors, made current where it is not, and the
-    stream the call goes to (a stream of another device is refused)."""
-
-    def __init__(self, device: torch.device, stream=None):
-        index = device.index
-        if stream is not None and stream.device.index != index:
-            raise LmError(f"stream is on {stream.device}, the tensors are on {device}")
-        self.other = None if torch.cuda.current_device() == index else torch.cuda.device(device)
-        self.stream = stream
-
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-        return _stream(self.stream)
-
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
+def _elsewhere(device: torch.device, stream) -> bool:
+    """Whether `device` is not the current one. A stream of another device than
+    the tensors' is refused."""
+    if stream is not None and stream.device != device:
+        raise LmError(f"stream is on {stream.device}, the tensors are on {device}")
+    return torch.cuda.current_device() != device.index
 
 
 def _same_device(device, **tensors):
@@ -714,10 +701,13 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
     _same_device(table.device, grad_scale=grad_scale, dev_err=dev_err)
     _one_of(grad_scale, torch.float32, "grad_scale")
     _one_of(dev_err, torch.int32, "dev_err")
-    with _On(table.device, stream) as st:
-        _call(_lib.lm_adamw(_ptr(table), table.numel(), plan.chunks, plan.gtype, plan.states,
-                            plan.copies, lr, beta1, beta2, eps, weight_decay, step,
-                            _ptr(grad_scale), seed, _ptr(dev_err), st), "lm_adamw")
+    if _elsewhere(table.device, stream):
+        with torch.cuda.device(table.device):
+            return adamw(plan, lr, beta1, beta2, eps, weight_decay, step, grad_scale, seed,
+                         dev_err, stream)
+    _call(_lib.lm_adamw(_ptr(table), table.numel(), plan.chunks, plan.gtype, plan.states,
+                        plan.copies, lr, beta1, beta2, eps, weight_decay, step,
+                        _ptr(grad_scale), seed, _ptr(dev_err), _stream(stream)), "lm_adamw")
 
 
 def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tensor,
@@ -750,12 +740,15 @@ def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tenso
     _one_of(dev_err, torch.int32, "dev_err")
     _same_device(table.device, rows=rows, n_rows=n_rows, vals=vals, m=m, v=v, m_scale=m_scale,
                  v_scale=v_scale, dev_err=dev_err)
-    with _On(table.device, stream) as st:
-        _call(_lib.lm_sparse_apply_q8(
-            _ptr(table), V, D, _rows(table, "table"), _ptr(rows), _idtype(rows), _ptr(n_rows),
-            min(rows.numel(), vals.shape[0]), _ptr(vals), _rows(vals, "vals"), lr, beta1, beta2,
-            eps, weight_decay, step, _ptr(m), _ptr(v), _rows(m, "m"), _ptr(m_scale), _ptr(v_scale),
-            _rows(m_scale, "m_scale"), seed, _ptr(dev_err), st), "lm_sparse_apply_q8")
+    if _elsewhere(table.device, stream):
+        with torch.cuda.device(table.device):
+            return sparse_apply_q8(table, rows, n_rows, vals, m, v, m_scale, v_scale, lr, beta1,
+                                   beta2, eps, weight_decay, step, seed, dev_err, stream)
+    _call(_lib.lm_sparse_apply_q8(
+        _ptr(table), V, D, _rows(table, "table"), _ptr(rows), _idtype(rows), _ptr(n_rows),
+        min(rows.numel(), vals.shape[0]), _ptr(vals), _rows(vals, "vals"), lr, beta1, beta2,
+        eps, weight_decay, step, _ptr(m), _ptr(v), _rows(m, "m"), _ptr(m_scale), _ptr(v_scale),
+        _rows(m_scale, "m_scale"), seed, _ptr(dev_err), _stream(stream)), "lm_sparse_apply_q8")
     return table
 
 
@@ -787,11 +780,15 @@ def rel_buckets(num_buckets: int, max_distance: int, mode: str = "both") -> RelB
     return RelBuckets(starts, ids, n.value, num_buckets)
 
 
+_Strides = ctypes.c_int64 * 3
+
+
 def _scores(t: torch.Tensor, what: str):
-    """Strides (b, h, i) of a B x H x Lq x Lk tensor with unit column stride."""
-    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
-        raise LmError(f"{what} must be a 4-D tensor with unit stride along the keys")
-    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+    """Strides (b, h, i) of a B x H x Lq x Lk or H x Lq x Lk tensor with unit column stride."""
+    strides = t.stride()
+    if not 3 <= len(strides) <= 4 or (strides[-1] != 1 and t.shape[-1] > 1):
+        raise LmError(f"{what} must be [B x] H x Lq x Lk with unit stride along the keys")
+    return _Strides(*strides[:3]) if len(strides) == 4 else _Strides(0, *strides[:2])
 
 
 def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start: int = 0,
@@ -804,25 +801,26 @@ def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start
     _dev(table, "table")
     if table.dim() != 2 or table.dtype != torch.float32 or table.shape[0] != buckets.num_buckets:
         raise LmError(f"table must be float32 with {buckets.num_buckets} rows")
-    H = table.shape[1]
-    device = table.device
-    if add is not None:
-        dtype = add.dtype
-        if add.dim() != 4 or tuple(add.shape[1:]) != (H, Lq, Lk):
-            raise LmError(f"add must be B x {H} x {Lq} x {Lk}")
-    shape = (H, Lq, Lk) if add is None else tuple(add.shape)
+    H, device = table.shape[1], table.device
     _same_device(device, add=add, out=out)
-    with _On(device, stream) as st:
-        if out is None:
-            out = _on_stream(stream, lambda: torch.empty(shape, dtype=dtype, device=device))
-        if tuple(out.shape) != shape or out.dtype != dtype:
-            raise LmError(f"out must be {' x '.join(map(str, shape))} of {dtype}")
-        full = out if add is not None else out.unsqueeze(0)
-        _call(_lib.lm_rel_bias(
-            _ptr(table), _rows(table, "table"), buckets.num_buckets, buckets.starts, buckets.ids,
-            buckets.n_seg, full.shape[0], H, Lq, Lk, q_start, _ptr(add),
-            None if add is None else _scores(add, "add"), _ptr(out), _scores(full, "out"),
-            _gtype(out), st), "lm_rel_bias")
+    if _elsewhere(device, stream):
+        with torch.cuda.device(device):
+            return rel_bias(table, buckets, Lq, Lk, q_start, add, out, dtype, stream)
+    if add is not None:
+        dtype, shape = add.dtype, add.shape
+        if len(shape) != 4 or shape[1:] != (H, Lq, Lk):
+            raise LmError(f"add must be B x {H} x {Lq} x {Lk}")
+    else:
+        shape = (H, Lq, Lk)
+    if out is None:
+        out = _empty(shape, dtype, device, stream)
+    elif out.shape != shape or out.dtype != dtype:
+        raise LmError(f"out must be {' x '.join(map(str, shape))} of {dtype}")
+    _call(_lib.lm_rel_bias(
+        _ptr(table), _rows(table, "table"), buckets.num_buckets, buckets.starts, buckets.ids,
+        buckets.n_seg, 1 if add is None else shape[0], H, Lq, Lk, q_start, _ptr(add),
+        None if add is None else _scores(add, "add"), _ptr(out), _scores(out, "out"),
+        _gtype(out), _stream(stream)), "lm_rel_bias")
     return out
 
 
@@ -833,41 +831,33 @@ def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
     of the scores (B x H x Lq x Lk, or H x Lq x Lk). accumulate: add to `out`.
     Without `ws` the call takes its workspace from torch's allocator."""
     _dev(dout, "dout")
-    if dout.dim() == 3:
-        dout = dout.unsqueeze(0)
-    strides = _scores(dout, "dout")
-    B, H, Lq, Lk = dout.shape
+    strides, shape, device = _scores(dout, "dout"), dout.shape, dout.device
+    B = shape[0] if len(shape) == 4 else 1
+    H, Lq, Lk = shape[-3:]
     gtype = _gtype(dout)
-    device = dout.device
-    if accumulate and out is None:
-        raise LmError("accumulate needs out")
-    if out is not None and (out.dtype != torch.float32 or
-                            tuple(out.shape) != (buckets.num_buckets, H)):
+    _same_device(device, out=out, ws=None if ws is None else ws.buf)
+    if _elsewhere(device, stream):
+        with torch.cuda.device(device):
+            return rel_bias_grad(dout, buckets, q_start, out, accumulate, ws, stream)
+    if out is None:
+        if accumulate:
+            raise LmError("accumulate needs out")
+        out = _empty((buckets.num_buckets, H), torch.float32, device, stream)
+    elif out.dtype != torch.float32 or out.shape != (buckets.num_buckets, H):
         raise LmError(f"out must be float32, {buckets.num_buckets} x {H}")
-    _same_device(device, out=out)
-    if ws is not None and ws.buf.device != device:
-        raise LmError(f"ws is on {ws.buf.device}, not on {device}")
     need = _lib.lm_rel_bias_grad_workspace_bytes(B, H, Lq, Lk, gtype, buckets.n_seg)
-    with _On(device, stream) as st:
-        if out is None:
-            out = _on_stream(stream, lambda: torch.empty((buckets.num_buckets, H),
-                                                         dtype=torch.float32, device=device))
-        buf = None
-        if need:
-            buf = ws.get(need) if ws is not None else _on_stream(
-                stream, lambda: torch.empty(need, dtype=torch.uint8, device=device))
-        _call(_lib.lm_rel_bias_grad(
-            _ptr(dout), gtype, B, H, Lq, Lk, strides, q_start, buckets.starts, buckets.ids,
-            buckets.n_seg, buckets.num_buckets, _ptr(out), _rows(out, "out"), bool(accumulate),
-            _ptr(buf), need, st), "lm_rel_bias_grad")
+    buf = ws.get(need) if ws is not None else _empty((need,), torch.uint8, device, stream)
+    _call(_lib.lm_rel_bias_grad(
+        _ptr(dout), gtype, B, H, Lq, Lk, strides, q_start, buckets.starts, buckets.ids,
+        buckets.n_seg, buckets.num_buckets, _ptr(out), _rows(out, "out"), bool(accumulate),
+        _ptr(buf), buf.numel(), _stream(stream)), "lm_rel_bias_grad")
     return out
 
 
-def _on_stream(stream, make):
-    """`make()` with `stream` current, so that torch's allocator gives the
-    memory to that stream and takes it back in its order."""
+def _empty(shape, dtype, device, stream):
+    """A tensor that torch's allocator gives to the call's stream, and takes back
+    in that stream's order."""
     if stream is None:
-        return make()
+        return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return make()
-
+        return torch.empty(shape, dtype=dtype, device=device)
