@@ -489,7 +489,9 @@ int lm_adamw(const void* plan, size_t plan_bytes, int64_t chunks, int32_t gtype,
  * m_scale, v_scale  device, V x ceil(D / LM_MOMENT_BLOCK) bytes, row stride
  *            ld_scale.
  * The other arguments and their errors are those of lm_sparse_apply, but
- * dev_err may be NULL and a V of 0 is no error; rows that are not named are untouched in all five arrays. A value whose new v
+ * dev_err may be NULL, a V of 0 is no error, rows_cap is below 2^31 and rows
+ * and vals hold rows_cap entries (those past *n_rows may be read); rows of
+ * the table that are not named are untouched in all five arrays. A value whose new v
  * is not finite keeps its parameter and moments and sets
  * LM_DEVERR_NONFINITE (its moments are rounded again where its block's scale
  * changes). */

@@ -247,34 +247,33 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
   constexpr int kPerWave = kWave / LANES * kRows;  // rows of a wave's turn
   __shared__ float inverse[kScales];
   const int lane = lane_id(), part = lane % LANES, group = lane / LANES;
-  const int64_t wave = first_lane(static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) +
-                                  (threadIdx.x >> 6));
-  const int64_t waves = static_cast<int64_t>(gridDim.x) * (kAdamwThreads / kWave);
-  int64_t count = first_lane(*n_rows);
+  const int64_t u0 = (static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) +
+                      first_lane(threadIdx.x >> 6)) * kPerWave;
+  // The ids come with the count, not after it (any entry below the capacity may be read).
+  int64_t id[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    const int64_t u = u0 + r * (kWave / LANES) + group;
+    id[r] = static_cast<int64_t>(rows[u < rows_cap ? u : rows_cap - 1]);
+  }
+  int64_t count = *n_rows;
   if (count > rows_cap) {
-    if (wave == 0 && lane == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
+    if (u0 == 0 && lane == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
     count = rows_cap;
   }
   if (static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) * kPerWave >= count) return;
   fill_scales(inverse, kAdamwThreads);
-  bool ok = true, range = true;
-  for (int64_t u0 = wave * kPerWave; u0 < count; u0 += waves * kPerWave) {
-    int64_t id[kRows];
-    bool live[kRows];
+  bool ok = true, range = true, live[kRows];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      const int64_t u = u0 + r * (kWave / LANES) + group;
-      id[r] = static_cast<int64_t>(rows[u < count ? u : count - 1]);
-      if constexpr (LANES == kWave) id[r] = first_lane(id[r]);
-      live[r] = u < count;
-    }
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      const bool in = id[r] >= 0 && id[r] < V;
-      range &= in || !live[r];
-      live[r] = live[r] && in;
-      id[r] = in ? id[r] : 0;  // any row of the table: loaded, not stored
-    }
+  for (int r = 0; r < kRows; ++r) {
+    live[r] = u0 + r * (kWave / LANES) + group < count;
+    const bool in = id[r] >= 0 && id[r] < V;
+    range &= in || !live[r];
+    live[r] = live[r] && in;
+    id[r] = in ? id[r] : 0;  // any row of the table: loaded, not stored
+    if constexpr (LANES == kWave) id[r] = first_lane(id[r]);
+  }
+  if (u0 < count) {
     for (int cb = 0; cb < D; cb += NV * LANES * kVec) {
       float p[kSlots][kVec], g[kSlots][kVec];
       uint32_t mc[kSlots], vc[kSlots];
@@ -286,7 +285,7 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
         const int cl = WHOLE ? (c < D ? c : D - kVec) : c;
         const int b = (c < D ? c : D - 1) / kMomentBlock;
         load4<WHOLE>(table + id[r] * ld_table, cl, D, p[s]);
-        load4<WHOLE>(vals + (u < count ? u : count - 1) * ld_vals, cl, D, g[s]);
+        load4<WHOLE>(vals + (u < rows_cap ? u : rows_cap - 1) * ld_vals, cl, D, g[s]);
         mc[s] = load_codes<WHOLE>(m + id[r] * ld_codes, cl, D);
         vc[s] = load_codes<WHOLE>(v + id[r] * ld_codes, cl, D);
         ms[s] = m_scale[id[r] * ld_scale + b];
@@ -430,8 +429,7 @@ struct Rows8 {
 template <typename KeyT, int LANES, int NV, bool WHOLE>
 static void rows8_launch(const Rows8& a, hipStream_t st) {
   constexpr int kPerBlock = kAdamwThreads / LANES * (kSlots / NV);
-  const int64_t turns = (a.rows_cap + kPerBlock - 1) / kPerBlock, most = int64_t(1) << 30;
-  const dim3 grid(static_cast<uint32_t>(turns < most ? turns : most));
+  const dim3 grid(static_cast<uint32_t>((a.rows_cap + kPerBlock - 1) / kPerBlock));
   k_rows8<KeyT, LANES, NV, WHOLE><<<grid, kAdamwThreads, 0, st>>>(
       a.table, a.V, a.D, a.ld_table, static_cast<const KeyT*>(a.rows), a.n_rows, a.rows_cap,
       a.vals, a.ld_vals, a.q, a.keys, a.m, a.v, a.ld_codes, a.m_scale, a.v_scale, a.ld_scale,

@@ -473,7 +473,7 @@ int lm_sparse_apply_q8(float* table, int64_t V, int64_t D, int64_t ld_table, con
   if (V < 0 || D < 0 || rows_cap < 0 || ld_table < D || ld_vals < D || ld_codes < D ||
       ld_scale < (D + LM_MOMENT_BLOCK - 1) / LM_MOMENT_BLOCK)
     return LM_E_INVAL;
-  if (D > (int64_t(1) << 24)) return LM_E_UNSUPPORTED;
+  if (D > (int64_t(1) << 24) || rows_cap > INT32_MAX) return LM_E_UNSUPPORTED;
   if (step < 1 || !valid_betas(beta1, beta2)) return LM_E_INVAL;
   if (rows_cap > 0 && D > 0 &&
       (!table || !rows || !n_rows || !vals || !m || !v || !m_scale || !v_scale))

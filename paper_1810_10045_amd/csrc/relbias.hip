@@ -465,7 +465,8 @@ static GradPlan grad_plan(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtyp
   GradPlan g;
   int64_t patches = nt * ct * B * H / 2048;  // of a wave (64 lanes')
   patches = patches < 1 ? 1 : patches > kMaxGroups ? kMaxGroups : patches;
-  g.batches = static_cast<int>(B < patches ? B : patches);
+  // batch entries in even shares
+  g.batches = static_cast<int>(B < patches ? B : ceil_div(B, ceil_div(B, patches)));
   g.groups = static_cast<int>(patches / g.batches);
   g.row_parts = static_cast<int>(ceil_div(nt, static_cast<int64_t>(g.groups) * kRelWaves));
   g.col_tiles = static_cast<int>(ct);

@@ -234,7 +234,8 @@ def test_adamw_refusals(lib):
              m=v, mv=v, ldc=40, ms=v, vs=v, lds=2):
         return lib.lm_sparse_apply_q8(table, V, D, ld, ids, idt, n, cap, vals, ldv, 1e-3, b1, 0.999,
                                       1e-8, 0.0, t, m, mv, ldc, ms, vs, lds, 0, None, None)
-    assert rows(idt=2) == UNSUPPORTED and rows(D=(1 << 24) + 1, ld=1 << 25, ldv=1 << 25,
+    assert rows(idt=2) == UNSUPPORTED and rows(cap=1 << 31) == UNSUPPORTED
+    assert rows(D=(1 << 24) + 1, ld=1 << 25, ldv=1 << 25,
                                                ldc=1 << 25, lds=1 << 25) == UNSUPPORTED
     for bad in (dict(V=-1), dict(D=-1), dict(cap=-1), dict(ld=39), dict(ldv=39), dict(ldc=39),
                 dict(lds=1), dict(b1=1.0), dict(t=0), dict(table=None), dict(ids=None),
