@@ -460,8 +460,8 @@ int lm_sparse_apply_f16(float* table, int64_t V, int64_t D, int64_t ld_table,
  * chunks     host, written: what lm_adamw takes.
  * Pieces of memory that a step writes and that meet each other or a
  * gradient return LM_E_INVAL. lm_adamw_plan_bytes returns 0 for sizes that
- * the library does not handle (negative, or more than LM_ADAMW_MAX_VALUES
- * together).
+ * the library does not handle (negative, more than LM_ADAMW_MAX_VALUES
+ * together, 2^31 or more pieces of 2048).
  *
  * lm_adamw: plan is the device copy of plan_bytes bytes; chunks, gtype,
  * states and copies (0 or 1) are those it was made with (others set
@@ -512,8 +512,8 @@ int lm_sparse_apply_q8(float* table, int64_t V, int64_t D, int64_t ld_table, con
  * Buckets are segments of the distance axis: segment s holds the distances
  * from starts[s] up to starts[s + 1] - 1 (the last one: all above), and
  * ids[s] is its table row, or -1: those places are masked (out is -infinity
- * whatever add holds, which is not read; dout there is left out of every
- * sum). starts ascend from INT32_MIN.
+ * whatever add holds; dout there is left out of every sum). A table entry of
+ * -infinity masks its places in out alike. starts ascend from INT32_MIN.
  *
  * lm_rel_buckets writes the segments of logarithmic buckets. A side of n
  * buckets gives the distances d below n / 2 one bucket each and puts the

@@ -401,7 +401,8 @@ size_t lm_adamw_plan_bytes(const int64_t* sizes, int64_t tensors) {
     if (sizes[i] < 0 || sizes[i] > LM_ADAMW_MAX_VALUES - total) return 0;
     total += sizes[i];
   }
-  return adamw_plan_bytes(adamw_plan_chunks(sizes, tensors));
+  const int64_t chunks = adamw_plan_chunks(sizes, tensors);
+  return chunks > INT32_MAX ? 0 : adamw_plan_bytes(chunks);
 }
 
 int lm_adamw_plan(void* const* p, const void* const* g, void* const* m, void* const* v,

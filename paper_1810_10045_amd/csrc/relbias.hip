@@ -103,8 +103,9 @@ struct Patch<bf16_t> {
   }
 };
 
-// Where a lane's patch lies in its rows: `have` of its P columns exist (0 or less:
-// it is outside). It loads from column `from`, inside the row wherever it lies, and
+// Where a lane's patch lies in its rows: `have` of its P columns exist and are used
+// (0 or less: none). It loads from column `from`, inside the row wherever it lies
+// (the wave's first patch, col0, where none is used: no further line of memory), and
 // its values start at number `by` of what it loads; so no load stands under a
 // condition and all of a patch's rows are under way at once. Rows of less than P
 // values (NARROW) are loaded one value at a time.
@@ -112,10 +113,10 @@ template <typename T, bool NARROW>
 struct Columns {
   static constexpr int P = Patch<T>::P;
   int from, by, have;
-  __device__ __forceinline__ Columns(int col, int Lk, bool use) {
-    have = col < 0 || !use ? 0 : Lk - col;
-    const int last = Lk - P;  // the last whole patch
-    from = have <= 0 || NARROW ? 0 : col < last ? col : last;
+  __device__ __forceinline__ Columns(int col0, int col, int Lk, bool use) {
+    have = use ? Lk - col : 0;
+    const int last = Lk - P, at = have > 0 ? col : col0;
+    from = NARROW ? 0 : at < last ? at : last;  // last: the last whole patch
     by = have <= 0 ? P : have < P && !NARROW ? P - have : 0;
   }
   __device__ __forceinline__ bool whole() const { return have >= P; }
@@ -139,6 +140,13 @@ struct Strides {
 
 __device__ __forceinline__ float read_lane(float v, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
+// LDS instructions of a wave take effect in their order; where lanes meet each
+// other's addresses, the compiler has to keep it too.
+__device__ __forceinline__ void in_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
 // The value of the lane below; 0 in lane 0.
@@ -172,8 +180,10 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
   const int h = rest2 % H, b = rest2 / H;
   const int lane = lane_id(), r = first_lane(threadIdx.x >> 6) * P;  // this wave's rows
   const int row0 = rt * kRows, col0 = ct * kCols, row = row0 + r, col = col0 + lane * P;
-  const Columns<T, NARROW> cols(col, Lk, true);
-  const bool read = ADD && row < Lq && col0 - (row + P - 1) - q_start < seg.masked;
+  // the smallest distance of a patch: one that is masked as a whole is not read
+  const int low = col - (row + P - 1) - q_start;
+  const Columns<T, NARROW> cols(col0, col, Lk, low < seg.masked);
+  const bool read = ADD && row < Lq && low - lane * P < seg.masked;
   raw_t raw[P];
   if (read) {  // on their way while the diagonals are looked up; rows past the last: the last
     const T* a = add + b * sa.b + h * sa.h;
@@ -216,12 +226,12 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
 #pragma unroll
       for (int e = 0; e < P; ++e) x[e] = d[P - 1 - i + e];
     }
-    if (cols.whole()) {
+    if (Lk - col >= P) {
       Patch<T>::store(o + i * so.q, x);
     } else {
 #pragma unroll
       for (int e = 0; e < P; ++e)
-        if (e < cols.have) Patch<T>::put(o + i * so.q + e, x[e]);
+        if (e < Lk - col) Patch<T>::put(o + i * so.q + e, x[e]);
     }
   }
 }
@@ -232,11 +242,13 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
 // same diagonals, so a lane's 2P - 1 sums stay in registers. After a row group they
 // are added to the wave's sums by distance in LDS, by a load, an add and a store:
 // each address belongs to one lane of an instruction (ds_add_f32, which needs no
-// such care, took about 195 clocks for a wave). Column tiles, not diagonal bands: a wave that walked down the diagonal kept its sums in registers
-// throughout, but its rows began between cache lines (16 x 16 x 2048 x 2048 bf16:
-// 450 us). At the end a workgroup adds its waves' sums by segment, into the
-// workspace; k_rel_join adds the workgroups' in their order, so results are the
-// same from run to run.
+// such care, took about 195 clocks for a wave). Column tiles, not diagonal bands: a
+// wave that walked down the diagonal kept its sums in registers throughout, but its
+// rows began between cache lines (16 x 16 x 2048 x 2048 bf16: 450 us, against 319 us
+// or 6.7 TB/s so). Loading a patch ahead did not help (329 us). At the end a
+// workgroup adds its waves' sums by distance, then by segment, into the workspace:
+// 3 us of a short call's 9. k_rel_join (4 us) adds the workgroups' in their order,
+// so results are the same from run to run.
 // ---------------------------------------------------------------------------
 constexpr int kMaxGroups = 16;
 
@@ -277,9 +289,10 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
     return;
   }
   for (int x = lane; x < P * kPlane; x += kWave) sums[wave][x] = 0.f;
+  in_order();
   for (int t = t0; t < t1; ++t) {
     if (low(col0, t) >= seg.masked) continue;
-    const Columns<T, NARROW> cols(col, Lk, low(col, t) < seg.masked);
+    const Columns<T, NARROW> cols(col0, col, Lk, low(col, t) < seg.masked);
     const int nr = Lq - t * P < P ? Lq - t * P : P;
     const bool edge = nr < P || ballot(!cols.whole());
     const T* p = dout + b0 * sd.b + h * sd.h + static_cast<int64_t>(t) * P * sd.q;
@@ -315,10 +328,7 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
 #pragma unroll
     for (int k = 0; k < P; ++k) at[k * kPlane] += acc[k];
     if (lane < P - 1) sums[wave][lane * kPlane + place - lane + kWave] += over;
-    // The next group's places are its neighbour lanes' of this one: in LDS a wave's
-    // instructions take effect in their order, which the compiler has to keep.
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    in_order();  // the next group's places are its neighbour lanes' of this one
   }
   for (int s = threadIdx.x; s < seg.n; s += kRelThreads) starts[s] = seg.starts[s];
   if (threadIdx.x == 0) starts[seg.n] = INT32_MAX;

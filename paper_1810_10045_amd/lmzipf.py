@@ -608,8 +608,11 @@ def _codes(t: torch.Tensor, what: str):
         raise LmError(f"{what} must hold e4m3 codes (float8_e4m3fn, or its bits as uint8)")
 
 
+_SCALES = (torch.uint8, getattr(torch, "float8_e8m0fnu", torch.uint8))
+
+
 def _scales(t: torch.Tensor, what: str):
-    if t.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+    if t.dtype not in _SCALES:
         raise LmError(f"{what} must hold scale bytes (uint8 or float8_e8m0fnu)")
 
 
