@@ -546,7 +546,7 @@ int lm_sparse_apply_q8(float* table, int64_t V, int64_t D, int64_t ld_table, con
  * row written (accumulate 0) or added to (1); sums in fp32 in a fixed order,
  * which depends on the sizes only: repeated calls give the same bits.
  * ws         device workspace of lm_rel_bias_grad_workspace_bytes(...), no
- *            initial contents required.
+ *            initial contents required (0 bytes for short sequences: NULL).
  * Lengths, heads and batch up to LM_REL_MAX_LENGTH, 2^40 elements together;
  * a length of 0 is valid (the gradient is then zero).
  * ------------------------------------------------------------------------ */

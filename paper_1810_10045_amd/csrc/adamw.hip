@@ -1,11 +1,24 @@
 // The AdamW step over many tensors in one launch, moments in fp32 or in 8 bits,
 // and the lazy step on table rows with 8-bit moments.
 //
-// The step reads and writes each parameter and its moments once: HBM bounds it.
+// The step reads and writes each parameter and its moments once: HBM bounds it
+// (fp32 moments with bf16 gradients and copies: 28 bytes a value, 202M values 960 us
+// or 5.9 TB/s; 8-bit moments: 16.1 bytes, 532 us or 6.1 TB/s, with its vector units
+// busy for about 80% of that: 87 instructions a value).
+//
 // A list of tensors is cut into chunks of kChunk values; one workgroup steps one
 // chunk, so a list of a thousand small tensors is one launch and a large tensor
-// spreads over the whole device. Which chunk belongs to which tensor comes from
-// the plan, a table in device memory that the caller builds once.
+// spreads over the whole device. Which chunk is whose comes from the plan, a table in
+// device memory that the caller builds once.
+//
+// - Streaming (non-temporal) loads and stores: nothing here is read again before the
+//   next step. 202M values: 1021 -> 948 us (fp32), 691 -> 560 us (8 bits, with the next
+//   point), 129,362 rows of 1024 455 -> 394 us.
+// - A workgroup ends with its chunk instead of going on to another: loads and stores
+//   are counted together, so a wave's next loads would wait for its last stores (8 bits:
+//   572 us against 691).
+// - Two vectors of each operand a lane. One or four were no faster at 202M values, and a
+//   list of 20 small tensors took 3.7 us with two, 5.0 with four.
 #include "moments.hpp"
 
 namespace lmz {

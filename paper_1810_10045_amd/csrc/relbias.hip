@@ -255,37 +255,65 @@ constexpr int kMaxGroups = 16;
 struct GradPlan {
   int groups, batches;                    // of a wave
   int row_parts, col_tiles, batch_parts;  // workgroups of a head: their product
+  bool direct;                            // one, of kDirectWaves waves
   int64_t parts() const { return static_cast<int64_t>(row_parts) * col_tiles * batch_parts; }
 };
 
-template <typename T, bool NARROW>
-__global__ __launch_bounds__(kRelThreads) void k_rel_grad(
+// The gradient's table: row n of head h, or what is added to it.
+struct GradTable {
+  float* at;
+  int64_t ld;
+  int rows, accumulate;
+};
+
+// dt[., h] (+)= the sums of n segments, in LDS like their ids. A row may have several
+// segments, or none.
+__device__ __forceinline__ void write_table(const float* sums, const int* ids, int n,
+                                            const GradTable& dt, int h) {
+  for (int row = threadIdx.x; row < dt.rows; row += blockDim.x) {
+    float y = 0.f;
+    for (int s = 0; s < n; ++s) y += ids[s] == row ? sums[s] : 0.f;
+    float* d = dt.at + row * dt.ld + h;
+    *d = dt.accumulate ? *d + y : y;
+  }
+}
+
+// WAVES waves a workgroup. kDirectWaves: a head's only workgroup, which writes the table
+// itself.
+constexpr int kDirectWaves = 16;
+
+template <typename T, bool NARROW, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
     const T* __restrict__ dout, Strides sd, Segments seg, int B, int Lq, int Lk, int q_start,
-    GradPlan g, float* __restrict__ ws) {
+    GradPlan g, float* __restrict__ ws, GradTable dt) {
   constexpr int P = Patch<T>::P;
+  constexpr bool kDirect = WAVES == kDirectWaves;
+  constexpr int kThreads = WAVES * kWave;
   // The sum of distance x of a wave is at plane x % P, place x / P: neighbouring
   // lanes' sums of one diagonal lie side by side.
   constexpr int kPlane = kWave + kMaxGroups + 1;
   constexpr int kLong = 32;  // distances of a segment that a whole wave adds
   using raw_t = typename Patch<T>::raw_t;
-  __shared__ float sums[kRelWaves][P * kPlane];
-  __shared__ float line[P * (kWave + kRelWaves * kMaxGroups)];
+  __shared__ float sums[WAVES][P * kPlane];
+  __shared__ float line[P * (kWave + WAVES * kMaxGroups)];
   __shared__ int32_t starts[LM_REL_MAX_SEGMENTS + 1];
+  __shared__ float total[kDirect ? LM_REL_MAX_SEGMENTS : 1];
+  __shared__ int ids[kDirect ? LM_REL_MAX_SEGMENTS : 1];
   const int lane = lane_id(), wave = first_lane(threadIdx.x >> 6);
   const int rp = blockIdx.x % g.row_parts, rest = blockIdx.x / g.row_parts;
   const int ct = rest % g.col_tiles, rest2 = rest / g.col_tiles;
   const int bp = rest2 % g.batch_parts, h = rest2 / g.batch_parts;
   const int nt = (Lq + P - 1) / P;
-  const int t0 = (rp * kRelWaves + wave) * g.groups;
+  const int t0 = (rp * WAVES + wave) * g.groups;
   const int t1 = t0 + g.groups < nt ? t0 + g.groups : nt;
   const int b0 = bp * g.batches, b1 = b0 + g.batches < B ? b0 + g.batches : B;
   const int col0 = ct * kWave * P, col = col0 + lane * P;
   // a patch's diagonal k has distance low + k
   auto low = [&](int column, int t) { return column - (t * P + P - 1) - q_start; };
-  float* mine = ws + static_cast<int64_t>(blockIdx.x) * seg.n;
-  const int first = low(col0, (rp + 1) * kRelWaves * g.groups - 1);  // the smallest distance
-  if (first >= seg.masked) {  // all of this workgroup's patches are
-    for (int s = threadIdx.x; s < seg.n; s += kRelThreads) mine[s] = 0.f;
+  float* mine = kDirect ? total : ws + static_cast<int64_t>(blockIdx.x) * seg.n;
+  const int first = low(col0, (rp + 1) * WAVES * g.groups - 1);  // the smallest distance
+  if (!kDirect && first >= seg.masked) {  // all of this workgroup's patches are
+    for (int s = threadIdx.x; s < seg.n; s += kThreads) mine[s] = 0.f;
     return;
   }
   for (int x = lane; x < P * kPlane; x += kWave) sums[wave][x] = 0.f;
@@ -330,17 +358,20 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
     if (lane < P - 1) sums[wave][lane * kPlane + place - lane + kWave] += over;
     in_order();  // the next group's places are its neighbour lanes' of this one
   }
-  for (int s = threadIdx.x; s < seg.n; s += kRelThreads) starts[s] = seg.starts[s];
+  for (int s = threadIdx.x; s < seg.n; s += kThreads) {
+    starts[s] = seg.starts[s];
+    if constexpr (kDirect) ids[s] = seg.ids[s];
+  }
   if (threadIdx.x == 0) starts[seg.n] = INT32_MAX;
   __syncthreads();
   // The waves' sums by distance: line[x] is that of distance first + x, sum x of wave
-  // w that of first + (kRelWaves - 1 - w) * below + x.
-  const int below = g.groups * P, length = P * kWave + kRelWaves * below - 1;
-  for (int x = threadIdx.x; x < length; x += kRelThreads) {
+  // w that of first + (WAVES - 1 - w) * below + x.
+  const int below = g.groups * P, length = P * kWave + WAVES * below - 1;
+  for (int x = threadIdx.x; x < length; x += kThreads) {
     float y = 0.f;
 #pragma unroll
-    for (int w = 0; w < kRelWaves; ++w) {
-      const int at = x - (kRelWaves - 1 - w) * below;
+    for (int w = 0; w < WAVES; ++w) {
+      const int at = x - (WAVES - 1 - w) * below;
       if (at >= 0 && at < P * kWave + below - 1) y += sums[w][at % P * kPlane + at / P];
     }
     line[x] = y;
@@ -351,7 +382,7 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
   auto end = [&](int s) {
     return starts[s + 1] < first + length ? starts[s + 1] - first : length;
   };
-  for (int s = wave; s < seg.n; s += kRelWaves) {
+  for (int s = wave; s < seg.n; s += WAVES) {
     const int x0 = begin(s), x1 = end(s);
     if (x1 - x0 <= kLong) continue;
     float y = 0.f;
@@ -360,7 +391,7 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
     for (int off = kWave / 2; off > 0; off >>= 1) y += __shfl_xor(y, off, kWave);
     if (lane == 0) mine[s] = y;
   }
-  for (int s0 = 0; s0 < seg.n; s0 += kRelThreads / 8) {
+  for (int s0 = 0; s0 < seg.n; s0 += kThreads / 8) {
     const int s = s0 + static_cast<int>(threadIdx.x) / 8;
     const int x0 = s < seg.n ? begin(s) : 0, x1 = s < seg.n ? end(s) : 0;
     const bool brief = x1 - x0 <= kLong;
@@ -371,6 +402,10 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
     for (int off = 4; off > 0; off >>= 1) y += __shfl_xor(y, off, kWave);
     if (s < seg.n && brief && threadIdx.x % 8 == 0) mine[s] = y;
   }
+  if constexpr (kDirect) {
+    __syncthreads();
+    write_table(total, ids, seg.n, dt, h);
+  }
 }
 
 // dtable[n, h] (+)= the sums of the segments with id n over a head's parts. One
@@ -380,8 +415,7 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_grad(
 constexpr int kJoinThreads = 1024;
 
 __global__ __launch_bounds__(kJoinThreads) void k_rel_join(
-    const float* __restrict__ ws, Segments seg, int parts, int num_buckets,
-    float* __restrict__ dtable, int64_t ld_table, int accumulate) {
+    const float* __restrict__ ws, Segments seg, int parts, GradTable dt) {
   __shared__ float part[kJoinThreads];
   __shared__ float sums[LM_REL_MAX_SEGMENTS];
   __shared__ int ids[LM_REL_MAX_SEGMENTS];
@@ -405,13 +439,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_rel_join(
     sums[threadIdx.x] = y;
   }
   __syncthreads();
-  // A row may have several segments, or none.
-  for (int row = threadIdx.x; row < num_buckets; row += kJoinThreads) {
-    float y = 0.f;
-    for (int s = 0; s < n; ++s) y += ids[s] == row ? sums[s] : 0.f;
-    float* d = dtable + row * ld_table + h;
-    *d = accumulate ? *d + y : y;
-  }
+  write_table(sums, ids, n, dt, h);
 }
 
 // ---------------------------------------------------------------------------
@@ -473,7 +501,22 @@ static GradPlan grad_plan(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtyp
   const int P = dtype == LM_BF16 ? Patch<bf16_t>::P : Patch<float>::P;
   const int64_t nt = ceil_div(Lq, P), ct = ceil_div(Lk, kWave * P);
   GradPlan g;
-  int64_t patches = nt * ct * B * H / 2048;  // of a wave (64 lanes')
+  // A head in one workgroup, one launch, where its waves have few patches, one after the
+  // other: 2 x 8 x 151 x 151 fp32 (6 patches of 4 rows) takes a caller 11.0 us so and 14.5
+  // with a second launch, 2 x 12 x 128 x 128 bf16 (2 of 8 rows) 12.2 and 13.7; in a graph,
+  // where launches cost less, 10.5 and 9.2, 11.7 and 11.0. 4 patches of 8 rows (1 x 16 x
+  // 512 x 512) would take 16.7 us in a graph, 10.8 with two launches.
+  g.groups = static_cast<int>(ceil_div(nt, kDirectWaves));
+  g.direct = ct == 1 && g.groups <= kMaxGroups && g.groups * B * P * P <= 128;
+  if (g.direct) {
+    g.batches = static_cast<int>(B);
+    g.row_parts = g.col_tiles = g.batch_parts = 1;
+    return g;
+  }
+  // Patches of a wave (64 lanes'): enough waves for 8 on each compute unit, and up to
+  // kMaxGroups patches each beyond that. 4 x 12 x 1024 x 1024 causal takes 21 us so, 26
+  // with a quarter as many patches each and 29 with twice as many.
+  int64_t patches = nt * ct * B * H / 2048;
   patches = patches < 1 ? 1 : patches > kMaxGroups ? kMaxGroups : patches;
   // batch entries in even shares
   g.batches = static_cast<int>(B < patches ? B : ceil_div(B, ceil_div(B, patches)));
@@ -487,17 +530,23 @@ static GradPlan grad_plan(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtyp
 // Workgroups of one head that write to the workspace.
 int64_t rel_grad_parts(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype) {
   if (B == 0 || H == 0 || Lq == 0 || Lk == 0) return 0;
-  return grad_plan(B, H, Lq, Lk, dtype).parts();
+  const GradPlan g = grad_plan(B, H, Lq, Lk, dtype);
+  return g.direct ? 0 : g.parts();
 }
 
 template <typename T>
 static void rel_grad_launch(const void* dout, const Strides& s, const Segments& seg, int64_t B,
                             int64_t H, int64_t Lq, int64_t Lk, int64_t q_start, const GradPlan& g,
-                            float* ws, hipStream_t st) {
-  auto kernel = Lk < Patch<T>::P ? k_rel_grad<T, true> : k_rel_grad<T, false>;
-  kernel<<<static_cast<uint32_t>(g.parts() * H), kRelThreads, 0, st>>>(
+                            float* ws, const GradTable& dt, hipStream_t st) {
+  const bool narrow = Lk < Patch<T>::P;
+  auto kernel = g.direct ? (narrow ? k_rel_grad<T, true, kDirectWaves>
+                                   : k_rel_grad<T, false, kDirectWaves>)
+                         : (narrow ? k_rel_grad<T, true, kRelWaves>
+                                   : k_rel_grad<T, false, kRelWaves>);
+  const int threads = (g.direct ? kDirectWaves : kRelWaves) * kWave;
+  kernel<<<static_cast<uint32_t>(g.parts() * H), threads, 0, st>>>(
       static_cast<const T*>(dout), s, seg, static_cast<int>(B), static_cast<int>(Lq),
-      static_cast<int>(Lk), static_cast<int>(q_start), g, ws);
+      static_cast<int>(Lk), static_cast<int>(q_start), g, ws, dt);
 }
 
 int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, int64_t Lk,
@@ -507,18 +556,19 @@ int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, 
   if (H == 0) return LM_OK;
   const Segments seg = make_segments(starts, ids, n_seg);
   float* sums = static_cast<float*>(ws);
+  const GradTable dt{dtable, ld_table, num_buckets, accumulate};
   int64_t parts = 0;
   if (B > 0 && Lq > 0 && Lk > 0) {
     const GradPlan g = grad_plan(B, H, Lq, Lk, dtype);
     const Strides s{sd[0], sd[1], sd[2]};
-    if (dtype == LM_BF16) rel_grad_launch<bf16_t>(dout, s, seg, B, H, Lq, Lk, q_start, g, sums, st);
-    else rel_grad_launch<float>(dout, s, seg, B, H, Lq, Lk, q_start, g, sums, st);
+    if (dtype == LM_BF16) rel_grad_launch<bf16_t>(dout, s, seg, B, H, Lq, Lk, q_start, g, sums, dt, st);
+    else rel_grad_launch<float>(dout, s, seg, B, H, Lq, Lk, q_start, g, sums, dt, st);
     const int rc = launch_status(hipGetLastError());
-    if (rc != LM_OK) return rc;
+    if (rc != LM_OK || g.direct) return rc;
     parts = g.parts();
   }
   k_rel_join<<<static_cast<uint32_t>(H), kJoinThreads, 0, st>>>(
-      sums, seg, static_cast<int>(parts), num_buckets, dtable, ld_table, accumulate);
+      sums, seg, static_cast<int>(parts), dt);
   return launch_status(hipGetLastError());
 }
 

@@ -849,11 +849,13 @@ def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
     elif out.dtype != torch.float32 or out.shape != (buckets.num_buckets, H):
         raise LmError(f"out must be float32, {buckets.num_buckets} x {H}")
     need = _lib.lm_rel_bias_grad_workspace_bytes(B, H, Lq, Lk, gtype, buckets.n_seg)
-    buf = ws.get(need) if ws is not None else _empty((need,), torch.uint8, device, stream)
+    buf = None
+    if need:
+        buf = ws.get(need) if ws is not None else _empty((need,), torch.uint8, device, stream)
     _call(_lib.lm_rel_bias_grad(
         _ptr(dout), gtype, B, H, Lq, Lk, strides, q_start, buckets.starts, buckets.ids,
         buckets.n_seg, buckets.num_buckets, _ptr(out), _rows(out, "out"), bool(accumulate),
-        _ptr(buf), buf.numel(), _stream(stream)), "lm_rel_bias_grad")
+        _ptr(buf), need, _stream(stream)), "lm_rel_bias_grad")
     return out
 
 

@@ -105,7 +105,7 @@ def test_rel_bias_refusals(lib):
         return lib.lm_rel_bias(table, ld, nb, st, i, k, B, H, Lq, Lk, q, add, sa, out, so, dtype,
                                None)
 
-    def grad(dout=v, dtype=0, B=1, H=2, Lq=4, Lk=8, s=S(64, 32, 8), q=0, st=starts, i=ids, k=n,
+    def grad(dout=v, dtype=0, B=64, H=2, Lq=4, Lk=8, s=S(64, 32, 8), q=0, st=starts, i=ids, k=n,
              nb=32, d=v, ld=2, ws=v, nbytes=1 << 30):
         return lib.lm_rel_bias_grad(dout, dtype, B, H, Lq, Lk, s, q, st, i, k, nb, d, ld, 0, ws,
                                     nbytes, None)
@@ -140,7 +140,7 @@ def test_rel_bias_refusals(lib):
     # nothing to do: no launch
     assert bias(Lq=0) == 0 and bias(B=0) == 0 and bias(H=0) == 0 and grad(H=0) == 0
     q = lib.lm_rel_bias_grad_workspace_bytes
-    assert q(1, 2, 4, 8, 0, n) >= 4 * 2 * n and q(1, 2, 0, 8, 0, n) == 0
+    assert q(64, 2, 4, 8, 0, n) >= 4 * 2 * n and q(1, 2, 4, 8, 0, n) == 0 and q(1, 2, 0, 8, 0, n) == 0
     assert q(1, 2, 4, 8, 7, n) == 0 and q(-1, 2, 4, 8, 0, n) == 0 and q(1, 2, 4, 8, 0, 0) == 0
 
 
