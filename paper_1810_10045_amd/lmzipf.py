@@ -581,6 +581,15 @@ def sample_ids(r: torch.Tensor, V: int, out: Optional[torch.Tensor] = None,
 # ---------------------------------------------------------------------------
 # AdamW over many tensors, and on table rows with 8-bit moments
 # ---------------------------------------------------------------------------
+def _on(device: torch.device, stream):
+    """The handle of the call's stream, `device` being the current one."""
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(device.index)
+
+
 def _elsewhere(device: torch.device, stream) -> bool:
     """Whether `device` is not the current one. A stream of another device than
     the tensors' is refused."""
@@ -589,10 +598,10 @@ def _elsewhere(device: torch.device, stream) -> bool:
     return torch.cuda.current_device() != device.index
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
+def _same_device(device, *tensors):
+    for t in tensors:
         if t is not None and t.device != device:
-            raise LmError(f"{name} is on {t.device}, not on {device}")
+            raise LmError(f"the call's tensors are on {device} and {t.device}")
 
 
 def _one_of(t: Optional[torch.Tensor], dtype, what: str):
@@ -701,7 +710,7 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
     launch. grad_scale: a device fp32 number that multiplies every gradient.
     seed: of the 8-bit moments' rounding; give every step its own."""
     table = plan.table
-    _same_device(table.device, grad_scale=grad_scale, dev_err=dev_err)
+    _same_device(table.device, grad_scale, dev_err)
     _one_of(grad_scale, torch.float32, "grad_scale")
     _one_of(dev_err, torch.int32, "dev_err")
     if _elsewhere(table.device, stream):
@@ -710,7 +719,8 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
                          dev_err, stream)
     _call(_lib.lm_adamw(_ptr(table), table.numel(), plan.chunks, plan.gtype, plan.states,
                         plan.copies, lr, beta1, beta2, eps, weight_decay, step,
-                        _ptr(grad_scale), seed, _ptr(dev_err), _stream(stream)), "lm_adamw")
+                        _ptr(grad_scale), seed, _ptr(dev_err), _on(table.device, stream)),
+          "lm_adamw")
 
 
 def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tensor,
@@ -726,32 +736,35 @@ def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tenso
     V, D = table.shape
     if table.dtype != torch.float32 or vals.dtype != torch.float32:
         raise LmError("table and vals must be float32")
-    if vals.dim() != 2 or vals.shape[1] != D:
+    cap, width = vals.shape
+    if width != D:
         raise LmError("vals and table widths differ")
+    if m.dtype not in _CODES or v.dtype not in _CODES:
+        raise LmError("m and v must hold e4m3 codes (float8_e4m3fn, or its bits as uint8)")
+    if m_scale.dtype not in _SCALES or v_scale.dtype not in _SCALES:
+        raise LmError("m_scale and v_scale must hold scale bytes (uint8 or float8_e8m0fnu)")
     blocks = -(-D // MOMENT_BLOCK)
-    for name, t, want, kind in (("m", m, D, _codes), ("v", v, D, _codes),
-                                ("m_scale", m_scale, blocks, _scales),
-                                ("v_scale", v_scale, blocks, _scales)):
-        kind(t, name)
-        if t.shape != (V, want):
-            raise LmError(f"{name} must be {V} x {want}")
+    if m.shape != (V, D) or v.shape != (V, D):
+        raise LmError(f"m and v must be {V} x {D}")
+    if m_scale.shape != (V, blocks) or v_scale.shape != (V, blocks):
+        raise LmError(f"m_scale and v_scale must be {V} x {blocks}")
     if m.stride() != v.stride() or m_scale.stride() != v_scale.stride():
         raise LmError("m and v, and their scales, must share their strides")
     if not rows.is_contiguous():
         raise LmError("rows must be contiguous")
     _one_of(n_rows, torch.int64, "n_rows")
     _one_of(dev_err, torch.int32, "dev_err")
-    _same_device(table.device, rows=rows, n_rows=n_rows, vals=vals, m=m, v=v, m_scale=m_scale,
-                 v_scale=v_scale, dev_err=dev_err)
+    _same_device(table.device, rows, n_rows, vals, m, v, m_scale, v_scale, dev_err)
     if _elsewhere(table.device, stream):
         with torch.cuda.device(table.device):
             return sparse_apply_q8(table, rows, n_rows, vals, m, v, m_scale, v_scale, lr, beta1,
                                    beta2, eps, weight_decay, step, seed, dev_err, stream)
     _call(_lib.lm_sparse_apply_q8(
         _ptr(table), V, D, _rows(table, "table"), _ptr(rows), _idtype(rows), _ptr(n_rows),
-        min(rows.numel(), vals.shape[0]), _ptr(vals), _rows(vals, "vals"), lr, beta1, beta2,
+        min(rows.numel(), cap), _ptr(vals), _rows(vals, "vals"), lr, beta1, beta2,
         eps, weight_decay, step, _ptr(m), _ptr(v), _rows(m, "m"), _ptr(m_scale), _ptr(v_scale),
-        _rows(m_scale, "m_scale"), seed, _ptr(dev_err), _stream(stream)), "lm_sparse_apply_q8")
+        _rows(m_scale, "m_scale"), seed, _ptr(dev_err), _on(table.device, stream)),
+          "lm_sparse_apply_q8")
     return table
 
 
@@ -805,7 +818,7 @@ def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start
     if table.dim() != 2 or table.dtype != torch.float32 or table.shape[0] != buckets.num_buckets:
         raise LmError(f"table must be float32 with {buckets.num_buckets} rows")
     H, device = table.shape[1], table.device
-    _same_device(device, add=add, out=out)
+    _same_device(device, add, out)
     if _elsewhere(device, stream):
         with torch.cuda.device(device):
             return rel_bias(table, buckets, Lq, Lk, q_start, add, out, dtype, stream)
@@ -823,7 +836,7 @@ def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start
         _ptr(table), _rows(table, "table"), buckets.num_buckets, buckets.starts, buckets.ids,
         buckets.n_seg, 1 if add is None else shape[0], H, Lq, Lk, q_start, _ptr(add),
         None if add is None else _scores(add, "add"), _ptr(out), _scores(out, "out"),
-        _gtype(out), _stream(stream)), "lm_rel_bias")
+        _gtype(out), _on(device, stream)), "lm_rel_bias")
     return out
 
 
@@ -838,7 +851,7 @@ def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
     B = shape[0] if len(shape) == 4 else 1
     H, Lq, Lk = shape[-3:]
     gtype = _gtype(dout)
-    _same_device(device, out=out, ws=None if ws is None else ws.buf)
+    _same_device(device, out, None if ws is None else ws.buf)
     if _elsewhere(device, stream):
         with torch.cuda.device(device):
             return rel_bias_grad(dout, buckets, q_start, out, accumulate, ws, stream)
@@ -855,7 +868,7 @@ def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
     _call(_lib.lm_rel_bias_grad(
         _ptr(dout), gtype, B, H, Lq, Lk, strides, q_start, buckets.starts, buckets.ids,
         buckets.n_seg, buckets.num_buckets, _ptr(out), _rows(out, "out"), bool(accumulate),
-        _ptr(buf), need, _stream(stream)), "lm_rel_bias_grad")
+        _ptr(buf), need, _on(device, stream)), "lm_rel_bias_grad")
     return out
 
 
