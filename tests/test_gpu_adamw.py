@@ -312,6 +312,39 @@ def test_adamw_many_small_tensors(lz):
     _run8(lz, [int(x) for x in rng.integers(0, 200, 700)], 1, True, False, 82)
 
 
+def test_adamw8_one_tensor_past_32_bits(lz):
+    """A tensor of more than 2^32 values between two small ones: its last values, whose
+    numbers and offsets pass 32 bits, and the tensor behind it."""
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB")
+    n, tail = (1 << 32) + 3 * 2048 + 37, 3 * 2048 + 37
+    sizes = [33, n, 100]
+    rng = np.random.default_rng(91)
+    g = [rng.normal(0, 1e-2, k).astype(np.float32) for k in (33, tail, 100)]
+    z = lambda k, d=torch.uint8: torch.zeros(k, dtype=d, device=DEV)  # noqa: E731
+    p = [z(k, torch.float32) for k in sizes]
+    grads = [z(k, torch.bfloat16) for k in sizes]
+    for t, x in zip(grads, g):
+        t[-len(x):] = torch.from_numpy(x).to(DEV)
+    m, v = [z(k) for k in sizes], [z(k) for k in sizes]
+    ms, vs = [z(R.blocks(k)) for k in sizes], [z(R.blocks(k)) for k in sizes]
+    lz.adamw(lz.adamw_plan(p, grads, m, v, m_scale=ms, v_scale=vs), seed=4, **_kw())
+    first = 0
+    for i, k in enumerate(sizes):
+        c = len(g[i])
+        x = grads[i][-c:].float().cpu().numpy()
+        zero, zb = np.zeros(c, np.uint8), np.zeros(R.blocks(c), np.uint8)
+        number = np.arange(first + k - c, first + k, dtype=np.uint64)
+        ref, bound, m8, v8, ms8, vs8, _ = R.step8(np.zeros(c, np.float32), x, zero, zero, zb, zb,
+                                                  HYPER, number, 4)
+        first += R.blocks(k) * 32
+        for got, want in ((m, m8), (v, v8), (ms, ms8), (vs, vs8)):
+            assert np.array_equal(got[i][-len(want):].cpu().numpy(), want), i
+        off = np.abs(p[i][-c:].cpu().numpy().astype(np.float64) - ref)
+        assert (off <= bound).all(), i
+    assert not p[1][:-tail].any() and not v[1][:-tail].any()  # zero gradients move nothing
+
+
 def test_adamw_refuses_another_list_with_the_plan(lz):
     """A plan used with other counts or types than it was made with steps nothing."""
     p, g, m, v = (torch.ones(5000, device=DEV) for _ in range(4))

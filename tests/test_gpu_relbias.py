@@ -208,6 +208,95 @@ def test_rel_bias_grad_masked_places_may_hold_anything(lz):
     assert torch.equal(got.isnan(), hit) and torch.equal(got[~hit], want[~hit])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rel_bias_offsets_past_32_bits(lz, dtype):
+    """Batch, head and row strides that put elements more than 2^32 apart."""
+    need = 3 * (1 << 32)
+    if torch.cuda.mem_get_info()[0] < need * 4 + (4 << 30):
+        pytest.skip("needs 56 GB")
+    big = torch.empty(need, dtype=dtype, device=DEV)
+    buckets, table = lz.rel_buckets(32, 128, "both"), torch.randn(32, 2, device=DEV)
+    for strides in (((1 << 32) + 64, 70_000, 128, 1), (9_000, (1 << 32) + 32, 128, 1),
+                    (9_000_000, 128, (1 << 32) // 50 + 3, 1)):
+        x = big.as_strided((2, 2, 60, 100), strides, 5)
+        whole = torch.randint(-3, 4, x.shape, device=DEV).to(dtype)
+        x.copy_(whole)
+        of = _of("both", 60, 100, 7)
+        assert torch.equal(lz.rel_bias_grad(x, buckets, q_start=7), _grad(whole, of, 32).float())
+        lz.rel_bias(table, buckets, 60, 100, q_start=7, add=x, out=x)
+        assert torch.equal(x, _want(table, whole, of).to(dtype))
+
+
+@pytest.mark.parametrize("q_start", [-(1 << 30), 1 << 30])
+@pytest.mark.parametrize("mode", ["both", "past", "causal"])
+def test_rel_bias_far_starts(lz, mode, q_start):
+    """Positions at the ends of the range: every key far before or far behind the query."""
+    H, Lq, Lk = 2, 20, 70
+    buckets, table = lz.rel_buckets(32, 128, mode), torch.randn(32, H, device=DEV)
+    row = R.bucket(-q_start, 32, 128, mode)
+    want = torch.full((H, Lq, Lk), -math.inf, device=DEV) if row < 0 else \
+        table[row][:, None, None].expand(H, Lq, Lk)
+    assert torch.equal(lz.rel_bias(table, buckets, Lq, Lk, q_start=q_start), want)
+    x = torch.randint(-3, 4, (1, H, Lq, Lk), device=DEV).float()
+    grad = torch.zeros(32, H, device=DEV)
+    if row >= 0:
+        grad[row] = x.sum((0, 2, 3))
+    assert torch.equal(lz.rel_bias_grad(x, buckets, q_start=q_start), grad)
+
+
+def test_rel_bias_long_rows(lz):
+    """One query against a long cache, and a long column of queries against one key."""
+    buckets = lz.rel_buckets(32, 128, "past")
+    table = torch.randn(32, 1, device=DEV)
+    n = (1 << 20) + 3
+    line = torch.arange(n, device=DEV)
+    for Lq, Lk, q_start in ((1, n, n - 1), (n, 1, 0)):
+        d = (n - 1 - line) if Lq == 1 else line
+        small = torch.tensor([R.bucket(-i, 32, 128, "past") for i in range(200)], device=DEV)
+        of = small[d.clamp(max=199)].view(Lq, Lk)
+        got = lz.rel_bias(table, buckets, Lq, Lk, q_start=q_start, dtype=torch.bfloat16)
+        assert torch.equal(got, table[of].permute(2, 0, 1).bfloat16())
+        x = torch.randint(-3, 4, (1, 1, Lq, Lk), device=DEV).bfloat16()
+        assert torch.equal(lz.rel_bias_grad(x, buckets, q_start=q_start),
+                           _grad(x, of, 32).float())
+
+
+def test_rel_bias_grad_on_two_streams_at_once(lz):
+    """Calls without a workspace of their own do not share one."""
+    buckets = lz.rel_buckets(32, 128, "both")
+    a, b = (torch.randint(-3, 4, (8, 8, 600, 600), device=DEV).bfloat16() for _ in range(2))
+    want = [lz.rel_bias_grad(x, buckets) for x in (a, b)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, x in enumerate((a, b)):
+            got[i].append(lz.rel_bias_grad(x, buckets, stream=streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+def test_rel_bias_custom_segments(lz):
+    """Segments of a caller's own: rows in any order, one row twice, a row of none, a mask
+    in the middle."""
+    import ctypes
+    starts = [-(1 << 31), -9, -2, 0, 1, 40, 300]
+    ids = [3, -1, 0, 5, 3, -1, 1]
+    pad = lambda x: (ctypes.c_int32 * lz.REL_MAX_SEGMENTS)(*x)  # noqa: E731
+    buckets = lz.RelBuckets(pad(starts), pad(ids), len(ids), 7)
+    H, Lq, Lk = 3, 100, 700
+    rel = torch.arange(Lk, device=DEV) - torch.arange(Lq, device=DEV)[:, None]
+    at = (rel[..., None] >= torch.tensor(starts, device=DEV)).sum(-1) - 1
+    of = torch.tensor(ids, device=DEV)[at]
+    table, add = torch.randn(7, H, device=DEV), torch.randn(2, H, Lq, Lk, device=DEV)
+    assert torch.equal(lz.rel_bias(table, buckets, Lq, Lk, add=add), _want(table, add, of))
+    x = torch.randint(-3, 4, (2, H, Lq, Lk), device=DEV).float()
+    assert torch.equal(lz.rel_bias_grad(x, buckets), _grad(x, of, 7).float())
+    x = x[..., :90, :80].masked_fill(of[:90, :80] < 0, math.nan)
+    assert torch.equal(lz.rel_bias_grad(x, buckets), _grad(x, of[:90, :80], 7).float())
+
+
 def test_rel_bias_empty(lz):
     buckets = lz.rel_buckets(32, 128, "both")
     for shape in ((0, 2, 4, 4), (1, 2, 0, 4), (1, 2, 4, 0)):
