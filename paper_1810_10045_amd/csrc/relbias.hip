@@ -272,6 +272,7 @@ __device__ __forceinline__ void write_table(const float* sums, const int* ids, i
                                             const GradTable& dt, int h) {
   for (int row = threadIdx.x; row < dt.rows; row += blockDim.x) {
     float y = 0.f;
+#pragma unroll 8
     for (int s = 0; s < n; ++s) y += ids[s] == row ? sums[s] : 0.f;
     float* d = dt.at + row * dt.ld + h;
     *d = dt.accumulate ? *d + y : y;
@@ -371,8 +372,11 @@ __global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
     float y = 0.f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const int at = x - (WAVES - 1 - w) * below;
-      if (at >= 0 && at < P * kWave + below - 1) y += sums[w][at % P * kPlane + at / P];
+      // (a load under no condition: the waves' loads are under way at once)
+      const unsigned at = x - (WAVES - 1 - w) * below, span = P * kWave + below - 1;
+      const unsigned in = at < span ? at : 0;
+      const float z = sums[w][in % P * kPlane + in / P];
+      y += at < span ? z : 0.f;
     }
     line[x] = y;
   }
@@ -386,6 +390,7 @@ __global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
     const int x0 = begin(s), x1 = end(s);
     if (x1 - x0 <= kLong) continue;
     float y = 0.f;
+#pragma unroll 4
     for (int x = x0 + lane; x < x1; x += kWave) y += line[x];
 #pragma unroll
     for (int off = kWave / 2; off > 0; off >>= 1) y += __shfl_xor(y, off, kWave);
