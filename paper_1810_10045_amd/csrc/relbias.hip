@@ -382,12 +382,12 @@ __global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
   }
   __syncthreads();
   // Segment sums: a wave for each of the long ones, 8 lanes for each of the others.
-  auto begin = [&](int s) { return starts[s] > first ? starts[s] - first : 0; };
-  auto end = [&](int s) {
-    return starts[s + 1] < first + length ? starts[s + 1] - first : length;
+  // (bounded before they are subtracted: starts may lie anywhere in 32 bits)
+  auto place_of = [&](int start) {
+    return (start < first ? first : start < first + length ? start : first + length) - first;
   };
   for (int s = wave; s < seg.n; s += WAVES) {
-    const int x0 = begin(s), x1 = end(s);
+    const int x0 = place_of(starts[s]), x1 = place_of(starts[s + 1]);
     if (x1 - x0 <= kLong) continue;
     float y = 0.f;
 #pragma unroll 4
@@ -398,7 +398,8 @@ __global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
   }
   for (int s0 = 0; s0 < seg.n; s0 += kThreads / 8) {
     const int s = s0 + static_cast<int>(threadIdx.x) / 8;
-    const int x0 = s < seg.n ? begin(s) : 0, x1 = s < seg.n ? end(s) : 0;
+    const int x0 = s < seg.n ? place_of(starts[s]) : 0;
+    const int x1 = s < seg.n ? place_of(starts[s + 1]) : 0;
     const bool brief = x1 - x0 <= kLong;
     float y = 0.f;
     for (int x = x0 + static_cast<int>(threadIdx.x) % 8; x < (brief ? x1 : x0); x += 8)

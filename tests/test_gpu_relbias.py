@@ -297,6 +297,23 @@ def test_rel_bias_custom_segments(lz):
     assert torch.equal(lz.rel_bias_grad(x, buckets), _grad(x, of[:90, :80], 7).float())
 
 
+@pytest.mark.parametrize("q_start", [-(1 << 30), 0, 1 << 30])
+def test_rel_bias_segments_at_the_ends_of_32_bits(lz, q_start):
+    """Starts next to the largest and smallest 32-bit numbers, positions at both ends."""
+    import ctypes
+    starts = [-(1 << 31), -(1 << 31) + 1, -5, 2, (1 << 31) - 2, (1 << 31) - 1]
+    ids = [0, 1, 2, 3, 4, -1]
+    pad = lambda x: (ctypes.c_int32 * lz.REL_MAX_SEGMENTS)(*x)  # noqa: E731
+    buckets = lz.RelBuckets(pad(starts), pad(ids), len(ids), 5)
+    for Lq, Lk in ((100, 70), (600, 900)):
+        rel = torch.arange(Lk, device=DEV) - torch.arange(Lq, device=DEV)[:, None] - q_start
+        of = torch.tensor(ids, device=DEV)[(rel[..., None] >= torch.tensor(starts, device=DEV)).sum(-1) - 1]
+        table = torch.randn(5, 2, device=DEV)
+        assert torch.equal(lz.rel_bias(table, buckets, Lq, Lk, q_start=q_start), _want(table, None, of))
+        x = torch.randint(-3, 4, (1, 2, Lq, Lk), device=DEV).float()
+        assert torch.equal(lz.rel_bias_grad(x, buckets, q_start=q_start), _grad(x, of, 5).float())
+
+
 def test_rel_bias_empty(lz):
     buckets = lz.rel_buckets(32, 128, "both")
     for shape in ((0, 2, 4, 4), (1, 2, 0, 4), (1, 2, 4, 0)):
