@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
 // rows began between cache lines (16 x 16 x 2048 x 2048 bf16: 450 us, against 319 us
 // or 6.7 TB/s so). Loading a patch ahead did not help (329 us). At the end a
 // workgroup adds its waves' sums by distance, then by segment, into the workspace:
-// 3 us of a short call's 9. k_rel_join (4 us) adds the workgroups' in their order,
+// 2 us of a short call's 10. k_rel_join (4 us) adds the workgroups' in their order,
 // so results are the same from run to run.
 // ---------------------------------------------------------------------------
 constexpr int kMaxGroups = 16;
@@ -510,7 +510,7 @@ static GradPlan grad_plan(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtyp
   // A head in one workgroup, one launch, where its waves have few patches, one after the
   // other: 2 x 8 x 151 x 151 fp32 (6 patches of 4 rows) takes a caller 11.0 us so and 14.5
   // with a second launch, 2 x 12 x 128 x 128 bf16 (2 of 8 rows) 12.2 and 13.7; in a graph,
-  // where launches cost less, 10.5 and 9.2, 11.7 and 11.0. 4 patches of 8 rows (1 x 16 x
+  // where launches cost less, 10.0 and 9.0, 11.3 and 10.7. 4 patches of 8 rows (1 x 16 x
   // 512 x 512) would take 16.7 us in a graph, 10.8 with two launches.
   g.groups = static_cast<int>(ceil_div(nt, kDirectWaves));
   g.direct = ct == 1 && g.groups <= kMaxGroups && g.groups * B * P * P <= 128;
