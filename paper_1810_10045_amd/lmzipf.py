@@ -627,14 +627,16 @@ def _scales(t: torch.Tensor, what: str):
 
 class AdamwPlan(NamedTuple):
     """A list of tensors as ``adamw`` steps it: the table that names their
-    memory on the device, and the tensors themselves, which it keeps alive.
-    It stands for the memory the tensors had when it was made."""
+    memory on the device, and that memory itself, which it keeps alive also
+    where a tensor has been given other memory since (`p.data = ...`). `home`:
+    the stream on which the table's memory was allocated."""
     table: torch.Tensor
     tensors: tuple
     chunks: int
     gtype: int
     states: int
     copies: bool
+    home: int
 
 
 def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
@@ -645,7 +647,8 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
     MOMENT_BLOCK values. copies: bf16 copies of the parameters, written with
     every step. decay: one truth value per tensor, whether weight_decay
     applies. Copies the table to the device; make a new plan when a tensor
-    (say, a gradient) gets other memory."""
+    (say, a gradient) gets other memory, and keep one as long as a captured
+    graph steps it."""
     params, grads, m, v = (list(x) for x in (params, grads, m, v))
     lists = {"grads": grads, "m": m, "v": v}
     for name, x in (("m_scale", m_scale), ("v_scale", v_scale), ("copies", copies)):
@@ -697,9 +700,10 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
         pointers(lists.get("v_scale")), pointers(lists.get("copies")), sizes,
         None if decay is None else (ctypes.c_int32 * n)(*decay), n, gtype, 8 if eight else 32,
         _ptr(host), need, ctypes.byref(chunks)), "lm_adamw_plan")
-    keep = tuple(tuple(x) for x in [params] + list(lists.values()))
-    return AdamwPlan(host.to(device), keep, chunks.value, gtype, 8 if eight else 32,
-                     "copies" in lists)
+    keep = tuple(tuple(t.detach() for t in x) for x in [params] + list(lists.values()))
+    with torch.cuda.device(device):
+        return AdamwPlan(host.to(device), keep, chunks.value, gtype, 8 if eight else 32,
+                         "copies" in lists, _on(device, None))
 
 
 def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
@@ -717,10 +721,12 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
         with torch.cuda.device(table.device):
             return adamw(plan, lr, beta1, beta2, eps, weight_decay, step, grad_scale, seed,
                          dev_err, stream)
+    handle = _on(table.device, stream)
+    if handle != plan.home:  # the table's memory is not to be reused before this stream is past it
+        table.record_stream(stream or torch.cuda.current_stream())
     _call(_lib.lm_adamw(_ptr(table), table.numel(), plan.chunks, plan.gtype, plan.states,
                         plan.copies, lr, beta1, beta2, eps, weight_decay, step,
-                        _ptr(grad_scale), seed, _ptr(dev_err), _on(table.device, stream)),
-          "lm_adamw")
+                        _ptr(grad_scale), seed, _ptr(dev_err), handle), "lm_adamw")
 
 
 def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tensor,

@@ -360,6 +360,30 @@ def test_adamw_refuses_another_list_with_the_plan(lz):
         lz.adamw(plan._replace(chunks=plan.chunks + 1), dev_err=err)
 
 
+def test_adamw_plan_holds_its_memory(lz):
+    """A parameter that is given other memory, and lists and plans that go away: a step
+    goes to the memory the plan was made with, and nothing else is touched."""
+    n = 300_000
+    p = torch.nn.Parameter(torch.zeros(n, device=DEV))
+    old = p.data
+    g, m, v = (torch.ones(n, device=DEV) for _ in range(3))
+    plan = lz.adamw_plan([p], [g], [m], [v])
+    p.data = torch.full((n,), 5.0, device=DEV)
+    del g, m, v
+    rest = [torch.full((n,), 7.0, device=DEV) for _ in range(8)]  # would take freed memory
+    lz.adamw(plan, lr=0.5, beta1=0.0, beta2=0.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    lz.adamw(plan, lr=0.5, beta1=0.0, beta2=0.0, stream=side)
+    with torch.cuda.stream(side):
+        lz.adamw(plan, lr=0.5, beta1=0.0, beta2=0.0)
+    del plan
+    more = [torch.full((n,), 7.0, device=DEV) for _ in range(8)]
+    torch.cuda.synchronize()
+    assert bool((p == 5).all()) and all(bool((x == 7).all()) for x in rest + more)
+    assert float((old + 1.5).abs().max()) < 1e-6  # three updates of lr
+
+
 def test_adamw_in_a_graph_and_on_another_stream(lz):
     """A captured step replayed between eager steps, the gradients rewritten in
     place: each equals the eager step from the same state."""
