@@ -52,70 +52,74 @@ static uint64_t plan_kind(int64_t chunks, int gtype, int states, bool copies) {
 
 // ---------------------------------------------------------------------------
 // A lane's vectors of n values, its own from number i on. Where a vector may pass
-// the end (not WHOLE), the last 4 values are loaded in its place and moved down, zeros
-// behind them (129,362 rows of 1,001: 583 us so, 687 with a load for each value); and
-// fewer than 4 values one by one. No load stands under a lane's condition, so all of a
-// lane's loads are under way at once.
+// the end (PART), the last 4 values are loaded in its place and, once every load is
+// under way, moved down, zeros behind them: 100,000 rows of 91 values take 55 us so, 77
+// where each vector is moved before the next is loaded, 75 with a load for each value
+// (129,362 rows of 1,001: 489, 549, 687). Fewer than 4 values (FEW) are loaded one by one.
 // ---------------------------------------------------------------------------
-struct Place {
-  int from, by;  // loaded from number `from`, `by` values too early (4 and more: none is wanted)
-  __device__ __forceinline__ Place(int i, int n) : from(i < n - 4 ? i : n - 4), by(i - from) {}
-  __device__ __forceinline__ void move(float* x) const {
-    if (!ballot(by > 0)) return;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = by & 2 ? (e < 2 ? x[e + 2] : 0.f) : x[e];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = by & 1 ? (e < 3 ? x[e + 1] : 0.f) : x[e];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = by > 3 ? 0.f : x[e];
-  }
-};
+enum End { WHOLE, PART, FEW };
 
-template <bool WHOLE>
+template <End END>
+__device__ __forceinline__ int load_from(int i, int n) {
+  return END == PART && i > n - 4 ? n - 4 : i;
+}
+
+template <End END>
 __device__ __forceinline__ void load4(const float* p, int i, int n, float* x) {
-  if (WHOLE || n >= 4) {
-    const Place at(i, n);
-    const f32x4 t = stream_load_e(reinterpret_cast<const f32x4e*>(p + (WHOLE ? i : at.from)));
+  if constexpr (END != FEW) {
+    const f32x4 t = stream_load_e(reinterpret_cast<const f32x4e*>(p + load_from<END>(i, n)));
     x[0] = t.x; x[1] = t.y; x[2] = t.z; x[3] = t.w;
-    if constexpr (!WHOLE) at.move(x);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = i + e < n ? p[i + e] : 0.f;
   }
 }
 
-template <bool WHOLE>
+template <End END>
 __device__ __forceinline__ void load4(const bf16_t* p, int i, int n, float* x) {
-  if (WHOLE || n >= 4) {
-    const Place at(i, n);
+  if constexpr (END != FEW) {
     const u32x2e t =
-        __builtin_nontemporal_load(reinterpret_cast<const u32x2e*>(p + (WHOLE ? i : at.from)));
+        __builtin_nontemporal_load(reinterpret_cast<const u32x2e*>(p + load_from<END>(i, n)));
     x[0] = __uint_as_float(t.x << 16); x[1] = __uint_as_float(t.x & 0xffff0000u);
     x[2] = __uint_as_float(t.y << 16); x[3] = __uint_as_float(t.y & 0xffff0000u);
-    if constexpr (!WHOLE) at.move(x);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = i + e < n ? bf16_to_f32(p[i + e].bits) : 0.f;
   }
 }
 
-template <bool WHOLE>
+template <End END>
 __device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int i, int n) {
-  if (WHOLE || n >= 4) {
-    const Place at(i, n);
-    const uint32_t w =
-        __builtin_nontemporal_load(reinterpret_cast<const u32e*>(p + (WHOLE ? i : at.from)));
-    return WHOLE ? w : at.by > 3 ? 0u : w >> (8 * at.by);
-  }
+  if constexpr (END != FEW)
+    return __builtin_nontemporal_load(reinterpret_cast<const u32e*>(p + load_from<END>(i, n)));
   uint32_t w = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) w |= (i + e < n ? uint32_t(p[i + e]) : 0u) << (8 * e);
   return w;
 }
 
-template <bool WHOLE>
+// The values of a PART vector moved to their places.
+template <End END>
+__device__ __forceinline__ void settle(int i, int n, float* x) {
+  const int by = i - load_from<END>(i, n);  // values too early; 4 and more: none is wanted
+  if (END != PART || !ballot(by > 0)) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = by & 2 ? (e < 2 ? x[e + 2] : 0.f) : x[e];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = by & 1 ? (e < 3 ? x[e + 1] : 0.f) : x[e];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = by > 3 ? 0.f : x[e];
+}
+
+template <End END>
+__device__ __forceinline__ uint32_t settle(int i, int n, uint32_t codes) {
+  const int by = i - load_from<END>(i, n);
+  return by > 3 ? 0u : codes >> (8 * by);
+}
+
+template <End END>
 __device__ __forceinline__ void store4(float* p, int i, int n, const float* x) {
-  if (WHOLE || i + 4 <= n) {
+  if (END == WHOLE || i + 4 <= n) {
     __builtin_nontemporal_store(f32x4e{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4e*>(p + i));
   } else {
 #pragma unroll
@@ -128,9 +132,9 @@ __device__ __forceinline__ uint32_t bf16_bits(float x) {
   return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
 }
 
-template <bool WHOLE>
+template <End END>
 __device__ __forceinline__ void store4(uint16_t* p, int i, int n, const float* x) {
-  if (WHOLE || i + 4 <= n) {
+  if (END == WHOLE || i + 4 <= n) {
     const u32x2e w = {bf16_bits(x[0]) | bf16_bits(x[1]) << 16,
                       bf16_bits(x[2]) | bf16_bits(x[3]) << 16};
     __builtin_nontemporal_store(w, reinterpret_cast<u32x2e*>(p + i));
@@ -141,9 +145,9 @@ __device__ __forceinline__ void store4(uint16_t* p, int i, int n, const float* x
   }
 }
 
-template <bool WHOLE>
+template <End END>
 __device__ __forceinline__ void store_codes(uint8_t* p, int i, int n, uint32_t w) {
-  if (WHOLE || i + 4 <= n) {
+  if (END == WHOLE || i + 4 <= n) {
     __builtin_nontemporal_store(w, reinterpret_cast<u32e*>(p + i));
   } else {
 #pragma unroll
@@ -157,7 +161,7 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int i, int n, uint32_t w
 // are a workgroup's width apart, so every load and store of a wave is one
 // contiguous piece.
 // ---------------------------------------------------------------------------
-template <typename GT, bool EIGHT, bool COPY, bool WHOLE, int NV>
+template <typename GT, bool EIGHT, bool COPY, End END, int NV>
 __device__ __forceinline__ bool step_vectors(const PlanChunk& t, int i0, float gs,
                                              const OptParams& o, const MomentParams& q,
                                              const StepKeys& keys, const float* inverse) {
@@ -168,17 +172,17 @@ __device__ __forceinline__ bool step_vectors(const PlanChunk& t, int i0, float g
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int i = i0 + j * kAdamwThreads * kVec;
-    load4<WHOLE>(t.p, i, n, p[j]);
-    load4<WHOLE>(static_cast<const GT*>(t.g), i, n, g[j]);
+    load4<END>(t.p, i, n, p[j]);
+    load4<END>(static_cast<const GT*>(t.g), i, n, g[j]);
     if constexpr (EIGHT) {
-      const int b = (WHOLE || i < n ? i : n - 1) / kMomentBlock;
-      mc[j] = load_codes<WHOLE>(static_cast<const uint8_t*>(t.m), i, n);
-      vc[j] = load_codes<WHOLE>(static_cast<const uint8_t*>(t.v), i, n);
+      const int b = (END == WHOLE || i < n ? i : n - 1) / kMomentBlock;
+      mc[j] = load_codes<END>(static_cast<const uint8_t*>(t.m), i, n);
+      vc[j] = load_codes<END>(static_cast<const uint8_t*>(t.v), i, n);
       ms[j] = t.m_scale[b];
       vs[j] = t.v_scale[b];
     } else {
-      load4<WHOLE>(static_cast<const float*>(t.m), i, n, m[j]);
-      load4<WHOLE>(static_cast<const float*>(t.v), i, n, v[j]);
+      load4<END>(static_cast<const float*>(t.m), i, n, m[j]);
+      load4<END>(static_cast<const float*>(t.v), i, n, v[j]);
     }
   }
   const float wd = t.decay ? o.wd : 0.f;
@@ -186,9 +190,14 @@ __device__ __forceinline__ bool step_vectors(const PlanChunk& t, int i0, float g
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int i = i0 + j * kAdamwThreads * kVec;
+    settle<END>(i, n, p[j]);
+    settle<END>(i, n, g[j]);
     if constexpr (EIGHT) {
-      decode4(mc[j], ms[j], m[j]);
-      decode4(vc[j], vs[j], v[j]);
+      decode4(settle<END>(i, n, mc[j]), ms[j], m[j]);
+      decode4(settle<END>(i, n, vc[j]), vs[j], v[j]);
+    } else {
+      settle<END>(i, n, m[j]);
+      settle<END>(i, n, v[j]);
     }
     uint32_t word[kVec], low[kVec];
 #pragma unroll
@@ -214,18 +223,18 @@ __device__ __forceinline__ bool step_vectors(const PlanChunk& t, int i0, float g
       mc[j] = encode4<false>(m[j], word, inverse, ms[j]);
       vc[j] = encode4<true>(v[j], low, inverse, vs[j]);
     }
-    store4<WHOLE>(t.p, i, n, p[j]);
-    if constexpr (COPY) store4<WHOLE>(t.copy, i, n, p[j]);
+    store4<END>(t.p, i, n, p[j]);
+    if constexpr (COPY) store4<END>(t.copy, i, n, p[j]);
     if constexpr (EIGHT) {
-      store_codes<WHOLE>(static_cast<uint8_t*>(t.m), i, n, mc[j]);
-      store_codes<WHOLE>(static_cast<uint8_t*>(t.v), i, n, vc[j]);
-      if ((threadIdx.x & 7) == 0 && (WHOLE || i < n)) {
+      store_codes<END>(static_cast<uint8_t*>(t.m), i, n, mc[j]);
+      store_codes<END>(static_cast<uint8_t*>(t.v), i, n, vc[j]);
+      if ((threadIdx.x & 7) == 0 && (END == WHOLE || i < n)) {
         t.m_scale[i / kMomentBlock] = static_cast<uint8_t>(ms[j]);
         t.v_scale[i / kMomentBlock] = static_cast<uint8_t>(vs[j]);
       }
     } else {
-      store4<WHOLE>(static_cast<float*>(t.m), i, n, m[j]);
-      store4<WHOLE>(static_cast<float*>(t.v), i, n, v[j]);
+      store4<END>(static_cast<float*>(t.m), i, n, m[j]);
+      store4<END>(static_cast<float*>(t.v), i, n, v[j]);
     }
   }
   return ok;
@@ -246,11 +255,13 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw(
   const int i0 = threadIdx.x * kVec;
   bool ok = true;
   if (t.n == kChunk) {
-    ok = step_vectors<GT, EIGHT, COPY, true, kVectors>(t, i0, gs, o, q, keys, inverse);
-  } else {
+    ok = step_vectors<GT, EIGHT, COPY, WHOLE, kVectors>(t, i0, gs, o, q, keys, inverse);
+  } else if (t.n >= kVec) {
 #pragma unroll 1  // a small copy of the code: a list of small tensors waits for it from memory
     for (int j = 0; j < t.n; j += kAdamwThreads * kVec)
-      ok &= step_vectors<GT, EIGHT, COPY, false, 1>(t, i0 + j, gs, o, q, keys, inverse);
+      ok &= step_vectors<GT, EIGHT, COPY, PART, 1>(t, i0 + j, gs, o, q, keys, inverse);
+  } else {
+    ok = step_vectors<GT, EIGHT, COPY, FEW, 1>(t, i0, gs, o, q, keys, inverse);
   }
   if (ballot(!ok) && lane_id() == 0) raise_err(dev_err, LM_DEVERR_NONFINITE);
 }
@@ -264,7 +275,7 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw(
 // ---------------------------------------------------------------------------
 constexpr int kSlots = 4;
 
-template <typename KeyT, int LANES, int NV, bool WHOLE>
+template <typename KeyT, int LANES, int NV, End END>
 __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
     float* __restrict__ table, int64_t V, int D, int64_t ld_table, const KeyT* __restrict__ rows,
     const int64_t* __restrict__ n_rows, int64_t rows_cap, const float* __restrict__ vals,
@@ -310,12 +321,12 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
       for (int s = 0; s < kSlots; ++s) {
         const int r = s / NV, c = cb + (s % NV * LANES + part) * kVec;
         const int64_t u = u0 + r * (kWave / LANES) + group;
-        const int cl = WHOLE && c >= D ? D - kVec : c;
+        const int cl = END == WHOLE && c >= D ? D - kVec : c;
         const int b = (c < D ? c : D - 1) / kMomentBlock;
-        load4<WHOLE>(table + id[r] * ld_table, cl, D, p[s]);
-        load4<WHOLE>(vals + (u < rows_cap ? u : rows_cap - 1) * ld_vals, cl, D, g[s]);
-        mc[s] = load_codes<WHOLE>(m + id[r] * ld_codes, cl, D);
-        vc[s] = load_codes<WHOLE>(v + id[r] * ld_codes, cl, D);
+        load4<END>(table + id[r] * ld_table, cl, D, p[s]);
+        load4<END>(vals + (u < rows_cap ? u : rows_cap - 1) * ld_vals, cl, D, g[s]);
+        mc[s] = load_codes<END>(m + id[r] * ld_codes, cl, D);
+        vc[s] = load_codes<END>(v + id[r] * ld_codes, cl, D);
         ms[s] = m_scale[id[r] * ld_scale + b];
         vs[s] = v_scale[id[r] * ld_scale + b];
       }
@@ -324,8 +335,10 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
         const int r = s / NV, c = cb + (s % NV * LANES + part) * kVec;
         float mx[kVec], vx[kVec];
         uint32_t word[kVec], low[kVec];
-        decode4(mc[s], ms[s], mx);
-        decode4(vc[s], vs[s], vx);
+        settle<END>(c, D, p[s]);
+        settle<END>(c, D, g[s]);
+        decode4(settle<END>(c, D, mc[s]), ms[s], mx);
+        decode4(settle<END>(c, D, vc[s]), vs[s], vx);
         const uint64_t number = static_cast<uint64_t>(id[r]) * D + c;
         bool fine = true;
 #pragma unroll
@@ -338,9 +351,9 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
         vc[s] = encode4<true>(vx, low, inverse, vs[s]);
         if (!live[r] || c >= D) continue;
         ok &= fine;
-        store4<WHOLE>(table + id[r] * ld_table, c, D, p[s]);
-        store_codes<WHOLE>(m + id[r] * ld_codes, c, D, mc[s]);
-        store_codes<WHOLE>(v + id[r] * ld_codes, c, D, vc[s]);
+        store4<END>(table + id[r] * ld_table, c, D, p[s]);
+        store_codes<END>(m + id[r] * ld_codes, c, D, mc[s]);
+        store_codes<END>(v + id[r] * ld_codes, c, D, vc[s]);
         if ((lane & 7) == 0) {
           m_scale[id[r] * ld_scale + c / kMomentBlock] = static_cast<uint8_t>(ms[s]);
           v_scale[id[r] * ld_scale + c / kMomentBlock] = static_cast<uint8_t>(vs[s]);
@@ -449,25 +462,38 @@ struct Rows8 {
   int32_t* dev_err;
 };
 
-template <typename KeyT, int LANES, int NV, bool WHOLE>
+template <typename KeyT, int LANES, int NV, End END>
 static void rows8_launch(const Rows8& a, hipStream_t st) {
   constexpr int kPerBlock = kAdamwThreads / LANES * (kSlots / NV);
   const dim3 grid(static_cast<uint32_t>((a.rows_cap + kPerBlock - 1) / kPerBlock));
-  k_rows8<KeyT, LANES, NV, WHOLE><<<grid, kAdamwThreads, 0, st>>>(
+  k_rows8<KeyT, LANES, NV, END><<<grid, kAdamwThreads, 0, st>>>(
       a.table, a.V, a.D, a.ld_table, static_cast<const KeyT*>(a.rows), a.n_rows, a.rows_cap,
       a.vals, a.ld_vals, a.q, a.keys, a.m, a.v, a.ld_codes, a.m_scale, a.v_scale, a.ld_scale,
       a.dev_err);
 }
 
-template <typename KeyT, bool WHOLE>
+// Lanes a row, vectors a lane. 100,000 rows of 32, 64, 128 values take 21, 29, 46 us so,
+// 52, 52, 63 with a wave for each; rows of 256 and 512 85 and 160 us, 149 and 182 with
+// 4 vectors a lane. Rows of whole vectors (WHOLE) of 128 and 512 values: 44 and 157 us, 49
+// and 159 as PART.
+template <typename KeyT, End END>
 static void rows8_shape(const Rows8& a, hipStream_t st) {
   const int vectors = (a.D + kVec - 1) / kVec;
-  if (vectors <= 8) rows8_launch<KeyT, 8, 1, WHOLE>(a, st);
-  else if (vectors <= 16) rows8_launch<KeyT, 16, 1, WHOLE>(a, st);
-  else if (vectors <= 32) rows8_launch<KeyT, 32, 1, WHOLE>(a, st);
-  else if (vectors <= 64) rows8_launch<KeyT, 64, 1, WHOLE>(a, st);
-  else if (vectors <= 128) rows8_launch<KeyT, 64, 2, WHOLE>(a, st);
-  else rows8_launch<KeyT, 64, 4, WHOLE>(a, st);
+  if (END == FEW || vectors <= 8) return rows8_launch<KeyT, 8, 1, END>(a, st);
+  if constexpr (END != FEW) {
+    if (vectors <= 16) rows8_launch<KeyT, 16, 1, END>(a, st);
+    else if (vectors <= 32) rows8_launch<KeyT, 32, 1, END>(a, st);
+    else if (vectors <= 64) rows8_launch<KeyT, 64, 1, END>(a, st);
+    else if (vectors <= 128) rows8_launch<KeyT, 64, 2, END>(a, st);
+    else rows8_launch<KeyT, 64, 4, END>(a, st);
+  }
+}
+
+template <typename KeyT>
+static void rows8_ends(const Rows8& a, hipStream_t st) {
+  if (a.D % kVec == 0) rows8_shape<KeyT, WHOLE>(a, st);
+  else if (a.D > kVec) rows8_shape<KeyT, PART>(a, st);
+  else rows8_shape<KeyT, FEW>(a, st);
 }
 
 int rows8_run(float* table, int64_t V, int64_t D, int64_t ld_table, const void* rows, int idtype,
@@ -480,11 +506,8 @@ int rows8_run(float* table, int64_t V, int64_t D, int64_t ld_table, const void* 
   const Rows8 a{table, V, static_cast<int>(D), ld_table, rows, n_rows, rows_cap, vals, ld_vals,
                 make_moment_params(o, beta2, step), step_keys(seed), m, v, ld_codes, m_scale,
                 v_scale, ld_scale, dev_err};
-  const bool whole = D % kVec == 0;
-  if (idtype == LM_I64)
-    whole ? rows8_shape<int64_t, true>(a, st) : rows8_shape<int64_t, false>(a, st);
-  else
-    whole ? rows8_shape<int32_t, true>(a, st) : rows8_shape<int32_t, false>(a, st);
+  if (idtype == LM_I64) rows8_ends<int64_t>(a, st);
+  else rows8_ends<int32_t>(a, st);
   return launch_status(hipGetLastError());
 }
 

@@ -381,7 +381,8 @@ __global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
     line[x] = y;
   }
   __syncthreads();
-  // Segment sums: a wave for each of the long ones, 8 lanes for each of the others.
+  // Segment sums: a wave for each of the long ones, 8 lanes for each of the others (4 x 12
+  // x 1024 x 1024 causal: 20.1 us, 21.4 with 8 lanes for all, 22.1 with waves for all).
   // (bounded before they are subtracted: starts may lie anywhere in 32 bits)
   auto place_of = [&](int start) {
     return (start < first ? first : start < first + length ? start : first + length) - first;
