@@ -535,7 +535,8 @@ int lm_sparse_apply_q8(float* table, int64_t V, int64_t D, int64_t ld_table, con
  * table      device, num_buckets x H fp32, row stride ld_table.
  * add        device, B x H x Lq x Lk of dtype `dtype` (LM_F32 / LM_BF16) with
  *            unit stride along Lk and add_strides (host: b, h, i) in elements
- *            (0 repeats a dimension), or NULL: the bias alone.
+ *            (0 repeats a dimension; up to 2^40, the matrices within 2^60
+ *            elements), or NULL: the bias alone.
  * out        device, the same shape and dtype, out_strides; sums in fp32,
  *            rounded once. It may be add itself, with the same strides;
  *            otherwise the two must not meet.

@@ -134,26 +134,26 @@ static int check_rel_sizes(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int64_t
   return LM_OK;
 }
 
-// Strides of a B x H x Lq x Lk operand: rows that do not meet (read only: any).
+// Strides of a B x H x Lq x Lk operand: rows that do not meet (read only: any), within
+// 2^60 elements.
 static bool check_strides(const int64_t* s, int64_t B, int64_t H, int64_t Lq, int64_t Lk,
                           bool written) {
   if (!s) return false;
   if (s[0] < 0 || s[1] < 0 || s[2] < 0) return false;
-  constexpr int64_t most = int64_t(1) << 40;  // products with B, H, Lq stay below 2^63
+  constexpr int64_t most = int64_t(1) << 40;
   if (s[0] > most || s[1] > most || s[2] > most) return false;
-  if (!written) return true;
   // In the order of their strides, each dimension steps over all of the ones inside it.
   struct Dim {
     int64_t n, stride;
   } d[3] = {{B, s[0]}, {H, s[1]}, {Lq, s[2]}};
   std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
-  int64_t inside = Lk;  // elements that the inner dimensions span
+  __int128 inside = Lk;  // elements that the inner dimensions span: three products below 2^64
   for (const Dim& x : d) {
     if (x.n <= 1) continue;
-    if (x.stride < inside) return false;
-    inside += (x.n - 1) * x.stride;
+    if (written && x.stride < inside) return false;
+    inside += static_cast<__int128>(x.n - 1) * x.stride;
   }
-  return true;
+  return inside <= static_cast<__int128>(1) << 60;  // so the kernels' offsets fit in 63 bits
 }
 
 }  // namespace lmz

@@ -1,0 +1,58 @@
+"""Host-side checks of what the AdamW and relative-bias entry points accept (no GPU):
+calls that are refused return before anything is launched."""
+import ctypes
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_1810_10045_amd", "liblmzipf.so")
+P, I64, I32, SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
+INVAL = 1
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(LIB):
+        from paper_1810_10045_amd import build
+        build.build()
+    L = ctypes.CDLL(LIB)
+    L.lm_rel_buckets.argtypes = [I32, I32, I32, P, P, P]
+    L.lm_rel_bias.argtypes = [P, I64, I32, P, P, I32, I64, I64, I64, I64, I64, P, P, P, P, I32, P]
+    L.lm_rel_bias_grad.argtypes = [P, I32, I64, I64, I64, I64, P, I64, P, P, I32, I32, P, I64, I32,
+                                   P, SZ, P]
+    return L
+
+
+class Bias:
+    """lm_rel_bias and lm_rel_bias_grad on made-up addresses (the host reads none of them)."""
+
+    def __init__(self, lib):
+        self.lib, self.starts, self.ids, n = lib, (I32 * 257)(), (I32 * 257)(), I32()
+        assert lib.lm_rel_buckets(32, 128, 0, self.starts, self.ids, ctypes.byref(n)) == 0
+        self.n = n.value
+
+    def bias(self, shape, out, out_strides, add=None, add_strides=None, dtype=0):
+        s = lambda x: None if x is None else (I64 * 3)(*x)  # noqa: E731
+        return self.lib.lm_rel_bias(P(0x1000), shape[1], 32, self.starts, self.ids, self.n, *shape,
+                                    0, add, s(add_strides), out, s(out_strides), dtype, None)
+
+    def grad(self, shape, strides):
+        return self.lib.lm_rel_bias_grad(P(0x100000), 0, *shape, (I64 * 3)(*strides), 0,
+                                         self.starts, self.ids, self.n, 32, P(0x1000), shape[1], 0,
+                                         P(0x2000), 1 << 40, None)
+
+
+def test_rel_bias_strides_past_64_bits(lib):
+    """A span of strides that does not fit in 63 bits: rows that meet are not let through by
+    its wrapping around, and nothing that no memory holds is read."""
+    f = Bias(lib)
+    far, v = 1 << 40, P(0x100000)
+    # (2^24 - 1) 2^40 wraps to a number below zero; b = 1, h = 0 and b = 0, h = 1 are one row
+    assert f.bias((1 << 24, 2, 1, 1), v, (far, far, 1)) == INVAL
+    assert f.bias((1 << 24, 2, 1, 1), v, (far, far - 1, 1)) == INVAL
+    for shape, strides in (((1 << 24, 1, 1, 1), (far, 1, 1)), ((1, 1, 1 << 24, 4), (0, 0, far)),
+                           ((2, 1 << 10, 1 << 21, 1), (1, far, far))):
+        whole = (shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3])
+        assert f.bias(shape, v, whole, P(1 << 44), strides) == INVAL
+        assert f.grad(shape, strides) == INVAL
