@@ -548,8 +548,10 @@ int lm_sparse_apply_q8(float* table, int64_t V, int64_t D, int64_t ld_table, con
  * which depends on the sizes only: repeated calls give the same bits.
  * ws         device workspace of lm_rel_bias_grad_workspace_bytes(...), no
  *            initial contents required (0 bytes for short sequences: NULL).
- * Lengths, heads and batch up to LM_REL_MAX_LENGTH, 2^40 elements together;
- * a length of 0 is valid (the gradient is then zero).
+ * Lengths, heads and batch up to LM_REL_MAX_LENGTH, 2^40 elements together and
+ * fewer than 2^31 workgroups (of 16 rows x 256 columns of fp32, 32 x 512 of
+ * bf16, of one head and batch entry; others LM_E_UNSUPPORTED); a length of 0 is
+ * valid (the gradient is then zero).
  * ------------------------------------------------------------------------ */
 enum { LM_REL_BOTH = 0, LM_REL_PAST = 1, LM_REL_CAUSAL = 2 };
 #define LM_REL_MAX_BUCKETS 256

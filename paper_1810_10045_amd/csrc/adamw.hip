@@ -19,6 +19,7 @@
 //   572 us against 691).
 // - Two vectors of each operand a lane. One or four were no faster at 202M values, and a
 //   list of 20 small tensors took 3.7 us with two, 5.0 with four.
+#include "launch_parts.hpp"
 #include "moments.hpp"
 
 namespace lmz {
@@ -281,13 +282,14 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
     const int64_t* __restrict__ n_rows, int64_t rows_cap, const float* __restrict__ vals,
     int64_t ld_vals, MomentParams q, StepKeys keys, uint8_t* __restrict__ m,
     uint8_t* __restrict__ v, int64_t ld_codes, uint8_t* __restrict__ m_scale,
-    uint8_t* __restrict__ v_scale, int64_t ld_scale, int32_t* __restrict__ dev_err) {
+    uint8_t* __restrict__ v_scale, int64_t ld_scale, int32_t* __restrict__ dev_err,
+    uint32_t first_block) {
   constexpr int kRows = kSlots / NV;              // rows a lane holds at once
   constexpr int kPerWave = kWave / LANES * kRows;  // rows of a wave's turn
   __shared__ float inverse[kScales];
   const int lane = lane_id(), part = lane % LANES, group = lane / LANES;
-  const int64_t u0 = (static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) +
-                      first_lane(threadIdx.x >> 6)) * kPerWave;
+  const int64_t block = first_block + blockIdx.x;
+  const int64_t u0 = (block * (kAdamwThreads / kWave) + first_lane(threadIdx.x >> 6)) * kPerWave;
   // The ids come with the count, not after it (any entry below the capacity may be read).
   int64_t id[kRows];
 #pragma unroll
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
     if (u0 == 0 && lane == 0) raise_err(dev_err, LM_DEVERR_CAPACITY);
     count = rows_cap;
   }
-  if (static_cast<int64_t>(blockIdx.x) * (kAdamwThreads / kWave) * kPerWave >= count) return;
+  if (block * (kAdamwThreads / kWave) * kPerWave >= count) return;
   fill_scales(inverse, kAdamwThreads);
   bool ok = true, range = true, live[kRows];
 #pragma unroll
@@ -415,17 +417,15 @@ void adamw_plan_write(void* const* p, const void* const* g, void* const* m, void
 }
 
 template <typename GT, bool EIGHT>
-static void adamw_launch(const void* plan, int64_t chunks, uint64_t kind, bool copies,
-                         const OptParams& o, const MomentParams& q, const StepKeys& keys,
-                         const float* grad_scale, int32_t* dev_err, hipStream_t st) {
-  const PlanChunk* c = static_cast<const PlanChunk*>(plan);
-  const dim3 grid(static_cast<uint32_t>(chunks));
-  if (copies)
-    k_adamw<GT, EIGHT, true><<<grid, kAdamwThreads, 0, st>>>(c, kind, o, q, keys, grad_scale,
-                                                             dev_err);
-  else
-    k_adamw<GT, EIGHT, false><<<grid, kAdamwThreads, 0, st>>>(c, kind, o, q, keys, grad_scale,
-                                                              dev_err);
+static int adamw_launch(const void* plan, int64_t chunks, uint64_t kind, bool copies,
+                        const OptParams& o, const MomentParams& q, const StepKeys& keys,
+                        const float* grad_scale, int32_t* dev_err, hipStream_t st) {
+  auto kernel = copies ? k_adamw<GT, EIGHT, true> : k_adamw<GT, EIGHT, false>;
+  return launch_parts(chunks, kAdamwThreads, [&](uint32_t first, uint32_t n) {
+    kernel<<<n, kAdamwThreads, 0, st>>>(static_cast<const PlanChunk*>(plan) + first, kind, o, q,
+                                        keys, grad_scale, dev_err);
+    return launch_status(hipGetLastError());
+  });
 }
 
 int adamw_run(const void* plan, int64_t chunks, int gtype, int states, bool copies, float lr,
@@ -439,8 +439,7 @@ int adamw_run(const void* plan, int64_t chunks, int gtype, int states, bool copi
   const bool eight = states == 8;
   auto launch = gtype == LM_BF16 ? (eight ? adamw_launch<bf16_t, true> : adamw_launch<bf16_t, false>)
                                  : (eight ? adamw_launch<float, true> : adamw_launch<float, false>);
-  launch(plan, chunks, kind, copies, o, q, keys, grad_scale, dev_err, st);
-  return launch_status(hipGetLastError());
+  return launch(plan, chunks, kind, copies, o, q, keys, grad_scale, dev_err, st);
 }
 
 struct Rows8 {
@@ -463,13 +462,16 @@ struct Rows8 {
 };
 
 template <typename KeyT, int LANES, int NV, End END>
-static void rows8_launch(const Rows8& a, hipStream_t st) {
+static int rows8_launch(const Rows8& a, hipStream_t st) {
   constexpr int kPerBlock = kAdamwThreads / LANES * (kSlots / NV);
-  const dim3 grid(static_cast<uint32_t>((a.rows_cap + kPerBlock - 1) / kPerBlock));
-  k_rows8<KeyT, LANES, NV, END><<<grid, kAdamwThreads, 0, st>>>(
-      a.table, a.V, a.D, a.ld_table, static_cast<const KeyT*>(a.rows), a.n_rows, a.rows_cap,
-      a.vals, a.ld_vals, a.q, a.keys, a.m, a.v, a.ld_codes, a.m_scale, a.v_scale, a.ld_scale,
-      a.dev_err);
+  const int64_t blocks = (a.rows_cap + kPerBlock - 1) / kPerBlock;
+  return launch_parts(blocks, kAdamwThreads, [&](uint32_t first, uint32_t n) {
+    k_rows8<KeyT, LANES, NV, END><<<n, kAdamwThreads, 0, st>>>(
+        a.table, a.V, a.D, a.ld_table, static_cast<const KeyT*>(a.rows), a.n_rows, a.rows_cap,
+        a.vals, a.ld_vals, a.q, a.keys, a.m, a.v, a.ld_codes, a.m_scale, a.v_scale, a.ld_scale,
+        a.dev_err, first);
+    return launch_status(hipGetLastError());
+  });
 }
 
 // Lanes a row, vectors a lane. 100,000 rows of 32, 64, 128 values take 21, 29, 46 us so,
@@ -477,23 +479,22 @@ static void rows8_launch(const Rows8& a, hipStream_t st) {
 // 4 vectors a lane. Rows of whole vectors (WHOLE) of 128 and 512 values: 44 and 157 us, 49
 // and 159 as PART.
 template <typename KeyT, End END>
-static void rows8_shape(const Rows8& a, hipStream_t st) {
+static int rows8_shape(const Rows8& a, hipStream_t st) {
   const int vectors = (a.D + kVec - 1) / kVec;
-  if (END == FEW || vectors <= 8) return rows8_launch<KeyT, 8, 1, END>(a, st);
   if constexpr (END != FEW) {
-    if (vectors <= 16) rows8_launch<KeyT, 16, 1, END>(a, st);
-    else if (vectors <= 32) rows8_launch<KeyT, 32, 1, END>(a, st);
-    else if (vectors <= 64) rows8_launch<KeyT, 64, 1, END>(a, st);
-    else if (vectors <= 128) rows8_launch<KeyT, 64, 2, END>(a, st);
-    else rows8_launch<KeyT, 64, 4, END>(a, st);
+    if (vectors > 128) return rows8_launch<KeyT, 64, 4, END>(a, st);
+    if (vectors > 64) return rows8_launch<KeyT, 64, 2, END>(a, st);
+    if (vectors > 32) return rows8_launch<KeyT, 64, 1, END>(a, st);
+    if (vectors > 16) return rows8_launch<KeyT, 32, 1, END>(a, st);
+    if (vectors > 8) return rows8_launch<KeyT, 16, 1, END>(a, st);
   }
+  return rows8_launch<KeyT, 8, 1, END>(a, st);
 }
 
 template <typename KeyT>
-static void rows8_ends(const Rows8& a, hipStream_t st) {
-  if (a.D % kVec == 0) rows8_shape<KeyT, WHOLE>(a, st);
-  else if (a.D > kVec) rows8_shape<KeyT, PART>(a, st);
-  else rows8_shape<KeyT, FEW>(a, st);
+static int rows8_ends(const Rows8& a, hipStream_t st) {
+  if (a.D % kVec == 0) return rows8_shape<KeyT, WHOLE>(a, st);
+  return a.D > kVec ? rows8_shape<KeyT, PART>(a, st) : rows8_shape<KeyT, FEW>(a, st);
 }
 
 int rows8_run(float* table, int64_t V, int64_t D, int64_t ld_table, const void* rows, int idtype,
@@ -506,9 +507,7 @@ int rows8_run(float* table, int64_t V, int64_t D, int64_t ld_table, const void* 
   const Rows8 a{table, V, static_cast<int>(D), ld_table, rows, n_rows, rows_cap, vals, ld_vals,
                 make_moment_params(o, beta2, step), step_keys(seed), m, v, ld_codes, m_scale,
                 v_scale, ld_scale, dev_err};
-  if (idtype == LM_I64) rows8_ends<int64_t>(a, st);
-  else rows8_ends<int32_t>(a, st);
-  return launch_status(hipGetLastError());
+  return idtype == LM_I64 ? rows8_ends<int64_t>(a, st) : rows8_ends<int32_t>(a, st);
 }
 
 }  // namespace lmz

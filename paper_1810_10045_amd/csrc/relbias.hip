@@ -10,6 +10,7 @@
 // many values in registers; the gradient adds a patch into that many sums. Each
 // element of the matrices is read or written once: HBM bounds both.
 #include "common.hpp"
+#include "launch_parts.hpp"
 
 namespace lmz {
 
@@ -167,7 +168,8 @@ __device__ __forceinline__ float from_lane_below(float v) {
 template <typename T, bool ADD, bool NARROW>
 __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
     const float* __restrict__ table, int64_t ld_table, Segments seg, int H, int Lq, int Lk,
-    int q_start, const T* add, Strides sa, T* out, Strides so, int col_tiles, int row_tiles) {
+    int q_start, const T* add, Strides sa, T* out, Strides so, int col_tiles, int row_tiles,
+    uint32_t first_block) {
   constexpr int P = Patch<T>::P;
   constexpr int kCols = kWave * P, kRows = kRelWaves * P;
   constexpr int kLine = kRows + kCols;
@@ -175,7 +177,8 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
   __shared__ __attribute__((aligned(16))) float line[kLine];
   __shared__ int32_t starts[LM_REL_MAX_SEGMENTS];
   __shared__ float value[LM_REL_MAX_SEGMENTS];
-  const int rt = blockIdx.x % row_tiles, rest = blockIdx.x / row_tiles;
+  const uint32_t block = first_block + blockIdx.x;
+  const int rt = block % row_tiles, rest = block / row_tiles;
   const int ct = rest % col_tiles, rest2 = rest / col_tiles;
   const int h = rest2 % H, b = rest2 / H;
   const int lane = lane_id(), r = first_lane(threadIdx.x >> 6) * P;  // this wave's rows
@@ -286,7 +289,7 @@ constexpr int kDirectWaves = 16;
 template <typename T, bool NARROW, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
     const T* __restrict__ dout, Strides sd, Segments seg, int B, int Lq, int Lk, int q_start,
-    GradPlan g, float* __restrict__ ws, GradTable dt) {
+    GradPlan g, float* __restrict__ ws, GradTable dt, uint32_t first_block) {
   constexpr int P = Patch<T>::P;
   constexpr bool kDirect = WAVES == kDirectWaves;
   constexpr int kThreads = WAVES * kWave;
@@ -301,7 +304,8 @@ __global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
   __shared__ float total[kDirect ? LM_REL_MAX_SEGMENTS : 1];
   __shared__ int ids[kDirect ? LM_REL_MAX_SEGMENTS : 1];
   const int lane = lane_id(), wave = first_lane(threadIdx.x >> 6);
-  const int rp = blockIdx.x % g.row_parts, rest = blockIdx.x / g.row_parts;
+  const uint32_t block = first_block + blockIdx.x;
+  const int rp = block % g.row_parts, rest = block / g.row_parts;
   const int ct = rest % g.col_tiles, rest2 = rest / g.col_tiles;
   const int bp = rest2 % g.batch_parts, h = rest2 / g.batch_parts;
   const int nt = (Lq + P - 1) / P;
@@ -311,7 +315,7 @@ __global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
   const int col0 = ct * kWave * P, col = col0 + lane * P;
   // a patch's diagonal k has distance low + k
   auto low = [&](int column, int t) { return column - (t * P + P - 1) - q_start; };
-  float* mine = kDirect ? total : ws + static_cast<int64_t>(blockIdx.x) * seg.n;
+  float* mine = kDirect ? total : ws + static_cast<int64_t>(block) * seg.n;
   const int first = low(col0, (rp + 1) * WAVES * g.groups - 1);  // the smallest distance
   if (!kDirect && first >= seg.masked) {  // all of this workgroup's patches are
     for (int s = threadIdx.x; s < seg.n; s += kThreads) mine[s] = 0.f;
@@ -422,11 +426,11 @@ __global__ __launch_bounds__(WAVES * kWave) void k_rel_grad(
 constexpr int kJoinThreads = 1024;
 
 __global__ __launch_bounds__(kJoinThreads) void k_rel_join(
-    const float* __restrict__ ws, Segments seg, int parts, GradTable dt) {
+    const float* __restrict__ ws, Segments seg, int parts, GradTable dt, uint32_t first_head) {
   __shared__ float part[kJoinThreads];
   __shared__ float sums[LM_REL_MAX_SEGMENTS];
   __shared__ int ids[LM_REL_MAX_SEGMENTS];
-  const int h = blockIdx.x, n = seg.n;
+  const int h = first_head + blockIdx.x, n = seg.n;
   int width = 32;  // segments of one turn
   while (width < n) width *= 2;
   const int column = threadIdx.x % width, first = threadIdx.x / width, step = kJoinThreads / width;
@@ -466,20 +470,22 @@ static Segments make_segments(const int32_t* starts, const int32_t* ids, int n) 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 template <typename T>
-static void rel_bias_launch(const float* table, int64_t ld_table, const Segments& seg, int64_t B,
-                            int64_t H, int64_t Lq, int64_t Lk, int64_t q_start, const void* add,
-                            const Strides& sa, void* out, const Strides& so, hipStream_t st) {
+static int rel_bias_launch(const float* table, int64_t ld_table, const Segments& seg, int64_t B,
+                           int64_t H, int64_t Lq, int64_t Lk, int64_t q_start, const void* add,
+                           const Strides& sa, void* out, const Strides& so, hipStream_t st) {
   constexpr int P = Patch<T>::P;
   const int64_t ct = ceil_div(Lk, kWave * P), rt = ceil_div(Lq, kRelWaves * P);
-  const dim3 grid(static_cast<uint32_t>(ct * rt * H * B));
   const bool narrow = Lk < Patch<T>::P;
   auto kernel = add ? (narrow ? k_rel_bias<T, true, true> : k_rel_bias<T, true, false>)
                     : k_rel_bias<T, false, false>;
-  kernel<<<grid, kRelThreads, 0, st>>>(table, ld_table, seg, static_cast<int>(H),
-                                       static_cast<int>(Lq), static_cast<int>(Lk),
-                                       static_cast<int>(q_start), static_cast<const T*>(add), sa,
-                                       static_cast<T*>(out), so, static_cast<int>(ct),
-                                       static_cast<int>(rt));
+  return launch_parts(ct * rt * H * B, kRelThreads, [&](uint32_t first, uint32_t n) {
+    kernel<<<n, kRelThreads, 0, st>>>(table, ld_table, seg, static_cast<int>(H),
+                                      static_cast<int>(Lq), static_cast<int>(Lk),
+                                      static_cast<int>(q_start), static_cast<const T*>(add), sa,
+                                      static_cast<T*>(out), so, static_cast<int>(ct),
+                                      static_cast<int>(rt), first);
+    return launch_status(hipGetLastError());
+  });
 }
 
 // Workgroups of a call, for the check of the grid's size.
@@ -496,11 +502,8 @@ int rel_bias_run(const float* table, int64_t ld_table, const int32_t* starts, co
   const Segments seg = make_segments(starts, ids, n_seg);
   const Strides a = add ? Strides{sa[0], sa[1], sa[2]} : Strides{0, 0, 0};
   const Strides o{so[0], so[1], so[2]};
-  if (dtype == LM_BF16)
-    rel_bias_launch<bf16_t>(table, ld_table, seg, B, H, Lq, Lk, q_start, add, a, out, o, st);
-  else
-    rel_bias_launch<float>(table, ld_table, seg, B, H, Lq, Lk, q_start, add, a, out, o, st);
-  return launch_status(hipGetLastError());
+  auto launch = dtype == LM_BF16 ? rel_bias_launch<bf16_t> : rel_bias_launch<float>;
+  return launch(table, ld_table, seg, B, H, Lq, Lk, q_start, add, a, out, o, st);
 }
 
 // How a head's matrices are shared out among waves.
@@ -542,18 +545,21 @@ int64_t rel_grad_parts(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dtype) 
 }
 
 template <typename T>
-static void rel_grad_launch(const void* dout, const Strides& s, const Segments& seg, int64_t B,
-                            int64_t H, int64_t Lq, int64_t Lk, int64_t q_start, const GradPlan& g,
-                            float* ws, const GradTable& dt, hipStream_t st) {
+static int rel_grad_launch(const void* dout, const Strides& s, const Segments& seg, int64_t B,
+                           int64_t H, int64_t Lq, int64_t Lk, int64_t q_start, const GradPlan& g,
+                           float* ws, const GradTable& dt, hipStream_t st) {
   const bool narrow = Lk < Patch<T>::P;
   auto kernel = g.direct ? (narrow ? k_rel_grad<T, true, kDirectWaves>
                                    : k_rel_grad<T, false, kDirectWaves>)
                          : (narrow ? k_rel_grad<T, true, kRelWaves>
                                    : k_rel_grad<T, false, kRelWaves>);
   const int threads = (g.direct ? kDirectWaves : kRelWaves) * kWave;
-  kernel<<<static_cast<uint32_t>(g.parts() * H), threads, 0, st>>>(
-      static_cast<const T*>(dout), s, seg, static_cast<int>(B), static_cast<int>(Lq),
-      static_cast<int>(Lk), static_cast<int>(q_start), g, ws, dt);
+  return launch_parts(g.parts() * H, threads, [&](uint32_t first, uint32_t n) {
+    kernel<<<n, threads, 0, st>>>(static_cast<const T*>(dout), s, seg, static_cast<int>(B),
+                                  static_cast<int>(Lq), static_cast<int>(Lk),
+                                  static_cast<int>(q_start), g, ws, dt, first);
+    return launch_status(hipGetLastError());
+  });
 }
 
 int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, int64_t Lk,
@@ -568,15 +574,15 @@ int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, 
   if (B > 0 && Lq > 0 && Lk > 0) {
     const GradPlan g = grad_plan(B, H, Lq, Lk, dtype);
     const Strides s{sd[0], sd[1], sd[2]};
-    if (dtype == LM_BF16) rel_grad_launch<bf16_t>(dout, s, seg, B, H, Lq, Lk, q_start, g, sums, dt, st);
-    else rel_grad_launch<float>(dout, s, seg, B, H, Lq, Lk, q_start, g, sums, dt, st);
-    const int rc = launch_status(hipGetLastError());
+    auto launch = dtype == LM_BF16 ? rel_grad_launch<bf16_t> : rel_grad_launch<float>;
+    const int rc = launch(dout, s, seg, B, H, Lq, Lk, q_start, g, sums, dt, st);
     if (rc != LM_OK || g.direct) return rc;
     parts = g.parts();
   }
-  k_rel_join<<<static_cast<uint32_t>(H), kJoinThreads, 0, st>>>(
-      sums, seg, static_cast<int>(parts), dt);
-  return launch_status(hipGetLastError());
+  return launch_parts(H, kJoinThreads, [&](uint32_t first, uint32_t n) {
+    k_rel_join<<<n, kJoinThreads, 0, st>>>(sums, seg, static_cast<int>(parts), dt, first);
+    return launch_status(hipGetLastError());
+  });
 }
 
 // The segments of the logarithmic buckets. One side has n buckets: distance d

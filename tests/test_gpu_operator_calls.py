@@ -1,0 +1,108 @@
+"""Calls of the AdamW and relative-bias entry points that their documentation allows at
+the edges: grids past one launch, memory across streams, state that is kept, autograd."""
+import ctypes
+import os
+import sys
+
+import numpy as np
+import pytest
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import moments_ref as M  # noqa: E402
+import relbias_ref as R  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+DEV = "cuda"
+ONE_LAUNCH = (1 << 24) - 1  # workgroups of 256 threads
+
+
+@pytest.fixture(scope="module")
+def lz():
+    from paper_1810_10045_amd import lmzipf
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    M.device_powers(torch)
+    return lmzipf
+
+
+def _room(gib):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gib << 30:
+        pytest.skip(f"needs {gib} GiB")
+
+
+# ---------------------------------------------------------------------------
+# More workgroups than one launch holds
+# ---------------------------------------------------------------------------
+def test_rel_bias_past_one_launch(lz):
+    """One workgroup a head and batch entry, more than 2^24 of them."""
+    _room(4)
+    B, H, Lk = (1 << 23) + 3, 2, 3
+    assert B * H > ONE_LAUNCH
+    table = torch.randn(32, H, device=DEV)
+    add = torch.randn(B, H, 1, Lk, device=DEV)
+    got = lz.rel_bias(table, lz.rel_buckets(32, 128, "both"), 1, Lk, q_start=1, add=add)
+    of = torch.tensor([R.bucket(j - 1, 32, 128, "both") for j in range(Lk)], device=DEV)
+    assert torch.equal(got, add + table[of].T[None, :, None])
+
+
+@pytest.mark.parametrize("B,H,Lk,threads", [(1, (1 << 22) + 5, 4, 1024),     # a head a workgroup
+                                            (9, (1 << 22) + 5, 4, 1024),     # the join's
+                                            (1, (1 << 23) + 1, 257, 256)])   # two a head
+def test_rel_bias_grad_past_one_launch(lz, B, H, Lk, threads):
+    _room(24)
+    assert H * (2 if Lk > 256 else 1) * threads >= 1 << 32
+    buckets = lz.rel_buckets(4, 3, "both")
+    of = torch.tensor([R.bucket(j, 4, 3, "both") for j in range(Lk)], device=DEV)
+    x = torch.randint(-3, 4, (B, H, 1, Lk), device=DEV, dtype=torch.int8).float()
+    got = lz.rel_bias_grad(x, buckets)
+    total = x.sum(0)[:, 0]
+    del x
+    for n in range(4):
+        assert torch.equal(got[n], total[:, of == n].sum(1)), n
+
+
+def test_rows8_past_one_launch(lz):
+    """A capacity of 2^31 - 1 rows of one value, most of whose ids name no row."""
+    _room(24)
+    cap, V = (1 << 31) - 1, 50
+    rows = torch.full((cap,), -1, dtype=torch.int32, device=DEV)
+    vals = torch.zeros(cap, 1, device=DEV)
+    at, ids = [0, 1 << 30, cap - 3, cap - 2, cap - 1], [4, 9, 20, 30, 49]
+    rows[at] = torch.tensor(ids, dtype=torch.int32, device=DEV)
+    vals[at] = 1.0
+    table = torch.zeros(V, 1, device=DEV)
+    m, v, ms, vs = (torch.zeros(V, 1, dtype=torch.uint8, device=DEV) for _ in range(4))
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    lz.sparse_apply_q8(table, rows, torch.tensor([cap], device=DEV), vals, m, v, ms, vs, lr=0.5,
+                       dev_err=err)
+    assert int(err.item()) == lz.DEVERR_ID_RANGE
+    for t in (table, m, v, ms, vs):
+        assert t[:, 0].nonzero().flatten().tolist() == ids
+    assert float((table[ids] + 0.5).abs().max()) < 1e-6
+
+
+def test_adamw_past_one_launch(lz):
+    """A list of more than 2^24 tensors of one value."""
+    _room(8)
+    n = ONE_LAUNCH + 4
+    p, m, v = (torch.zeros(n, device=DEV) for _ in range(3))
+    g = torch.ones(n, device=DEV)
+    at = lambda t: np.uint64(t.data_ptr()) + 4 * np.arange(n, dtype=np.uint64)  # noqa: E731
+    lists = [at(t) for t in (p, g, m, v)]
+    sizes = np.ones(n, np.int64)
+    ptr = lambda a: a.ctypes.data  # noqa: E731
+    need = lz.lib().lm_adamw_plan_bytes(ptr(sizes), n)
+    table = np.zeros(need // 8, np.uint64)
+    chunks = ctypes.c_int64()
+    assert lz.lib().lm_adamw_plan(*[ptr(a) for a in lists], None, None, None, ptr(sizes), None, n,
+                                  lz.F32, 32, ptr(table), need, ctypes.byref(chunks)) == 0
+    assert chunks.value == n
+    plan = torch.from_numpy(table.view(np.int64)).to(DEV)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    assert lz.lib().lm_adamw(plan.data_ptr(), need, n, lz.F32, 32, 0, 0.5, 0.0, 0.0, 1e-8, 0.0, 1,
+                             None, 0, err.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    lz.check(err)
+    assert bool((m == 1).all()) and bool((v == 1).all()) and float((p + 0.5).abs().max()) < 1e-6

@@ -2,6 +2,7 @@
 calls that are refused return before anything is launched."""
 import ctypes
 import os
+import subprocess
 
 import pytest
 
@@ -56,3 +57,41 @@ def test_rel_bias_strides_past_64_bits(lib):
         whole = (shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3])
         assert f.bias(shape, v, whole, P(1 << 44), strides) == INVAL
         assert f.grad(shape, strides) == INVAL
+
+
+LAUNCHES = r"""
+#include "launch_parts.hpp"
+extern "C" int64_t parts(int64_t blocks, int threads, int fail_at, uint32_t* first, uint32_t* n,
+                         int room) {
+  int k = 0;
+  const int rc = lmz::launch_parts(blocks, threads, [&](uint32_t f, uint32_t c) {
+    if (k < room) first[k] = f, n[k] = c;
+    return ++k == fail_at ? 4 : 0;
+  });
+  return rc * 1000 + k;
+}
+"""
+
+
+def test_launches_stay_below_2_32_threads(tmp_path):
+    """Every workgroup in one launch, and no launch of 2^32 threads."""
+    (tmp_path / "parts.cpp").write_text(LAUNCHES)
+    so = str(tmp_path / "parts.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-shared", "-fPIC", "-I",
+                    os.path.join(ROOT, "paper_1810_10045_amd", "csrc"), "-o", so,
+                    str(tmp_path / "parts.cpp")], check=True)
+    f = ctypes.CDLL(so).parts
+    f.argtypes, f.restype = [I64, I32, I32, P, P, I32], I64
+    for threads in (256, 1024):
+        most = (1 << 32) // threads - 1
+        for blocks in (0, 1, 5, most - 1, most, most + 1, 2 * most, 2 * most + 1, (1 << 31) - 1):
+            first, n = (ctypes.c_uint32 * 600)(), (ctypes.c_uint32 * 600)()
+            k = f(blocks, threads, 0, first, n, 600)
+            assert k == -(-blocks // most)
+            at = 0
+            for i in range(k):
+                assert first[i] == at and 0 < n[i] * threads < 1 << 32
+                at += n[i]
+            assert at == blocks
+    first, n = (ctypes.c_uint32 * 8)(), (ctypes.c_uint32 * 8)()
+    assert f(1 << 26, 256, 2, first, n, 8) == 4002, "an error ends the launches"
