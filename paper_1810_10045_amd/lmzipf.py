@@ -628,15 +628,16 @@ def _scales(t: torch.Tensor, what: str):
 class AdamwPlan(NamedTuple):
     """A list of tensors as ``adamw`` steps it: the table that names their
     memory on the device, and that memory itself, which it keeps alive also
-    where a tensor has been given other memory since (`p.data = ...`). `home`:
-    the stream on which the table's memory was allocated."""
+    where a tensor has been given other memory since (`p.data = ...`), until
+    every stream that stepped it is past its steps. `streams`: the handles of
+    those that the allocator knows of."""
     table: torch.Tensor
     tensors: tuple
     chunks: int
     gtype: int
     states: int
     copies: bool
-    home: int
+    streams: set
 
 
 def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
@@ -703,7 +704,7 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
     keep = tuple(tuple(t.detach() for t in x) for x in [params] + list(lists.values()))
     with torch.cuda.device(device):
         return AdamwPlan(host.to(device), keep, chunks.value, gtype, 8 if eight else 32,
-                         "copies" in lists, _on(device, None))
+                         "copies" in lists, set())
 
 
 def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
@@ -722,8 +723,13 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
             return adamw(plan, lr, beta1, beta2, eps, weight_decay, step, grad_scale, seed,
                          dev_err, stream)
     handle = _on(table.device, stream)
-    if handle != plan.home:  # the table's memory is not to be reused before this stream is past it
-        table.record_stream(stream or torch.cuda.current_stream())
+    if handle not in plan.streams:
+        # The plan may hold the last reference to its memory, which is not to be reused before
+        # this stream is past its steps (recording a tensor's own stream does nothing).
+        at = stream or torch.cuda.current_stream()
+        for t in (table, *(t for x in plan.tensors for t in x)):
+            t.record_stream(at)
+        plan.streams.add(handle)
     _call(_lib.lm_adamw(_ptr(table), table.numel(), plan.chunks, plan.gtype, plan.states,
                         plan.copies, lr, beta1, beta2, eps, weight_decay, step,
                         _ptr(grad_scale), seed, _ptr(dev_err), handle), "lm_adamw")

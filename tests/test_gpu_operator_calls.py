@@ -106,3 +106,32 @@ def test_adamw_past_one_launch(lz):
     torch.cuda.synchronize()
     lz.check(err)
     assert bool((m == 1).all()) and bool((v == 1).all()) and float((p + 0.5).abs().max()) < 1e-6
+
+
+# ---------------------------------------------------------------------------
+# Memory across streams
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("states", [32, 8])
+def test_adamw_plan_memory_outlives_a_late_side_stream(lz, states):
+    """A step that waits on a side stream when the plan, the last owner of its tensors, goes
+    away: their memory goes to no new tensor of the first stream before the step is over."""
+    n = 300_000
+    dt = torch.uint8 if states == 8 else torch.float32
+    p, g = torch.zeros(n, device=DEV), torch.ones(n, device=DEV)
+    m, v = (torch.zeros(n, dtype=dt, device=DEV) for _ in range(2))
+    copy = torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    scales = [[torch.zeros(M.blocks(n), dtype=torch.uint8, device=DEV)] for _ in range(2)]
+    kw = dict(m_scale=scales[0], v_scale=scales[1]) if states == 8 else {}
+    plan = lz.adamw_plan([p], [g], [m], [v], copies=[copy], **kw)
+    sizes = [(t.numel(), t.dtype) for t in (g, m, v, copy, *scales[0], *scales[1])]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)  # 10 to 200 ms by the clock it counts
+    lz.adamw(plan, lr=0.5, beta1=0.0, beta2=0.0, stream=side)
+    del plan, g, m, v, copy, scales, kw
+    new = [torch.full((k,), 7, dtype=d, device=DEV) for k, d in sizes for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(bool((x == 7).all()) for x in new)
+    assert float((p + 0.5).abs().max()) < 1e-6
