@@ -432,8 +432,11 @@ int lm_sparse_apply_f16(float* table, int64_t V, int64_t D, int64_t ld_table,
  * R the high (m) or low (v) 20 bits of the value's random word and 2^-k the
  * fp32 power that the device's math library gives (for some k half a unit in
  * the last place low: torch.ldexp's, so torch operations give the same
- * codes); a nonzero root of v never gets the code zero. The words are a function of `seed` and
- * the value's number: the values of a list count through, each tensor from
+ * codes); a nonzero root of v never gets the code zero. The moments of a value
+ * that keeps m and v (above) are scaled by 2^-k itself: they stay the same
+ * numbers, but for those that the grid of a block whose scale grows no longer
+ * holds, which are rounded. The words are a function of `seed` and the value's
+ * number: the values of a list count through, each tensor from
  * the next multiple of LM_MOMENT_BLOCK (of a table: id * D + column). Give
  * every step and every list its own seed; the same seed repeats a call bit
  * for bit. State that starts from zero starts from zero bytes.
@@ -492,9 +495,8 @@ int lm_adamw(const void* plan, size_t plan_bytes, int64_t chunks, int32_t gtype,
  * dev_err may be NULL, a V of 0 is no error, rows_cap is below 2^31 and rows
  * and vals hold rows_cap entries (those past *n_rows may be read); rows of
  * the table that are not named are untouched in all five arrays. A value whose new v
- * is not finite keeps its parameter and moments and sets
- * LM_DEVERR_NONFINITE (its moments are rounded again where its block's scale
- * changes). */
+ * is not finite keeps its parameter and moments, as above, and sets
+ * LM_DEVERR_NONFINITE. */
 int lm_sparse_apply_q8(float* table, int64_t V, int64_t D, int64_t ld_table, const void* rows,
                        int32_t idtype, const int64_t* n_rows, int64_t rows_cap, const float* vals,
                        int64_t ld_vals, float lr, float beta1, float beta2, float eps,

@@ -200,12 +200,12 @@ __device__ __forceinline__ bool step_vectors(const PlanChunk& t, int i0, float g
       settle<END>(i, n, m[j]);
       settle<END>(i, n, v[j]);
     }
-    uint32_t word[kVec], low[kVec];
+    uint32_t word[kVec], low[kVec], kept = 0;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       const float x = g[j][e] * gs;
       if constexpr (EIGHT) {
-        ok &= adamw_value8(p[j][e], m[j][e], v[j][e], x, wd, q);
+        kept |= adamw_value8(p[j][e], m[j][e], v[j][e], x, wd, q) ? 0u : 1u << e;
         word[e] = value_word(static_cast<uint64_t>(t.first + i + e), keys);
         low[e] = word[e] << 12;
       } else {
@@ -221,8 +221,9 @@ __device__ __forceinline__ bool step_vectors(const PlanChunk& t, int i0, float g
       }
     }
     if constexpr (EIGHT) {
-      mc[j] = encode4<false>(m[j], word, inverse, ms[j]);
-      vc[j] = encode4<true>(v[j], low, inverse, vs[j]);
+      ok &= kept == 0;
+      mc[j] = encode4<false>(m[j], word, kept, inverse, ms[j]);
+      vc[j] = encode4<true>(v[j], low, kept, inverse, vs[j]);
     }
     store4<END>(t.p, i, n, p[j]);
     if constexpr (COPY) store4<END>(t.copy, i, n, p[j]);
@@ -336,23 +337,22 @@ __global__ __launch_bounds__(kAdamwThreads) void k_rows8(
       for (int s = 0; s < kSlots; ++s) {
         const int r = s / NV, c = cb + (s % NV * LANES + part) * kVec;
         float mx[kVec], vx[kVec];
-        uint32_t word[kVec], low[kVec];
+        uint32_t word[kVec], low[kVec], kept = 0;
         settle<END>(c, D, p[s]);
         settle<END>(c, D, g[s]);
         decode4(settle<END>(c, D, mc[s]), ms[s], mx);
         decode4(settle<END>(c, D, vc[s]), vs[s], vx);
         const uint64_t number = static_cast<uint64_t>(id[r]) * D + c;
-        bool fine = true;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-          fine &= adamw_value8(p[s][e], mx[e], vx[e], g[s][e], q.wd, q);
+          kept |= adamw_value8(p[s][e], mx[e], vx[e], g[s][e], q.wd, q) ? 0u : 1u << e;
           word[e] = value_word(number + e, keys);
           low[e] = word[e] << 12;
         }
-        mc[s] = encode4<false>(mx, word, inverse, ms[s]);
-        vc[s] = encode4<true>(vx, low, inverse, vs[s]);
+        mc[s] = encode4<false>(mx, word, kept, inverse, ms[s]);
+        vc[s] = encode4<true>(vx, low, kept, inverse, vs[s]);
         if (!live[r] || c >= D) continue;
-        ok &= fine;
+        ok &= kept == 0;
         store4<END>(table + id[r] * ld_table, c, D, p[s]);
         store_codes<END>(m + id[r] * ld_codes, c, D, mc[s]);
         store_codes<END>(v + id[r] * ld_codes, c, D, vc[s]);

@@ -3,10 +3,12 @@
 //
 // Format. 32 consecutive values share a scale 2^k, k the smallest integer with
 // max|x| <= 448 * 2^k (448: the largest e4m3 number), kept as the byte k + 127.
-// A value is its e4m3 code times the scale. A power of two makes decoding and
-// scaling exact, so a value that does not change stays the same number when its
-// block's scale shrinks (and, down to the grid's subnormals, when it grows), and
-// costs e4m3 no precision: its step is relative. The second moment is kept as its square
+// A value is its e4m3 code times the scale. A power of two makes decoding exact and
+// costs e4m3 no precision: its step is relative. A value that the step leaves as it
+// is (its new second moment is not finite) is scaled by the exact power too, so it
+// stays the same number when its block's scale shrinks (and, down to the grid's
+// subnormals, when it grows); the others by a power that may be half a unit low
+// (fill_scales), which is within their rounding. The second moment is kept as its square
 // root: codes reach 2^-18 below a block's largest, which is 2^-36 in v.
 //
 // Rounding is stochastic. With beta2 = 0.999 a step moves sqrt(v) by 0.05% of
@@ -94,9 +96,10 @@ __device__ __forceinline__ void fill_scales(float* inverse, int threads) {
 }
 
 // The codes of 4 values of this lane's block (8 lanes) and the block's scale byte.
-// FLOOR: values above zero round to no code below 1.
+// FLOOR: values above zero round to no code below 1. kept: a bit for each value that
+// the step did not change.
 template <bool FLOOR>
-__device__ __forceinline__ uint32_t encode4(const float* x, const uint32_t* word,
+__device__ __forceinline__ uint32_t encode4(const float* x, const uint32_t* word, uint32_t kept,
                                             const float* inverse, int& scale) {
   uint32_t top = 0;
 #pragma unroll
@@ -108,9 +111,17 @@ __device__ __forceinline__ uint32_t encode4(const float* x, const uint32_t* word
   const float by = inverse[scale];
   float y[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    y[e] = x[e] * by;
-    if (FLOOR) y[e] = x[e] > 0.f ? fmaxf(y[e], 0x1p-9f) : 0.f;
+  for (int e = 0; e < 4; ++e) y[e] = x[e] * by;
+  if (ballot(kept != 0)) {
+    // A kept value is on the grid unless its block's scale grew past it, and stays there: a
+    // power half a unit low would take it a whole step down where its random part is 0.
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      y[e] = kept >> e & 1 ? __builtin_amdgcn_ldexpf(x[e], 127 - scale) : y[e];
+  }
+  if (FLOOR) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = x[e] > 0.f ? fmaxf(y[e], 0x1p-9f) : 0.f;
   }
   int c = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], word[0], 0, 0);
   c = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], word[1], c, 1);

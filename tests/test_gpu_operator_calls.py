@@ -135,3 +135,78 @@ def test_adamw_plan_memory_outlives_a_late_side_stream(lz, states):
     torch.cuda.synchronize()
     assert all(bool((x == 7).all()) for x in new)
     assert float((p + 0.5).abs().max()) < 1e-6
+
+
+# ---------------------------------------------------------------------------
+# Values that a step leaves as they are
+# ---------------------------------------------------------------------------
+def _state_that_rounds_down(lz, shape):
+    """8-bit moments whose blocks keep their scale (each holds 448), at scales whose power the
+    device's math library gives half a unit low, and a seed for which some codes of both moments
+    are rounded with the random part 0: scaled by such a power they would lose a step."""
+    rng = np.random.default_rng(7)
+    n = shape[0] * shape[1]
+    bytes_ = np.arange(1, 255)
+    low = bytes_[M.INVERSE[1:255] < np.exp2(127.0 - bytes_)]
+    low = low if len(low) else bytes_
+    m = rng.integers(1, 0x7F, shape).astype(np.uint8) | \
+        (rng.integers(0, 2, shape).astype(np.uint8) << 7)
+    v = rng.integers(1, 0x7F, shape).astype(np.uint8)
+    m[:, ::32] = v[:, ::32] = 0x7E
+    ms, vs = (rng.choice(low, (shape[0], M.blocks(shape[1]))).astype(np.uint8) for _ in range(2))
+    for seed in range(100):
+        w = M.words(np.arange(n, dtype=np.uint64), seed)
+        if ((w >> np.uint32(12)) == 0).any() and ((w & np.uint32(0xFFFFF)) == 0).any():
+            break
+    else:
+        raise AssertionError("no seed with a random part of 0")
+    return seed, [torch.from_numpy(x).to(DEV) for x in (m, v, ms, vs)]
+
+
+def test_adamw8_values_without_a_finite_moment_keep_their_codes(lz):
+    seed, state = _state_that_rounds_down(lz, (1, 1 << 22))
+    state = [x[0] for x in state]
+    p = torch.randn(1 << 22, device=DEV)
+    t = [x.clone() for x in (p, *state)]
+    g = torch.full_like(p, float("nan"))
+    plan = lz.adamw_plan([t[0]], [g], [t[1]], [t[2]], m_scale=[t[3]], v_scale=[t[4]])
+    lz.adamw(plan, seed=seed, weight_decay=0.1)
+    for got, was in zip(t, (p, *state)):
+        assert torch.equal(got, was)
+
+
+def test_rows8_values_without_a_finite_moment_keep_their_codes(lz):
+    V, D = 4096, 1024
+    seed, state = _state_that_rounds_down(lz, (V, D))
+    p = torch.randn(V, D, device=DEV)
+    t = [x.clone() for x in (p, *state)]
+    rows = torch.arange(V, dtype=torch.int32, device=DEV)
+    lz.sparse_apply_q8(t[0], rows, torch.tensor([V], device=DEV),
+                       torch.full((V, D), float("inf"), device=DEV), *t[1:], seed=seed)
+    for got, was in zip(t, (p, *state)):
+        assert torch.equal(got, was)
+
+
+@pytest.mark.parametrize("states_kept", [True, False])
+def test_adamw8_kept_values_in_a_block_whose_scale_shrinks(lz, states_kept):
+    """The block's largest value decays until its scale halves (its gradient is finite, and
+    beta = 0); the others, kept, are the same numbers on the finer grid."""
+    n = 1 << 20
+    seed, state = _state_that_rounds_down(lz, (1, n))
+    m, v, ms, vs = [x[0] for x in state]
+    for c in (m, v):                     # the others: at most 224, so the scale can halve
+        rest = c.view(-1, 32)[:, 1:]
+        rest.copy_(torch.where((rest & 0x7F) > 0x76, (rest & 0x80) | 0x76, rest))
+    ms.clamp_(60, 170)                   # (squares of the roots are finite)
+    vs.clamp_(60, 170)
+    before = [M.decode(c.cpu().numpy(), s.cpu().numpy()) for c, s in ((m, ms), (v, vs))]
+    g = torch.full((n,), float("nan"), device=DEV)
+    if not states_kept:
+        g[::32] = 0.0
+    p = torch.randn(n, device=DEV)
+    plan = lz.adamw_plan([p], [g], [m], [v], m_scale=[ms], v_scale=[vs])
+    lz.adamw(plan, seed=seed, beta1=0.0, beta2=0.0)
+    for was, c, s in zip(before, (m, v), (ms, vs)):
+        got = M.decode(c.cpu().numpy(), s.cpu().numpy()).reshape(-1, 32)
+        assert np.array_equal(got[:, 1:], was.reshape(-1, 32)[:, 1:])
+        assert np.array_equal(got[:, 0], was[::32] if states_kept else np.zeros(n // 32))
