@@ -541,7 +541,9 @@ int lm_sparse_apply_q8(float* table, int64_t V, int64_t D, int64_t ld_table, con
  *            elements), or NULL: the bias alone.
  * out        device, the same shape and dtype, out_strides; sums in fp32,
  *            rounded once. It may be add itself, with the same strides;
- *            otherwise the two must not meet.
+ *            otherwise two that meet are refused (and two of different
+ *            strides whose spans meet, where add has more than 2^22 rows:
+ *            LM_E_UNSUPPORTED).
  * q_start    the position of query 0 where key 0 is at 0 (one new token
  *            against a cache of Lk: Lk - 1); within +-LM_REL_MAX_START.
  *

@@ -5,6 +5,7 @@
 #include <new>
 
 #include "common.hpp"
+#include "rows_meet.hpp"
 
 namespace lmz {
 
@@ -510,7 +511,17 @@ int lm_rel_bias(const float* table, int64_t ld_table, int32_t num_buckets, const
   if ((reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(add)) & mask)
     return LM_E_INVAL;
   if (!check_strides(out_strides, B, H, Lq, Lk, true)) return LM_E_INVAL;
-  if (add && !check_strides(add_strides, B, H, Lq, Lk, false)) return LM_E_INVAL;
+  if (add) {
+    if (!check_strides(add_strides, B, H, Lq, Lk, false)) return LM_E_INVAL;
+    // In place a workgroup reads before it writes, and no other uses its elements.
+    const int64_t n[3] = {B, H, Lq};
+    bool in_place = add == out;
+    for (int i = 0; i < 3; ++i) in_place &= n[i] == 1 || add_strides[i] == out_strides[i];
+    const __int128 at = (static_cast<__int128>(reinterpret_cast<uintptr_t>(add)) -
+                         reinterpret_cast<uintptr_t>(out)) / (dtype == LM_BF16 ? 2 : 4);
+    const Meet meet = in_place ? Meet::NO : rows_meet(n, Lk, out_strides, add_strides, at);
+    if (meet != Meet::NO) return meet == Meet::YES ? LM_E_INVAL : LM_E_UNSUPPORTED;
+  }
   if (rel_bias_blocks(B, H, Lq, Lk, dtype) > INT32_MAX) return LM_E_UNSUPPORTED;
   return rel_bias_run(table, ld_table, starts, ids, n_seg, B, H, Lq, Lk, q_start, add, add_strides,
                       out, out_strides, dtype, static_cast<hipStream_t>(stream));

@@ -210,3 +210,27 @@ def test_adamw8_kept_values_in_a_block_whose_scale_shrinks(lz, states_kept):
         got = M.decode(c.cpu().numpy(), s.cpu().numpy()).reshape(-1, 32)
         assert np.array_equal(got[:, 1:], was.reshape(-1, 32)[:, 1:])
         assert np.array_equal(got[:, 0], was[::32] if states_kept else np.zeros(n // 32))
+
+
+# ---------------------------------------------------------------------------
+# Scores and output in one buffer
+# ---------------------------------------------------------------------------
+def test_rel_bias_scores_beside_the_output(lz):
+    """Halves of a buffer's columns and of its heads, and a view in another order beside the
+    output: taken, and right."""
+    B, H, L = 2, 4, 70
+    table, buckets = torch.randn(32, H, device=DEV), lz.rel_buckets(32, 128, "both")
+    of = torch.tensor([[R.bucket(j - i, 32, 128, "both") for j in range(L)] for i in range(L)],
+                      device=DEV)
+    wide, tall = torch.randn(B, H, L, 2 * L, device=DEV), torch.randn(B, 2 * H, L, L, device=DEV)
+    both = torch.randn(2 * H, B, L, L, device=DEV)
+    for add, out in ((wide[..., :L], wide[..., L:]), (wide[..., L:], wide[..., :L]),
+                     (tall[:, H:], tall[:, :H]), (tall[:, ::2], tall[:, 1::2]),
+                     (both[:H].transpose(0, 1), both[H:].view(B, H, L, L))):
+        was = add.clone()
+        lz.rel_bias(table, buckets, L, L, add=add, out=out)
+        assert torch.equal(out, was + table[of].permute(2, 0, 1)) and torch.equal(add, was)
+    with pytest.raises(lz.LmError):
+        lz.rel_bias(table, buckets, L, L, add=wide[..., 1:L + 1], out=wide[..., :L])
+    with pytest.raises(lz.LmError):
+        lz.rel_bias(table, buckets, L, L, add=tall[:, 1:H + 1], out=tall[:, :H])

@@ -4,6 +4,7 @@ import ctypes
 import os
 import subprocess
 
+import numpy as np
 import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -95,3 +96,81 @@ def test_launches_stay_below_2_32_threads(tmp_path):
             assert at == blocks
     first, n = (ctypes.c_uint32 * 8)(), (ctypes.c_uint32 * 8)()
     assert f(1 << 26, 256, 2, first, n, 8) == 4002, "an error ends the launches"
+
+
+MEET = r"""
+#include "rows_meet.hpp"
+extern "C" int meet(const int64_t* n, int64_t Lk, const int64_t* out, const int64_t* add,
+                    int64_t at) {
+  return static_cast<int>(lmz::rows_meet(n, Lk, out, add, at));
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def meet(tmp_path_factory):
+    d = tmp_path_factory.mktemp("meet")
+    (d / "meet.cpp").write_text(MEET)
+    so = str(d / "meet.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-shared", "-fPIC", "-I",
+                    os.path.join(ROOT, "paper_1810_10045_amd", "csrc"), "-o", so,
+                    str(d / "meet.cpp")], check=True)
+    f = ctypes.CDLL(so).meet
+    f.argtypes = [P, I64, P, P, I64]
+    return lambda n, Lk, out, add, at: f((I64 * 3)(*n), Lk, (I64 * 3)(*out), (I64 * 3)(*add), at)
+
+
+def _places(n, Lk, s, at):
+    i = [np.arange(k) * x for k, x in zip(n, s)]
+    x = i[0][:, None, None, None] + i[1][:, None, None] + i[2][:, None] + np.arange(Lk)
+    return set((x + at).ravel().tolist())
+
+
+def _outs(rng, n, Lk):
+    """Strides of rows that do not meet, in any order of the dimensions, with gaps."""
+    s, inside = [0, 0, 0], Lk
+    for d in rng.permutation(3):
+        s[d] = inside + int(rng.integers(0, 4))
+        if n[d] > 1:
+            inside += (n[d] - 1) * s[d]
+    return s
+
+
+def test_rows_meet_as_counted(meet):
+    """Against the elements themselves: equal strides (interleaved halves, shifts), strides in
+    another order, repeated dimensions."""
+    rng = np.random.default_rng(3)
+    seen = {0: 0, 1: 0}
+    for turn in range(6000):
+        n, Lk = [int(x) for x in rng.integers(1, 5, 3)], int(rng.integers(1, 5))
+        out = _outs(rng, n, Lk)
+        add = list(out) if turn % 3 == 0 else _outs(rng, n, Lk) if turn % 3 == 1 else \
+            [int(x) for x in rng.integers(0, 12, 3)]
+        a = _places(n, Lk, out, 0)
+        at = int(rng.integers(-max(a) - 3, max(a) + 4))
+        if turn % 6 == 0:
+            at = int(rng.integers(-2 * Lk, 2 * Lk + 1))
+        want = bool(a & _places(n, Lk, add, at))
+        assert meet(n, Lk, out, add, at) == want, (n, Lk, out, add, at)
+        seen[want] += 1
+    assert min(seen.values()) > 1000
+    # two halves of a buffer's rows, of its heads; one element further; more rows than are tried
+    assert meet([8, 16, 2048], 2048, [1 << 27, 1 << 23, 4096], [1 << 27, 1 << 23, 4096], 2048) == 0
+    assert meet([8, 16, 2048], 2048, [1 << 27, 1 << 23, 4096], [1 << 27, 1 << 23, 4096], 2047) == 1
+    assert meet([8, 16, 2048], 2048, [1 << 27, 1 << 22, 2048], [1 << 27, 1 << 22, 2048], 1 << 26) == 0
+    assert meet([1 << 20, 16, 8], 4, [512, 32, 4], [512, 4, 64], 3) == 2
+    assert meet([1 << 24, 1 << 8, 1 << 8], 1, [1 << 40, 1 << 8, 1], [1 << 40, 1 << 8, 1], 1 << 16) == 0
+
+
+def test_rel_bias_refuses_scores_that_meet_the_output(lib):
+    """The output over other rows of the scores; in place and side by side is taken (tried
+    above: taken calls are launched)."""
+    f = Bias(lib)
+    v, shape, s = 1 << 20, (2, 3, 4, 8), (96, 32, 8)
+    for dtype, size in ((0, 4), (1, 2)):
+        for at in (size, -size, 32 * size, 7 * size, 191 * size, -191 * size):
+            assert f.bias(shape, P(v), s, P(v + at), s, dtype) == INVAL
+        # the same memory in another order, a repeated row of it
+        assert f.bias(shape, P(v), s, P(v), (32, 64, 8), dtype) == INVAL
+        assert f.bias(shape, P(v), s, P(v), (0, 0, 0), dtype) == INVAL
+        assert f.bias((1 << 20, 16, 8, 4), P(v), (512, 32, 4), P(v), (512, 4, 64), dtype) == 5
