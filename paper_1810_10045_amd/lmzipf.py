@@ -808,6 +808,13 @@ def rel_buckets(num_buckets: int, max_distance: int, mode: str = "both") -> RelB
     return RelBuckets(starts, ids, n.value, num_buckets)
 
 
+def _no_graph(what: str, *tensors):
+    """A tensor that requires grad would come out of the call without its graph."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise LmError(f"{what} is not recorded by autograd: call it under torch.no_grad() or in"
+                      " an autograd.Function (rel_bias_grad is the gradient of rel_bias)")
+
+
 _Strides = ctypes.c_int64 * 3
 
 
@@ -825,7 +832,9 @@ def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start
     """lm_rel_bias: table[bucket(j - (q_start + i)), h] for every head, query i
     and key j, as an H x Lq x Lk tensor of `dtype`; with `add` (B x H x Lq x Lk
     attention scores) the scores plus the bias, of their shape and dtype. `out`
-    may be `add` itself."""
+    may be `add` itself. Not recorded by autograd: tensors that require grad are
+    refused while grad mode is on."""
+    _no_graph("rel_bias", table, add, out)
     _dev(table, "table")
     if table.dim() != 2 or table.dtype != torch.float32 or table.shape[0] != buckets.num_buckets:
         raise LmError(f"table must be float32 with {buckets.num_buckets} rows")
@@ -857,7 +866,9 @@ def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
                   ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
     """lm_rel_bias_grad: the table's gradient, num_buckets x H fp32, from that
     of the scores (B x H x Lq x Lk, or H x Lq x Lk). accumulate: add to `out`.
-    Without `ws` the call takes its workspace from torch's allocator."""
+    Without `ws` the call takes its workspace from torch's allocator. Not
+    recorded by autograd, as ``rel_bias``."""
+    _no_graph("rel_bias_grad", dout, out)
     _dev(dout, "dout")
     strides, shape, device = _scores(dout, "dout"), dout.shape, dout.device
     B = shape[0] if len(shape) == 4 else 1

@@ -234,3 +234,53 @@ def test_rel_bias_scores_beside_the_output(lz):
         lz.rel_bias(table, buckets, L, L, add=wide[..., 1:L + 1], out=wide[..., :L])
     with pytest.raises(lz.LmError):
         lz.rel_bias(table, buckets, L, L, add=tall[:, 1:H + 1], out=tall[:, :H])
+
+
+# ---------------------------------------------------------------------------
+# Autograd
+# ---------------------------------------------------------------------------
+def test_rel_bias_refuses_to_drop_a_graph(lz):
+    buckets = lz.rel_buckets(32, 128, "causal")
+    table, add = torch.randn(32, 2, device=DEV), torch.randn(1, 2, 8, 8, device=DEV)
+    leaf = lambda t: t.clone().requires_grad_()  # noqa: E731
+    calls = [lambda: lz.rel_bias(leaf(table), buckets, 8, 8),
+             lambda: lz.rel_bias(table, buckets, 8, 8, add=leaf(add)),
+             lambda: lz.rel_bias(table, buckets, 8, 8, add=leaf(add) * 2),
+             lambda: lz.rel_bias(table, buckets, 8, 8, add=add, out=leaf(add)),
+             lambda: lz.rel_bias_grad(leaf(add), buckets),
+             lambda: lz.rel_bias_grad(add, buckets, out=leaf(table))]
+    for call in calls:
+        with pytest.raises(lz.LmError, match="autograd"):
+            call()
+        with torch.no_grad():
+            call()
+        with torch.inference_mode():
+            call()
+
+
+def test_rel_bias_in_an_autograd_function(lz):
+    """The way that the refusal names: the table's gradient is that of the formula."""
+    H, L = 2, 50
+    buckets = lz.rel_buckets(32, 128, "causal")
+
+    class Bias(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, scores, table):
+            return lz.rel_bias(table, buckets, L, L, add=scores)
+
+        @staticmethod
+        def backward(ctx, dout):
+            # (softmax gives masked places no gradient)
+            return dout, lz.rel_bias_grad(dout.contiguous(), buckets)
+    table = torch.randn(32, H, device=DEV, requires_grad=True)
+    scores = torch.randn(2, H, L, L, device=DEV, requires_grad=True)
+    w = torch.randn(2, H, L, L, device=DEV)
+    got = torch.autograd.grad((Bias.apply(scores, table).softmax(-1) * w).sum(), (scores, table))
+    of = torch.tensor([[R.bucket(j - i, 32, 128, "causal") for j in range(L)] for i in range(L)],
+                      device=DEV)
+    s, t = scores.detach().double().requires_grad_(), table.detach().double().requires_grad_()
+    x = (s + t[of.clamp(min=0)].permute(2, 0, 1)).masked_fill(of < 0, -float("inf"))
+    want = torch.autograd.grad((x.softmax(-1) * w.double()).sum(), (s, t))
+    for a, b in zip(got, want):
+        # a softmax over at most 50 places and sums of under 5,000 terms: 1000 half steps
+        assert float((a.double() - b).norm()) <= 1000 * 2.0 ** -24 * float(b.norm())
