@@ -604,6 +604,11 @@ def _same_device(device, *tensors):
             raise LmError(f"the call's tensors are on {device} and {t.device}")
 
 
+# Autograd's note that the tensors were written in place: a backward pass that has saved
+# one of them raises, as after torch's own operations.
+_written = torch.autograd.graph.increment_version
+
+
 def _one_of(t: Optional[torch.Tensor], dtype, what: str):
     if t is not None and (t.dtype != dtype or t.numel() < 1):
         raise LmError(f"{what} must be a {dtype} tensor of one element")
@@ -630,7 +635,8 @@ class AdamwPlan(NamedTuple):
     memory on the device, and that memory itself, which it keeps alive also
     where a tensor has been given other memory since (`p.data = ...`), until
     every stream that stepped it is past its steps. `streams`: the handles of
-    those that the allocator knows of."""
+    those that the allocator knows of; `versions`: the tensors of which autograd
+    is told that they were written."""
     table: torch.Tensor
     tensors: tuple
     chunks: int
@@ -638,6 +644,7 @@ class AdamwPlan(NamedTuple):
     states: int
     copies: bool
     streams: set
+    versions: tuple
 
 
 def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
@@ -702,9 +709,12 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
         None if decay is None else (ctypes.c_int32 * n)(*decay), n, gtype, 8 if eight else 32,
         _ptr(host), need, ctypes.byref(chunks)), "lm_adamw_plan")
     keep = tuple(tuple(t.detach() for t in x) for x in [params] + list(lists.values()))
+    # (views of one tensor share its version: one of them is enough)
+    written = {id(t if t._base is None else t._base): t for t in params + lists.get("copies", [])}
+    written = tuple(t.detach() for t in written.values())
     with torch.cuda.device(device):
         return AdamwPlan(host.to(device), keep, chunks.value, gtype, 8 if eight else 32,
-                         "copies" in lists, set())
+                         "copies" in lists, set(), written)
 
 
 def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
@@ -715,14 +725,15 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
     launch. grad_scale: a device fp32 number that multiplies every gradient.
     seed: of the 8-bit moments' rounding; give every step its own."""
     table = plan.table
-    _same_device(table.device, grad_scale, dev_err)
+    device = table.device
+    _same_device(device, grad_scale, dev_err)
     _one_of(grad_scale, torch.float32, "grad_scale")
     _one_of(dev_err, torch.int32, "dev_err")
-    if _elsewhere(table.device, stream):
-        with torch.cuda.device(table.device):
+    if _elsewhere(device, stream):
+        with torch.cuda.device(device):
             return adamw(plan, lr, beta1, beta2, eps, weight_decay, step, grad_scale, seed,
                          dev_err, stream)
-    handle = _on(table.device, stream)
+    handle = _on(device, stream)
     if handle not in plan.streams:
         # The plan may hold the last reference to its memory, which is not to be reused before
         # this stream is past its steps (recording a tensor's own stream does nothing).
@@ -733,6 +744,7 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
     _call(_lib.lm_adamw(_ptr(table), table.numel(), plan.chunks, plan.gtype, plan.states,
                         plan.copies, lr, beta1, beta2, eps, weight_decay, step,
                         _ptr(grad_scale), seed, _ptr(dev_err), handle), "lm_adamw")
+    _written(plan.versions)
 
 
 def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tensor,
@@ -777,6 +789,7 @@ def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tenso
         eps, weight_decay, step, _ptr(m), _ptr(v), _rows(m, "m"), _ptr(m_scale), _ptr(v_scale),
         _rows(m_scale, "m_scale"), seed, _ptr(dev_err), _on(table.device, stream)),
           "lm_sparse_apply_q8")
+    _written(table)
     return table
 
 
@@ -810,9 +823,10 @@ def rel_buckets(num_buckets: int, max_distance: int, mode: str = "both") -> RelB
 
 def _no_graph(what: str, *tensors):
     """A tensor that requires grad would come out of the call without its graph."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        raise LmError(f"{what} is not recorded by autograd: call it under torch.no_grad() or in"
-                      " an autograd.Function (rel_bias_grad is the gradient of rel_bias)")
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise LmError(f"{what} is not recorded by autograd: call it under torch.no_grad() or"
+                          " in an autograd.Function (rel_bias_grad is the gradient of rel_bias)")
 
 
 _Strides = ctypes.c_int64 * 3
@@ -836,9 +850,10 @@ def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start
     refused while grad mode is on."""
     _no_graph("rel_bias", table, add, out)
     _dev(table, "table")
-    if table.dim() != 2 or table.dtype != torch.float32 or table.shape[0] != buckets.num_buckets:
+    size = table.shape
+    if len(size) != 2 or table.dtype != torch.float32 or size[0] != buckets.num_buckets:
         raise LmError(f"table must be float32 with {buckets.num_buckets} rows")
-    H, device = table.shape[1], table.device
+    H, device = size[1], table.device
     _same_device(device, add, out)
     if _elsewhere(device, stream):
         with torch.cuda.device(device):
@@ -849,6 +864,7 @@ def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start
             raise LmError(f"add must be B x {H} x {Lq} x {Lk}")
     else:
         shape = (H, Lq, Lk)
+    given = out
     if out is None:
         out = _empty(shape, dtype, device, stream)
     elif out.shape != shape or out.dtype != dtype:
@@ -858,6 +874,8 @@ def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start
         buckets.n_seg, 1 if add is None else shape[0], H, Lq, Lk, q_start, _ptr(add),
         None if add is None else _scores(add, "add"), _ptr(out), _scores(out, "out"),
         _gtype(out), _on(device, stream)), "lm_rel_bias")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -878,6 +896,7 @@ def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
     if _elsewhere(device, stream):
         with torch.cuda.device(device):
             return rel_bias_grad(dout, buckets, q_start, out, accumulate, ws, stream)
+    given = out
     if out is None:
         if accumulate:
             raise LmError("accumulate needs out")
@@ -892,6 +911,8 @@ def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
         _ptr(dout), gtype, B, H, Lq, Lk, strides, q_start, buckets.starts, buckets.ids,
         buckets.n_seg, buckets.num_buckets, _ptr(out), _rows(out, "out"), bool(accumulate),
         _ptr(buf), need, _on(device, stream)), "lm_rel_bias_grad")
+    if given is not None:
+        _written(given)
     return out
 
 

@@ -284,3 +284,35 @@ def test_rel_bias_in_an_autograd_function(lz):
     for a, b in zip(got, want):
         # a softmax over at most 50 places and sums of under 5,000 terms: 1000 half steps
         assert float((a.double() - b).norm()) <= 1000 * 2.0 ** -24 * float(b.norm())
+
+
+def test_writes_in_place_are_seen_by_autograd(lz):
+    """A backward pass that saved a tensor which a call has written since raises."""
+    u8 = lambda *n: torch.zeros(*n, dtype=torch.uint8, device=DEV)  # noqa: E731
+    f = lambda *n, d=torch.float32: torch.ones(*n, dtype=d, device=DEV)  # noqa: E731
+
+    def raises(saved, write):
+        x = f(*saved.shape, d=saved.dtype).requires_grad_()
+        y = (x * saved).sum()
+        write()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    p = torch.nn.Parameter(f(50))
+    copy = torch.nn.Parameter(f(50, d=torch.bfloat16))
+    plan = lz.adamw_plan([p], [f(50)], [f(50)], [f(50)], copies=[copy])
+    for t in (p, copy):
+        raises(t, lambda: lz.adamw(plan))
+    flat = f(100)
+    plan = lz.adamw_plan([flat[:50], flat[50:90]], [f(50), f(40)], [f(50), f(40)], [f(50), f(40)])
+    for t in (flat, flat[:50], flat[50:90], flat[90:]):
+        raises(t, lambda: lz.adamw(plan))
+    with torch.inference_mode():
+        q = f(50)
+    lz.adamw(lz.adamw_plan([q], [f(50)], [u8(50)], [u8(50)], m_scale=[u8(2)], v_scale=[u8(2)]))
+    table = f(10, 40)
+    raises(table, lambda: lz.sparse_apply_q8(
+        table, u8(3).int(), torch.ones(1, dtype=torch.int64, device=DEV), f(3, 40), u8(10, 40),
+        u8(10, 40), u8(10, 2), u8(10, 2)))
+    buckets, scores, grad = lz.rel_buckets(32, 128, "both"), f(1, 2, 8, 8), f(32, 2)
+    raises(scores, lambda: lz.rel_bias(f(32, 2), buckets, 8, 8, add=scores, out=scores))
+    raises(grad, lambda: lz.rel_bias_grad(scores, buckets, out=grad))
