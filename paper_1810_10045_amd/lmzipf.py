@@ -19,6 +19,7 @@ table rows with 8-bit moments), ``rel_buckets``, ``rel_bias`` and
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import NamedTuple, Optional
 
@@ -630,13 +631,23 @@ def _scales(t: torch.Tensor, what: str):
         raise LmError(f"{what} must hold scale bytes (uint8 or float8_e8m0fnu)")
 
 
+_grad_of = operator.attrgetter("grad")
+
+
+def _owns(t: torch.Tensor, grad: torch.Tensor) -> bool:
+    """Whether the memory of `grad` is that of `t.grad`."""
+    own = t.grad if t.is_leaf else None
+    return own is not None and own.layout == torch.strided and own.data_ptr() == grad.data_ptr()
+
+
 class AdamwPlan(NamedTuple):
     """A list of tensors as ``adamw`` steps it: the table that names their
     memory on the device, and that memory itself, which it keeps alive also
     where a tensor has been given other memory since (`p.data = ...`), until
     every stream that stepped it is past its steps. `streams`: the handles of
     those that the allocator knows of; `versions`: the tensors of which autograd
-    is told that they were written."""
+    is told that they were written; `owners`: the parameters and copies whose
+    `.grad` the plan steps, `grads`: its addresses."""
     table: torch.Tensor
     tensors: tuple
     chunks: int
@@ -645,6 +656,8 @@ class AdamwPlan(NamedTuple):
     copies: bool
     streams: set
     versions: tuple
+    owners: tuple
+    grads: list
 
 
 def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
@@ -656,7 +669,9 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
     every step. decay: one truth value per tensor, whether weight_decay
     applies. Copies the table to the device; make a new plan when a tensor
     (say, a gradient) gets other memory, and keep one as long as a captured
-    graph steps it."""
+    graph steps it. A gradient that is the `.grad` of its parameter or copy has
+    to stay that: ``adamw`` refuses the plan once it is not (after
+    `zero_grad(set_to_none=True)`, say), as it would step an old gradient."""
     params, grads, m, v = (list(x) for x in (params, grads, m, v))
     lists = {"grads": grads, "m": m, "v": v}
     for name, x in (("m_scale", m_scale), ("v_scale", v_scale), ("copies", copies)):
@@ -712,9 +727,13 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
     # (views of one tensor share its version: one of them is enough)
     written = {id(t if t._base is None else t._base): t for t in params + lists.get("copies", [])}
     written = tuple(t.detach() for t in written.values())
+    owned = [(o, g.data_ptr()) for owners in (params, lists.get("copies", []))
+             for o, g in zip(owners, grads) if g.numel() and _owns(o, g)]
     with torch.cuda.device(device):
         return AdamwPlan(host.to(device), keep, chunks.value, gtype, 8 if eight else 32,
-                         "copies" in lists, set(), written)
+                         "copies" in lists, set(), written,
+                         tuple(o for o, _ in owned), [a for _, a in owned])
+
 
 
 def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
@@ -726,9 +745,16 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
     seed: of the 8-bit moments' rounding; give every step its own."""
     table = plan.table
     device = table.device
-    _same_device(device, grad_scale, dev_err)
-    _one_of(grad_scale, torch.float32, "grad_scale")
-    _one_of(dev_err, torch.int32, "dev_err")
+    if grad_scale is not None:
+        _same_device(device, grad_scale)
+        _one_of(grad_scale, torch.float32, "grad_scale")
+    if dev_err is not None:
+        _same_device(device, dev_err)
+        _one_of(dev_err, torch.int32, "dev_err")
+    if plan.owners and plan.grads != [g is not None and g.data_ptr()
+                                      for g in map(_grad_of, plan.owners)]:
+        raise LmError("a gradient is no longer the one that the plan names: keep its memory"
+                      " (zero_grad(set_to_none=False)) or make a new plan")
     if _elsewhere(device, stream):
         with torch.cuda.device(device):
             return adamw(plan, lr, beta1, beta2, eps, weight_decay, step, grad_scale, seed,

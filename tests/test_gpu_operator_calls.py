@@ -316,3 +316,46 @@ def test_writes_in_place_are_seen_by_autograd(lz):
     buckets, scores, grad = lz.rel_buckets(32, 128, "both"), f(1, 2, 8, 8), f(32, 2)
     raises(scores, lambda: lz.rel_bias(f(32, 2), buckets, 8, 8, add=scores, out=scores))
     raises(grad, lambda: lz.rel_bias_grad(scores, buckets, out=grad))
+
+
+@pytest.mark.parametrize("copies", [False, True])
+def test_adamw_refuses_gradients_that_were_replaced(lz, copies):
+    """After zero_grad() the parameters' (the bf16 copies') gradients are other memory: the plan
+    would step the old ones. Gradients zeroed in place, and gradients of the caller's own, stay."""
+    f = lambda n: torch.zeros(n, device=DEV)  # noqa: E731
+    sizes = [50, 0, 70]
+    p = [torch.nn.Parameter(f(n) + 1) for n in sizes]
+    owners = [torch.nn.Parameter(t.detach().bfloat16()) for t in p] if copies else p
+
+    def backward(x):
+        sum((t * x).sum() for t in owners).backward()
+
+    def plan():
+        return lz.adamw_plan(p, [t.grad for t in owners], [f(n) for n in sizes],
+                             [f(n) for n in sizes], copies=owners if copies else None)
+    step = lambda a: lz.adamw(a, lr=0.5, beta1=0.0, beta2=0.0)  # noqa: E731
+    mean = lambda: [float(t.detach().mean()) for t in p if t.numel()]  # noqa: E731
+    backward(2.0)
+    first = plan()
+    step(first)
+    assert mean() == pytest.approx([0.5, 0.5])
+    for t in owners:
+        t.grad.zero_()
+    backward(-1.0)
+    step(first)
+    assert mean() == pytest.approx([1.0, 1.0])
+    for t in owners:
+        t.grad = None
+    for _ in range(2):  # no gradients, then new ones
+        with pytest.raises(lz.LmError, match="gradient"):
+            step(first)
+        assert mean() == pytest.approx([1.0, 1.0])
+        backward(3.0)
+    step(plan())
+    assert mean() == pytest.approx([0.5, 0.5])
+    owners[2].grad = None  # one of them is enough
+    with pytest.raises(lz.LmError, match="gradient"):
+        step(first)
+    own = lz.adamw_plan(p, [f(n) - 1 for n in sizes], [f(n) for n in sizes], [f(n) for n in sizes])
+    step(own)
+    assert mean() == pytest.approx([1.0, 1.0])
