@@ -682,6 +682,10 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, copies=None,
     for name, x in list(lists.items()) + ([] if decay is None else [("decay", decay)]):
         if len(x) != n:
             raise LmError(f"{name} has {len(x)} entries, params has {n}")
+    for name, x in (("params", params), *lists.items()):
+        for i, t in enumerate(x):
+            if not isinstance(t, torch.Tensor):
+                raise LmError(f"{name}[{i}] must be a tensor, got {type(t).__name__}")
     eight = "m_scale" in lists
     if eight != ("v_scale" in lists):
         raise LmError("8-bit moments need m_scale and v_scale")

@@ -174,3 +174,16 @@ def test_rel_bias_refuses_scores_that_meet_the_output(lib):
         assert f.bias(shape, P(v), s, P(v), (32, 64, 8), dtype) == INVAL
         assert f.bias(shape, P(v), s, P(v), (0, 0, 0), dtype) == INVAL
         assert f.bias((1 << 20, 16, 8, 4), P(v), (512, 32, 4), P(v), (512, 4, 64), dtype) == 5
+
+
+def test_adamw_plan_names_an_entry_that_is_no_tensor():
+    """A parameter without a gradient (None) is refused as other wrong entries are."""
+    torch = pytest.importorskip("torch")
+    from paper_1810_10045_amd import lmzipf as lz
+    t = [torch.zeros(4), torch.zeros(4)]
+    for name, i in (("grads", 0), ("grads", 1), ("m", 1), ("v", 0), ("copies", 1), ("m_scale", 0),
+                    ("params", 1)):
+        lists = dict(params=list(t), grads=list(t), m=list(t), v=list(t))
+        lists.setdefault(name, list(t))[i] = None
+        with pytest.raises(lz.LmError, match=f"{name}.{i}. must be a tensor"):
+            lz.adamw_plan(**lists)
