@@ -10,6 +10,7 @@ import pytest
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 import moments_ref as M  # noqa: E402
 import relbias_ref as R  # noqa: E402
+import test_gpu_adamw as adamw_tests  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -359,3 +360,47 @@ def test_adamw_refuses_gradients_that_were_replaced(lz, copies):
     own = lz.adamw_plan(p, [f(n) - 1 for n in sizes], [f(n) for n in sizes], [f(n) for n in sizes])
     step(own)
     assert mean() == pytest.approx([1.0, 1.0])
+
+
+# ---------------------------------------------------------------------------
+# Every form of the 8-bit rows
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("idt", [torch.int32, torch.int64])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("D", [2, 3, 4, 36, 40, 61, 96, 100, 127, 128, 129, 130, 255, 256, 257, 259,
+                               260, 509, 512, 513, 516])
+def test_rows8_widths(lz, idt, pad, D):
+    """Rows of 8 to 64 lanes of 1 to 4 vectors, with ends inside a vector and lanes past the
+    end: bit for bit, counts that are no multiple of a wave's or a workgroup's rows."""
+    for V, U in ((400, 131), (9, 1), (60, 33)):
+        adamw_tests.test_rows8(lz, idt, V, D, U, pad)
+
+
+@pytest.mark.parametrize("D", [3, 40, 96, 130, 257, 513])
+def test_rows8_from_blocks_of_one_large_value(lz, D):
+    """The last value of each row far above its block: the lanes past the end, which hold values
+    again, neither raise a block's scale nor lose it."""
+    V, U = 50, 37
+    rng = np.random.default_rng(D)
+    p = rng.normal(0, 0.02, (V, D)).astype(np.float32)
+    g = (rng.normal(0, 1, (U, D)) * 1e-6).astype(np.float32)
+    g[:, -1] = 100.0
+    g[::2, D // 2] = 3.0
+    ids = np.sort(rng.permutation(V)[:U])
+    z = [np.zeros((V, n), np.uint8) for n in (D, D, M.blocks(D), M.blocks(D))]
+    t = [torch.from_numpy(x).to(DEV) for x in (p, *z)]
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    hyper = (1e-2, 0.9, 0.999, 1e-8, 0.1, 1)
+    for turn in range(3):
+        lz.sparse_apply_q8(t[0], torch.from_numpy(ids).to(DEV), torch.tensor([U], device=DEV),
+                           torch.from_numpy(g).to(DEV), *t[1:], lr=1e-2, weight_decay=0.1,
+                           step=1, seed=turn, dev_err=err)
+        number = ids[:, None].astype(np.uint64) * np.uint64(D) + np.arange(D, dtype=np.uint64)
+        ref, bound, *new, _ = M.step8(p[ids], g, *[x[ids] for x in z], hyper, number, turn)
+        for got, old, want in zip(t[1:], z, new):
+            old[ids] = want
+            assert np.array_equal(got.cpu().numpy(), old), turn
+        got = t[0].cpu().numpy()
+        assert (np.abs(got[ids].astype(np.float64) - ref) <= bound).all(), turn
+        p = got
+    lz.check(err)
