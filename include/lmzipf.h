@@ -440,6 +440,11 @@ int lm_sparse_apply_f16(float* table, int64_t V, int64_t D, int64_t ld_table,
  * the next multiple of LM_MOMENT_BLOCK (of a table: id * D + column). Give
  * every step and every list its own seed; the same seed repeats a call bit
  * for bit. State that starts from zero starts from zero bytes.
+ * The root is rounded without bias, its square, which the next step starts
+ * from, is not: with normal gradients v settles 4 to 5% above that of fp32
+ * moments, its root scattering by 15%, for roots down to 2^-12 of their block's
+ * largest; 14% high at 2^-15 of it, 2.3 times at 2^-17.4. Values of sizes that
+ * far apart belong into different blocks, or into fp32 moments.
  *
  * The plan is a table that names the list's memory. lm_adamw_plan writes it
  * into host memory, the caller copies it to the device (256-byte aligned, as
