@@ -476,8 +476,13 @@ int lm_sparse_apply_f16(float* table, int64_t V, int64_t D, int64_t ld_table,
  * LM_DEVERR_CAPACITY and nothing is stepped).
  * grad_scale device fp32 or NULL (1): multiplies every gradient (gradient
  *            clipping, loss scales).
- * dev_err    device int32 or NULL.
- * step       >= 1; beta1, beta2 in [0, 1).
+ * dev_err    device int32 or NULL: nothing then tells of values that were
+ *            kept, nor of a plan made otherwise.
+ * step       >= 1; beta1, beta2 in [0, 1). step, seed and the rates are taken
+ *            when the call is made: a captured call repeats them with every
+ *            replay, the same bias corrections and random words, so a training
+ *            that goes on needs a capture for each step or eager calls
+ *            (grad_scale is read from the device with every replay).
  * ------------------------------------------------------------------------ */
 #define LM_MOMENT_BLOCK 32
 #define LM_ADAMW_MAX_VALUES ((int64_t)1 << 42)

@@ -746,7 +746,10 @@ def adamw(plan: AdamwPlan, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 
           dev_err: Optional[torch.Tensor] = None, stream=None) -> None:
     """lm_adamw: one AdamW step of every tensor of the plan, in place, in one
     launch. grad_scale: a device fp32 number that multiplies every gradient.
-    seed: of the 8-bit moments' rounding; give every step its own."""
+    seed: of the 8-bit moments' rounding; give every step its own. dev_err tells
+    of values that were kept as they were, since their second moment would not be
+    finite; without it nothing does. A captured call repeats its step, seed and
+    rates with every replay."""
     table = plan.table
     device = table.device
     if grad_scale is not None:
@@ -785,7 +788,8 @@ def sparse_apply_q8(table: torch.Tensor, rows: torch.Tensor, n_rows: torch.Tenso
                     stream=None) -> torch.Tensor:
     """lm_sparse_apply_q8: the lazy AdamW step of ``sparse_apply(opt="adam")``
     with 8-bit moments, in place: m and v V x D codes (v of its square root),
-    m_scale and v_scale V x ceil(D / MOMENT_BLOCK) bytes."""
+    m_scale and v_scale V x ceil(D / MOMENT_BLOCK) bytes. seed, dev_err and
+    captured calls as ``adamw``'s."""
     _dev(table, "table")
     V, D = table.shape
     if table.dtype != torch.float32 or vals.dtype != torch.float32:
