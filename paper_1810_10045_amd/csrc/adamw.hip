@@ -2,9 +2,9 @@
 // and the lazy step on table rows with 8-bit moments.
 //
 // The step reads and writes each parameter and its moments once: HBM bounds it
-// (fp32 moments with bf16 gradients and copies: 28 bytes a value, 202M values 960 us
-// or 5.9 TB/s; 8-bit moments: 16.1 bytes, 532 us or 6.1 TB/s, with its vector units
-// busy for about 80% of that: 87 instructions a value).
+// (fp32 moments with bf16 gradients and copies: 28 bytes a value, 202M values 974 us
+// or 5.8 TB/s; 8-bit moments: 16.1 bytes, 531 us or 6.1 TB/s, with its vector units
+// busy for about 85% of that: 91 instructions a value).
 //
 // A list of tensors is cut into chunks of kChunk values; one workgroup steps one
 // chunk, so a list of a thousand small tensors is one launch and a large tensor
@@ -12,11 +12,11 @@
 // device memory that the caller builds once.
 //
 // - Streaming (non-temporal) loads and stores: nothing here is read again before the
-//   next step. 202M values: 1021 -> 948 us (fp32), 691 -> 560 us (8 bits, with the next
-//   point), 129,362 rows of 1024 455 -> 394 us.
+//   next step. Through the caches 202M values take 8% longer (fp32) and 129,362 rows of
+//   1024 in 8 bits 15%.
 // - A workgroup ends with its chunk instead of going on to another: loads and stores
 //   are counted together, so a wave's next loads would wait for its last stores (8 bits:
-//   572 us against 691).
+//   21% longer).
 // - Two vectors of each operand a lane. One or four were no faster at 202M values, and a
 //   list of 20 small tensors took 3.7 us with two, 5.0 with four.
 #include "launch_parts.hpp"
@@ -54,9 +54,9 @@ static uint64_t plan_kind(int64_t chunks, int gtype, int states, bool copies) {
 // ---------------------------------------------------------------------------
 // A lane's vectors of n values, its own from number i on. Where a vector may pass
 // the end (PART), the last 4 values are loaded in its place and, once every load is
-// under way, moved down, zeros behind them: 100,000 rows of 91 values take 55 us so, 77
-// where each vector is moved before the next is loaded, 75 with a load for each value
-// (129,362 rows of 1,001: 489, 549, 687). Fewer than 4 values (FEW) are loaded one by one.
+// under way, moved down, zeros behind them: 100,000 rows of 91 values in a table of a
+// million take 64 us so, 40% more where each vector is moved before the next is loaded, 36%
+// more with a load for each value (129,362 rows of 1,001: 581 us, 12% and 40% more). Fewer than 4 values (FEW) are loaded one by one.
 // ---------------------------------------------------------------------------
 enum End { WHOLE, PART, FEW };
 
@@ -474,10 +474,10 @@ static int rows8_launch(const Rows8& a, hipStream_t st) {
   });
 }
 
-// Lanes a row, vectors a lane. 100,000 rows of 32, 64, 128 values take 21, 29, 46 us so,
-// 52, 52, 63 with a wave for each; rows of 256 and 512 85 and 160 us, 149 and 182 with
-// 4 vectors a lane. Rows of whole vectors (WHOLE) of 128 and 512 values: 44 and 157 us, 49
-// and 159 as PART.
+// Lanes a row, vectors a lane. 100,000 rows of 32, 64, 128 values in a table of a million
+// take 23, 30, 47 us so, with a wave for each 2.5, 1.8, 1.4 times as long; rows of 256 and
+// 512 86 and 166 us, with 4 vectors a lane 1.8 and 1.1 times. Rows of whole vectors (WHOLE)
+// of 128 values would take 11% longer as PART, of 512 1%.
 template <typename KeyT, End END>
 static int rows8_shape(const Rows8& a, hipStream_t st) {
   const int vectors = (a.D + kVec - 1) / kVec;

@@ -54,7 +54,10 @@ static inline StepKeys step_keys(uint64_t seed) {
   return {static_cast<uint32_t>(z), static_cast<uint32_t>(z >> 32)};
 }
 
-// The random word of value number e: two rounds of multiply and xor-shift.
+// The random word of value number e: two rounds of multiply and xor-shift. The
+// multipliers here and above are published ones, known to mix well: three primes of Y.
+// Collet's 32-bit hash (2012), 2^64 over the golden ratio (Knuth) and that of a published
+// 64-bit mixer (0xD6E8FEB86659FD93); the rounds are this file's.
 __device__ __forceinline__ uint32_t value_word(uint64_t e, const StepKeys& k) {
   uint32_t h = (static_cast<uint32_t>(e) ^ k.k0) * 0x9E3779B1u;
   h ^= h >> 15;
@@ -96,8 +99,8 @@ __device__ __forceinline__ void decode4(uint32_t codes, int scale, float* x) {
 // program that computes codes with torch operations gets the kernels', bit for
 // bit. A rounding's threshold moves by 2^-20 of a step at most, the resolution of
 // its random part; none is high, so no value passes 448. A thread's one call of
-// powf serves the 8 values of its vectors: 545 us a step of 202M parameters against
-// 526 with exact powers.
+// powf serves the 8 values of its vectors: 4% more of a step of 202M parameters than
+// exact powers take.
 constexpr int kScales = 256;
 
 __device__ __forceinline__ void fill_scales(float* inverse, int threads) {
@@ -173,7 +176,7 @@ __device__ __forceinline__ bool adamw_value8(float& p, float& m, float& r, float
   const bool ok = v1 < __builtin_inff();  // false for NaN too
   const float r1 = sqrtf(v1);
   // v_rcp_f32 is within an ulp of the quotient, far below what the update's sum
-  // keeps of it (545 us a step of 202M parameters, 559 with a division).
+  // keeps of it (a division makes a step of 202M parameters 3% longer).
   const float step = (m1 * o.inv_c1) * __builtin_amdgcn_rcpf(__builtin_fmaf(r1, o.root_c2, o.eps));
   const float p1 = __builtin_fmaf(-o.lr, __builtin_fmaf(wd, p, step), p);
   p = ok ? p1 : p;

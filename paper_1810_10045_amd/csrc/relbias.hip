@@ -161,9 +161,9 @@ __device__ __forceinline__ float from_lane_below(float v) {
 // waves, one below the other, in one head of one batch entry: it looks up the
 // numbers of its diagonals once, in LDS, and each lane takes its patch's from there.
 // Tiles of one column come one after the other (row tiles first), a batch entry
-// after the other: 8 x 16 x 2048 x 2048 causal bf16 scores take 288 us so (5.6 TB/s),
-// 321 to 328 where a workgroup keeps its diagonals for several batch entries, 339
-// with column tiles first, 377 to 420 with two and four patches of each wave.
+// after the other: 8 x 16 x 2048 x 2048 causal bf16 scores take 275 us so (5.9 TB/s),
+// 12% more where a workgroup keeps its diagonals for several batch entries, 18% with
+// column tiles first, 31 to 46% with two and four patches of each wave.
 // ---------------------------------------------------------------------------
 template <typename T, bool ADD, bool NARROW>
 __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
@@ -247,8 +247,8 @@ __global__ __launch_bounds__(kRelThreads) void k_rel_bias(
 // each address belongs to one lane of an instruction (ds_add_f32, which needs no
 // such care, took about 195 clocks for a wave). Column tiles, not diagonal bands: a
 // wave that walked down the diagonal kept its sums in registers throughout, but its
-// rows began between cache lines (16 x 16 x 2048 x 2048 bf16: 450 us, against 319 us
-// or 6.7 TB/s so). Loading a patch ahead did not help (329 us). At the end a
+// rows began between cache lines (16 x 16 x 2048 x 2048 bf16: 450 us, against 318 us
+// or 6.8 TB/s so). Loading a patch ahead did not help. At the end a
 // workgroup adds its waves' sums by distance, then by segment, into the workspace:
 // 2 us of a short call's 10. k_rel_join (4 us) adds the workgroups' in their order,
 // so results are the same from run to run.
