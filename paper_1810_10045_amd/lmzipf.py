@@ -644,8 +644,9 @@ class AdamwPlan(NamedTuple):
     """A list of tensors as ``adamw`` steps it: the table that names their
     memory on the device, and that memory itself, which it keeps alive also
     where a tensor has been given other memory since (`p.data = ...`), until
-    every stream that stepped it is past its steps. `streams`: the handles of
-    those that the allocator knows of; `versions`: the tensors of which autograd
+    every stream that stepped it is past its steps (so a stream of the caller's
+    own making has to outlive these tensors, as for `Tensor.record_stream`).
+    `streams`: the handles of those that the allocator knows of; `versions`: the tensors of which autograd
     is told that they were written; `owners`: the parameters and copies whose
     `.grad` the plan steps, `grads`: its addresses."""
     table: torch.Tensor
