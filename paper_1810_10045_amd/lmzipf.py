@@ -646,9 +646,9 @@ class AdamwPlan(NamedTuple):
     where a tensor has been given other memory since (`p.data = ...`), until
     every stream that stepped it is past its steps (so a stream of the caller's
     own making has to outlive these tensors, as for `Tensor.record_stream`).
-    `streams`: the handles of those that the allocator knows of; `versions`: the tensors of which autograd
-    is told that they were written; `owners`: the parameters and copies whose
-    `.grad` the plan steps, `grads`: its addresses."""
+    `streams`: the handles of those that the allocator knows of; `versions`: the
+    tensors of which autograd is told that they were written; `owners`: the
+    parameters and copies whose `.grad` the plan steps, `grads`: its addresses."""
     table: torch.Tensor
     tensors: tuple
     chunks: int
