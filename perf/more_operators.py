@@ -7,8 +7,8 @@ same results from elementary torch operations (``own`` false).
 - ``norm``: h = add + dropout(x), y = (h - mean) / sqrt(var + eps) * w + b of
   every row; with neither add nor p, h is x.
 - ``norm_grad``: the gradients of x, of h's other summand, and of w and b.
-- ``logp``: each row's log probability of its target, entropy, log of the sum of
-  exponentials, and the largest alternatives.
+- ``logp``: each row's log probability of its target, entropy, largest logit
+  (``peak``), log of the sum of exp(scale (logit - peak)), and likeliest words.
 - ``logp_grad``: the gradient of the log probability and of the entropy.
 
 Random words. Row i, column j of x with D columns belongs to word number
@@ -157,13 +157,14 @@ def _prepare_logp(s, case, gen, dt):
     t[torch.arange(N, device=DEV) % 8 == 5] = IGNORE
     s.update(logits=z, targets=t)
     if case["op"] == "logp_grad":
-        lse, ent = (torch.empty(N, device=DEV) for _ in range(2))
+        log_sum, ent = (torch.empty(N, device=DEV) for _ in range(2))
         for i in range(0, N, 256):
-            y = z[i:i + 256].double() * _f32(case["scale"])
+            y = z[i:i + 256].double()
+            y = (y - y.amax(1, keepdim=True)) * _f32(case["scale"])
             a = torch.logsumexp(y, 1, keepdim=True)
-            lse[i:i + 256] = a[:, 0]
+            log_sum[i:i + 256] = a[:, 0]
             ent[i:i + 256] = -((y - a).exp() * (y - a).clamp(min=-1e30)).sum(1)
-        s.update(lse=lse, entropy=ent)
+        s.update(peak=z.amax(1).float(), log_sum=log_sum, entropy=ent)
         s["dlogp"] = -torch.rand(N, generator=gen, device=DEV) / N
         s["dentropy"] = _randn(gen, N, std=0.1 / N) if case["entropy"] else None
 
@@ -278,21 +279,21 @@ def _logp(s):
         from paper_1810_10045_amd import lmzipf as lz
         r = lz.token_logprobs(s["logits"], s["targets"], scale=c["scale"], top=c["top"],
                               ignore=IGNORE)
-        out = {"logp": r.logp, "entropy": r.entropy, "lse": r.lse}
+        out = {"logp": r.logp, "entropy": r.entropy, "peak": r.peak, "log_sum": r.log_sum}
         if c["top"]:
             out.update(top_logp=r.top_logp, top_ids=r.top_ids)
         return out
-    z = s["logits"].float() * c["scale"]
-    m = z.amax(1, keepdim=True)
-    d = z - m
+    z = s["logits"].float()
+    peak = z.amax(1)
+    d = (z - peak[:, None]) * c["scale"]
     e = torch.exp(d)
     total = e.sum(1)
     logs = torch.log(total)
-    lse = m[:, 0] + logs
     entropy = logs - torch.where(e > 0, e * d, 0.0).sum(1) / total
     t = s["targets"]
     at = d[torch.arange(c["N"], device=DEV), t.clamp(min=0)] - logs
-    out = {"logp": torch.where(t == IGNORE, 0.0, at), "entropy": entropy, "lse": lse}
+    out = {"logp": torch.where(t == IGNORE, 0.0, at), "entropy": entropy, "peak": peak,
+           "log_sum": logs}
     if c["top"]:
         # One number orders the logits, equal ones by their ids.
         bits = (s["logits"].float() + 0.0).view(torch.int32).long()
@@ -308,11 +309,11 @@ def _logp_grad(s):
     c = s["case"]
     if own:
         from paper_1810_10045_amd import lmzipf as lz
-        return lz.token_logprobs_grad(s["logits"], s["targets"], s["lse"], s["entropy"],
-                                      dlogp=s["dlogp"], dentropy=s["dentropy"],
-                                      scale=c["scale"], ignore=IGNORE)
+        return lz.token_logprobs_grad(s["logits"], s["targets"], s["peak"], s["log_sum"],
+                                      dlogp=s["dlogp"], entropy=s["entropy"],
+                                      dentropy=s["dentropy"], scale=c["scale"], ignore=IGNORE)
     t = s["targets"]
-    l = s["logits"].float() * c["scale"] - s["lse"][:, None]
+    l = (s["logits"].float() - s["peak"][:, None]) * c["scale"] - s["log_sum"][:, None]
     prob = torch.exp(l)
     dlogp = torch.where(t == IGNORE, 0.0, s["dlogp"])
     d = -dlogp[:, None] * prob
@@ -332,8 +333,8 @@ def work(case):
     if case["op"] in ("logp", "logp_grad"):
         N, V = case["N"], case["V"]
         if case["op"] == "logp":
-            return {"bytes": N * V * size + N * (8 + 12 + 8 * case["top"]), "flops": 6 * N * V}
-        return {"bytes": 2 * N * V * size + N * (8 + 4 + 4 + (8 if case["entropy"] else 0)),
+            return {"bytes": N * V * size + N * (8 + 16 + 8 * case["top"]), "flops": 6 * N * V}
+        return {"bytes": 2 * N * V * size + N * (8 + 4 + 8 + (8 if case["entropy"] else 0)),
                 "flops": (8 if case["entropy"] else 5) * N * V}
     rows, D, add, p = (case[k] for k in ("rows", "D", "add", "p"))
     n = rows * D
@@ -432,7 +433,7 @@ def _exact_logp(s):
     c, z = s["case"], s["logits"]
     scale = _f32(c["scale"])
     out = {k: torch.empty(c["N"], device=DEV, dtype=torch.float64)
-           for k in ("logp", "entropy", "lse")}
+           for k in ("logp", "entropy", "peak", "log_sum")}
     if c["top"]:
         out["top_logp"] = torch.empty(c["N"], c["top"], device=DEV, dtype=torch.float64)
         out["top_ids"] = torch.empty(c["N"], c["top"], device=DEV, dtype=torch.int32)
@@ -440,7 +441,8 @@ def _exact_logp(s):
         y = z[i:i + 256].double()
         l = torch.log_softmax(y * scale, 1)
         part = slice(i, i + len(l))
-        out["lse"][part] = torch.logsumexp(y * scale, 1)
+        out["peak"][part] = y.max(1).values
+        out["log_sum"][part] = -l.max(1).values
         out["entropy"][part] = torch.special.entr(l.exp()).sum(1)
         t = s["targets"][part]
         out["logp"][part] = torch.where(t < 0, 0.0, l.gather(1, t.clamp(min=0)[:, None])[:, 0])
@@ -458,7 +460,8 @@ def _exact_logp_grad(s):
     scale = _f32(c["scale"])
     for i in range(0, c["N"], 256):
         part = slice(i, i + 256)
-        l = s["logits"][part].double() * scale - s["lse"][part, None]
+        l = scale * s["logits"][part].double() - scale * s["peak"][part, None].double()
+        l -= s["log_sum"][part, None]
         prob = l.exp()
         hit = (s["targets"][part, None] == words).double()
         dlogp = torch.where(s["targets"][part] < 0, 0.0, s["dlogp"][part].double())
