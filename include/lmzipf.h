@@ -587,6 +587,122 @@ int lm_rel_bias_grad(const void* dout, int32_t dtype, int64_t B, int64_t H, int6
                      void* stream);
 
 /* ------------------------------------------------------------------------
+ * Rows of activations — dropout, layer norm, and the log probabilities of
+ * given tokens. Common to these entry points:
+ * - A matrix is rows x D elements of `dtype` (LM_F32 / LM_BF16) at the
+ *   alignment of an element, ld_* elements from row to row (>= D, up to 2^40);
+ *   rows and N are below 2^31. Sums and statistics are fp32, results are
+ *   rounded once. Parameters and statistics are contiguous fp32.
+ * - A matrix that is written may take the place of one that is read (same
+ *   address and ld); any other two operands of which one is written and that
+ *   meet in memory are refused (LM_E_INVAL; LM_E_UNSUPPORTED for two of
+ *   different ld whose spans meet, where they have more than 2^22 rows).
+ * - Sums are added in an order that depends on the sizes only: repeated calls
+ *   give the same bits.
+ *
+ * Dropout's mask is a function of the seed and an element's place, and stored
+ * nowhere. With T = round(65536 p), element (i, j) of rows x D belongs to word
+ * i * ceil(D / 2) + j / 2 (the random words of lm_adamw: value numbers are word
+ * numbers here), to its low 16 bits where j is even, its high ones where j is
+ * odd. It is kept where they are >= T, and multiplied by 65536 / (65536 - T);
+ * dropped elements are 0 whatever they were (p 1: all of them).
+ * p          in [0, 1].
+ * seed       the seed, or
+ * seed_at    device int64: read instead of `seed` when the call runs (with
+ *            every replay of a captured call, which would repeat `seed`), or NULL.
+ * Give every call of a step its own seed, and its gradient the same one.
+ *
+ * lm_dropout: out = add + dropout(x) (add NULL: dropout(x)). The gradient of x
+ * is the same call on that of out, without add.
+ * D          below 2^31.
+ * ------------------------------------------------------------------------ */
+int lm_dropout(const void* x, int64_t ld_x, const void* add, int64_t ld_add, void* out,
+               int64_t ld_out, int64_t rows, int64_t D, int32_t dtype, float p, uint64_t seed,
+               const int64_t* seed_at, void* stream);
+
+/* lm_layer_norm: h = add + dropout(x),
+ *     y = (h - mean) * rstd * weight + bias,  rstd = 1 / sqrt(var + eps)
+ * with the mean and the (biased) variance of each row of h, before h is rounded.
+ * add        or NULL (nothing is added).
+ * weight, bias  D values, or NULL (1, 0).
+ * eps        >= 0.
+ * h          written, or NULL.
+ * mean, rstd written, one value a row.
+ * D          1 to LM_NORM_MAX_WIDTH.
+ *
+ * lm_layer_norm_grad: from dy, h (x itself where nothing was added or dropped)
+ * and the statistics, with n = (h - mean) * rstd, g = dy * weight and E the
+ * mean over a row:
+ *     dh = add + rstd * (g - E g - n * E(g n)),   dx = dropout(dh),
+ *     dweight = sum over rows of dy * n,   dbias = sum over rows of dy.
+ * add        the gradient that reaches h past the norm, or NULL. dh is the
+ *            gradient of the forward's add, dx that of its x.
+ * p, seed, seed_at  the forward's; looked at for dx only.
+ * dx         written, or NULL.
+ * dweight, dbias  every value written (accumulate 0) or added to (1), or NULL.
+ * ws         device workspace of lm_layer_norm_grad_workspace_bytes(...) bytes
+ *            where dweight or dbias is given, 4-byte aligned, no initial
+ *            contents required (0 rows: NULL). */
+#define LM_NORM_MAX_WIDTH 16384
+int lm_layer_norm(const void* x, int64_t ld_x, const void* add, int64_t ld_add, int64_t rows,
+                  int64_t D, int32_t dtype, const float* weight, const float* bias, float eps,
+                  float p, uint64_t seed, const int64_t* seed_at, void* y, int64_t ld_y, void* h,
+                  int64_t ld_h, float* mean, float* rstd, void* stream);
+size_t lm_layer_norm_grad_workspace_bytes(int64_t rows, int64_t D, int32_t dtype);
+int lm_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* add,
+                       int64_t ld_add, int64_t rows, int64_t D, int32_t dtype, const float* mean,
+                       const float* rstd, const float* weight, float p, uint64_t seed,
+                       const int64_t* seed_at, void* dh, int64_t ld_dh, void* dx, int64_t ld_dx,
+                       float* dweight, float* dbias, int32_t accumulate, void* ws, size_t ws_bytes,
+                       void* stream);
+
+/* lm_token_logprobs: of each row x of N x V logits, z = scale * x,
+ *     peak = max x,   log_sum = log sum e^(z - scale * peak)
+ *     (log sum e^z is scale * peak + log_sum),
+ *     logp = z[target] - scale * peak - log_sum   (target == ignore: 0),
+ *     entropy = -sum q log q,  q = e^(z - scale * peak - log_sum),
+ * and the `top` likeliest words, of equal logits the lowest ids first, with
+ * their log probabilities. A logit of -infinity is masked: no word, no
+ * alternative. Where a row has fewer than `top` words left, the places behind
+ * the last hold id -1 and -infinity.
+ * A row with nothing left: peak, log_sum and logp -infinity, entropy 0. A row
+ * with a NaN or +infinity: NaN, ids -1.
+ * targets    device, N ids of dtype `idtype`, or NULL (logp is not written).
+ *            One outside [0, V) that is not `ignore` gives NaN and sets
+ *            LM_DEVERR_ID_RANGE.
+ * scale      above 0 (the inverse of a temperature), below 1e38.
+ * top        0 to LM_TOP_MAX; top_logp, top_ids: N x top, contiguous.
+ * V          1 to LM_LOGP_MAX_V.
+ * dev_err    device int32 or NULL.
+ * ws         device workspace of lm_token_logprobs_workspace_bytes(...), 16-byte
+ *            aligned, no initial contents required (0 bytes where rows are many
+ *            or short: NULL). More than 1024 equal logits at the border of the
+ *            alternatives cost `top` further passes over their row.
+ *
+ * lm_token_logprobs_grad: the logits' gradient from those of logp and entropy,
+ * l = log q:
+ *     out = scale * (dlogp * (1 at target - q) - dentropy * q * (l + entropy)).
+ * dlogp      N values, or NULL (then targets may be NULL); a row whose target
+ *            is `ignore` has none, its value is not used; a target outside [0,
+ *            V): NaN.
+ * entropy, dentropy  N values, or NULL (both).
+ * A row with nothing left, and one whose dlogp and dentropy are 0, get zeros
+ * whatever their logits are. */
+#define LM_TOP_MAX 64
+#define LM_LOGP_MAX_V (((int64_t)1 << 31) - 1)
+size_t lm_token_logprobs_workspace_bytes(int64_t N, int64_t V, int32_t dtype, int32_t top);
+int lm_token_logprobs(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype,
+                      const void* targets, int32_t idtype, int64_t ignore, float scale,
+                      int32_t top, float* logp, float* entropy, float* peak, float* log_sum,
+                      float* top_logp, int32_t* top_ids, int32_t* dev_err, void* ws,
+                      size_t ws_bytes, void* stream);
+int lm_token_logprobs_grad(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype,
+                           const void* targets, int32_t idtype, int64_t ignore, float scale,
+                           const float* peak, const float* log_sum, const float* dlogp,
+                           const float* entropy, const float* dentropy, void* out, int64_t ld_out,
+                           void* stream);
+
+/* ------------------------------------------------------------------------
  * Candidate sampler — Sec. II-A (sampled softmax) and Sec. III-B
  * (controlled randomness): the output embedding is updated at a random,
  * uniformly drawn subset of the vocabulary plus the batch's own words.

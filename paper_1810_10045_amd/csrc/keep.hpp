@@ -1,0 +1,56 @@
+// Dropout's mask: a function of the seed and a value's place, computed where it is used
+// and stored nowhere, so a backward pass that is given the seed makes the same mask.
+//
+// Word w of a call is value_word(w, keys of the seed), 32 bits for two neighbouring
+// columns: row i of D columns has ceil(D / 2) words, column j the low (j even) or high (j
+// odd) half of word i * ceil(D / 2) + j / 2. A value is kept where its half is at least
+// round(65536 p), and multiplied by 1 over the share that is kept: the expectation is
+// exact for the p that is drawn, which is within 2^-17 of the caller's. Two values to a
+// word: the hash's two 32-bit products take a quarter of the vector rate, and a word for
+// each value would cost as much as a large call's memory.
+#pragma once
+
+#include <math.h>
+
+#include "moments.hpp"
+
+namespace lmz {
+
+struct KeepArgs {
+  uint64_t seed;
+  const int64_t* seed_at;  // on the device: read instead of seed, or nullptr
+  uint32_t least;          // 0 to 65536
+  float scale;
+};
+
+static inline bool valid_p(float p) { return p >= 0.f && p <= 1.f; }
+
+static inline KeepArgs make_keep(float p, uint64_t seed, const int64_t* seed_at) {
+  KeepArgs k{seed, seed_at, 0, 1.f};
+  k.least = static_cast<uint32_t>(nearbyint(65536.0 * static_cast<double>(p)));
+  if (k.least) k.scale = k.least < 65536 ? static_cast<float>(65536.0 / (65536 - k.least)) : 0.f;
+  return k;
+}
+
+struct Keep {
+  StepKeys keys;
+  uint32_t least;
+  float scale;
+  __device__ __forceinline__ explicit Keep(const KeepArgs& a)
+      : keys(step_keys(a.seed_at ? static_cast<uint64_t>(*a.seed_at) : a.seed)),
+        least(a.least),
+        scale(a.scale) {}
+  // P values from an even column on, the first two of word `word`. A dropped value is 0
+  // whatever it was (infinity, NaN).
+  template <int P>
+  __device__ __forceinline__ void apply(uint64_t word, float* x) const {
+#pragma unroll
+    for (int e = 0; e < P; e += 2) {
+      const uint32_t h = value_word(word + e / 2, keys);
+      x[e] = (h & 0xffffu) >= least ? x[e] * scale : 0.f;
+      x[e + 1] = (h >> 16) >= least ? x[e + 1] * scale : 0.f;
+    }
+  }
+};
+
+}  // namespace lmz

@@ -1,6 +1,7 @@
 // The C ABI declared in include/lmzipf.h: argument validation (before any
 // launch), dtype dispatch and stream plumbing. The kernels live in
-// unique.hip, segsum.hip, fill.hip, adamw.hip and relbias.hip.
+// unique.hip, segsum.hip, fill.hip, adamw.hip, relbias.hip, dropout.hip, norm.hip,
+// norm_grad.hip and logprobs.hip.
 #include <algorithm>
 #include <new>
 
@@ -68,6 +69,30 @@ int rel_grad_run(const void* dout, int dtype, int64_t B, int64_t H, int64_t Lq, 
                  const int64_t* sd, int64_t q_start, const int32_t* starts, const int32_t* ids,
                  int n_seg, int num_buckets, float* dtable, int64_t ld_table, int accumulate,
                  void* ws, hipStream_t st);
+
+int dropout_run(const void* x, int64_t ld_x, const void* add, int64_t ld_add, void* out,
+                int64_t ld_out, int64_t rows, int64_t D, int dtype, float p, uint64_t seed,
+                const int64_t* seed_at, hipStream_t st);
+int norm_run(const void* x, int64_t ld_x, const void* add, int64_t ld_add, int64_t rows, int64_t D,
+             int dtype, const float* weight, const float* bias, float eps, float p, uint64_t seed,
+             const int64_t* seed_at, void* y, int64_t ld_y, void* h, int64_t ld_h, float* mean,
+             float* rstd, hipStream_t st);
+size_t norm_grad_workspace_bytes(int64_t rows, int64_t D, int dtype);
+int norm_grad_run(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* add,
+                  int64_t ld_add, int64_t rows, int64_t D, int dtype, const float* mean,
+                  const float* rstd, const float* weight, float p, uint64_t seed,
+                  const int64_t* seed_at, void* dh, int64_t ld_dh, void* dx, int64_t ld_dx,
+                  float* dweight, float* dbias, int accumulate, void* ws, hipStream_t st);
+size_t logp_workspace_bytes(int64_t N, int64_t V, int dtype, int k);
+int logp_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtype, const void* targets,
+             int idtype, int64_t ignore, float scale, int k, float* logp, float* entropy,
+             float* peak, float* log_sum, float* top_logp, int32_t* top_ids, int32_t* dev_err,
+             void* ws, hipStream_t st);
+int64_t logp_grad_blocks(int64_t N, int64_t V, int dtype);
+int logp_grad_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtype,
+                  const void* targets, int idtype, int64_t ignore, float scale, const float* peak,
+                  const float* log_sum, const float* dlogp, const float* entropy,
+                  const float* dentropy, void* out, int64_t ld_out, hipStream_t st);
 
 int sample_run(const uint64_t* r, int64_t n, int64_t V, void* ids, int idtype, hipStream_t st);
 void segsum_force_wait_failure(bool enable, uint32_t limit);
@@ -156,6 +181,59 @@ static bool check_strides(const int64_t* s, int64_t B, int64_t H, int64_t Lq, in
   }
   return inside <= static_cast<__int128>(1) << 60;  // so the kernels' offsets fit in 63 bits
 }
+
+// The operands of a call on rows: which of them may meet in memory.
+class Operands {
+ public:
+  // A rows x D matrix of elements of `size` bytes, or (rows 1) a vector.
+  void put(const void* at, int64_t rows, int64_t D, int64_t ld, int size, bool written) {
+    if (!at || rows == 0 || D == 0) return;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(at);
+    bad_ |= (a & (size - 1)) != 0 || ld < D || ld > (int64_t(1) << 40);
+    all_[n_++] = {a, rows, D * size, rows > 1 ? ld * size : 0, written};
+  }
+  // LM_E_INVAL where an operand that is written meets another one, but for a matrix that takes
+  // the place of one that is read, row for row.
+  int check() const {
+    if (bad_) return LM_E_INVAL;
+    for (int i = 0; i < n_; ++i)
+      for (int k = 0; k < n_; ++k) {
+        const Operand &w = all_[i], &o = all_[k];
+        if (i == k || !w.written || (o.written && k < i)) continue;
+        if (!o.written && w.at == o.at && w.ld == o.ld && w.rows == o.rows && w.row == o.row)
+          continue;
+        if (const int rc = meet(w, o)) return rc;
+      }
+    return LM_OK;
+  }
+
+ private:
+  struct Operand {
+    uintptr_t at;
+    int64_t rows, row, ld;  // row, ld: bytes
+    bool written;
+  };
+  static int meet(const Operand& w, const Operand& o) {
+    const __int128 w_end = static_cast<__int128>(w.at) + static_cast<__int128>(w.rows - 1) * w.ld + w.row;
+    const __int128 o_end = static_cast<__int128>(o.at) + static_cast<__int128>(o.rows - 1) * o.ld + o.row;
+    if (o.at >= w_end || w.at >= o_end) return LM_OK;
+    // Spans that meet: matrices of the same rows may lie beside each other in wider ones.
+    if (w.rows != o.rows || w.row != o.row) return LM_E_INVAL;
+    const int64_t n[3] = {1, 1, w.rows}, sw[3] = {0, 0, w.ld}, so[3] = {0, 0, o.ld};
+    const Meet m = rows_meet(n, w.row, sw, so,
+                             static_cast<__int128>(o.at) - static_cast<__int128>(w.at));
+    return m == Meet::NO ? LM_OK : m == Meet::YES ? LM_E_INVAL : LM_E_UNSUPPORTED;
+  }
+  Operand all_[12];
+  int n_ = 0;
+  bool bad_ = false;
+};
+
+static int element_size(int32_t dtype) { return dtype == LM_BF16 ? 2 : 4; }
+
+static bool in_unit(float p) { return p >= 0.f && p <= 1.f; }
+
+static bool finite_positive(float x) { return x > 0.f && x < 1e38f; }
 
 }  // namespace lmz
 
@@ -559,6 +637,156 @@ int lm_rel_bias_grad(const void* dout, int32_t dtype, int64_t B, int64_t H, int6
   return rel_grad_run(dout, dtype, B, H, Lq, Lk, dout_strides, q_start, starts, ids, n_seg,
                       num_buckets, dtable, ld_table, accumulate, ws,
                       static_cast<hipStream_t>(stream));
+}
+
+int lm_dropout(const void* x, int64_t ld_x, const void* add, int64_t ld_add, void* out,
+               int64_t ld_out, int64_t rows, int64_t D, int32_t dtype, float p, uint64_t seed,
+               const int64_t* seed_at, void* stream) {
+  if (!valid_dtype(dtype)) return LM_E_UNSUPPORTED;
+  if (rows < 0 || D < 0 || !in_unit(p)) return LM_E_INVAL;
+  if (rows > INT32_MAX || D > INT32_MAX) return LM_E_UNSUPPORTED;
+  if (rows == 0 || D == 0) return LM_OK;
+  if (!x || !out || (reinterpret_cast<uintptr_t>(seed_at) & 7)) return LM_E_INVAL;
+  Operands o;
+  const int size = element_size(dtype);
+  o.put(out, rows, D, ld_out, size, true);
+  o.put(x, rows, D, ld_x, size, false);
+  o.put(add, rows, D, ld_add, size, false);
+  o.put(seed_at, 1, 1, 1, 8, false);
+  if (const int rc = o.check()) return rc;
+  return dropout_run(x, ld_x, add, ld_add, out, ld_out, rows, D, dtype, p, seed, seed_at,
+                     static_cast<hipStream_t>(stream));
+}
+
+int lm_layer_norm(const void* x, int64_t ld_x, const void* add, int64_t ld_add, int64_t rows,
+                  int64_t D, int32_t dtype, const float* weight, const float* bias, float eps,
+                  float p, uint64_t seed, const int64_t* seed_at, void* y, int64_t ld_y, void* h,
+                  int64_t ld_h, float* mean, float* rstd, void* stream) {
+  if (!valid_dtype(dtype)) return LM_E_UNSUPPORTED;
+  if (rows < 0 || D < 1 || !in_unit(p) || !(eps >= 0.f && eps < 1e38f)) return LM_E_INVAL;
+  if (rows > INT32_MAX || D > LM_NORM_MAX_WIDTH) return LM_E_UNSUPPORTED;
+  if (rows == 0) return LM_OK;
+  if (!x || !y || !mean || !rstd) return LM_E_INVAL;
+  Operands o;
+  const int size = element_size(dtype);
+  o.put(y, rows, D, ld_y, size, true);
+  o.put(h, rows, D, ld_h, size, true);
+  o.put(mean, 1, rows, rows, 4, true);
+  o.put(rstd, 1, rows, rows, 4, true);
+  o.put(x, rows, D, ld_x, size, false);
+  o.put(add, rows, D, ld_add, size, false);
+  o.put(weight, 1, D, D, 4, false);
+  o.put(bias, 1, D, D, 4, false);
+  o.put(seed_at, 1, 1, 1, 8, false);
+  if (const int rc = o.check()) return rc;
+  return norm_run(x, ld_x, add, ld_add, rows, D, dtype, weight, bias, eps, p, seed, seed_at, y,
+                  ld_y, h, ld_h, mean, rstd, static_cast<hipStream_t>(stream));
+}
+
+size_t lm_layer_norm_grad_workspace_bytes(int64_t rows, int64_t D, int32_t dtype) {
+  if (!valid_dtype(dtype) || rows < 0 || rows > INT32_MAX || D < 1 || D > LM_NORM_MAX_WIDTH)
+    return 0;
+  return norm_grad_workspace_bytes(rows, D, dtype);
+}
+
+int lm_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* add,
+                       int64_t ld_add, int64_t rows, int64_t D, int32_t dtype, const float* mean,
+                       const float* rstd, const float* weight, float p, uint64_t seed,
+                       const int64_t* seed_at, void* dh, int64_t ld_dh, void* dx, int64_t ld_dx,
+                       float* dweight, float* dbias, int32_t accumulate, void* ws, size_t ws_bytes,
+                       void* stream) {
+  if (!valid_dtype(dtype)) return LM_E_UNSUPPORTED;
+  if (rows < 0 || D < 1 || !in_unit(p)) return LM_E_INVAL;
+  if (rows > INT32_MAX || D > LM_NORM_MAX_WIDTH) return LM_E_UNSUPPORTED;
+  if (rows > 0 && (!dy || !h || !mean || !rstd || !dh)) return LM_E_INVAL;
+  const bool sums = dweight || dbias;
+  const size_t need = sums ? norm_grad_workspace_bytes(rows, D, dtype) : 0;
+  if (need > 0 && !ws) return LM_E_INVAL;
+  if (ws_bytes < need) return LM_E_WORKSPACE;
+  Operands o;
+  const int size = element_size(dtype);
+  o.put(dh, rows, D, ld_dh, size, true);
+  o.put(dx, rows, D, ld_dx, size, true);
+  o.put(dweight, 1, D, D, 4, true);
+  o.put(dbias, 1, D, D, 4, true);
+  o.put(need ? ws : nullptr, 1, static_cast<int64_t>(need / 4), static_cast<int64_t>(need / 4), 4,
+        true);
+  o.put(dy, rows, D, ld_dy, size, false);
+  o.put(h, rows, D, ld_h, size, false);
+  o.put(add, rows, D, ld_add, size, false);
+  o.put(mean, 1, rows, rows, 4, false);
+  o.put(rstd, 1, rows, rows, 4, false);
+  o.put(weight, 1, D, D, 4, false);
+  o.put(seed_at, 1, 1, 1, 8, false);
+  if (const int rc = o.check()) return rc;
+  return norm_grad_run(dy, ld_dy, h, ld_h, add, ld_add, rows, D, dtype, mean, rstd, weight, p,
+                       seed, seed_at, dh, ld_dh, dx, ld_dx, dweight, dbias, accumulate, ws,
+                       static_cast<hipStream_t>(stream));
+}
+
+size_t lm_token_logprobs_workspace_bytes(int64_t N, int64_t V, int32_t dtype, int32_t top) {
+  if (!valid_dtype(dtype) || N < 0 || N > INT32_MAX || V < 1 || V > LM_LOGP_MAX_V || top < 0 ||
+      top > LM_TOP_MAX)
+    return 0;
+  return logp_workspace_bytes(N, V, dtype, top);
+}
+
+int lm_token_logprobs(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype,
+                      const void* targets, int32_t idtype, int64_t ignore, float scale,
+                      int32_t top, float* logp, float* entropy, float* peak, float* log_sum,
+                      float* top_logp, int32_t* top_ids, int32_t* dev_err, void* ws,
+                      size_t ws_bytes, void* stream) {
+  if (!valid_dtype(dtype) || (targets && !valid_idtype(idtype))) return LM_E_UNSUPPORTED;
+  if (N < 0 || V < 1 || top < 0 || !finite_positive(scale)) return LM_E_INVAL;
+  if (N > INT32_MAX || V > LM_LOGP_MAX_V || top > LM_TOP_MAX) return LM_E_UNSUPPORTED;
+  if (N == 0) return LM_OK;
+  if (!logits || !entropy || !peak || !log_sum || (targets && !logp) ||
+      (top > 0 && (!top_logp || !top_ids)))
+    return LM_E_INVAL;
+  const size_t need = logp_workspace_bytes(N, V, dtype, top);
+  if (need > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 15))) return LM_E_INVAL;
+  if (ws_bytes < need) return LM_E_WORKSPACE;
+  Operands o;
+  o.put(targets ? logp : nullptr, 1, N, N, 4, true);
+  o.put(entropy, 1, N, N, 4, true);
+  o.put(peak, 1, N, N, 4, true);
+  o.put(log_sum, 1, N, N, 4, true);
+  o.put(top_logp, 1, N * top, N * top, 4, true);
+  o.put(top_ids, 1, N * top, N * top, 4, true);
+  o.put(dev_err, 1, 1, 1, 4, true);
+  o.put(need ? ws : nullptr, 1, static_cast<int64_t>(need), static_cast<int64_t>(need), 1, true);
+  o.put(logits, N, V, ld, element_size(dtype), false);
+  o.put(targets, 1, N, N, idtype == LM_I64 ? 8 : 4, false);
+  if (const int rc = o.check()) return rc;
+  return logp_run(logits, ld, N, V, dtype, targets, idtype, ignore, scale, top, logp, entropy,
+                  peak, log_sum, top_logp, top_ids, dev_err, ws, static_cast<hipStream_t>(stream));
+}
+
+int lm_token_logprobs_grad(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype,
+                           const void* targets, int32_t idtype, int64_t ignore, float scale,
+                           const float* peak, const float* log_sum, const float* dlogp,
+                           const float* entropy, const float* dentropy, void* out, int64_t ld_out,
+                           void* stream) {
+  if (!valid_dtype(dtype) || (targets && !valid_idtype(idtype))) return LM_E_UNSUPPORTED;
+  if (N < 0 || V < 1 || !finite_positive(scale)) return LM_E_INVAL;
+  if (N > INT32_MAX || V > LM_LOGP_MAX_V) return LM_E_UNSUPPORTED;
+  if (N == 0) return LM_OK;
+  if (!logits || !peak || !log_sum || !out || (dlogp && !targets) || (dentropy && !entropy))
+    return LM_E_INVAL;
+  if (logp_grad_blocks(N, V, dtype) > INT32_MAX) return LM_E_UNSUPPORTED;
+  Operands o;
+  const int size = element_size(dtype);
+  o.put(out, N, V, ld_out, size, true);
+  o.put(logits, N, V, ld, size, false);
+  o.put(dlogp ? targets : nullptr, 1, N, N, idtype == LM_I64 ? 8 : 4, false);
+  o.put(peak, 1, N, N, 4, false);
+  o.put(log_sum, 1, N, N, 4, false);
+  o.put(dlogp, 1, N, N, 4, false);
+  o.put(dentropy ? entropy : nullptr, 1, N, N, 4, false);
+  o.put(dentropy, 1, N, N, 4, false);
+  if (const int rc = o.check()) return rc;
+  return logp_grad_run(logits, ld, N, V, dtype, targets, idtype, ignore, scale, peak, log_sum,
+                       dlogp, entropy, dentropy, out, ld_out, static_cast<hipStream_t>(stream));
 }
 
 int lm_sample_ids(const uint64_t* r, int64_t n, int64_t V, void* ids, int32_t idtype,

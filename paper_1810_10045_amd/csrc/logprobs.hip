@@ -1,0 +1,536 @@
+// Log probabilities of given tokens with entropy and top alternatives, and their
+// gradient. Of a row of logits x, with c = scale and m = max x,
+//     S = sum e^(c (x - m)),  E = sum e^(c (x - m)) c (x - m),  log_sum = log S,
+//     logp = c (x_t - m) - log_sum,  entropy = log_sum - E / S,
+// and, with l = c (x - m) - log_sum and q = e^l,
+//     dx = c (dlogp (1 at t - q) - dentropy q (l + entropy)).
+// The statistics are relative to m, not one number log sum e^(c x): l then keeps its
+// digits however far from zero a row lies.
+//
+// Forward: one pass over the logits, each lane with a running m, S and E (in base 2: one
+// v_exp_f32 a logit); HBM bounds it, the vector units come close behind. A row goes to one
+// workgroup; few rows are cut into parts, which k_logp_join puts together. Backward:
+// one pass that reads and writes each element once.
+#include "launch_parts.hpp"
+#include "patch.hpp"
+
+namespace lmz {
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+constexpr float kFarBelow = -1000.f;  // 2^this is 0
+constexpr int kTopKeys = 1024;        // candidates of a row's alternatives
+static_assert(LM_TOP_MAX == kWave, "a wave ranks the groups' maxima");
+
+// A row's sums so far, relative to its maximum so far (S, E 0 while that is -infinity).
+struct Sums {
+  float m, s, e;
+  // The factor that takes sums relative to m to those relative to `to` >= m, and the
+  // difference of the two in base 2.
+  static __device__ __forceinline__ float shift(float m, float to, float c, float& by) {
+    const float a = m == -__builtin_inff() ? 0.f : m, b = to == -__builtin_inff() ? 0.f : to;
+    by = __builtin_fmaxf((a - b) * c, kFarBelow);  // (where m is, S and E are 0: by is finite)
+    by = m == -__builtin_inff() ? 0.f : by;
+    return __builtin_amdgcn_exp2f(by);
+  }
+  __device__ __forceinline__ void rebase(float to, float c) {
+    float by;
+    const float f = shift(m, to, c, by);
+    e = f * __builtin_fmaf(s, by, e);
+    s *= f;
+    m = to;
+  }
+  __device__ __forceinline__ void add(Sums o, float c) {
+    const float to = __builtin_fmaxf(m, o.m);
+    rebase(to, c);
+    o.rebase(to, c);
+    s += o.s;
+    e += o.e;
+  }
+};
+
+// N logits (masked ones -infinity). A NaN, and an infinite maximum, make S NaN for good.
+template <int N>
+__device__ __forceinline__ void add_logits(Sums& t, const float* x, float c) {
+  float top = t.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = __builtin_fmaxf(top, x[i]);
+  t.rebase(top, c);
+  const float m = top == -__builtin_inff() ? 0.f : top;
+  float s = 0.f, e = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = (x[i] - m) * c;
+    const float p = __builtin_amdgcn_exp2f(d);
+    s += p;
+    e = __builtin_fmaf(p, __builtin_fmaxf(d, kFarBelow), e);  // 0 times no infinity
+  }
+  t.s += s;
+  t.e += e;
+}
+
+// One number for a logit and its id: larger logits first, of equal ones the lowest id; 0 is
+// below all of them.
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t id) {
+  const uint32_t b = __float_as_uint(x + 0.f);  // -0 is 0
+  const uint32_t up = b & 0x80000000u ? ~b : b | 0x80000000u;
+  return static_cast<uint64_t>(up) << 32 | ~id;
+}
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t up = static_cast<uint32_t>(k >> 32);
+  return __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up);
+}
+__device__ __forceinline__ uint32_t key_id(uint64_t k) { return ~static_cast<uint32_t>(k); }
+
+template <int THREADS>
+struct TopSpace {
+  float best[THREADS];
+  uint64_t keys[kTopKeys];
+  uint64_t top[LM_TOP_MAX];
+  uint64_t most[THREADS / kWave];
+  int n;
+};
+
+struct NoSpace {
+  static constexpr const uint64_t* top = nullptr;
+};
+
+__device__ __forceinline__ uint64_t wave_max(uint64_t x) {
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) {
+    const uint64_t y = __shfl_xor(x, off, kWave);
+    x = y > x ? y : x;
+  }
+  return x;
+}
+
+// The k largest keys into t.top, 0 behind the last: `mine` is the largest of the thread's
+// logits, scan(f) calls f(logit, id) for all of them. Of the 64 maxima of groups of threads
+// the k-th is a bound that k logits reach; only threads that reach it look through their
+// logits again, and the few they find are ranked. Where more than kTopKeys reach the bound
+// (many equal logits), each key is found by a pass of its own.
+template <int THREADS, typename Scan>
+__device__ __forceinline__ void select_top(float mine, int k, TopSpace<THREADS>& t, Scan scan) {
+  const int tid = threadIdx.x, lane = lane_id();
+  t.best[tid] = mine;
+  if (tid == 0) t.n = 0;
+  if (tid < LM_TOP_MAX) t.top[tid] = 0;
+  __syncthreads();
+  float group = t.best[lane];
+#pragma unroll
+  for (int i = 1; i < THREADS / kWave; ++i)
+    group = __builtin_fmaxf(group, t.best[lane + i * kWave]);
+  int above = 0;
+#pragma unroll
+  for (int i = 0; i < kWave; ++i) {
+    const float x = read_lane(group, i);
+    above += x > group || (x == group && i < lane) ? 1 : 0;
+  }
+  const uint64_t at = ballot(above == k - 1);
+  const float bound = read_lane(group, at ? __builtin_ctzll(at) : 0);
+  if (mine >= bound && mine > -__builtin_inff()) {
+    scan([&](float x, uint32_t id) {
+      if (x >= bound && x > -__builtin_inff()) {
+        const int i = atomicAdd(&t.n, 1);
+        if (i < kTopKeys) t.keys[i] = key_of(x, id);
+      }
+    });
+  }
+  __syncthreads();
+  const int n = t.n;
+  if (n <= kTopKeys) {
+    for (int i = tid; i < n; i += THREADS) {
+      const uint64_t key = t.keys[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += t.keys[j] > key ? 1 : 0;
+      if (rank < k) t.top[rank] = key;
+    }
+    __syncthreads();
+    return;
+  }
+  uint64_t last = ~uint64_t(0);
+  for (int r = 0; r < k; ++r) {
+    uint64_t best = 0;
+    scan([&](float x, uint32_t id) {
+      if (!(x > -__builtin_inff())) return;
+      const uint64_t key = key_of(x, id);
+      best = key < last && key > best ? key : best;
+    });
+    best = wave_max(best);
+    if (lane == 0) t.most[tid / kWave] = best;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / kWave; ++w) best = t.most[w] > best ? t.most[w] : best;
+    __syncthreads();
+    if (best == 0) break;
+    if (tid == 0) t.top[r] = best;
+    last = best;
+  }
+  __syncthreads();
+}
+
+struct LogpArgs {
+  const void* logits;
+  int64_t ld, N;
+  int V, parts, part_vectors, k;
+  const void* targets;
+  int64_t ignore;
+  int wide;  // targets are int64
+  float scale, c;
+  float *logp, *entropy, *peak, *log_sum, *top_logp;
+  int32_t *top_ids, *dev_err;
+  Sums* sums;      // [N][parts], where rows are cut
+  uint64_t* keys;  // [N][parts][k]
+};
+
+template <typename T>
+__device__ __forceinline__ float logit_at(const T* p) {
+  return Patch<T>::one(p);
+}
+
+// What a row's sums and keys come to, by all of the workgroup's threads.
+template <typename T>
+__device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const Sums& t,
+                                           const uint64_t* top) {
+  const bool bad = !(t.s == t.s);  // a NaN or +infinity among the logits
+  const float nan = __builtin_nanf("");
+  const float log_sum = logf(t.s);
+  if (threadIdx.x == 0) {
+    if (a.logp) {
+      const int64_t id = a.wide ? static_cast<const int64_t*>(a.targets)[row]
+                                : static_cast<const int32_t*>(a.targets)[row];
+      float y = 0.f;
+      if (id != a.ignore) {
+        if (id < 0 || id >= a.V) {
+          raise_err(a.dev_err, LM_DEVERR_ID_RANGE);
+          y = nan;
+        } else {
+          const float x = logit_at(static_cast<const T*>(a.logits) + row * a.ld + id);
+          y = x == -__builtin_inff() ? x : (x - t.m) * a.scale - log_sum;
+          y = bad ? nan : y;
+        }
+      }
+      a.logp[row] = y;
+    }
+    const float h = log_sum - kLn2 * (t.e / t.s);
+    a.entropy[row] = bad ? nan : t.s == 0.f || h < 0.f ? 0.f : h;
+    a.peak[row] = bad ? nan : t.m;
+    a.log_sum[row] = bad ? nan : log_sum;
+  }
+  for (int i = threadIdx.x; i < a.k; i += blockDim.x) {
+    const uint64_t key = top[i];
+    const bool any = key != 0 && !bad;
+    a.top_ids[row * a.k + i] = any ? static_cast<int32_t>(key_id(key)) : -1;
+    a.top_logp[row * a.k + i] =
+        bad ? nan : any ? (key_value(key) - t.m) * a.scale - log_sum : -__builtin_inff();
+  }
+}
+
+// The sums of the workgroup's threads, added in a fixed order, in all of them.
+template <int THREADS>
+__device__ __forceinline__ Sums join_sums(Sums t, float c, Sums (&lds)[THREADS / kWave]) {
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const Sums o{__shfl_xor(t.m, off, kWave), __shfl_xor(t.s, off, kWave),
+                 __shfl_xor(t.e, off, kWave)};
+    t.add(o, c);
+  }
+  if constexpr (THREADS > kWave) {
+    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = t;
+    __syncthreads();
+    t = lds[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / kWave; ++w) t.add(lds[w], c);
+  }
+  return t;
+}
+
+template <typename T, int THREADS, bool TOP, bool NARROW>
+__global__ __launch_bounds__(THREADS) void k_logp(LogpArgs a, uint32_t first) {
+  constexpr int P = Patch<T>::P, U = 4;
+  using raw_t = typename Patch<T>::raw_t;
+  __shared__ Sums lds[THREADS / kWave];
+  __shared__ std::conditional_t<TOP, TopSpace<THREADS>, NoSpace> space;
+  const uint32_t b = first + blockIdx.x;
+  const int64_t row = b / static_cast<uint32_t>(a.parts);
+  const int part = static_cast<int>(b - row * a.parts);
+  const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+  const int vectors = (a.V + P - 1) / P, whole = a.V / P;
+  const int v0 = part * a.part_vectors;
+  const int v1 = a.part_vectors < vectors - v0 ? v0 + a.part_vectors : vectors;
+  const int w1 = whole < v1 ? whole : v1;  // whole vectors
+  // A vector at the row's end is loaded as its last P logits: those that belong to the
+  // vector before count as masked here.
+  auto load = [&](int v) { return Span<T, NARROW>(static_cast<int64_t>(v) * P, a.V, v < v1).load(x); };
+  auto place = [&](int v, const raw_t& r, float* y) {
+    const Span<T, NARROW> s(static_cast<int64_t>(v) * P, a.V, v < v1);
+    s.widen(r, y);
+#pragma unroll
+    for (int e = 0; e < P; ++e) y[e] = e < s.have ? y[e] : -__builtin_inff();
+  };
+  Sums t{-__builtin_inff(), 0.f, 0.f};
+  int v = v0 + threadIdx.x;
+  int base = v0;
+  if constexpr (!NARROW) {
+    for (; base + THREADS * U <= w1; base += THREADS * U, v += THREADS * U) {
+      raw_t r[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) r[u] = Patch<T>::load(x + static_cast<int64_t>(v + u * THREADS) * P);
+      float y[U * P];
+#pragma unroll
+      for (int u = 0; u < U; ++u) Patch<T>::widen(r[u], y + u * P);
+      add_logits<U * P>(t, y, a.c);
+    }
+  }
+  for (; base < v1; base += THREADS * U, v += THREADS * U) {
+    raw_t r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = load(v + u * THREADS);
+    float y[U * P];
+#pragma unroll
+    for (int u = 0; u < U; ++u) place(v + u * THREADS, r[u], y + u * P);
+    add_logits<U * P>(t, y, a.c);
+  }
+  const float mine = t.m;
+  t = join_sums<THREADS>(t, a.c, lds);
+  if constexpr (TOP) {
+    select_top<THREADS>(mine, a.k, space, [&](auto f) {
+      for (int i = v0 + threadIdx.x; i < v1; i += THREADS * U) {
+        raw_t r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) r[u] = load(i + u * THREADS);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float y[P];
+          place(i + u * THREADS, r[u], y);
+#pragma unroll
+          for (int e = 0; e < P; ++e) f(y[e], static_cast<uint32_t>((i + u * THREADS) * P + e));
+        }
+      }
+    });
+  }
+  if (a.parts == 1) {
+    finish_row<T>(a, row, t, space.top);
+    return;
+  }
+  const int64_t at = row * a.parts + part;
+  if (threadIdx.x == 0) a.sums[at] = t;
+  if constexpr (TOP) {
+    for (int i = threadIdx.x; i < a.k; i += THREADS) a.keys[at * a.k + i] = space.top[i];
+  }
+}
+
+// One workgroup a row: the parts' sums and keys.
+constexpr int kJoinThreads = 256;
+
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kJoinThreads) void k_logp_join(LogpArgs a, uint32_t first) {
+  __shared__ Sums lds[kJoinThreads / kWave];
+  __shared__ std::conditional_t<TOP, TopSpace<kJoinThreads>, NoSpace> space;
+  const int64_t row = first + static_cast<int64_t>(blockIdx.x);
+  Sums t{-__builtin_inff(), 0.f, 0.f};
+  for (int i = threadIdx.x; i < a.parts; i += kJoinThreads) t.add(a.sums[row * a.parts + i], a.c);
+  t = join_sums<kJoinThreads>(t, a.c, lds);
+  if constexpr (TOP) {
+    const uint64_t* keys = a.keys + row * a.parts * a.k;
+    const int n = a.parts * a.k;
+    float mine = -__builtin_inff();
+    for (int i = threadIdx.x; i < n; i += kJoinThreads)
+      mine = keys[i] ? __builtin_fmaxf(mine, key_value(keys[i])) : mine;
+    select_top<kJoinThreads>(mine, a.k, space, [&](auto f) {
+      for (int i = threadIdx.x; i < n; i += kJoinThreads)
+        if (keys[i]) f(key_value(keys[i]), key_id(keys[i]));
+    });
+  }
+  finish_row<T>(a, row, t, space.top);
+}
+
+// ---------------------------------------------------------------------------
+// Gradient
+// ---------------------------------------------------------------------------
+struct LogpGradArgs {
+  const void* logits;
+  int64_t ld, N;
+  int V, tiles;
+  const void* targets;
+  int64_t ignore;
+  int wide;
+  float scale;
+  const float *peak, *log_sum, *dlogp, *entropy, *dentropy;
+  void* out;
+  int64_t ld_out;
+};
+
+// A workgroup: kGradThreads / LANES rows, of each a tile of LANES * kGradVectors vectors.
+constexpr int kGradThreads = 256, kGradVectors = 4;
+
+template <typename T, int LANES, bool ENTROPY, bool NARROW>
+__global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint32_t first) {
+  constexpr int P = Patch<T>::P, U = kGradVectors, kRows = kGradThreads / LANES;
+  using raw_t = typename Patch<T>::raw_t;
+  const uint32_t b = first + blockIdx.x;
+  const uint32_t group = b / static_cast<uint32_t>(a.tiles);
+  const int tile = static_cast<int>(b - group * a.tiles);
+  int64_t row = static_cast<int64_t>(group) * kRows;
+  if constexpr (kRows > 1) row += threadIdx.x / LANES;
+  const bool live = row < a.N;
+  row = live ? row : a.N - 1;
+  const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+  T* out = static_cast<T*>(a.out) + row * a.ld_out;
+  const int vectors = (a.V + P - 1) / P;
+  const int v0 = tile * LANES * U + threadIdx.x % LANES;
+  raw_t r[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int v = v0 + u * LANES;
+    r[u] = Span<T, NARROW>(static_cast<int64_t>(v) * P, a.V, v < vectors).load(x);
+  }
+  float dlogp = 0.f;
+  int target = -1;
+  if (a.dlogp) {
+    const int64_t id = a.wide ? static_cast<const int64_t*>(a.targets)[row]
+                              : static_cast<const int32_t*>(a.targets)[row];
+    if (id != a.ignore) {
+      dlogp = id < 0 || id >= a.V ? __builtin_nanf("") : a.dlogp[row] * a.scale;
+      target = id < 0 || id >= a.V ? -1 : static_cast<int>(id);
+    }
+  }
+  const float peak = a.peak[row], log_sum = a.log_sum[row];
+  float entropy = 0.f, dentropy = 0.f;
+  if constexpr (ENTROPY) {
+    entropy = a.entropy[row];
+    dentropy = a.dentropy[row] * a.scale;
+  }
+  // Nothing is left of the row, or nothing depends on it: zeros, whatever its logits are.
+  const bool none = peak == -__builtin_inff() || (dlogp == 0.f && dentropy == 0.f);
+  if (!live) return;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int v = v0 + u * LANES;
+    if (v >= vectors) break;
+    const Span<T, NARROW> s(static_cast<int64_t>(v) * P, a.V);
+    float y[P];
+    s.widen(r[u], y);
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+      const float l = __builtin_fmaf(y[e] - peak, a.scale, -log_sum);
+      const float z = l * kLog2e;
+      float q = __builtin_amdgcn_exp2f(z);
+      if constexpr (sizeof(T) == 4) {
+        // fp32 gradients: z's rounding and the rest of log2 e, to first order
+        constexpr float kRest = 1.925963033e-8f;  // log2 e - kLog2e
+        const float rest = __builtin_fmaf(l, kLog2e, -z) + l * kRest;
+        q = l > kFarBelow ? __builtin_fmaf(q, rest * kLn2, q) : q;
+      }
+      float d = -dlogp * q;
+      if constexpr (ENTROPY)
+        d = __builtin_fmaf(-dentropy * q, __builtin_fmaxf(l, kFarBelow) + entropy, d);
+      d += v * P + e == target ? dlogp : 0.f;
+      y[e] = none ? 0.f : d;
+    }
+    s.store(out, y);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+struct LogpPlan {
+  int64_t parts, part_vectors;
+};
+
+static LogpPlan logp_plan(int64_t N, int64_t V, int dtype) {
+  const int P = dtype == LM_BF16 ? Patch<bf16_t>::P : Patch<float>::P;
+  const int64_t vectors = (V + P - 1) / P;
+  int64_t parts = N > 0 ? 1024 / N : 1;
+  const int64_t most = (vectors + 1023) / 1024;
+  parts = parts < 1 ? 1 : parts > most ? most : parts;
+  const int64_t each = (vectors + parts - 1) / parts;
+  return {(vectors + each - 1) / each, each};
+}
+
+static size_t sums_bytes(int64_t n) { return (static_cast<size_t>(n) * sizeof(Sums) + 15) / 16 * 16; }
+
+size_t logp_workspace_bytes(int64_t N, int64_t V, int dtype, int k) {
+  const int64_t parts = logp_plan(N, V, dtype).parts;
+  return parts == 1 ? 0 : sums_bytes(N * parts) + static_cast<size_t>(N * parts) * k * 8;
+}
+
+template <typename T>
+static int logp_launch(const LogpArgs& a, hipStream_t st) {
+  constexpr int P = Patch<T>::P;
+  const bool top = a.k > 0, narrow = a.V < P, few = a.V <= 256 * P;
+  const int threads = few ? kWave : 256;
+  auto kernel = narrow ? (top ? k_logp<T, kWave, true, true> : k_logp<T, kWave, false, true>)
+                : few ? (top ? k_logp<T, kWave, true, false> : k_logp<T, kWave, false, false>)
+                      : (top ? k_logp<T, 256, true, false> : k_logp<T, 256, false, false>);
+  const int rc = launch_parts(a.N * a.parts, threads, [&](uint32_t first, uint32_t n) {
+    kernel<<<n, threads, 0, st>>>(a, first);
+    return launch_status(hipGetLastError());
+  });
+  if (rc != LM_OK || a.parts == 1) return rc;
+  auto join = top ? k_logp_join<T, true> : k_logp_join<T, false>;
+  return launch_parts(a.N, kJoinThreads, [&](uint32_t first, uint32_t n) {
+    join<<<n, kJoinThreads, 0, st>>>(a, first);
+    return launch_status(hipGetLastError());
+  });
+}
+
+int logp_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtype, const void* targets,
+             int idtype, int64_t ignore, float scale, int k, float* logp, float* entropy,
+             float* peak, float* log_sum, float* top_logp, int32_t* top_ids, int32_t* dev_err,
+             void* ws, hipStream_t st) {
+  if (N == 0) return LM_OK;
+  const LogpPlan p = logp_plan(N, V, dtype);
+  char* keys = ws ? static_cast<char*>(ws) + sums_bytes(N * p.parts) : nullptr;
+  const LogpArgs a{logits, ld, N, static_cast<int>(V), static_cast<int>(p.parts),
+                   static_cast<int>(p.part_vectors), k, targets, ignore, idtype == LM_I64, scale,
+                   static_cast<float>(static_cast<double>(scale) * 1.4426950408889634),
+                   targets ? logp : nullptr, entropy, peak, log_sum, top_logp, top_ids, dev_err,
+                   static_cast<Sums*>(ws),
+                   reinterpret_cast<uint64_t*>(keys)};
+  return dtype == LM_BF16 ? logp_launch<bf16_t>(a, st) : logp_launch<float>(a, st);
+}
+
+template <typename T, int LANES>
+static int grad_launch(LogpGradArgs a, hipStream_t st) {
+  constexpr int P = Patch<T>::P, kRows = kGradThreads / LANES;
+  const int64_t vectors = (static_cast<int64_t>(a.V) + P - 1) / P;
+  a.tiles = static_cast<int>((vectors + LANES * kGradVectors - 1) / (LANES * kGradVectors));
+  auto kernel = a.dentropy ? k_logp_grad<T, LANES, true, false> : k_logp_grad<T, LANES, false, false>;
+  if constexpr (LANES == 16)
+    if (a.V < P)
+      kernel = a.dentropy ? k_logp_grad<T, LANES, true, true> : k_logp_grad<T, LANES, false, true>;
+  return launch_parts((a.N + kRows - 1) / kRows * a.tiles, kGradThreads,
+                      [&](uint32_t first, uint32_t n) {
+                        kernel<<<n, kGradThreads, 0, st>>>(a, first);
+                        return launch_status(hipGetLastError());
+                      });
+}
+
+template <typename T>
+static int grad_lanes(const LogpGradArgs& a, hipStream_t st) {
+  const int64_t vectors = (static_cast<int64_t>(a.V) + Patch<T>::P - 1) / Patch<T>::P;
+  if (vectors <= 16 * kGradVectors) return grad_launch<T, 16>(a, st);
+  if (vectors <= 64 * kGradVectors) return grad_launch<T, 64>(a, st);
+  return grad_launch<T, 256>(a, st);
+}
+
+// Workgroups of a call, for the check of the grid's size.
+int64_t logp_grad_blocks(int64_t N, int64_t V, int dtype) {
+  const int P = dtype == LM_BF16 ? Patch<bf16_t>::P : Patch<float>::P;
+  const int64_t vectors = (V + P - 1) / P;
+  return (vectors + 256 * kGradVectors - 1) / (256 * kGradVectors) * N;
+}
+
+int logp_grad_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtype,
+                  const void* targets, int idtype, int64_t ignore, float scale, const float* peak,
+                  const float* log_sum, const float* dlogp, const float* entropy,
+                  const float* dentropy, void* out, int64_t ld_out, hipStream_t st) {
+  if (N == 0) return LM_OK;
+  const LogpGradArgs a{logits, ld, N, static_cast<int>(V), 0, targets, ignore, idtype == LM_I64,
+                       scale, peak, log_sum, targets ? dlogp : nullptr, entropy, dentropy, out,
+                       ld_out};
+  return dtype == LM_BF16 ? grad_lanes<bf16_t>(a, st) : grad_lanes<float>(a, st);
+}
+
+}  // namespace lmz

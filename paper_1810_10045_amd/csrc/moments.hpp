@@ -46,8 +46,8 @@ struct StepKeys {
   uint32_t k0, k1;
 };
 
-// Two words from the caller's 64-bit seed (host).
-static inline StepKeys step_keys(uint64_t seed) {
+// Two words from the caller's 64-bit seed.
+__host__ __device__ static inline StepKeys step_keys(uint64_t seed) {
   uint64_t z = seed * 0x9E3779B97F4A7C15ull + 0x632BE59BD9B4E019ull;
   z = (z ^ (z >> 29)) * 0xD6E8FEB86659FD93ull;
   z ^= z >> 32;

@@ -11,6 +11,7 @@
 // element of the matrices is read or written once: HBM bounds both.
 #include "common.hpp"
 #include "launch_parts.hpp"
+#include "patch.hpp"
 
 namespace lmz {
 
@@ -33,76 +34,6 @@ __device__ __forceinline__ int segment_of(const int32_t* starts, int n, int r) {
   }
   return lo;
 }
-
-// P values of a row: 16 bytes at the alignment of an element. Matrices are read
-// once: past the caches.
-template <typename T>
-struct Patch;
-
-template <>
-struct Patch<float> {
-  static constexpr int P = 4;
-  using raw_t = f32x4;
-  static __device__ __forceinline__ raw_t load(const float* p) {
-    return stream_load_e(reinterpret_cast<const f32x4e*>(p));
-  }
-  static __device__ __forceinline__ void widen(const raw_t& r, float* x) {
-    x[0] = r.x; x[1] = r.y; x[2] = r.z; x[3] = r.w;
-  }
-  // The values from number `by` (0 to 4) on, zeros behind them.
-  static __device__ __forceinline__ raw_t shift(const raw_t& r, int by) {
-    raw_t a = by & 2 ? raw_t{r.z, r.w, 0.f, 0.f} : r;
-    a = by & 1 ? raw_t{a.y, a.z, a.w, 0.f} : a;
-    return by & 4 ? raw_t{0.f, 0.f, 0.f, 0.f} : a;
-  }
-  static __device__ __forceinline__ raw_t pack(const float* x) {
-    return raw_t{x[0], x[1], x[2], x[3]};
-  }
-  static __device__ __forceinline__ void store(float* p, const float* x) {
-    __builtin_nontemporal_store(f32x4e{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4e*>(p));
-  }
-  static __device__ __forceinline__ float one(const float* p) { return *p; }
-  static __device__ __forceinline__ void put(float* p, float x) { *p = x; }
-};
-
-template <>
-struct Patch<bf16_t> {
-  static constexpr int P = 8;
-  using raw_t = u32x4;
-  static __device__ __forceinline__ raw_t load(const bf16_t* p) {
-    return stream_load_e(reinterpret_cast<const u32x4e*>(p));
-  }
-  static __device__ __forceinline__ void widen(const raw_t& r, float* x) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[2 * e] = __uint_as_float(w[e] << 16);
-      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ raw_t shift(const raw_t& r, int by) {
-    raw_t a = by & 4 ? raw_t{r.z, r.w, 0u, 0u} : r;
-    a = by & 2 ? raw_t{a.y, a.z, a.w, 0u} : a;
-    if (by & 1)
-      a = raw_t{a.x >> 16 | a.y << 16, a.y >> 16 | a.z << 16, a.z >> 16 | a.w << 16, a.w >> 16};
-    return by & 8 ? raw_t{0u, 0u, 0u, 0u} : a;
-  }
-  static __device__ __forceinline__ uint32_t bits(float x) {
-    return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
-  }
-  static __device__ __forceinline__ raw_t pack(const float* x) {
-    return raw_t{bits(x[0]) | bits(x[1]) << 16, bits(x[2]) | bits(x[3]) << 16,
-                 bits(x[4]) | bits(x[5]) << 16, bits(x[6]) | bits(x[7]) << 16};
-  }
-  static __device__ __forceinline__ void store(bf16_t* p, const float* x) {
-    const raw_t w = pack(x);
-    __builtin_nontemporal_store(u32x4e{w.x, w.y, w.z, w.w}, reinterpret_cast<u32x4e*>(p));
-  }
-  static __device__ __forceinline__ float one(const bf16_t* p) { return bf16_to_f32(p->bits); }
-  static __device__ __forceinline__ void put(bf16_t* p, float x) {
-    p->bits = static_cast<uint16_t>(bits(x));
-  }
-};
 
 // Where a lane's patch lies in its rows: `have` of its P columns exist and are used
 // (0 or less: none). It loads from column `from`, inside the row wherever it lies
@@ -138,10 +69,6 @@ struct Columns {
 struct Strides {
   int64_t b, h, q;
 };
-
-__device__ __forceinline__ float read_lane(float v, int lane) {
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
-}
 
 // LDS instructions of a wave take effect in their order; where lanes meet each
 // other's addresses, the compiler has to keep it too.

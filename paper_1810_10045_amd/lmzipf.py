@@ -14,7 +14,10 @@ payload forms ``fill_values_f16`` and ``sparse_apply_f16``, and
 Beside the embedding's path: ``adamw_plan`` and ``adamw`` (the AdamW step over
 many tensors, moments in fp32 or 8 bits), ``sparse_apply_q8`` (the lazy step on
 table rows with 8-bit moments), ``rel_buckets``, ``rel_bias`` and
-``rel_bias_grad`` (a learned relative position bias and its gradient).
+``rel_bias_grad`` (a learned relative position bias and its gradient),
+``dropout``, ``layer_norm`` and ``layer_norm_grad``, ``token_logprobs`` and
+``token_logprobs_grad`` (log probabilities of given tokens, entropy, top
+alternatives).
 """
 from __future__ import annotations
 
@@ -40,6 +43,7 @@ FILL_EXPAND, FILL_SCATTER, FILL_SCATTER_ADD = 0, 1, 2
 OPT_SGD, OPT_ADAM = 0, 1
 REL_BOTH, REL_PAST, REL_CAUSAL = 0, 1, 2
 MOMENT_BLOCK, REL_MAX_SEGMENTS = 32, 257
+NORM_MAX_WIDTH, TOP_MAX = 16384, 64
 MAX_K = 1 << 30
 
 EXPORTS = ("lm_status_string", "lm_abi_version", "lm_workspace_clear",
@@ -48,7 +52,9 @@ EXPORTS = ("lm_status_string", "lm_abi_version", "lm_workspace_clear",
            "lm_fill_values_f16", "lm_sparse_apply_f16", "lm_sample_ids",
            "lm_adamw_plan_bytes", "lm_adamw_plan", "lm_adamw", "lm_sparse_apply_q8",
            "lm_rel_buckets", "lm_rel_bias", "lm_rel_bias_grad_workspace_bytes",
-           "lm_rel_bias_grad")
+           "lm_rel_bias_grad", "lm_dropout", "lm_layer_norm", "lm_layer_norm_grad_workspace_bytes",
+           "lm_layer_norm_grad", "lm_token_logprobs_workspace_bytes", "lm_token_logprobs",
+           "lm_token_logprobs_grad")
 
 
 class LmError(RuntimeError):
@@ -107,6 +113,19 @@ def _load():
     L.lm_rel_bias_grad_workspace_bytes.restype = SZ
     L.lm_rel_bias_grad.argtypes = [P, I32_, I64_, I64_, I64_, I64_, P, I64_, P, P, I32_, I32_, P,
                                    I64_, I32_, P, SZ, P]
+    L.lm_dropout.argtypes = [P, I64_, P, I64_, P, I64_, I64_, I64_, I32_, F, U64, P, P]
+    L.lm_layer_norm.argtypes = [P, I64_, P, I64_, I64_, I64_, I32_, P, P, F, F, U64, P, P, I64_, P,
+                                I64_, P, P, P]
+    L.lm_layer_norm_grad_workspace_bytes.argtypes = [I64_, I64_, I32_]
+    L.lm_layer_norm_grad_workspace_bytes.restype = SZ
+    L.lm_layer_norm_grad.argtypes = [P, I64_, P, I64_, P, I64_, I64_, I64_, I32_, P, P, P, F, U64, P,
+                                     P, I64_, P, I64_, P, P, I32_, P, SZ, P]
+    L.lm_token_logprobs_workspace_bytes.argtypes = [I64_, I64_, I32_, I32_]
+    L.lm_token_logprobs_workspace_bytes.restype = SZ
+    L.lm_token_logprobs.argtypes = [P, I64_, I64_, I64_, I32_, P, I32_, I64_, F, I32_, P, P, P, P, P,
+                                    P, P, P, SZ, P]
+    L.lm_token_logprobs_grad.argtypes = [P, I64_, I64_, I64_, I32_, P, I32_, I64_, F, P, P, P, P, P,
+                                         P, I64_, P]
     L.lm_segsum_set_two_launches.argtypes = [I32_]
     L.lm_test_force_wait_failure.argtypes = [I32_, ctypes.c_uint32]
     for f in ("lm_abi_version", "lm_workspace_clear", "lm_unique", "lm_unique_noalloc",
@@ -114,7 +133,8 @@ def _load():
               "lm_fill_values", "lm_sparse_apply", "lm_fill_values_f16", "lm_sparse_apply_f16",
               "lm_sample_ids", "lm_segsum_set_two_launches", "lm_test_force_wait_failure",
               "lm_adamw_plan", "lm_adamw", "lm_sparse_apply_q8", "lm_rel_buckets", "lm_rel_bias",
-              "lm_rel_bias_grad"):
+              "lm_rel_bias_grad", "lm_dropout", "lm_layer_norm", "lm_layer_norm_grad",
+              "lm_token_logprobs", "lm_token_logprobs_grad"):
         getattr(L, f).restype = ctypes.c_int
     return L
 
@@ -856,12 +876,12 @@ def rel_buckets(num_buckets: int, max_distance: int, mode: str = "both") -> RelB
     return RelBuckets(starts, ids, n.value, num_buckets)
 
 
-def _no_graph(what: str, *tensors):
+def _no_graph(what: str, *tensors, gradient="rel_bias_grad is the gradient of rel_bias"):
     """A tensor that requires grad would come out of the call without its graph."""
     for t in tensors:
         if t is not None and t.requires_grad and torch.is_grad_enabled():
             raise LmError(f"{what} is not recorded by autograd: call it under torch.no_grad() or"
-                          " in an autograd.Function (rel_bias_grad is the gradient of rel_bias)")
+                          f" in an autograd.Function ({gradient})")
 
 
 _Strides = ctypes.c_int64 * 3
@@ -946,6 +966,306 @@ def rel_bias_grad(dout: torch.Tensor, buckets: RelBuckets, q_start: int = 0,
         _ptr(dout), gtype, B, H, Lq, Lk, strides, q_start, buckets.starts, buckets.ids,
         buckets.n_seg, buckets.num_buckets, _ptr(out), _rows(out, "out"), bool(accumulate),
         _ptr(buf), need, _on(device, stream)), "lm_rel_bias_grad")
+    if given is not None:
+        _written(given)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Dropout and layer norm
+# ---------------------------------------------------------------------------
+def _matrix(t: torch.Tensor, what: str):
+    """(rows, D, ld) of a tensor whose last dimension is the columns; the others, one behind
+    the other, are the rows."""
+    shape = t.shape
+    if not shape:
+        raise LmError(f"{what} must have a dimension")
+    D = shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // D if D else 0), D, D
+    strides = t.stride()
+    rows, ld = 1, None
+    for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if n != 1 and rows and s != (s if ld is None else rows * ld):
+            raise LmError(f"{what} must have its rows at equal distances")
+        ld = s if n != 1 and ld is None else ld
+        rows *= n
+    if strides[-1] != 1 and D > 1:
+        raise LmError(f"{what} must have unit column stride")
+    return rows, D, D if ld is None else ld
+
+
+def _like(t: Optional[torch.Tensor], x: torch.Tensor, what: str):
+    """The row stride of an operand of x's shape and dtype (None: 0)."""
+    if t is None:
+        return 0
+    if t.shape != x.shape or t.dtype != x.dtype:
+        raise LmError(f"{what} must be {' x '.join(map(str, x.shape))} of {x.dtype}")
+    return _matrix(t, what)[2]
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str):
+    if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
+        raise LmError(f"{what} must be contiguous float32 with {n} elements")
+
+
+def _seed(seed, device):
+    """(number, address) of a seed that the host or the device holds."""
+    if not isinstance(seed, torch.Tensor):
+        return seed, None
+    _one_of(seed, torch.int64, "seed")
+    _same_device(device, seed)
+    return 0, seed.data_ptr()
+
+
+def dropout(x: torch.Tensor, p: float, seed, add: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """lm_dropout: x with each element dropped with probability p (to multiples
+    of 2^-16) and the others divided by 1 - p, plus `add`; x float32 or bfloat16,
+    its last dimension the columns. The mask is a function of `seed`, the
+    element's row and column and the number of columns: the gradient is
+    `dropout(dout, p, seed)`. seed: a number, or an int64 tensor of one element
+    on the device, which a captured call reads with every replay. `out` may be x
+    or `add`. Not recorded by autograd, as ``rel_bias``."""
+    _no_graph("dropout", x, add, out, gradient="its gradient is dropout with the same seed")
+    _dev(x, "x")
+    device = x.device
+    rows, D, ld = _matrix(x, "x")
+    dtype = _gtype(x)
+    _same_device(device, add, out)
+    number, at = _seed(seed, device)
+    if _elsewhere(device, stream):
+        with torch.cuda.device(device):
+            return dropout(x, p, seed, add, out, stream)
+    ld_add = _like(add, x, "add")
+    given = out
+    if out is None:
+        out = _empty(x.shape, x.dtype, device, stream)
+    _call(_lib.lm_dropout(_ptr(x), ld, _ptr(add), ld_add, _ptr(out), _like(out, x, "out"), rows, D,
+                          dtype, p, number, at, _on(device, stream)), "lm_dropout")
+    if given is not None:
+        _written(given)
+    return out
+
+
+class NormResult(NamedTuple):
+    """y, what it is the norm of, and the statistics that the gradient takes."""
+    y: torch.Tensor
+    h: torch.Tensor
+    mean: torch.Tensor
+    rstd: torch.Tensor
+
+
+_NORM_GRADIENT = "layer_norm_grad is the gradient of layer_norm"
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
+               bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               add: Optional[torch.Tensor] = None, p: float = 0.0, seed=0,
+               out: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
+               stream=None) -> NormResult:
+    """lm_layer_norm: y, the norm of h = add + dropout(x) over its last
+    dimension (up to NORM_MAX_WIDTH), with float32 weight and bias. h is x itself
+    where nothing is added or dropped, else `sum_out` (which may be `add`: the
+    residual stream) or a new tensor; y goes to `out` (which may be x) or a new
+    one. p and seed as ``dropout``'s. Not recorded by autograd, as ``rel_bias``."""
+    _no_graph("layer_norm", x, weight, bias, add, out, sum_out, gradient=_NORM_GRADIENT)
+    _dev(x, "x")
+    device = x.device
+    rows, D, ld = _matrix(x, "x")
+    dtype = _gtype(x)
+    _vector(weight, D, "weight")
+    _vector(bias, D, "bias")
+    _same_device(device, weight, bias, add, out, sum_out)
+    number, at = _seed(seed, device)
+    if _elsewhere(device, stream):
+        with torch.cuda.device(device):
+            return layer_norm(x, weight, bias, eps, add, p, seed, out, sum_out, stream)
+    ld_add = _like(add, x, "add")
+    given = [t for t in (out, sum_out) if t is not None]
+    if sum_out is None and (add is not None or p > 0):
+        sum_out = _empty(x.shape, x.dtype, device, stream)
+    if out is None:
+        out = _empty(x.shape, x.dtype, device, stream)
+    mean, rstd = _empty((2, *x.shape[:-1]), torch.float32, device, stream).unbind()
+    _call(_lib.lm_layer_norm(
+        _ptr(x), ld, _ptr(add), ld_add, rows, D, dtype, _ptr(weight), _ptr(bias), eps, p, number, at,
+        _ptr(out), _like(out, x, "out"), _ptr(sum_out), _like(sum_out, x, "sum_out"), _ptr(mean),
+        _ptr(rstd), _on(device, stream)), "lm_layer_norm")
+    for t in given:
+        _written(t)
+    return NormResult(out, x if sum_out is None else sum_out, mean, rstd)
+
+
+class NormGrad(NamedTuple):
+    """Gradients: of h (and of the forward's `add`), of x (dh itself without
+    dropout), of the weight and of the bias (None where there is none)."""
+    dh: torch.Tensor
+    dx: torch.Tensor
+    dweight: Optional[torch.Tensor]
+    dbias: Optional[torch.Tensor]
+
+
+def layer_norm_grad(dy: torch.Tensor, h: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                    weight: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
+                    p: float = 0.0, seed=0, out: Optional[torch.Tensor] = None,
+                    dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                    dbias: Optional[torch.Tensor] = None, bias: Optional[bool] = None,
+                    accumulate: bool = False, ws: Optional[Workspace] = None,
+                    stream=None) -> NormGrad:
+    """lm_layer_norm_grad: from the gradient of y and what ``layer_norm``
+    returned. add: the gradient that reaches h past the norm (the residual
+    stream's). p and seed: the forward's. out (dh), dx: written, new where not
+    given; they may be dy, h or add. dweight, dbias: float32, written, or with
+    `accumulate` added to; new where not given, dweight where there is a weight,
+    dbias as `bias` says (None: as the weight). Without `ws` the call takes its
+    workspace from torch's allocator. Not recorded by autograd, as ``rel_bias``."""
+    _no_graph("layer_norm_grad", dy, h, weight, add, out, dx, dweight, dbias,
+              gradient=_NORM_GRADIENT)
+    _dev(dy, "dy")
+    device = dy.device
+    rows, D, ld = _matrix(dy, "dy")
+    dtype = _gtype(dy)
+    for t, n, what in ((mean, rows, "mean"), (rstd, rows, "rstd"), (weight, D, "weight"),
+                       (dweight, D, "dweight"), (dbias, D, "dbias")):
+        _vector(t, n, what)
+    _same_device(device, h, mean, rstd, weight, add, out, dx, dweight, dbias,
+                 None if ws is None else ws.buf)
+    number, at = _seed(seed, device)
+    if _elsewhere(device, stream):
+        with torch.cuda.device(device):
+            return layer_norm_grad(dy, h, mean, rstd, weight, add, p, seed, out, dx, dweight, dbias,
+                                   bias, accumulate, ws, stream)
+    bias = weight is not None if bias is None else bias
+    new = (dweight is None and weight is not None) + (dbias is None and bool(bias))
+    if accumulate and (new or (dweight is None and dbias is None)):
+        raise LmError("accumulate needs dweight, and dbias where there is a bias")
+    ld_h, ld_add = _like(h, dy, "h"), _like(add, dy, "add")
+    given = [t for t in (out, dx, dweight, dbias) if t is not None]
+    if out is None:
+        out = _empty(dy.shape, dy.dtype, device, stream)
+    if dx is None and p > 0:
+        dx = _empty(dy.shape, dy.dtype, device, stream)
+    if new:
+        fresh = list(_empty((new, D), torch.float32, device, stream).unbind())
+        dweight = fresh.pop(0) if dweight is None and weight is not None else dweight
+        dbias = fresh.pop(0) if dbias is None and bias else dbias
+    buf, need = None, 0
+    if dweight is not None or dbias is not None:
+        need = _lib.lm_layer_norm_grad_workspace_bytes(rows, D, dtype)
+        if need:
+            buf = ws.get(need) if ws is not None else _empty((need,), torch.uint8, device, stream)
+    _call(_lib.lm_layer_norm_grad(
+        _ptr(dy), ld, _ptr(h), ld_h, _ptr(add), ld_add, rows, D, dtype, _ptr(mean), _ptr(rstd),
+        _ptr(weight), p, number, at, _ptr(out), _like(out, dy, "out"), _ptr(dx),
+        _like(dx, dy, "dx"), _ptr(dweight), _ptr(dbias), bool(accumulate), _ptr(buf), need,
+        _on(device, stream)), "lm_layer_norm_grad")
+    for t in given:
+        _written(t)
+    return NormGrad(out, out if dx is None else dx, dweight, dbias)
+
+
+# ---------------------------------------------------------------------------
+# Log probabilities of given tokens
+# ---------------------------------------------------------------------------
+class TokenLogprobs(NamedTuple):
+    """Per row: the target's log probability (None without targets), the
+    entropy, the largest logit and log sum exp(scale * (logit - peak)); the likeliest
+    words' log probabilities and ids (None without `top`)."""
+    logp: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    peak: torch.Tensor
+    log_sum: torch.Tensor
+    top_logp: Optional[torch.Tensor]
+    top_ids: Optional[torch.Tensor]
+
+
+_LOGP_GRADIENT = "token_logprobs_grad is the gradient of token_logprobs"
+
+
+def _targets(targets: Optional[torch.Tensor], logits: torch.Tensor) -> int:
+    if targets is None:
+        return I32
+    if targets.shape != logits.shape[:-1] or not targets.is_contiguous():
+        raise LmError("targets must be contiguous, of the logits' shape without the last dimension")
+    return _idtype(targets)
+
+
+def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None,
+                   scale: float = 1.0, top: int = 0, ignore: int = -100,
+                   dev_err: Optional[torch.Tensor] = None, ws: Optional[Workspace] = None,
+                   stream=None) -> TokenLogprobs:
+    """lm_token_logprobs: log softmax(scale * logits) at each row's target (0
+    where it is `ignore`), the entropy, and the `top` (up to TOP_MAX) likeliest
+    words, of equal ones the lowest ids first. logits float32 or bfloat16, the
+    words along the last dimension, -infinity where a word is masked. dev_err
+    tells of targets outside the vocabulary (their logp is NaN). Without `ws` the
+    call takes its workspace from torch's allocator. Not recorded by autograd, as
+    ``rel_bias``."""
+    _no_graph("token_logprobs", logits, gradient=_LOGP_GRADIENT)
+    _dev(logits, "logits")
+    device = logits.device
+    N, V, ld = _matrix(logits, "logits")
+    dtype, idtype = _gtype(logits), _targets(targets, logits)
+    _same_device(device, targets, dev_err, None if ws is None else ws.buf)
+    _one_of(dev_err, torch.int32, "dev_err")
+    if _elsewhere(device, stream):
+        with torch.cuda.device(device):
+            return token_logprobs(logits, targets, scale, top, ignore, dev_err, ws, stream)
+    shape = logits.shape[:-1]
+    found = _empty((3 if targets is None else 4, *shape), torch.float32, device, stream).unbind()
+    entropy, peak, log_sum = found[:3]
+    logp = None if targets is None else found[3]
+    top_logp = top_ids = None
+    if top > 0:
+        top_logp = _empty((*shape, top), torch.float32, device, stream)
+        top_ids = _empty((*shape, top), torch.int32, device, stream)
+    need = _lib.lm_token_logprobs_workspace_bytes(N, V, dtype, top)
+    buf = None
+    if need:
+        buf = ws.get(need) if ws is not None else _empty((need,), torch.uint8, device, stream)
+    _call(_lib.lm_token_logprobs(
+        _ptr(logits), ld, N, V, dtype, _ptr(targets), idtype, ignore, scale, top, _ptr(logp),
+        _ptr(entropy), _ptr(peak), _ptr(log_sum), _ptr(top_logp), _ptr(top_ids), _ptr(dev_err),
+        _ptr(buf), need, _on(device, stream)), "lm_token_logprobs")
+    return TokenLogprobs(logp, entropy, peak, log_sum, top_logp, top_ids)
+
+
+def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor],
+                        peak: torch.Tensor, log_sum: torch.Tensor,
+                        dlogp: Optional[torch.Tensor] = None,
+                        entropy: Optional[torch.Tensor] = None,
+                        dentropy: Optional[torch.Tensor] = None, scale: float = 1.0,
+                        ignore: int = -100, out: Optional[torch.Tensor] = None,
+                        stream=None) -> torch.Tensor:
+    """lm_token_logprobs_grad: the logits' gradient, in their dtype, from those
+    of logp (dlogp) and of the entropy (dentropy, with the entropy itself), and
+    what ``token_logprobs`` returned. `out` may be the logits. Not recorded by
+    autograd, as ``rel_bias``."""
+    _no_graph("token_logprobs_grad", logits, dlogp, dentropy, out, gradient=_LOGP_GRADIENT)
+    _dev(logits, "logits")
+    device = logits.device
+    N, V, ld = _matrix(logits, "logits")
+    dtype, idtype = _gtype(logits), _targets(targets, logits)
+    for t, what in ((peak, "peak"), (log_sum, "log_sum"), (dlogp, "dlogp"), (entropy, "entropy"),
+                    (dentropy, "dentropy")):
+        _vector(t, N, what)
+    if dlogp is not None and targets is None:
+        raise LmError("dlogp needs targets")
+    if dentropy is not None and entropy is None:
+        raise LmError("dentropy needs entropy")
+    _same_device(device, targets, peak, log_sum, dlogp, entropy, dentropy, out)
+    if _elsewhere(device, stream):
+        with torch.cuda.device(device):
+            return token_logprobs_grad(logits, targets, peak, log_sum, dlogp, entropy, dentropy,
+                                       scale, ignore, out, stream)
+    given = out
+    if out is None:
+        out = _empty(logits.shape, logits.dtype, device, stream)
+    _call(_lib.lm_token_logprobs_grad(
+        _ptr(logits), ld, N, V, dtype, _ptr(targets), idtype, ignore, scale, _ptr(peak),
+        _ptr(log_sum), _ptr(dlogp), _ptr(entropy), _ptr(dentropy), _ptr(out),
+        _like(out, logits, "out"), _on(device, stream)), "lm_token_logprobs_grad")
     if given is not None:
         _written(given)
     return out
