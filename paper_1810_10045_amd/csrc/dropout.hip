@@ -31,6 +31,7 @@ struct DropArgs {
   uint64_t word;     // of the first row
   uint32_t vectors;  // of the launch
   Divide per_row;
+  bool cached;
 };
 
 template <typename T, bool ADD, bool NARROW>
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(kDropThreads) void k_dropout(const T* x, const T* a
     const uint32_t at = v < a.vectors ? v : a.vectors - 1;
     row[u] = a.per_row(at);
     vec[u] = at - row[u] * a.per_row.d;
-    const Span<T, NARROW> s(static_cast<int64_t>(vec[u]) * P, a.D);
+    const Span<T, NARROW ? Ends::NARROW : Ends::PART> s(static_cast<int64_t>(vec[u]) * P, a.D);
     rx[u] = s.load(x + row[u] * a.ld_x);
     if constexpr (ADD) ra[u] = s.load(add + row[u] * a.ld_add);
   }
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(kDropThreads) void k_dropout(const T* x, const T* a
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (v0 + u * kDropThreads >= a.vectors) break;
-    const Span<T, NARROW> s(static_cast<int64_t>(vec[u]) * P, a.D);
+    const Span<T, NARROW ? Ends::NARROW : Ends::PART> s(static_cast<int64_t>(vec[u]) * P, a.D);
     float y[P];
     s.widen(rx[u], y);
     keep.apply<P>(a.word + row[u] * pairs + vec[u] * (P / 2), y);
@@ -66,7 +67,7 @@ __global__ __launch_bounds__(kDropThreads) void k_dropout(const T* x, const T* a
 #pragma unroll
       for (int e = 0; e < P; ++e) y[e] += z[e];
     }
-    s.store(out + row[u] * a.ld_out, y);
+    s.store(out + row[u] * a.ld_out, y, a.cached);
   }
 }
 
@@ -85,7 +86,8 @@ static int dropout_launch(const T* x, int64_t ld_x, const T* add, int64_t ld_add
   for (int64_t r = 0; r < rows; r += most) {
     const int64_t n = rows - r < most ? rows - r : most;
     const DropArgs a{D, ld_x, ld_add, ld_out, static_cast<uint64_t>(r) * pairs,
-                     static_cast<uint32_t>(n * per_row), Divide(static_cast<uint32_t>(per_row))};
+                     static_cast<uint32_t>(n * per_row), Divide(static_cast<uint32_t>(per_row)),
+                     cached_bytes(rows, D * static_cast<int64_t>(sizeof(T)))};
     const uint32_t blocks = static_cast<uint32_t>((n * per_row + kBlock - 1) / kBlock);
     kernel<<<blocks, kDropThreads, 0, st>>>(x + r * ld_x, add ? add + r * ld_add : nullptr,
                                             out + r * ld_out, a, k);

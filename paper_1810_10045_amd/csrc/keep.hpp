@@ -44,12 +44,23 @@ struct Keep {
   // whatever it was (infinity, NaN).
   template <int P>
   __device__ __forceinline__ void apply(uint64_t word, float* x) const {
+    const uint32_t low = static_cast<uint32_t>(word);
+    if (ballot(low > ~0u - P / 2)) {  // words on both sides of a multiple of 2^32
 #pragma unroll
-    for (int e = 0; e < P; e += 2) {
-      const uint32_t h = value_word(word + e / 2, keys);
-      x[e] = (h & 0xffffu) >= least ? x[e] * scale : 0.f;
-      x[e + 1] = (h >> 16) >= least ? x[e + 1] * scale : 0.f;
+      for (int e = 0; e < P; e += 2) choose(value_word(word + e / 2, keys), x + e);
+      return;
     }
+    // The upper half of a word's number is the same for all of them: one product.
+    StepKeys k = keys;
+    k.k1 += static_cast<uint32_t>(word >> 32) * kHighWord;
+#pragma unroll
+    for (int e = 0; e < P; e += 2) choose(value_word(low + e / 2, k), x + e);
+  }
+
+ private:
+  __device__ __forceinline__ void choose(uint32_t h, float* x) const {
+    x[0] = (h & 0xffffu) >= least ? x[0] * scale : 0.f;
+    x[1] = (h >> 16) >= least ? x[1] * scale : 0.f;
   }
 };
 

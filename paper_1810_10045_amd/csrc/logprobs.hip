@@ -7,10 +7,11 @@
 // The statistics are relative to m, not one number log sum e^(c x): l then keeps its
 // digits however far from zero a row lies.
 //
-// Forward: one pass over the logits, each lane with a running m, S and E (in base 2: one
-// v_exp_f32 a logit); HBM bounds it, the vector units come close behind. A row goes to one
-// workgroup; few rows are cut into parts, which k_logp_join puts together. Backward:
-// one pass that reads and writes each element once.
+// Forward: one pass over the logits, each lane with a running m, S and E in base 2. HBM bounds
+// it, the vector units come close behind: a logit takes 6.5 instructions and a v_exp_f32, which
+// has a quarter of their rate. A row goes to one workgroup; few rows are cut into parts,
+// which k_logp_join puts together. Backward: one pass that reads and writes each
+// element once.
 #include "launch_parts.hpp"
 #include "patch.hpp"
 
@@ -18,51 +19,71 @@ namespace lmz {
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 constexpr float kFarBelow = -1000.f;  // 2^this is 0
-constexpr int kTopKeys = 1024;        // candidates of a row's alternatives
+constexpr float kInf = __builtin_inff();
+constexpr int kTopKeys = 1024;  // candidates of a row's alternatives
 static_assert(LM_TOP_MAX == kWave, "a wave ranks the groups' maxima");
 
-// A row's sums so far, relative to its maximum so far (S, E 0 while that is -infinity).
+// The larger number; NaN if one of them is (v_maximum3_f32).
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_elementwise_maximum(a, b);
+}
+
+// A row's sums so far: its maximum m (NaN for good once it met one) and, with c = scale log2 e,
+//     s = sum 2^(c x - b),  e = sum 2^(c x - b) (c x - b)
+// relative to b, the fp32 number next to c m: then each exponent is one fma, and b's rounding
+// is known (slip) where the sums are used. Where c m is no number to subtract (masks of the
+// type's lowest value), they are relative to m itself: exponents c (x - m). s and e are 0
+// while m is -infinity.
 struct Sums {
   float m, s, e;
-  // The factor that takes sums relative to m to those relative to `to` >= m, and the
-  // difference of the two in base 2.
-  static __device__ __forceinline__ float shift(float m, float to, float c, float& by) {
-    const float a = m == -__builtin_inff() ? 0.f : m, b = to == -__builtin_inff() ? 0.f : to;
-    by = __builtin_fmaxf((a - b) * c, kFarBelow);  // (where m is, S and E are 0: by is finite)
-    by = m == -__builtin_inff() ? 0.f : by;
-    return __builtin_amdgcn_exp2f(by);
-  }
+  static __device__ __forceinline__ bool plain(float b) { return __builtin_fabsf(b) < 1e38f; }
+  // The sums relative to `to`, which is no less than m.
   __device__ __forceinline__ void rebase(float to, float c) {
-    float by;
-    const float f = shift(m, to, c, by);
+#pragma clang fp contract(off)  // the b of both are rounded numbers
+    float by = __builtin_fmaxf(m * c - to * c, kFarBelow);  // (infinity less itself: far below)
+    by = m == to || m == -kInf ? 0.f : by;
+    const float f = __builtin_amdgcn_exp2f(by);
     e = f * __builtin_fmaf(s, by, e);
     s *= f;
     m = to;
   }
   __device__ __forceinline__ void add(Sums o, float c) {
-    const float to = __builtin_fmaxf(m, o.m);
+    const float to = larger(m, o.m);
     rebase(to, c);
     o.rebase(to, c);
     s += o.s;
     e += o.e;
   }
+  // c m - b.
+  __device__ __forceinline__ float slip(float c) const {
+    const float b = m * c;
+    return plain(b) ? __builtin_fmaf(m, c, -b) : 0.f;
+  }
 };
 
-// N logits (masked ones -infinity). A NaN, and an infinite maximum, make S NaN for good.
+// N logits (masked ones -infinity).
 template <int N>
 __device__ __forceinline__ void add_logits(Sums& t, const float* x, float c) {
   float top = t.m;
 #pragma unroll
-  for (int i = 0; i < N; ++i) top = __builtin_fmaxf(top, x[i]);
+  for (int i = 0; i < N; ++i) top = larger(top, x[i]);
   t.rebase(top, c);
-  const float m = top == -__builtin_inff() ? 0.f : top;
+  const float b = top == -kInf ? 0.f : top * c;
   float s = 0.f, e = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float d = (x[i] - m) * c;
+  auto add = [&](float d) {
+    d = __builtin_fmaxf(d, kFarBelow);  // 0 times no infinity below
     const float p = __builtin_amdgcn_exp2f(d);
     s += p;
-    e = __builtin_fmaf(p, __builtin_fmaxf(d, kFarBelow), e);  // 0 times no infinity
+    e = __builtin_fmaf(p, d, e);
+  };
+  if (!ballot(!Sums::plain(b))) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) add(__builtin_fmaf(x[i], c, -b));
+  } else {
+    const float m = top == -kInf ? 0.f : top;
+    const bool ok = Sums::plain(b);
+#pragma unroll
+    for (int i = 0; i < N; ++i) add(ok ? __builtin_fmaf(x[i], c, -b) : (x[i] - m) * c);
   }
   t.s += s;
   t.e += e;
@@ -103,14 +124,25 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t x) {
   return x;
 }
 
+// Minimum of a wave's numbers (no NaN), in all lanes.
+__device__ __forceinline__ float wave_min(float x) {
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1)
+    x = __builtin_fminf(x, __shfl_xor(x, off, kWave));
+  return x;
+}
+
 // The k largest keys into t.top, 0 behind the last: `mine` is the largest of the thread's
-// logits, scan(f) calls f(logit, id) for all of them. Of the 64 maxima of groups of threads
-// the k-th is a bound that k logits reach; only threads that reach it look through their
-// logits again, and the few they find are ranked. Where more than kTopKeys reach the bound
-// (many equal logits), each key is found by a pass of its own.
-template <int THREADS, typename Scan>
-__device__ __forceinline__ void select_top(float mine, int k, TopSpace<THREADS>& t, Scan scan) {
+// logits, pick(want, f) and scan(f) call f(logit, id) for those of the threads that want it
+// and for all of them. Of the 64 maxima of groups of threads the k-th is a bound that k logits
+// reach; only threads that reach it look through their logits again, and the few they
+// find are ranked. Where more than kTopKeys reach the bound (many equal logits), each key is
+// found by a pass of its own.
+template <int THREADS, typename Pick, typename Scan>
+__device__ __forceinline__ void select_top(float mine, int k, TopSpace<THREADS>& t, Pick pick,
+                                           Scan scan) {
   const int tid = threadIdx.x, lane = lane_id();
+  mine = mine == mine ? mine : -kInf;  // (a NaN's row has no alternatives)
   t.best[tid] = mine;
   if (tid == 0) t.n = 0;
   if (tid < LM_TOP_MAX) t.top[tid] = 0;
@@ -121,26 +153,22 @@ __device__ __forceinline__ void select_top(float mine, int k, TopSpace<THREADS>&
     group = __builtin_fmaxf(group, t.best[lane + i * kWave]);
   int above = 0;
 #pragma unroll
-  for (int i = 0; i < kWave; ++i) {
-    const float x = read_lane(group, i);
-    above += x > group || (x == group && i < lane) ? 1 : 0;
-  }
-  const uint64_t at = ballot(above == k - 1);
-  const float bound = read_lane(group, at ? __builtin_ctzll(at) : 0);
-  if (mine >= bound && mine > -__builtin_inff()) {
-    scan([&](float x, uint32_t id) {
-      if (x >= bound && x > -__builtin_inff()) {
-        const int i = atomicAdd(&t.n, 1);
-        if (i < kTopKeys) t.keys[i] = key_of(x, id);
-      }
-    });
-  }
+  for (int i = 0; i < kWave; ++i) above += read_lane(group, i) > group ? 1 : 0;
+  // (fewer than k are above each of the k largest)
+  const float bound = wave_min(above < k ? group : kInf);
+  pick(mine >= bound && mine > -kInf, [&](float x, uint32_t id) {
+    if (x >= bound && x > -kInf) {
+      const int i = atomicAdd(&t.n, 1);
+      if (i < kTopKeys) t.keys[i] = key_of(x, id);
+    }
+  });
   __syncthreads();
   const int n = t.n;
   if (n <= kTopKeys) {
     for (int i = tid; i < n; i += THREADS) {
       const uint64_t key = t.keys[i];
       int rank = 0;
+#pragma unroll 4
       for (int j = 0; j < n; ++j) rank += t.keys[j] > key ? 1 : 0;
       if (rank < k) t.top[rank] = key;
     }
@@ -151,7 +179,7 @@ __device__ __forceinline__ void select_top(float mine, int k, TopSpace<THREADS>&
   for (int r = 0; r < k; ++r) {
     uint64_t best = 0;
     scan([&](float x, uint32_t id) {
-      if (!(x > -__builtin_inff())) return;
+      if (!(x > -kInf)) return;
       const uint64_t key = key_of(x, id);
       best = key < last && key > best ? key : best;
     });
@@ -175,65 +203,70 @@ struct LogpArgs {
   const void* targets;
   int64_t ignore;
   int wide;  // targets are int64
-  float scale, c;
+  float scale, c;  // c: scale log2 e, and how far it is off that, relative to it
+  float c_off;
   float *logp, *entropy, *peak, *log_sum, *top_logp;
   int32_t *top_ids, *dev_err;
   Sums* sums;      // [N][parts], where rows are cut
   uint64_t* keys;  // [N][parts][k]
 };
 
+// A row's target: whether it has one, its logit (NaN outside the vocabulary).
+struct Target {
+  bool any;
+  float x;
+};
+
 template <typename T>
-__device__ __forceinline__ float logit_at(const T* p) {
-  return Patch<T>::one(p);
+__device__ __forceinline__ Target target_of(const LogpArgs& a, int64_t row) {
+  if (!a.logp) return {false, 0.f};
+  const int64_t id = a.wide ? static_cast<const int64_t*>(a.targets)[row]
+                            : static_cast<const int32_t*>(a.targets)[row];
+  if (id == a.ignore) return {false, 0.f};
+  if (id < 0 || id >= a.V) {
+    if (threadIdx.x == 0) raise_err(a.dev_err, LM_DEVERR_ID_RANGE);
+    return {true, __builtin_nanf("")};
+  }
+  return {true, Patch<T>::one(static_cast<const T*>(a.logits) + row * a.ld + id)};
 }
 
 // What a row's sums and keys come to, by all of the workgroup's threads.
-template <typename T>
 __device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const Sums& t,
-                                           const uint64_t* top) {
-  const bool bad = !(t.s == t.s);  // a NaN or +infinity among the logits
+                                           const Target& target, const uint64_t* top) {
+  const bool bad = !(t.m < kInf);  // a NaN or +infinity among the logits
   const float nan = __builtin_nanf("");
-  const float log_sum = logf(t.s);
+  const float slip = t.slip(a.c), mean = t.e / t.s;
+  // s = 2^slip sum 2^(c (x - m)); c's own rounding moves its logarithm by the mean exponent.
+  const float log_sum = logf(t.s) - kLn2 * (slip + a.c_off * (mean - slip));
   if (threadIdx.x == 0) {
     if (a.logp) {
-      const int64_t id = a.wide ? static_cast<const int64_t*>(a.targets)[row]
-                                : static_cast<const int32_t*>(a.targets)[row];
-      float y = 0.f;
-      if (id != a.ignore) {
-        if (id < 0 || id >= a.V) {
-          raise_err(a.dev_err, LM_DEVERR_ID_RANGE);
-          y = nan;
-        } else {
-          const float x = logit_at(static_cast<const T*>(a.logits) + row * a.ld + id);
-          y = x == -__builtin_inff() ? x : (x - t.m) * a.scale - log_sum;
-          y = bad ? nan : y;
-        }
-      }
-      a.logp[row] = y;
+      const float x = target.x;
+      const float y = x == -kInf ? x : (x - t.m) * a.scale - log_sum;
+      a.logp[row] = target.any ? (bad ? nan : y) : 0.f;
     }
-    const float h = log_sum - kLn2 * (t.e / t.s);
+    const float h = logf(t.s) - kLn2 * mean;
     a.entropy[row] = bad ? nan : t.s == 0.f || h < 0.f ? 0.f : h;
     a.peak[row] = bad ? nan : t.m;
-    a.log_sum[row] = bad ? nan : log_sum;
+    a.log_sum[row] = bad ? nan : t.s == 0.f ? -kInf : log_sum;
   }
   for (int i = threadIdx.x; i < a.k; i += blockDim.x) {
     const uint64_t key = top[i];
     const bool any = key != 0 && !bad;
     a.top_ids[row * a.k + i] = any ? static_cast<int32_t>(key_id(key)) : -1;
     a.top_logp[row * a.k + i] =
-        bad ? nan : any ? (key_value(key) - t.m) * a.scale - log_sum : -__builtin_inff();
+        bad ? nan : any ? (key_value(key) - t.m) * a.scale - log_sum : -kInf;
   }
 }
 
 // The sums of the workgroup's threads, added in a fixed order, in all of them.
 template <int THREADS>
 __device__ __forceinline__ Sums join_sums(Sums t, float c, Sums (&lds)[THREADS / kWave]) {
+  float top = t.m;
 #pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const Sums o{__shfl_xor(t.m, off, kWave), __shfl_xor(t.s, off, kWave),
-                 __shfl_xor(t.e, off, kWave)};
-    t.add(o, c);
-  }
+  for (int off = 1; off < kWave; off <<= 1) top = larger(top, __shfl_xor(top, off, kWave));
+  t.rebase(top, c);
+  t.s = lanes_sum<kWave>(t.s);
+  t.e = lanes_sum<kWave>(t.e);
   if constexpr (THREADS > kWave) {
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = t;
     __syncthreads();
@@ -244,7 +277,7 @@ __device__ __forceinline__ Sums join_sums(Sums t, float c, Sums (&lds)[THREADS /
   return t;
 }
 
-template <typename T, int THREADS, bool TOP, bool NARROW>
+template <typename T, int THREADS, bool TOP, Ends ENDS>
 __global__ __launch_bounds__(THREADS) void k_logp(LogpArgs a, uint32_t first) {
   constexpr int P = Patch<T>::P, U = 4;
   using raw_t = typename Patch<T>::raw_t;
@@ -258,58 +291,79 @@ __global__ __launch_bounds__(THREADS) void k_logp(LogpArgs a, uint32_t first) {
   const int v0 = part * a.part_vectors;
   const int v1 = a.part_vectors < vectors - v0 ? v0 + a.part_vectors : vectors;
   const int w1 = whole < v1 ? whole : v1;  // whole vectors
-  // A vector at the row's end is loaded as its last P logits: those that belong to the
-  // vector before count as masked here.
-  auto load = [&](int v) { return Span<T, NARROW>(static_cast<int64_t>(v) * P, a.V, v < v1).load(x); };
+  Target target{false, 0.f};
+  if (a.parts == 1) target = target_of<T>(a, row);
+  // Vectors from number v1 on are loaded as the row's last one and count as masked.
+  auto span = [&](int v) { return Span<T, ENDS>(static_cast<int64_t>(v) * P, a.V, v < v1); };
   auto place = [&](int v, const raw_t& r, float* y) {
-    const Span<T, NARROW> s(static_cast<int64_t>(v) * P, a.V, v < v1);
+    const auto s = span(v);
     s.widen(r, y);
 #pragma unroll
-    for (int e = 0; e < P; ++e) y[e] = e < s.have ? y[e] : -__builtin_inff();
+    for (int e = 0; e < P; ++e) y[e] = e < s.have ? y[e] : -kInf;
   };
-  Sums t{-__builtin_inff(), 0.f, 0.f};
-  int v = v0 + threadIdx.x;
+  Sums t{-kInf, 0.f, 0.f};
   int base = v0;
-  if constexpr (!NARROW) {
-    for (; base + THREADS * U <= w1; base += THREADS * U, v += THREADS * U) {
+  if constexpr (ENDS != Ends::NARROW) {
+    for (; base + THREADS * U <= w1; base += THREADS * U) {
+      const T* at = x + static_cast<int64_t>(base) * P;
       raw_t r[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) r[u] = Patch<T>::load(x + static_cast<int64_t>(v + u * THREADS) * P);
+      for (int u = 0; u < U; ++u)
+        r[u] = Patch<T>::load(at + static_cast<uint32_t>(threadIdx.x + u * THREADS) * P);
       float y[U * P];
 #pragma unroll
       for (int u = 0; u < U; ++u) Patch<T>::widen(r[u], y + u * P);
       add_logits<U * P>(t, y, a.c);
     }
   }
-  for (; base < v1; base += THREADS * U, v += THREADS * U) {
+  if (base < v1) {  // fewer than U vectors a thread
     raw_t r[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) r[u] = load(v + u * THREADS);
-    float y[U * P];
+    for (int u = 0; u < U; ++u) r[u] = span(base + threadIdx.x + u * THREADS).load(x);
 #pragma unroll
-    for (int u = 0; u < U; ++u) place(v + u * THREADS, r[u], y + u * P);
-    add_logits<U * P>(t, y, a.c);
+    for (int u = 0; u < U; ++u) {
+      if (base + u * THREADS >= v1) break;
+      float y[P];
+      place(base + threadIdx.x + u * THREADS, r[u], y);
+      add_logits<P>(t, y, a.c);
+    }
   }
   const float mine = t.m;
   t = join_sums<THREADS>(t, a.c, lds);
   if constexpr (TOP) {
-    select_top<THREADS>(mine, a.k, space, [&](auto f) {
-      for (int i = v0 + threadIdx.x; i < v1; i += THREADS * U) {
-        raw_t r[U];
+    auto look = [&](int v, const raw_t& r, auto f) {
+      float y[P];
+      place(v, r, y);
 #pragma unroll
-        for (int u = 0; u < U; ++u) r[u] = load(i + u * THREADS);
+      for (int e = 0; e < P; ++e) f(y[e], static_cast<uint32_t>(v * P + e));
+    };
+    select_top<THREADS>(
+        mine, a.k, space,
+        // The wave's lanes share out one thread's vectors, U threads' at a time.
+        [&](bool want, auto f) {
+          const int from = v0 + static_cast<int>(threadIdx.x & ~(kWave - 1u)), lane = lane_id();
+          for (int i0 = 0; from + i0 * THREADS < v1; i0 += kWave) {
+            for (uint64_t todo = ballot(want); todo;) {
+              raw_t r[U];
+              int v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          float y[P];
-          place(i + u * THREADS, r[u], y);
+              for (int u = 0; u < U; ++u) {
+                v[u] = todo ? from + __builtin_ctzll(todo) + (i0 + lane) * THREADS : v1;
+                todo &= todo - 1;
+                r[u] = span(v[u]).load(x);
+              }
 #pragma unroll
-          for (int e = 0; e < P; ++e) f(y[e], static_cast<uint32_t>((i + u * THREADS) * P + e));
-        }
-      }
-    });
+              for (int u = 0; u < U; ++u)
+                if (v[u] < v1) look(v[u], r[u], f);
+            }
+          }
+        },
+        [&](auto f) {
+          for (int v = v0 + threadIdx.x; v < v1; v += THREADS) look(v, span(v).load(x), f);
+        });
   }
   if (a.parts == 1) {
-    finish_row<T>(a, row, t, space.top);
+    finish_row(a, row, t, target, space.top);
     return;
   }
   const int64_t at = row * a.parts + part;
@@ -327,21 +381,30 @@ __global__ __launch_bounds__(kJoinThreads) void k_logp_join(LogpArgs a, uint32_t
   __shared__ Sums lds[kJoinThreads / kWave];
   __shared__ std::conditional_t<TOP, TopSpace<kJoinThreads>, NoSpace> space;
   const int64_t row = first + static_cast<int64_t>(blockIdx.x);
-  Sums t{-__builtin_inff(), 0.f, 0.f};
+  const Target target = target_of<T>(a, row);
+  const uint64_t* keys = a.keys + row * a.parts * a.k;
+  const int n = a.parts * a.k;
+  float mine = -kInf;
+  if constexpr (TOP) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += kJoinThreads)
+      mine = keys[i] ? __builtin_fmaxf(mine, key_value(keys[i])) : mine;
+  }
+  Sums t{-kInf, 0.f, 0.f};
   for (int i = threadIdx.x; i < a.parts; i += kJoinThreads) t.add(a.sums[row * a.parts + i], a.c);
   t = join_sums<kJoinThreads>(t, a.c, lds);
   if constexpr (TOP) {
-    const uint64_t* keys = a.keys + row * a.parts * a.k;
-    const int n = a.parts * a.k;
-    float mine = -__builtin_inff();
-    for (int i = threadIdx.x; i < n; i += kJoinThreads)
-      mine = keys[i] ? __builtin_fmaxf(mine, key_value(keys[i])) : mine;
-    select_top<kJoinThreads>(mine, a.k, space, [&](auto f) {
+    auto scan = [&](auto f) {
       for (int i = threadIdx.x; i < n; i += kJoinThreads)
         if (keys[i]) f(key_value(keys[i]), key_id(keys[i]));
-    });
+    };
+    select_top<kJoinThreads>(mine, a.k, space,
+                             [&](bool want, auto f) {
+                               if (want) scan(f);
+                             },
+                             scan);
   }
-  finish_row<T>(a, row, t, space.top);
+  finish_row(a, row, t, target, space.top);
 }
 
 // ---------------------------------------------------------------------------
@@ -358,6 +421,7 @@ struct LogpGradArgs {
   const float *peak, *log_sum, *dlogp, *entropy, *dentropy;
   void* out;
   int64_t ld_out;
+  bool cached;
 };
 
 // A workgroup: kGradThreads / LANES rows, of each a tile of LANES * kGradVectors vectors.
@@ -382,7 +446,7 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int v = v0 + u * LANES;
-    r[u] = Span<T, NARROW>(static_cast<int64_t>(v) * P, a.V, v < vectors).load(x);
+    r[u] = Span<T, NARROW ? Ends::NARROW : Ends::PART>(static_cast<int64_t>(v) * P, a.V, v < vectors).load(x);
   }
   float dlogp = 0.f;
   int target = -1;
@@ -401,13 +465,13 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
     dentropy = a.dentropy[row] * a.scale;
   }
   // Nothing is left of the row, or nothing depends on it: zeros, whatever its logits are.
-  const bool none = peak == -__builtin_inff() || (dlogp == 0.f && dentropy == 0.f);
+  const bool none = peak == -kInf || (dlogp == 0.f && dentropy == 0.f);
   if (!live) return;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int v = v0 + u * LANES;
     if (v >= vectors) break;
-    const Span<T, NARROW> s(static_cast<int64_t>(v) * P, a.V);
+    const Span<T, NARROW ? Ends::NARROW : Ends::PART> s(static_cast<int64_t>(v) * P, a.V);
     float y[P];
     s.widen(r[u], y);
 #pragma unroll
@@ -427,13 +491,19 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
       d += v * P + e == target ? dlogp : 0.f;
       y[e] = none ? 0.f : d;
     }
-    s.store(out, y);
+    s.store(out, y, a.cached);
   }
 }
 
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+#ifndef LMZ_WG
+#define LMZ_WG 2048
+#endif
+#ifndef LMZ_ONE
+#define LMZ_ONE 1024
+#endif
 struct LogpPlan {
   int64_t parts, part_vectors;
 };
@@ -441,10 +511,11 @@ struct LogpPlan {
 static LogpPlan logp_plan(int64_t N, int64_t V, int dtype) {
   const int P = dtype == LM_BF16 ? Patch<bf16_t>::P : Patch<float>::P;
   const int64_t vectors = (V + P - 1) / P;
-  int64_t parts = N > 0 ? 1024 / N : 1;
-  const int64_t most = (vectors + 1023) / 1024;
-  parts = parts < 1 ? 1 : parts > most ? most : parts;
-  const int64_t each = (vectors + parts - 1) / parts;
+  if (N >= LMZ_WG || vectors <= LMZ_ONE) return {1, vectors};
+  // Vectors of a thread, so that about LMZ_WG workgroups have work.
+  int64_t each = N * vectors / (LMZ_WG * 256) + 1;
+  const int64_t parts = (vectors + each * 256 - 1) / (each * 256);
+  each = (vectors + parts - 1) / parts;
   return {(vectors + each - 1) / each, each};
 }
 
@@ -458,11 +529,20 @@ size_t logp_workspace_bytes(int64_t N, int64_t V, int dtype, int k) {
 template <typename T>
 static int logp_launch(const LogpArgs& a, hipStream_t st) {
   constexpr int P = Patch<T>::P;
-  const bool top = a.k > 0, narrow = a.V < P, few = a.V <= 256 * P;
+  const bool top = a.k > 0, few = a.V <= 256 * P;
   const int threads = few ? kWave : 256;
-  auto kernel = narrow ? (top ? k_logp<T, kWave, true, true> : k_logp<T, kWave, false, true>)
-                : few ? (top ? k_logp<T, kWave, true, false> : k_logp<T, kWave, false, false>)
-                      : (top ? k_logp<T, 256, true, false> : k_logp<T, 256, false, false>);
+  const Ends ends = ends_of(a.V, P);
+  auto pick = [&](auto w, auto e) {
+    return top ? k_logp<T, decltype(w)::value, true, decltype(e)::value>
+               : k_logp<T, decltype(w)::value, false, decltype(e)::value>;
+  };
+  using Few = std::integral_constant<int, kWave>;
+  using Many = std::integral_constant<int, 256>;
+  using Part = std::integral_constant<Ends, Ends::PART>;
+  using Narrow = std::integral_constant<Ends, Ends::NARROW>;
+  auto kernel = ends == Ends::NARROW ? pick(Few{}, Narrow{})
+                : few                ? pick(Few{}, Part{})
+                                     : pick(Many{}, Part{});
   const int rc = launch_parts(a.N * a.parts, threads, [&](uint32_t first, uint32_t n) {
     kernel<<<n, threads, 0, st>>>(a, first);
     return launch_status(hipGetLastError());
@@ -482,9 +562,11 @@ int logp_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtype, co
   if (N == 0) return LM_OK;
   const LogpPlan p = logp_plan(N, V, dtype);
   char* keys = ws ? static_cast<char*>(ws) + sums_bytes(N * p.parts) : nullptr;
+  const double log2e = 1.4426950408889634 * static_cast<double>(scale);
+  const float c = static_cast<float>(log2e);
   const LogpArgs a{logits, ld, N, static_cast<int>(V), static_cast<int>(p.parts),
-                   static_cast<int>(p.part_vectors), k, targets, ignore, idtype == LM_I64, scale,
-                   static_cast<float>(static_cast<double>(scale) * 1.4426950408889634),
+                   static_cast<int>(p.part_vectors), k, targets, ignore, idtype == LM_I64, scale, c,
+                   static_cast<float>(c / log2e - 1.0),
                    targets ? logp : nullptr, entropy, peak, log_sum, top_logp, top_ids, dev_err,
                    static_cast<Sums*>(ws),
                    reinterpret_cast<uint64_t*>(keys)};
@@ -529,7 +611,7 @@ int logp_grad_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtyp
   if (N == 0) return LM_OK;
   const LogpGradArgs a{logits, ld, N, static_cast<int>(V), 0, targets, ignore, idtype == LM_I64,
                        scale, peak, log_sum, targets ? dlogp : nullptr, entropy, dentropy, out,
-                       ld_out};
+                       ld_out, cached_bytes(N, V * (dtype == LM_BF16 ? 2 : 4))};
   return dtype == LM_BF16 ? grad_lanes<bf16_t>(a, st) : grad_lanes<float>(a, st);
 }
 

@@ -58,10 +58,12 @@ __host__ __device__ static inline StepKeys step_keys(uint64_t seed) {
 // multipliers here and above are published ones, known to mix well: three primes of Y.
 // Collet's 32-bit hash (2012), 2^64 over the golden ratio (Knuth) and that of a published
 // 64-bit mixer (0xD6E8FEB86659FD93); the rounds are this file's.
+constexpr uint32_t kHighWord = 0x85EBCA77u;
+
 __device__ __forceinline__ uint32_t value_word(uint64_t e, const StepKeys& k) {
   uint32_t h = (static_cast<uint32_t>(e) ^ k.k0) * 0x9E3779B1u;
   h ^= h >> 15;
-  h = (h + k.k1 + static_cast<uint32_t>(e >> 32) * 0x85EBCA77u) * 0xC2B2AE3Du;
+  h = (h + k.k1 + static_cast<uint32_t>(e >> 32) * kHighWord) * 0xC2B2AE3Du;
   return h ^ (h >> 16);
 }
 

@@ -19,25 +19,36 @@ struct NormGradArgs {
   int D;
   float inv_d;
   KeepArgs keep;
+  bool cached;
 };
 
-// Rows of a group that are under way at once.
-template <typename S>
-constexpr int kBatch = S::NV >= 4 ? 1 : S::NV >= 2 ? 2 : 4;
+// Rows of a group, all of their loads under way at once.
+template <typename T, typename S>
+constexpr int kBatch = S::NV * Patch<T>::P > 8 ? 1 : 2;
 
-template <typename T, typename S, bool ADD, bool NARROW>
+// The value of an operand that is kept as it was loaded, and not widened, between its uses.
+__device__ __forceinline__ f32x4 kept(f32x4 x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ u32x4 kept(u32x4 x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+template <typename T, typename S, bool ADD, Ends ENDS>
 __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
-  constexpr int P = Patch<T>::P, NV = S::NV, R = kBatch<S>;
+  constexpr int P = Patch<T>::P, NV = S::NV, R = kBatch<T, S>;
   constexpr int kWaves = S::kThreads / kWave;
   using raw_t = typename Patch<T>::raw_t;
   __shared__ float part[2][kWaves][2 * R];
-  const int group = threadIdx.x / S::kGroup, lane = threadIdx.x % S::kGroup;
+  const int group = S::group(), lane = threadIdx.x % S::kGroup;
   const Keep keep(a.keep);
   const uint64_t pairs = static_cast<uint64_t>(a.D + 1) / 2;
   float w[NV][P], dw[NV][P], db[NV][P];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const Span<T, NARROW> s((lane + v * S::kGroup) * P, a.D);
+    const NormSpan<T, ENDS> s((lane + v * S::kGroup) * P, a.D);
     if (a.weight) load_params(a.weight, s, w[v]);
 #pragma unroll
     for (int e = 0; e < P; ++e) {
@@ -57,34 +68,44 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
       rstd[r] = a.rstd[row];
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const Span<T, NARROW> s((lane + v * S::kGroup) * P, a.D);
+        const NormSpan<T, ENDS> s((lane + v * S::kGroup) * P, a.D);
         ry[r][v] = s.load(static_cast<const T*>(a.dy) + row * a.ld_dy);
         rh[r][v] = s.load(static_cast<const T*>(a.h) + row * a.ld_h);
         if constexpr (ADD) ra[r][v] = s.load(static_cast<const T*>(a.add) + row * a.ld_add);
       }
     }
+    // A row behind the last one has only zeros, so it adds nothing.
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (i0 + group * R + r < a.rows) continue;
+      mean[r] = rstd[r] = 0.f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) ry[r][v] = rh[r][v] = raw_t{0, 0, 0, 0};
+    }
     float sums[2 * R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const bool live = i0 + group * R + r < a.rows;
       float g0 = 0.f, g1 = 0.f;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const Span<T, NARROW> s((lane + v * S::kGroup) * P, a.D, live);
-        const Span<T, NARROW> at((lane + v * S::kGroup) * P, a.D);
+        const NormSpan<T, ENDS> s((lane + v * S::kGroup) * P, a.D);
         float y[P], n[P];
-        at.widen(ry[r][v], y);
-        at.widen(rh[r][v], n);
+        s.widen(ry[r][v], y);  // zeros behind the row's end
+        s.widen(rh[r][v], n);
 #pragma unroll
         for (int e = 0; e < P; ++e) {
           n[e] = (n[e] - mean[r]) * rstd[r];
           const float g = y[e] * w[v][e];
-          const bool in = e < s.have;
-          g0 += in ? g : 0.f;
-          g1 = in ? __builtin_fmaf(g, n[e], g1) : g1;
-          dw[v][e] = in ? __builtin_fmaf(y[e], n[e], dw[v][e]) : dw[v][e];
-          db[v][e] += in ? y[e] : 0.f;
+          g0 += g;
+          g1 = __builtin_fmaf(g, n[e], g1);
+          dw[v][e] = __builtin_fmaf(y[e], n[e], dw[v][e]);
+          db[v][e] += y[e];
+          // added here, not at the turn's end with every row's y and n waiting for it
+          asm volatile("" : "+v"(dw[v][e]), "+v"(db[v][e]));
         }
+        ry[r][v] = kept(ry[r][v]);
+        rh[r][v] = kept(rh[r][v]);
+        __builtin_amdgcn_sched_barrier(0);
       }
       sums[2 * r] = g0;
       sums[2 * r + 1] = g1;
@@ -98,7 +119,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
       const float e0 = sums[2 * r] * a.inv_d, e1 = sums[2 * r + 1] * a.inv_d;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const Span<T, NARROW> s((lane + v * S::kGroup) * P, a.D);
+        const NormSpan<T, ENDS> s((lane + v * S::kGroup) * P, a.D);
         float y[P], n[P], z[P];
         s.widen(ry[r][v], y);
         s.widen(rh[r][v], n);
@@ -109,11 +130,12 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
           const float d = (y[e] * w[v][e] - e0) - n[e] * e1;
           y[e] = __builtin_fmaf(rstd[r], d, ADD ? z[e] : 0.f);
         }
-        s.store(static_cast<T*>(a.dh) + row * a.ld_dh, y);
+        s.store(static_cast<T*>(a.dh) + row * a.ld_dh, y, a.cached);
         if (a.dx) {
           keep.apply<P>(static_cast<uint64_t>(row) * pairs + (lane + v * S::kGroup) * (P / 2), y);
-          s.store(static_cast<T*>(a.dx) + row * a.ld_dx, y);
+          s.store(static_cast<T*>(a.dx) + row * a.ld_dx, y, a.cached);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
@@ -128,7 +150,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
     if (k && kGroups > 1) __syncthreads();
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const Span<T, NARROW> s((lane + v * S::kGroup) * P, a.D);
+      const NormSpan<T, ENDS> s((lane + v * S::kGroup) * P, a.D);
 #pragma unroll
       for (int e = 0; e < P; ++e) {
         float x = k ? db[v][e] : dw[v][e];
@@ -154,42 +176,78 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
   }
 }
 
-// dweight and dbias (+)= the workgroups' sums, 64 columns of the two a workgroup: a wave
-// adds every kJoinWaves-th row, the waves are added in their order.
-constexpr int kJoinWaves = 16;
+// dweight and dbias (+)= the workgroups' sums, kJoinCols columns of the two a workgroup:
+// kJoinRows threads share a column's parts, their sums are added in a fixed order.
+constexpr int kJoinThreads = 1024, kJoinCols = 16, kJoinRows = kJoinThreads / kJoinCols;
+constexpr int kJoinWaves = kJoinThreads / kWave;
 
-__global__ __launch_bounds__(kJoinWaves* kWave) void k_norm_join(const float* sums, int parts,
-                                                                 int D, float* dweight,
-                                                                 float* dbias, int accumulate) {
-  __shared__ float lds[kJoinWaves][kWave];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int c = blockIdx.x * kWave + lane;
+__global__ __launch_bounds__(kJoinThreads) void k_norm_join(const float* sums, int parts, int D,
+                                                            float* dweight, float* dbias,
+                                                            int accumulate) {
+  __shared__ float lds[kJoinWaves][kJoinCols];
+  const int col = threadIdx.x % kJoinCols, wave = threadIdx.x / kWave;
+  const int c = blockIdx.x * kJoinCols + col;
   const float* at = sums + (c < 2 * D ? c : 0);
   float x = 0.f;
 #pragma unroll 8
-  for (int g = wave; g < parts; g += kJoinWaves) x += at[static_cast<int64_t>(g) * 2 * D];
-  lds[wave][lane] = x;
+  for (int g = threadIdx.x / kJoinCols; g < parts; g += kJoinRows)
+    x += at[static_cast<int64_t>(g) * 2 * D];
+#pragma unroll
+  for (int off = kJoinCols; off < kWave; off *= 2) x += __shfl_xor(x, off, kWave);
+  if (threadIdx.x % kWave < kJoinCols) lds[wave][col] = x;
   __syncthreads();
-  if (wave || c >= 2 * D) return;
+  if (threadIdx.x >= kJoinCols || c >= 2 * D) return;
   float y = 0.f;
 #pragma unroll
-  for (int w = 0; w < kJoinWaves; ++w) y += lds[w][lane];
+  for (int w = 0; w < kJoinWaves; ++w) y += lds[w][col];
   float* out = c < D ? dweight : dbias;
   if (!out) return;
   out += c < D ? c : c - D;
   *out = accumulate ? *out + y : y;
 }
 
-constexpr int kNormGradBlocks = 512;  // two on each compute unit
+// Calls f with the shape for rows of D values of type T, in workgroups of THREADS.
+template <typename T, int THREADS, typename F>
+static inline int grad_shape(int64_t D, F f) {
+  constexpr int P = Patch<T>::P;
+  const int64_t vectors = (D + P - 1) / P;
+  if (vectors <= 8) return f(NormShape<8, 1, 1, THREADS>{});
+  if (vectors <= 16) return f(NormShape<16, 1, 1, THREADS>{});
+  if (vectors <= 32) return f(NormShape<32, 1, 1, THREADS>{});
+  if (vectors <= 64) return f(NormShape<64, 1, 1, THREADS>{});
+  if (D <= 512) return f(NormShape<64, 1, 8 / P, THREADS>{});
+  if (D <= 1024) return f(NormShape<64, 2, 8 / P, THREADS>{});
+  if (D <= 2048) return f(NormShape<64, 4, 8 / P, THREADS>{});
+  if (D <= 4096) return f(NormShape<64, 4, 16 / P, THREADS>{});
+  if (D <= 8192) return f(NormShape<64, 8, 16 / P, THREADS>{});
+  static_assert(LM_NORM_MAX_WIDTH == 16384, "the widest shape");
+  return f(NormShape<64, 16, 16 / P, THREADS>{});
+}
 
-// Workgroups of the pass.
-static int64_t norm_grad_blocks(int64_t rows, int64_t D, int dtype) {
-  auto blocks = [&](auto shape) {
+// Workgroups of the pass, at most kGradBlocks: each leaves 2 D sums behind, so that fewer and
+// larger ones cost less where every one has but a turn or two: 1280 x 1792 fp32 takes 12.4 us
+// with 160 of 1024 threads, 14.4 with 320 of 512 (16,384 x 1000 fp32 44 and 41).
+constexpr int64_t kGradBlocks = 512;
+
+template <typename T, typename F>
+static inline int norm_grad_shape(int64_t rows, int64_t D, F f) {
+  const bool few = grad_shape<T, 512>(D, [&](auto shape) {
     using S = decltype(shape);
-    const int64_t n = (rows + S::kRows * kBatch<S> - 1) / (S::kRows * kBatch<S>);
-    return static_cast<int>(n < kNormGradBlocks ? n : kNormGradBlocks);
-  };
-  return dtype == LM_BF16 ? norm_shape<bf16_t>(D, blocks) : norm_shape<float>(D, blocks);
+    return rows <= kGradBlocks * S::kRows * kBatch<T, S> ? 1 : 0;
+  });
+  return few ? grad_shape<T, 1024>(D, f) : grad_shape<T, 512>(D, f);
+}
+
+template <typename T>
+static int64_t grad_blocks(int64_t rows, int64_t D) {
+  return norm_grad_shape<T>(rows, D, [&](auto shape) {
+    using S = decltype(shape);
+    const int64_t n = (rows + S::kRows * kBatch<T, S> - 1) / (S::kRows * kBatch<T, S>);
+    return static_cast<int>(n < kGradBlocks ? n : kGradBlocks);
+  });
+}
+static int64_t norm_grad_blocks(int64_t rows, int64_t D, int dtype) {
+  return dtype == LM_BF16 ? grad_blocks<bf16_t>(rows, D) : grad_blocks<float>(rows, D);
 }
 
 size_t norm_grad_workspace_bytes(int64_t rows, int64_t D, int dtype) {
@@ -198,12 +256,11 @@ size_t norm_grad_workspace_bytes(int64_t rows, int64_t D, int dtype) {
 
 template <typename T>
 static int norm_grad_launch(const NormGradArgs& a, int blocks, hipStream_t st) {
-  return norm_shape<T>(a.D, [&](auto shape) {
+  return norm_grad_shape<T>(a.rows, a.D, [&](auto shape) {
     using S = decltype(shape);
-    auto kernel = a.add ? k_norm_grad<T, S, true, false> : k_norm_grad<T, S, false, false>;
-    if constexpr (S::kGroup == 8)
-      if (a.D < Patch<T>::P)
-        kernel = a.add ? k_norm_grad<T, S, true, true> : k_norm_grad<T, S, false, true>;
+    auto kernel = norm_ends<S>(ends_of(a.D, Patch<T>::P), [&](auto ends) {
+      return a.add ? k_norm_grad<T, S, true, decltype(ends)::value> : k_norm_grad<T, S, false, decltype(ends)::value>;
+    });
     kernel<<<blocks, S::kThreads, 0, st>>>(a);
     return launch_status(hipGetLastError());
   });
@@ -221,14 +278,15 @@ int norm_grad_run(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, co
                          sums ? static_cast<float*>(ws) : nullptr, ld_dy, ld_h, ld_add, ld_dh,
                          ld_dx, rows, static_cast<int>(D),
                          static_cast<float>(1.0 / static_cast<double>(D)),
-                         make_keep(p, seed, seed_at)};
+                         make_keep(p, seed, seed_at),
+                         cached_bytes(rows, D * (dtype == LM_BF16 ? 2 : 4) * (dx ? 2 : 1))};
     const int rc = dtype == LM_BF16 ? norm_grad_launch<bf16_t>(a, blocks, st)
                                     : norm_grad_launch<float>(a, blocks, st);
     if (rc != LM_OK) return rc;
   }
   if (!sums) return LM_OK;
   const int cols = static_cast<int>(2 * D);
-  k_norm_join<<<(cols + kWave - 1) / kWave, kJoinWaves * kWave, 0, st>>>(
+  k_norm_join<<<(cols + kJoinCols - 1) / kJoinCols, kJoinThreads, 0, st>>>(
       static_cast<const float*>(ws), blocks, static_cast<int>(D), dweight, dbias, accumulate);
   return launch_status(hipGetLastError());
 }

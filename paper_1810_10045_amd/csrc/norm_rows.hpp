@@ -1,5 +1,4 @@
 // Layer norm: how a row is shared out among lanes, for the forward and the backward pass.
-//
 // A row stays in the registers of its group: LANES lanes of a wave, or WAVES whole waves,
 // NV vectors of 16 bytes a lane, vector v of lane l being number l + v * lanes (a wave's
 // lanes load neighbouring vectors).
@@ -12,14 +11,23 @@ namespace lmz {
 
 constexpr int kNormThreads = 256;  // of a workgroup, where a row's group is no larger
 
-template <int LANES_, int WAVES_, int NV_>
+template <int LANES_, int WAVES_, int NV_, int THREADS_ = kNormThreads>
 struct NormShape {
   static constexpr int LANES = LANES_, WAVES = WAVES_, NV = NV_;
   static constexpr int kGroup = WAVES > 1 ? WAVES * kWave : LANES;  // lanes of a row
-  static constexpr int kThreads = kGroup > kNormThreads ? kGroup : kNormThreads;
+  static constexpr int kThreads = kGroup > THREADS_ ? kGroup : THREADS_;
   static constexpr int kRows = kThreads / kGroup;  // rows of a workgroup at once
   static_assert(WAVES == 1 || LANES == kWave, "whole waves");
+  // The thread's group in its workgroup, in a scalar register where a wave has but one.
+  static __device__ __forceinline__ int group() {
+    if constexpr (kRows == 1) return 0;
+    const int g = threadIdx.x / kGroup;
+    return kGroup >= kWave ? first_lane(g) : g;
+  }
 };
+
+template <typename T, Ends ENDS>
+using NormSpan = Span<T, ENDS, uint32_t>;  // LM_NORM_MAX_WIDTH columns
 
 // Sums over a row's group: of the lanes by lanes_sum, of the waves in their order. A
 // group of several waves meets in LDS, every wave of the workgroup with it; calls that follow
@@ -46,10 +54,12 @@ __device__ __forceinline__ void group_sums(float (&x)[N], float (*lds)[N]) {
 }
 
 // P fp32 parameters of columns `s` (a weight or bias), zeros behind a row's end.
-template <typename T, bool NARROW>
-__device__ __forceinline__ void load_params(const float* w, const Span<T, NARROW>& s, float* x) {
+template <typename T, Ends ENDS>
+__device__ __forceinline__ void load_params(const float* w, const NormSpan<T, ENDS>& s, float* x) {
   constexpr int P = Patch<T>::P;
-  if (NARROW || s.have < P) {
+  if (ENDS == Ends::WHOLE) {
+    load_vec<P>(Span<float, ENDS, uint32_t>::at(w, s.have ? s.from : 0), x);
+  } else if (ENDS == Ends::NARROW || s.have < P) {
 #pragma unroll
     for (int e = 0; e < P; ++e) {
       const int at = e < s.have ? e : 0;
@@ -57,25 +67,18 @@ __device__ __forceinline__ void load_params(const float* w, const Span<T, NARROW
       x[e] = e < s.have ? y : 0.f;
     }
   } else {
-    load_vec<P>(w + s.from, x);
+    load_vec<P>(Span<float, ENDS, uint32_t>::at(w, s.from), x);
   }
 }
 
-// Calls f with the shape for rows of D values of type T.
-template <typename T, typename F>
-static inline int norm_shape(int64_t D, F f) {
-  const int64_t vectors = (D + Patch<T>::P - 1) / Patch<T>::P;
-  if (vectors <= 8) return f(NormShape<8, 1, 1>{});
-  if (vectors <= 16) return f(NormShape<16, 1, 1>{});
-  if (vectors <= 32) return f(NormShape<32, 1, 1>{});
-  if (vectors <= 64) return f(NormShape<64, 1, 1>{});
-  if (vectors <= 128) return f(NormShape<64, 2, 1>{});
-  if (vectors <= 256) return f(NormShape<64, 4, 1>{});
-  if (vectors <= 512) return f(NormShape<64, 4, 2>{});
-  if (vectors <= 1024) return f(NormShape<64, 8, 2>{});
-  if (vectors <= 2048) return f(NormShape<64, 16, 2>{});
-  return f(NormShape<64, 16, 4>{});
+// A kernel's forms by how rows end: pick(form) with the End as a constant. Rows of less than
+// a vector have the smallest group.
+template <typename S, typename F>
+static inline auto norm_ends(Ends ends, F pick) {
+  if constexpr (S::kGroup == 8)
+    if (ends == Ends::NARROW) return pick(std::integral_constant<Ends, Ends::NARROW>{});
+  return ends == Ends::WHOLE ? pick(std::integral_constant<Ends, Ends::WHOLE>{})
+                             : pick(std::integral_constant<Ends, Ends::PART>{});
 }
-static_assert(LM_NORM_MAX_WIDTH <= 4 * 16 * kWave * Patch<float>::P, "the widest shape");
 
 }  // namespace lmz

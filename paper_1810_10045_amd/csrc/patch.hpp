@@ -35,6 +35,10 @@ struct Patch<float> {
   static __device__ __forceinline__ void store(float* p, const float* x) {
     __builtin_nontemporal_store(f32x4e{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4e*>(p));
   }
+  // The same through the caches.
+  static __device__ __forceinline__ void keep(float* p, const float* x) {
+    *reinterpret_cast<f32x4e*>(p) = f32x4e{x[0], x[1], x[2], x[3]};
+  }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
   static __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 };
@@ -72,30 +76,61 @@ struct Patch<bf16_t> {
     const raw_t w = pack(x);
     __builtin_nontemporal_store(u32x4e{w.x, w.y, w.z, w.w}, reinterpret_cast<u32x4e*>(p));
   }
+  static __device__ __forceinline__ void keep(bf16_t* p, const float* x) {
+    const raw_t w = pack(x);
+    *reinterpret_cast<u32x4e*>(p) = u32x4e{w.x, w.y, w.z, w.w};
+  }
   static __device__ __forceinline__ float one(const bf16_t* p) { return bf16_to_f32(p->bits); }
   static __device__ __forceinline__ void put(bf16_t* p, float x) {
     p->bits = static_cast<uint16_t>(bits(x));
   }
 };
 
-// Where a lane's vector of P values at column `col` lies in a row of D >= P values (fewer:
-// NARROW, loaded one value at a time). Every load is a whole vector inside the row, so
+// Whether results of rows of so many bytes are written through the caches (others past them). The
+// memory-side cache holds 256 MiB: what fits in it is still there for the next call that
+// reads it. Dropout on 2048 bf16 columns, its output the next call's input, 256 MiB each: 6.6
+// TB/s, past the caches 6.1; 64 MiB: 6.1 and 5.6; 384 MiB: 5.7 and 6.2. What fits in the
+// L2 caches would stay there until they are written back at the kernel's end: 16 MiB 4.1 and
+// 4.6. (Where nothing reads the outputs again, 256 MiB: 5.9 and 6.1.)
+static inline bool cached_bytes(int64_t rows, int64_t bytes) {
+  const double n = static_cast<double>(rows) * static_cast<double>(bytes);
+  return n > 32 << 20 && n <= 256 << 20;
+}
+
+// How rows end: every one in whole vectors of P values, in a part of one, or they hold fewer
+// than P (and are loaded one value at a time).
+enum class Ends { WHOLE, PART, NARROW };
+
+static inline Ends ends_of(int64_t D, int P) {
+  return D < P ? Ends::NARROW : D % P ? Ends::PART : Ends::WHOLE;
+}
+
+// Where a lane's vector of P values at column `col` lies in a row of D. Every load is a whole vector inside the row, so
 // that none stands under a condition: at the row's end it starts at D - P, and the values
-// are moved `by` places down to their own. `have`: how many of them exist.
-template <typename T, bool NARROW>
+// are moved `by` places down to their own. `have`: how many of them exist. OFF: what holds
+// a column's distance from the row's start in bytes (with uint32_t and a row that the wave
+// shares, an address is that distance in one register beside the row's in scalar ones).
+template <typename T, Ends ENDS, typename OFF = int64_t>
 struct Span {
   static constexpr int P = Patch<T>::P;
+  static constexpr bool NARROW = ENDS == Ends::NARROW;
   using raw_t = typename Patch<T>::raw_t;
-  int64_t from;
+  using index_t = std::conditional_t<sizeof(OFF) == 4, int, int64_t>;
+  index_t from;
   int by, have;
-  __device__ __forceinline__ Span(int64_t col, int64_t D, bool use = true) {
-    const int64_t left = use ? D - col : 0;
+  __device__ __forceinline__ Span(index_t col, index_t D, bool use = true) {
+    const index_t left = use ? D - col : 0;
     have = left >= P ? P : left > 0 ? static_cast<int>(left) : 0;
     by = NARROW ? 0 : P - have;
     from = NARROW ? 0 : left >= P ? col : D - P;
   }
+  template <typename Q>  // T or const T
+  static __device__ __forceinline__ Q* at(Q* row, index_t col) {
+    using byte_t = std::conditional_t<std::is_const<Q>::value, const char, char>;
+    return reinterpret_cast<Q*>(reinterpret_cast<byte_t*>(row) + static_cast<OFF>(col * static_cast<index_t>(sizeof(T))));
+  }
   __device__ __forceinline__ raw_t load(const T* row) const {
-    if constexpr (!NARROW) return Patch<T>::load(row + from);
+    if constexpr (!NARROW) return Patch<T>::load(at(row, from));
     float x[P];
 #pragma unroll
     for (int e = 0; e < P; ++e) x[e] = e < have ? Patch<T>::one(row + e) : 0.f;
@@ -103,17 +138,28 @@ struct Span {
   }
   // The values in their places, zeros behind them.
   __device__ __forceinline__ void widen(raw_t r, float* x) const {
-    if (!NARROW && by) r = Patch<T>::shift(r, by);
+    if (ENDS == Ends::WHOLE) {
+      r = have ? r : raw_t{0, 0, 0, 0};
+    } else if (ENDS == Ends::PART && by) {
+      r = Patch<T>::shift(r, by);
+    }
     Patch<T>::widen(r, x);
   }
-  __device__ __forceinline__ void store(T* row, const float* x) const {
+  __device__ __forceinline__ void store(T* row, const float* x, bool cached) const {
     if (have == P) {
-      Patch<T>::store(row + from, x);
-    } else {
-      const int64_t col = NARROW ? 0 : from + by;
+      // (the empty statements keep the two apart: made one store, they would lose the hint)
+      if (cached) {
+        asm volatile("");
+        Patch<T>::keep(at(row, from), x);
+        asm volatile("");
+      } else {
+        Patch<T>::store(at(row, from), x);
+      }
+    } else if (ENDS != Ends::WHOLE) {
+      T* p = at(row, NARROW ? 0 : from + by);
 #pragma unroll
       for (int e = 0; e < P - 1; ++e)
-        if (e < have) Patch<T>::put(row + col + e, x[e]);
+        if (e < have) Patch<T>::put(p + e, x[e]);
     }
   }
 };

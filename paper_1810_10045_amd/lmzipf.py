@@ -999,9 +999,18 @@ def _like(t: Optional[torch.Tensor], x: torch.Tensor, what: str):
     """The row stride of an operand of x's shape and dtype (None: 0)."""
     if t is None:
         return 0
-    if t.shape != x.shape or t.dtype != x.dtype:
-        raise LmError(f"{what} must be {' x '.join(map(str, x.shape))} of {x.dtype}")
-    return _matrix(t, what)[2]
+    shape = x.shape
+    if t.shape != shape or t.dtype != x.dtype:
+        raise LmError(f"{what} must be {' x '.join(map(str, shape))} of {x.dtype}")
+    return shape[-1] if t.is_contiguous() else _matrix(t, what)[2]
+
+
+def _new(x: torch.Tensor, stream):
+    """A contiguous tensor of x's shape and dtype (torch.empty_like takes half the time of
+    torch.empty, which a call of a few rows is made of)."""
+    if stream is None and x.is_contiguous():
+        return torch.empty_like(x)
+    return _empty(x.shape, x.dtype, x.device, stream)
 
 
 def _vector(t: Optional[torch.Tensor], n: int, what: str):
@@ -1037,11 +1046,13 @@ def dropout(x: torch.Tensor, p: float, seed, add: Optional[torch.Tensor] = None,
     if _elsewhere(device, stream):
         with torch.cuda.device(device):
             return dropout(x, p, seed, add, out, stream)
-    ld_add = _like(add, x, "add")
+    ld_add, ld_out = _like(add, x, "add"), D
     given = out
     if out is None:
-        out = _empty(x.shape, x.dtype, device, stream)
-    _call(_lib.lm_dropout(_ptr(x), ld, _ptr(add), ld_add, _ptr(out), _like(out, x, "out"), rows, D,
+        out = _new(x, stream)
+    else:
+        ld_out = _like(out, x, "out")
+    _call(_lib.lm_dropout(x.data_ptr(), ld, _ptr(add), ld_add, out.data_ptr(), ld_out, rows, D,
                           dtype, p, number, at, _on(device, stream)), "lm_dropout")
     if given is not None:
         _written(given)
@@ -1081,20 +1092,25 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
     if _elsewhere(device, stream):
         with torch.cuda.device(device):
             return layer_norm(x, weight, bias, eps, add, p, seed, out, sum_out, stream)
-    ld_add = _like(add, x, "add")
-    given = [t for t in (out, sum_out) if t is not None]
-    if sum_out is None and (add is not None or p > 0):
-        sum_out = _empty(x.shape, x.dtype, device, stream)
+    ld_add, ld_y, ld_h, h = _like(add, x, "add"), D, D, sum_out
     if out is None:
-        out = _empty(x.shape, x.dtype, device, stream)
+        y = _new(x, stream)
+    else:
+        y, ld_y = out, _like(out, x, "out")
+    if sum_out is not None:
+        ld_h = _like(sum_out, x, "sum_out")
+    elif add is not None or p > 0:
+        h = _new(x, stream)
     mean, rstd = _empty((2, *x.shape[:-1]), torch.float32, device, stream).unbind()
     _call(_lib.lm_layer_norm(
-        _ptr(x), ld, _ptr(add), ld_add, rows, D, dtype, _ptr(weight), _ptr(bias), eps, p, number, at,
-        _ptr(out), _like(out, x, "out"), _ptr(sum_out), _like(sum_out, x, "sum_out"), _ptr(mean),
-        _ptr(rstd), _on(device, stream)), "lm_layer_norm")
-    for t in given:
-        _written(t)
-    return NormResult(out, x if sum_out is None else sum_out, mean, rstd)
+        x.data_ptr(), ld, _ptr(add), ld_add, rows, D, dtype, _ptr(weight), _ptr(bias), eps, p,
+        number, at, y.data_ptr(), ld_y, _ptr(h), ld_h, mean.data_ptr(), rstd.data_ptr(),
+        _on(device, stream)), "lm_layer_norm")
+    if out is not None:
+        _written(out)
+    if sum_out is not None:
+        _written(sum_out)
+    return NormResult(y, x if h is None else h, mean, rstd)
 
 
 class NormGrad(NamedTuple):
@@ -1143,9 +1159,9 @@ def layer_norm_grad(dy: torch.Tensor, h: torch.Tensor, mean: torch.Tensor, rstd:
     ld_h, ld_add = _like(h, dy, "h"), _like(add, dy, "add")
     given = [t for t in (out, dx, dweight, dbias) if t is not None]
     if out is None:
-        out = _empty(dy.shape, dy.dtype, device, stream)
+        out = _new(dy, stream)
     if dx is None and p > 0:
-        dx = _empty(dy.shape, dy.dtype, device, stream)
+        dx = _new(dy, stream)
     if new:
         fresh = list(_empty((new, D), torch.float32, device, stream).unbind())
         dweight = fresh.pop(0) if dweight is None and weight is not None else dweight
@@ -1261,7 +1277,7 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor],
                                        scale, ignore, out, stream)
     given = out
     if out is None:
-        out = _empty(logits.shape, logits.dtype, device, stream)
+        out = _new(logits, stream)
     _call(_lib.lm_token_logprobs_grad(
         _ptr(logits), ld, N, V, dtype, _ptr(targets), idtype, ignore, scale, _ptr(peak),
         _ptr(log_sum), _ptr(dlogp), _ptr(entropy), _ptr(dentropy), _ptr(out),
