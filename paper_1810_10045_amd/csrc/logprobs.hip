@@ -61,14 +61,10 @@ struct Sums {
   }
 };
 
-// N logits (masked ones -infinity).
+// N logits (masked ones -infinity), none above t.m.
 template <int N>
-__device__ __forceinline__ void add_logits(Sums& t, const float* x, float c) {
-  float top = t.m;
-#pragma unroll
-  for (int i = 0; i < N; ++i) top = larger(top, x[i]);
-  t.rebase(top, c);
-  const float b = top == -kInf ? 0.f : top * c;
+__device__ __forceinline__ void sum_logits(Sums& t, const float* x, float c) {
+  const float m = t.m == -kInf ? 0.f : t.m, b = m * c;
   float s = 0.f, e = 0.f;
   auto add = [&](float d) {
     d = __builtin_fmaxf(d, kFarBelow);  // 0 times no infinity below
@@ -76,17 +72,26 @@ __device__ __forceinline__ void add_logits(Sums& t, const float* x, float c) {
     s += p;
     e = __builtin_fmaf(p, d, e);
   };
-  if (!ballot(!Sums::plain(b))) {
+  const bool ok = Sums::plain(b);
+  if (!ballot(!ok)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) add(__builtin_fmaf(x[i], c, -b));
   } else {
-    const float m = top == -kInf ? 0.f : top;
-    const bool ok = Sums::plain(b);
 #pragma unroll
     for (int i = 0; i < N; ++i) add(ok ? __builtin_fmaf(x[i], c, -b) : (x[i] - m) * c);
   }
   t.s += s;
   t.e += e;
+}
+
+// N logits, any.
+template <int N>
+__device__ __forceinline__ void add_logits(Sums& t, const float* x, float c) {
+  float top = t.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = larger(top, x[i]);
+  t.rebase(top, c);
+  sum_logits<N>(t, x, c);
 }
 
 // One number for a logit and its id: larger logits first, of equal ones the lowest id; 0 is
@@ -105,10 +110,11 @@ __device__ __forceinline__ uint32_t key_id(uint64_t k) { return ~static_cast<uin
 template <int THREADS>
 struct TopSpace {
   float best[THREADS];
+  uint32_t list[kTopKeys];
   uint64_t keys[kTopKeys];
   uint64_t top[LM_TOP_MAX];
   uint64_t most[THREADS / kWave];
-  int n;
+  int n, groups;
 };
 
 struct NoSpace {
@@ -124,17 +130,23 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t x) {
   return x;
 }
 
-// Minimum of a wave's numbers (no NaN), in all lanes.
-__device__ __forceinline__ float wave_min(float x) {
+// The largest number of groups of LANES lanes, in all of them; NaN if one is.
+template <int LANES>
+__device__ __forceinline__ float lanes_larger(float x) {
+  return lanes_fold<LANES>(x, [](float a, float b) { return larger(a, b); });
+}
+
+// The k-th largest of a wave's numbers (no NaN): fewer than k are above each of the k largest.
+__device__ __forceinline__ float kth_largest(float x, int k) {
+  int above = 0;
 #pragma unroll
-  for (int off = 1; off < kWave; off <<= 1)
-    x = __builtin_fminf(x, __shfl_xor(x, off, kWave));
-  return x;
+  for (int i = 0; i < kWave; ++i) above += read_lane(x, i) > x ? 1 : 0;
+  return -lanes_larger<kWave>(above < k ? -x : -kInf);
 }
 
 // The k largest keys into t.top, 0 behind the last: `mine` is the largest of the thread's
-// logits, pick(want, f) and scan(f) call f(logit, id) for those of the threads that want it
-// and for all of them. Of the 64 maxima of groups of threads the k-th is a bound that k logits
+// logits; pick(bound, want, f) calls f(logit, id) for those logits at least that may reach the
+// bound (want: the thread's do), scan(f) for all of the thread's. Of the 64 maxima of groups of threads the k-th is a bound that k logits
 // reach; only threads that reach it look through their logits again, and the few they
 // find are ranked. Where more than kTopKeys reach the bound (many equal logits), each key is
 // found by a pass of its own.
@@ -144,19 +156,15 @@ __device__ __forceinline__ void select_top(float mine, int k, TopSpace<THREADS>&
   const int tid = threadIdx.x, lane = lane_id();
   mine = mine == mine ? mine : -kInf;  // (a NaN's row has no alternatives)
   t.best[tid] = mine;
-  if (tid == 0) t.n = 0;
+  if (tid == 0) t.n = t.groups = 0;
   if (tid < LM_TOP_MAX) t.top[tid] = 0;
   __syncthreads();
   float group = t.best[lane];
 #pragma unroll
   for (int i = 1; i < THREADS / kWave; ++i)
     group = __builtin_fmaxf(group, t.best[lane + i * kWave]);
-  int above = 0;
-#pragma unroll
-  for (int i = 0; i < kWave; ++i) above += read_lane(group, i) > group ? 1 : 0;
-  // (fewer than k are above each of the k largest)
-  const float bound = wave_min(above < k ? group : kInf);
-  pick(mine >= bound && mine > -kInf, [&](float x, uint32_t id) {
+  const float bound = kth_largest(group, k);
+  pick(bound, mine >= bound && mine > -kInf, [&](float x, uint32_t id) {
     if (x >= bound && x > -kInf) {
       const int i = atomicAdd(&t.n, 1);
       if (i < kTopKeys) t.keys[i] = key_of(x, id);
@@ -196,6 +204,8 @@ __device__ __forceinline__ void select_top(float mine, int k, TopSpace<THREADS>&
   __syncthreads();
 }
 
+constexpr int kPartThreads = 256, kMaxima = kPartThreads / 4, kMostParts = 128;
+
 struct LogpArgs {
   const void* logits;
   int64_t ld, N;
@@ -207,40 +217,40 @@ struct LogpArgs {
   float c_off;
   float *logp, *entropy, *peak, *log_sum, *top_logp;
   int32_t *top_ids, *dev_err;
-  Sums* sums;      // [N][parts], where rows are cut
-  uint64_t* keys;  // [N][parts][k]
+  Sums* sums;     // [N][parts], where rows are cut
+  float* maxima;  // [N][parts][kMaxima]: of kPartThreads / kMaxima neighbouring threads
 };
 
-// A row's target: whether it has one, its logit (NaN outside the vocabulary).
+// A row's target: whether it has one, its logit (NaN outside the vocabulary). The logit's
+// load is under way until it is used.
 struct Target {
-  bool any;
+  bool any, in;
   float x;
 };
 
 template <typename T>
 __device__ __forceinline__ Target target_of(const LogpArgs& a, int64_t row) {
-  if (!a.logp) return {false, 0.f};
+  if (!a.logp) return {false, false, 0.f};
   const int64_t id = a.wide ? static_cast<const int64_t*>(a.targets)[row]
                             : static_cast<const int32_t*>(a.targets)[row];
-  if (id == a.ignore) return {false, 0.f};
-  if (id < 0 || id >= a.V) {
-    if (threadIdx.x == 0) raise_err(a.dev_err, LM_DEVERR_ID_RANGE);
-    return {true, __builtin_nanf("")};
-  }
-  return {true, Patch<T>::one(static_cast<const T*>(a.logits) + row * a.ld + id)};
+  const bool in = id >= 0 && id < a.V;
+  return {id != a.ignore, in,
+          Patch<T>::one(static_cast<const T*>(a.logits) + row * a.ld + (in ? id : 0))};
 }
 
-// What a row's sums and keys come to, by all of the workgroup's threads.
+// What a row's sums and keys come to, by thread `tid` of `threads`.
 __device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const Sums& t,
-                                           const Target& target, const uint64_t* top) {
+                                           const Target& target, const uint64_t* top, int tid,
+                                           int threads) {
   const bool bad = !(t.m < kInf);  // a NaN or +infinity among the logits
   const float nan = __builtin_nanf("");
   const float slip = t.slip(a.c), mean = t.e / t.s;
   // s = 2^slip sum 2^(c (x - m)); c's own rounding moves its logarithm by the mean exponent.
   const float log_sum = logf(t.s) - kLn2 * (slip + a.c_off * (mean - slip));
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     if (a.logp) {
-      const float x = target.x;
+      const float x = target.in ? target.x : nan;
+      if (target.any && !target.in) raise_err(a.dev_err, LM_DEVERR_ID_RANGE);
       const float y = x == -kInf ? x : (x - t.m) * a.scale - log_sum;
       a.logp[row] = target.any ? (bad ? nan : y) : 0.f;
     }
@@ -249,7 +259,7 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const
     a.peak[row] = bad ? nan : t.m;
     a.log_sum[row] = bad ? nan : t.s == 0.f ? -kInf : log_sum;
   }
-  for (int i = threadIdx.x; i < a.k; i += blockDim.x) {
+  for (int i = tid; i < a.k; i += threads) {
     const uint64_t key = top[i];
     const bool any = key != 0 && !bad;
     a.top_ids[row * a.k + i] = any ? static_cast<int32_t>(key_id(key)) : -1;
@@ -261,10 +271,7 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const
 // The sums of the workgroup's threads, added in a fixed order, in all of them.
 template <int THREADS>
 __device__ __forceinline__ Sums join_sums(Sums t, float c, Sums (&lds)[THREADS / kWave]) {
-  float top = t.m;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) top = larger(top, __shfl_xor(top, off, kWave));
-  t.rebase(top, c);
+  t.rebase(lanes_larger<kWave>(t.m), c);
   t.s = lanes_sum<kWave>(t.s);
   t.e = lanes_sum<kWave>(t.e);
   if constexpr (THREADS > kWave) {
@@ -277,24 +284,137 @@ __device__ __forceinline__ Sums join_sums(Sums t, float c, Sums (&lds)[THREADS /
   return t;
 }
 
-template <typename T, int THREADS, bool TOP, Ends ENDS>
-__global__ __launch_bounds__(THREADS) void k_logp(LogpArgs a, uint32_t first) {
-  constexpr int P = Patch<T>::P, U = 4;
+// LDS instructions of a wave take effect in their order; the compiler has to keep it where
+// lanes read what others wrote.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Rows that LANES lanes hold in registers, kRowVectors vectors each: no wave waits for another.
+constexpr int kRowVectors = 4, kRowKeys = 256;
+
+template <typename T, int LANES, bool TOP, Ends ENDS>
+__global__ __launch_bounds__(kPartThreads) void k_logp_rows(LogpArgs a, uint32_t first) {
+  static_assert(!TOP || LANES == kWave, "a wave ranks");
+  constexpr int P = Patch<T>::P, U = kRowVectors, kRows = kPartThreads / LANES;
+  constexpr int kWaves = kPartThreads / kWave;
+  using raw_t = typename Patch<T>::raw_t;
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  const int64_t i = (first + static_cast<int64_t>(blockIdx.x)) * kRows +
+                    (LANES == kWave ? first_lane(group) : group);
+  const bool live = i < a.N;
+  const int64_t row = live ? i : a.N - 1;
+  const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+  const int vectors = (a.V + P - 1) / P;
+  raw_t r[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    r[u] = Span<T, ENDS, uint32_t>((lane + u * LANES) * P, a.V).load(x);
+  const Target target = target_of<T>(a, row);
+  float y[U * P];
+  Sums t{-kInf, 0.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (u * LANES >= vectors) break;
+    const Span<T, ENDS, uint32_t> s((lane + u * LANES) * P, a.V);
+    s.widen(r[u], y + u * P);
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+      y[u * P + e] = e < s.have ? y[u * P + e] : -kInf;
+      t.m = larger(t.m, y[u * P + e]);
+    }
+  }
+  float mine = t.m;
+  t.m = lanes_larger<LANES>(t.m);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (u * LANES >= vectors) break;
+    sum_logits<P>(t, y + u * P, a.c);
+  }
+  t.s = lanes_sum<LANES>(t.s);
+  t.e = lanes_sum<LANES>(t.e);
+  if constexpr (!TOP) {
+    if (live) finish_row(a, row, t, target, nullptr, lane, LANES);
+  } else {
+    // As select_top, with the logits at hand and every wave for itself.
+    __shared__ uint64_t keys[kWaves][kRowKeys], top[kWaves][LM_TOP_MAX];
+    uint64_t *key = keys[group], *best = top[group];
+    best[lane] = 0;
+    mine = mine == mine ? mine : -kInf;
+    const float bound = kth_largest(mine, a.k);
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u * LANES >= vectors) break;
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+        const float z = y[u * P + e];
+        const bool hit = z >= bound && z > -kInf;
+        const uint64_t hits = ballot(hit);
+        if (!hits) continue;
+        const int at = n + popc_below(hits);
+        if (hit && at < kRowKeys)
+          key[at] = key_of(z, static_cast<uint32_t>((lane + u * LANES) * P + e));
+        n += __popcll(hits);
+      }
+    }
+    wave_order();
+    if (n <= kRowKeys) {
+      for (int j = lane; j < n; j += kWave) {
+        const uint64_t k = key[j];
+        int rank = 0;
+        for (int l = 0; l < n; ++l) rank += key[l] > k ? 1 : 0;
+        if (rank < a.k) best[rank] = k;
+      }
+    } else {
+      uint64_t last = ~uint64_t(0);
+      for (int rank = 0; rank < a.k; ++rank) {
+        uint64_t k = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (u * LANES >= vectors) break;
+#pragma unroll
+          for (int e = 0; e < P; ++e) {
+            const uint64_t z = y[u * P + e] > -kInf
+                                   ? key_of(y[u * P + e],
+                                            static_cast<uint32_t>((lane + u * LANES) * P + e))
+                                   : 0;
+            k = z < last && z > k ? z : k;
+          }
+        }
+        k = wave_max(k);
+        if (k == 0) break;
+        if (lane == 0) best[rank] = k;
+        last = k;
+      }
+    }
+    wave_order();
+    if (live) finish_row(a, row, t, target, best, lane, LANES);
+  }
+}
+
+// A row, or a part of one, by a workgroup.
+template <typename T, bool TOP, bool PARTS>
+__global__ __launch_bounds__(kPartThreads) void k_logp(LogpArgs a, uint32_t first) {
+  constexpr int P = Patch<T>::P, U = 4, THREADS = kPartThreads;
   using raw_t = typename Patch<T>::raw_t;
   __shared__ Sums lds[THREADS / kWave];
-  __shared__ std::conditional_t<TOP, TopSpace<THREADS>, NoSpace> space;
+  __shared__ std::conditional_t<TOP && !PARTS, TopSpace<THREADS>, NoSpace> space;
   const uint32_t b = first + blockIdx.x;
-  const int64_t row = b / static_cast<uint32_t>(a.parts);
-  const int part = static_cast<int>(b - row * a.parts);
+  const int64_t row = PARTS ? b / static_cast<uint32_t>(a.parts) : b;
+  const int part = PARTS ? static_cast<int>(b - row * a.parts) : 0;
   const T* x = static_cast<const T*>(a.logits) + row * a.ld;
   const int vectors = (a.V + P - 1) / P, whole = a.V / P;
   const int v0 = part * a.part_vectors;
   const int v1 = a.part_vectors < vectors - v0 ? v0 + a.part_vectors : vectors;
   const int w1 = whole < v1 ? whole : v1;  // whole vectors
-  Target target{false, 0.f};
-  if (a.parts == 1) target = target_of<T>(a, row);
+  Target target{};
+  if constexpr (!PARTS) target = target_of<T>(a, row);
   // Vectors from number v1 on are loaded as the row's last one and count as masked.
-  auto span = [&](int v) { return Span<T, ENDS>(static_cast<int64_t>(v) * P, a.V, v < v1); };
+  auto span = [&](int v) {
+    return Span<T, Ends::PART>(static_cast<int64_t>(v) * P, a.V, v < v1);
+  };
   auto place = [&](int v, const raw_t& r, float* y) {
     const auto s = span(v);
     s.widen(r, y);
@@ -303,18 +423,16 @@ __global__ __launch_bounds__(THREADS) void k_logp(LogpArgs a, uint32_t first) {
   };
   Sums t{-kInf, 0.f, 0.f};
   int base = v0;
-  if constexpr (ENDS != Ends::NARROW) {
-    for (; base + THREADS * U <= w1; base += THREADS * U) {
-      const T* at = x + static_cast<int64_t>(base) * P;
-      raw_t r[U];
+  for (; base + THREADS * U <= w1; base += THREADS * U) {
+    const T* at = x + static_cast<int64_t>(base) * P;
+    raw_t r[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        r[u] = Patch<T>::load(at + static_cast<uint32_t>(threadIdx.x + u * THREADS) * P);
-      float y[U * P];
+    for (int u = 0; u < U; ++u)
+      r[u] = Patch<T>::load(at + static_cast<uint32_t>(threadIdx.x + u * THREADS) * P);
+    float y[U * P];
 #pragma unroll
-      for (int u = 0; u < U; ++u) Patch<T>::widen(r[u], y + u * P);
-      add_logits<U * P>(t, y, a.c);
-    }
+    for (int u = 0; u < U; ++u) Patch<T>::widen(r[u], y + u * P);
+    add_logits<U * P>(t, y, a.c);
   }
   if (base < v1) {  // fewer than U vectors a thread
     raw_t r[U];
@@ -330,81 +448,135 @@ __global__ __launch_bounds__(THREADS) void k_logp(LogpArgs a, uint32_t first) {
   }
   const float mine = t.m;
   t = join_sums<THREADS>(t, a.c, lds);
-  if constexpr (TOP) {
-    auto look = [&](int v, const raw_t& r, auto f) {
-      float y[P];
-      place(v, r, y);
+  if constexpr (PARTS) {
+    const int64_t at = row * a.parts + part;
+    if (threadIdx.x == 0) a.sums[at] = t;
+    if constexpr (TOP) {
+      static_assert(THREADS / kMaxima == 4, "a quad's maximum");
+      const float quad = lanes_fold<4>(mine, [](float p, float q) { return larger(p, q); });
+      if (threadIdx.x % 4 == 0) a.maxima[at * kMaxima + threadIdx.x / 4] = quad;
+    }
+  } else {
+    if constexpr (TOP) {
+      auto look = [&](int v, const raw_t& r, auto f) {
+        float y[P];
+        place(v, r, y);
 #pragma unroll
-      for (int e = 0; e < P; ++e) f(y[e], static_cast<uint32_t>(v * P + e));
-    };
-    select_top<THREADS>(
-        mine, a.k, space,
-        // The wave's lanes share out one thread's vectors, U threads' at a time.
-        [&](bool want, auto f) {
-          const int from = v0 + static_cast<int>(threadIdx.x & ~(kWave - 1u)), lane = lane_id();
-          for (int i0 = 0; from + i0 * THREADS < v1; i0 += kWave) {
-            for (uint64_t todo = ballot(want); todo;) {
-              raw_t r[U];
-              int v[U];
+        for (int e = 0; e < P; ++e) f(y[e], static_cast<uint32_t>(v * P + e));
+      };
+      select_top<THREADS>(
+          mine, a.k, space,
+          // Several lanes of the wave share out one thread's vectors.
+          [&](float, bool want, auto f) {
+            const int from = threadIdx.x & ~(kWave - 1), lane = lane_id();
+            const int count = (v1 + THREADS - 1) / THREADS;  // vectors of a thread
+            const int lanes = count <= 16 ? 16 : count <= 32 ? 32 : 64;
+            for (int i0 = lane % lanes; i0 - lane % lanes < count; i0 += lanes) {
+              for (uint64_t todo = ballot(want); todo;) {
+                raw_t r[U];
+                int v[U];
 #pragma unroll
-              for (int u = 0; u < U; ++u) {
-                v[u] = todo ? from + __builtin_ctzll(todo) + (i0 + lane) * THREADS : v1;
-                todo &= todo - 1;
-                r[u] = span(v[u]).load(x);
+                for (int u = 0; u < U; ++u) {
+                  v[u] = v1;
+                  for (int l = 0; l < kWave; l += lanes) {
+                    if (todo && lane / lanes == l / lanes)
+                      v[u] = from + __builtin_ctzll(todo) + i0 * THREADS;
+                    todo &= todo - 1;
+                  }
+                  r[u] = span(v[u]).load(x);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                  if (v[u] < v1) look(v[u], r[u], f);
               }
-#pragma unroll
-              for (int u = 0; u < U; ++u)
-                if (v[u] < v1) look(v[u], r[u], f);
             }
-          }
-        },
-        [&](auto f) {
-          for (int v = v0 + threadIdx.x; v < v1; v += THREADS) look(v, span(v).load(x), f);
-        });
-  }
-  if (a.parts == 1) {
-    finish_row(a, row, t, target, space.top);
-    return;
-  }
-  const int64_t at = row * a.parts + part;
-  if (threadIdx.x == 0) a.sums[at] = t;
-  if constexpr (TOP) {
-    for (int i = threadIdx.x; i < a.k; i += THREADS) a.keys[at * a.k + i] = space.top[i];
+          },
+          [&](auto f) {
+            for (int v = threadIdx.x; v < v1; v += THREADS) look(v, span(v).load(x), f);
+          });
+    }
+    finish_row(a, row, t, target, space.top, threadIdx.x, THREADS);
   }
 }
 
-// One workgroup a row: the parts' sums and keys.
+// One workgroup a row that is cut into parts: adds their sums, and looks through the logits
+// of those groups of threads whose maxima reach the bound.
 constexpr int kJoinThreads = 256;
 
 template <typename T, bool TOP>
 __global__ __launch_bounds__(kJoinThreads) void k_logp_join(LogpArgs a, uint32_t first) {
+  constexpr int P = Patch<T>::P;
   __shared__ Sums lds[kJoinThreads / kWave];
   __shared__ std::conditional_t<TOP, TopSpace<kJoinThreads>, NoSpace> space;
   const int64_t row = first + static_cast<int64_t>(blockIdx.x);
-  const Target target = target_of<T>(a, row);
-  const uint64_t* keys = a.keys + row * a.parts * a.k;
-  const int n = a.parts * a.k;
-  float mine = -kInf;
+  // Everything is loaded at once: a thread's part, its share of the maxima.
+  constexpr int kShare = kMostParts * kMaxima / kJoinThreads;
+  static_assert(kMostParts <= kJoinThreads, "a part a thread");
+  const int n = a.parts * kMaxima, mine_at = static_cast<int>(threadIdx.x);
+  const Sums* sums = a.sums + row * a.parts;
+  Sums t = sums[mine_at < a.parts ? mine_at : 0];
+  float maxima[kShare], mine = -kInf;
   if constexpr (TOP) {
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n; i += kJoinThreads)
-      mine = keys[i] ? __builtin_fmaxf(mine, key_value(keys[i])) : mine;
+    const float* at = a.maxima + row * n;
+#pragma unroll
+    for (int j = 0; j < kShare; ++j) {
+      if (j * kJoinThreads >= n) break;
+      const int i = mine_at + j * kJoinThreads;
+      maxima[j] = at[i < n ? i : 0];
+    }
   }
-  Sums t{-kInf, 0.f, 0.f};
-  for (int i = threadIdx.x; i < a.parts; i += kJoinThreads) t.add(a.sums[row * a.parts + i], a.c);
+  const Target target = target_of<T>(a, row);
+  if (mine_at >= a.parts) t = Sums{-kInf, 0.f, 0.f};
+  if constexpr (TOP) {
+#pragma unroll
+    for (int j = 0; j < kShare; ++j) {
+      if (j * kJoinThreads >= n) break;
+      maxima[j] = mine_at + j * kJoinThreads < n ? maxima[j] : -kInf;
+      mine = larger(mine, maxima[j]);
+    }
+  }
   t = join_sums<kJoinThreads>(t, a.c, lds);
   if constexpr (TOP) {
-    auto scan = [&](auto f) {
-      for (int i = threadIdx.x; i < n; i += kJoinThreads)
-        if (keys[i]) f(key_value(keys[i]), key_id(keys[i]));
+    const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+    const int vectors = (a.V + P - 1) / P;
+    auto look = [&](int v, int end, auto f) {
+      if (v >= end) return;
+      const Span<T, Ends::PART> s(static_cast<int64_t>(v) * P, a.V);
+      float y[P];
+      s.widen(s.load(x), y);
+#pragma unroll
+      for (int e = 0; e < P; ++e)
+        if (e < s.have) f(y[e], static_cast<uint32_t>(v * P + e));
     };
-    select_top<kJoinThreads>(mine, a.k, space,
-                             [&](bool want, auto f) {
-                               if (want) scan(f);
-                             },
-                             scan);
+    select_top<kJoinThreads>(
+        mine, a.k, space,
+        [&](float bound, bool want, auto f) {
+#pragma unroll
+          for (int j = 0; j < kShare; ++j) {
+            if (j * kJoinThreads >= n) break;
+            if (!want || !(maxima[j] >= bound && maxima[j] > -kInf)) continue;
+            const int at = atomicAdd(&space.groups, 1);
+            if (at < kTopKeys) space.list[at] = mine_at + j * kJoinThreads;
+          }
+          __syncthreads();
+          const int groups = space.groups;
+          if (groups > kTopKeys) {
+            if (threadIdx.x == 0) space.n = kTopKeys + 1;
+            return;
+          }
+          const int turns = (a.part_vectors + kPartThreads - 1) / kPartThreads;
+          for (int i = threadIdx.x; i < groups * turns * 4; i += kJoinThreads) {
+            const int g = space.list[i / (turns * 4)], j = i % (turns * 4);
+            const int v0 = g / kMaxima * a.part_vectors;
+            const int v1 = a.part_vectors < vectors - v0 ? v0 + a.part_vectors : vectors;
+            look(v0 + g % kMaxima * 4 + j % 4 + j / 4 * kPartThreads, v1, f);
+          }
+        },
+        [&](auto f) {
+          for (int v = threadIdx.x; v < vectors; v += kJoinThreads) look(v, vectors, f);
+        });
   }
-  finish_row(a, row, t, target, space.top);
+  finish_row(a, row, t, target, space.top, threadIdx.x, kJoinThreads);
 }
 
 // ---------------------------------------------------------------------------
@@ -498,61 +670,66 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-#ifndef LMZ_WG
-#define LMZ_WG 2048
-#endif
-#ifndef LMZ_ONE
-#define LMZ_ONE 1024
-#endif
 struct LogpPlan {
   int64_t parts, part_vectors;
 };
 
+// Rows go to a workgroup each where there are kFullGroups of them, or where they are short;
+// others are cut into parts, at most kMostParts (each more costs the one workgroup that joins
+// them), so that about that many workgroups have work. 64 rows of 800,000
+// bf16, 8 alternatives: 31 us so, with half as many workgroups 38, with twice as many 31; 1 x
+// 800,000, 20 alternatives: 14 us in 98 parts, 27 in 391.
+constexpr int64_t kFullGroups = 1024, kWholeVectors = 1024;
+
 static LogpPlan logp_plan(int64_t N, int64_t V, int dtype) {
   const int P = dtype == LM_BF16 ? Patch<bf16_t>::P : Patch<float>::P;
   const int64_t vectors = (V + P - 1) / P;
-  if (N >= LMZ_WG || vectors <= LMZ_ONE) return {1, vectors};
-  // Vectors of a thread, so that about LMZ_WG workgroups have work.
-  int64_t each = N * vectors / (LMZ_WG * 256) + 1;
-  const int64_t parts = (vectors + each * 256 - 1) / (each * 256);
-  each = (vectors + parts - 1) / parts;
-  return {(vectors + each - 1) / each, each};
+  if (N >= kFullGroups || vectors <= kWholeVectors) return {1, vectors};
+  // Vectors of a thread.
+  int64_t each = N * vectors / (kFullGroups * kPartThreads) + 1;
+  const int64_t least = (vectors - 1) / (kMostParts * kPartThreads) + 1;
+  each = each > least ? each : least;
+  const int64_t parts = (vectors - 1) / (each * kPartThreads) + 1;
+  each = (vectors - 1) / parts + 1;
+  return {(vectors - 1) / each + 1, each};
 }
 
 static size_t sums_bytes(int64_t n) { return (static_cast<size_t>(n) * sizeof(Sums) + 15) / 16 * 16; }
 
 size_t logp_workspace_bytes(int64_t N, int64_t V, int dtype, int k) {
   const int64_t parts = logp_plan(N, V, dtype).parts;
-  return parts == 1 ? 0 : sums_bytes(N * parts) + static_cast<size_t>(N * parts) * k * 8;
+  if (parts == 1) return 0;
+  return sums_bytes(N * parts) + (k ? static_cast<size_t>(N * parts) * kMaxima * 4 : 0);
 }
 
 template <typename T>
 static int logp_launch(const LogpArgs& a, hipStream_t st) {
   constexpr int P = Patch<T>::P;
-  const bool top = a.k > 0, few = a.V <= 256 * P;
-  const int threads = few ? kWave : 256;
-  const Ends ends = ends_of(a.V, P);
-  auto pick = [&](auto w, auto e) {
-    return top ? k_logp<T, decltype(w)::value, true, decltype(e)::value>
-               : k_logp<T, decltype(w)::value, false, decltype(e)::value>;
+  const bool top = a.k > 0;
+  auto launch = [&](auto kernel, int64_t blocks, int threads) {
+    return launch_parts(blocks, threads, [&](uint32_t first, uint32_t n) {
+      kernel<<<n, threads, 0, st>>>(a, first);
+      return launch_status(hipGetLastError());
+    });
   };
-  using Few = std::integral_constant<int, kWave>;
-  using Many = std::integral_constant<int, 256>;
-  using Part = std::integral_constant<Ends, Ends::PART>;
-  using Narrow = std::integral_constant<Ends, Ends::NARROW>;
-  auto kernel = ends == Ends::NARROW ? pick(Few{}, Narrow{})
-                : few                ? pick(Few{}, Part{})
-                                     : pick(Many{}, Part{});
-  const int rc = launch_parts(a.N * a.parts, threads, [&](uint32_t first, uint32_t n) {
-    kernel<<<n, threads, 0, st>>>(a, first);
-    return launch_status(hipGetLastError());
-  });
-  if (rc != LM_OK || a.parts == 1) return rc;
-  auto join = top ? k_logp_join<T, true> : k_logp_join<T, false>;
-  return launch_parts(a.N, kJoinThreads, [&](uint32_t first, uint32_t n) {
-    join<<<n, kJoinThreads, 0, st>>>(a, first);
-    return launch_status(hipGetLastError());
-  });
+  const int64_t vectors = (static_cast<int64_t>(a.V) + P - 1) / P;
+  if (vectors <= kWave * kRowVectors) {
+    const bool part = !top && vectors <= 16 * kRowVectors;  // 16 lanes a row
+    const bool narrow = a.V < P;
+    auto kernel = narrow ? (top ? k_logp_rows<T, kWave, true, Ends::NARROW>
+                                : k_logp_rows<T, 16, false, Ends::NARROW>)
+                  : top  ? k_logp_rows<T, kWave, true, Ends::PART>
+                  : part ? k_logp_rows<T, 16, false, Ends::PART>
+                         : k_logp_rows<T, kWave, false, Ends::PART>;
+    const int rows = kPartThreads / (part ? 16 : kWave);
+    return launch(kernel, (a.N + rows - 1) / rows, kPartThreads);
+  }
+  if (a.parts == 1)
+    return launch(top ? k_logp<T, true, false> : k_logp<T, false, false>, a.N, kPartThreads);
+  const int rc = launch(top ? k_logp<T, true, true> : k_logp<T, false, true>, a.N * a.parts,
+                        kPartThreads);
+  if (rc != LM_OK) return rc;
+  return launch(top ? k_logp_join<T, true> : k_logp_join<T, false>, a.N, kJoinThreads);
 }
 
 int logp_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtype, const void* targets,
@@ -561,7 +738,7 @@ int logp_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtype, co
              void* ws, hipStream_t st) {
   if (N == 0) return LM_OK;
   const LogpPlan p = logp_plan(N, V, dtype);
-  char* keys = ws ? static_cast<char*>(ws) + sums_bytes(N * p.parts) : nullptr;
+  char* maxima = ws ? static_cast<char*>(ws) + sums_bytes(N * p.parts) : nullptr;
   const double log2e = 1.4426950408889634 * static_cast<double>(scale);
   const float c = static_cast<float>(log2e);
   const LogpArgs a{logits, ld, N, static_cast<int>(V), static_cast<int>(p.parts),
@@ -569,7 +746,7 @@ int logp_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtype, co
                    static_cast<float>(c / log2e - 1.0),
                    targets ? logp : nullptr, entropy, peak, log_sum, top_logp, top_ids, dev_err,
                    static_cast<Sums*>(ws),
-                   reinterpret_cast<uint64_t*>(keys)};
+                   reinterpret_cast<float*>(maxima)};
   return dtype == LM_BF16 ? logp_launch<bf16_t>(a, st) : logp_launch<float>(a, st);
 }
 

@@ -168,22 +168,27 @@ __device__ __forceinline__ float read_lane(float v, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
 
-// Sum over groups of LANES neighbouring lanes, in all of them, in an order that depends
-// on LANES only.
-template <int LANES>
-__device__ __forceinline__ float lanes_sum(float x) {
+// f over groups of LANES neighbouring lanes, in all of them, in an order that depends on
+// LANES only.
+template <int LANES, typename F>
+__device__ __forceinline__ float lanes_fold(float x, F f) {
   auto from = [](float v, auto ctrl) {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value,
                                                       0xf, 0xf, true));
   };
-  x += from(x, std::integral_constant<int, 0xB1>{});   // lane ^ 1
-  x += from(x, std::integral_constant<int, 0x4E>{});   // lane ^ 2
-  x += from(x, std::integral_constant<int, 0x141>{});  // the other 4 of 8
-  if constexpr (LANES >= 16) x += from(x, std::integral_constant<int, 0x140>{});  // 8 of 16
-  if constexpr (LANES == 32) x += __shfl_xor(x, 16, kWave);
+  x = f(x, from(x, std::integral_constant<int, 0xB1>{}));  // lane ^ 1
+  x = f(x, from(x, std::integral_constant<int, 0x4E>{}));  // lane ^ 2
+  if constexpr (LANES >= 8) x = f(x, from(x, std::integral_constant<int, 0x141>{}));  // 4 of 8
+  if constexpr (LANES >= 16) x = f(x, from(x, std::integral_constant<int, 0x140>{}));  // 8 of 16
+  if constexpr (LANES == 32) x = f(x, __shfl_xor(x, 16, kWave));
   if constexpr (LANES == 64)
-    x = (read_lane(x, 0) + read_lane(x, 16)) + (read_lane(x, 32) + read_lane(x, 48));
+    x = f(f(read_lane(x, 0), read_lane(x, 16)), f(read_lane(x, 32), read_lane(x, 48)));
   return x;
+}
+
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float x) {
+  return lanes_fold<LANES>(x, [](float a, float b) { return a + b; });
 }
 
 }  // namespace lmz

@@ -30,6 +30,8 @@ import torch
 
 # The current stream's handle (not a public name of torch: the public call where it is absent).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# The current device's number, of a process whose device is in use: a third of the public call's time.
+_this_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "liblmzipf.so")
@@ -616,7 +618,7 @@ def _elsewhere(device: torch.device, stream) -> bool:
     the tensors' is refused."""
     if stream is not None and stream.device != device:
         raise LmError(f"stream is on {stream.device}, the tensors are on {device}")
-    return torch.cuda.current_device() != device.index
+    return _this_device() != device.index
 
 
 def _same_device(device, *tensors):
