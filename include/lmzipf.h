@@ -689,7 +689,7 @@ int lm_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int64_t ld_
  * A row with nothing left, and one whose dlogp and dentropy are 0, get zeros
  * whatever their logits are. */
 #define LM_TOP_MAX 64
-#define LM_LOGP_MAX_V (((int64_t)1 << 31) - 1)
+#define LM_LOGP_MAX_V ((int64_t)1 << 30)
 size_t lm_token_logprobs_workspace_bytes(int64_t N, int64_t V, int32_t dtype, int32_t top);
 int lm_token_logprobs(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype,
                       const void* targets, int32_t idtype, int64_t ignore, float scale,

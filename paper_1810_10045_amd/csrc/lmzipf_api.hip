@@ -185,12 +185,19 @@ static bool check_strides(const int64_t* s, int64_t B, int64_t H, int64_t Lq, in
 // The operands of a call on rows: which of them may meet in memory.
 class Operands {
  public:
-  // A rows x D matrix of elements of `size` bytes, or (rows 1) a vector.
-  void put(const void* at, int64_t rows, int64_t D, int64_t ld, int size, bool written) {
+  // A rows x D matrix of elements of `size` bytes.
+  void matrix(const void* at, int64_t rows, int64_t D, int64_t ld, int size, bool written) {
     if (!at || rows == 0 || D == 0) return;
     const uintptr_t a = reinterpret_cast<uintptr_t>(at);
     bad_ |= (a & (size - 1)) != 0 || ld < D || ld > (int64_t(1) << 40);
-    all_[n_++] = {a, rows, D * size, rows > 1 ? ld * size : 0, written};
+    all_[n_++] = {a, rows, D * size, rows > 1 ? ld * size : 0, written, true};
+  }
+  // n elements of `size` bytes.
+  void vector(const void* at, int64_t n, int size, bool written) {
+    if (!at || n == 0) return;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(at);
+    bad_ |= (a & (size - 1)) != 0;
+    all_[n_++] = {a, 1, n * size, 0, written, false};
   }
   // LM_E_INVAL where an operand that is written meets another one, but for a matrix that takes
   // the place of one that is read, row for row.
@@ -200,8 +207,7 @@ class Operands {
       for (int k = 0; k < n_; ++k) {
         const Operand &w = all_[i], &o = all_[k];
         if (i == k || !w.written || (o.written && k < i)) continue;
-        if (!o.written && w.at == o.at && w.ld == o.ld && w.rows == o.rows && w.row == o.row)
-          continue;
+        if (!o.written && w.matrix && o.matrix && w.at == o.at && w.ld == o.ld) continue;
         if (const int rc = meet(w, o)) return rc;
       }
     return LM_OK;
@@ -211,14 +217,14 @@ class Operands {
   struct Operand {
     uintptr_t at;
     int64_t rows, row, ld;  // row, ld: bytes
-    bool written;
+    bool written, matrix;
   };
   static int meet(const Operand& w, const Operand& o) {
     const __int128 w_end = static_cast<__int128>(w.at) + static_cast<__int128>(w.rows - 1) * w.ld + w.row;
     const __int128 o_end = static_cast<__int128>(o.at) + static_cast<__int128>(o.rows - 1) * o.ld + o.row;
     if (o.at >= w_end || w.at >= o_end) return LM_OK;
     // Spans that meet: matrices of the same rows may lie beside each other in wider ones.
-    if (w.rows != o.rows || w.row != o.row) return LM_E_INVAL;
+    if (!w.matrix || !o.matrix) return LM_E_INVAL;
     const int64_t n[3] = {1, 1, w.rows}, sw[3] = {0, 0, w.ld}, so[3] = {0, 0, o.ld};
     const Meet m = rows_meet(n, w.row, sw, so,
                              static_cast<__int128>(o.at) - static_cast<__int128>(w.at));
@@ -649,10 +655,10 @@ int lm_dropout(const void* x, int64_t ld_x, const void* add, int64_t ld_add, voi
   if (!x || !out || (reinterpret_cast<uintptr_t>(seed_at) & 7)) return LM_E_INVAL;
   Operands o;
   const int size = element_size(dtype);
-  o.put(out, rows, D, ld_out, size, true);
-  o.put(x, rows, D, ld_x, size, false);
-  o.put(add, rows, D, ld_add, size, false);
-  o.put(seed_at, 1, 1, 1, 8, false);
+  o.matrix(out, rows, D, ld_out, size, true);
+  o.matrix(x, rows, D, ld_x, size, false);
+  o.matrix(add, rows, D, ld_add, size, false);
+  o.vector(seed_at, 1, 8, false);
   if (const int rc = o.check()) return rc;
   return dropout_run(x, ld_x, add, ld_add, out, ld_out, rows, D, dtype, p, seed, seed_at,
                      static_cast<hipStream_t>(stream));
@@ -669,15 +675,15 @@ int lm_layer_norm(const void* x, int64_t ld_x, const void* add, int64_t ld_add, 
   if (!x || !y || !mean || !rstd) return LM_E_INVAL;
   Operands o;
   const int size = element_size(dtype);
-  o.put(y, rows, D, ld_y, size, true);
-  o.put(h, rows, D, ld_h, size, true);
-  o.put(mean, 1, rows, rows, 4, true);
-  o.put(rstd, 1, rows, rows, 4, true);
-  o.put(x, rows, D, ld_x, size, false);
-  o.put(add, rows, D, ld_add, size, false);
-  o.put(weight, 1, D, D, 4, false);
-  o.put(bias, 1, D, D, 4, false);
-  o.put(seed_at, 1, 1, 1, 8, false);
+  o.matrix(y, rows, D, ld_y, size, true);
+  o.matrix(h, rows, D, ld_h, size, true);
+  o.vector(mean, rows, 4, true);
+  o.vector(rstd, rows, 4, true);
+  o.matrix(x, rows, D, ld_x, size, false);
+  o.matrix(add, rows, D, ld_add, size, false);
+  o.vector(weight, D, 4, false);
+  o.vector(bias, D, 4, false);
+  o.vector(seed_at, 1, 8, false);
   if (const int rc = o.check()) return rc;
   return norm_run(x, ld_x, add, ld_add, rows, D, dtype, weight, bias, eps, p, seed, seed_at, y,
                   ld_y, h, ld_h, mean, rstd, static_cast<hipStream_t>(stream));
@@ -705,19 +711,18 @@ int lm_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int64_t ld_
   if (ws_bytes < need) return LM_E_WORKSPACE;
   Operands o;
   const int size = element_size(dtype);
-  o.put(dh, rows, D, ld_dh, size, true);
-  o.put(dx, rows, D, ld_dx, size, true);
-  o.put(dweight, 1, D, D, 4, true);
-  o.put(dbias, 1, D, D, 4, true);
-  o.put(need ? ws : nullptr, 1, static_cast<int64_t>(need / 4), static_cast<int64_t>(need / 4), 4,
-        true);
-  o.put(dy, rows, D, ld_dy, size, false);
-  o.put(h, rows, D, ld_h, size, false);
-  o.put(add, rows, D, ld_add, size, false);
-  o.put(mean, 1, rows, rows, 4, false);
-  o.put(rstd, 1, rows, rows, 4, false);
-  o.put(weight, 1, D, D, 4, false);
-  o.put(seed_at, 1, 1, 1, 8, false);
+  o.matrix(dh, rows, D, ld_dh, size, true);
+  o.matrix(dx, rows, D, ld_dx, size, true);
+  o.vector(dweight, D, 4, true);
+  o.vector(dbias, D, 4, true);
+  o.vector(need ? ws : nullptr, static_cast<int64_t>(need / 4), 4, true);
+  o.matrix(dy, rows, D, ld_dy, size, false);
+  o.matrix(h, rows, D, ld_h, size, false);
+  o.matrix(add, rows, D, ld_add, size, false);
+  o.vector(mean, rows, 4, false);
+  o.vector(rstd, rows, 4, false);
+  o.vector(weight, D, 4, false);
+  o.vector(seed_at, 1, 8, false);
   if (const int rc = o.check()) return rc;
   return norm_grad_run(dy, ld_dy, h, ld_h, add, ld_add, rows, D, dtype, mean, rstd, weight, p,
                        seed, seed_at, dh, ld_dh, dx, ld_dx, dweight, dbias, accumulate, ws,
@@ -747,16 +752,16 @@ int lm_token_logprobs(const void* logits, int64_t ld, int64_t N, int64_t V, int3
   if (need > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 15))) return LM_E_INVAL;
   if (ws_bytes < need) return LM_E_WORKSPACE;
   Operands o;
-  o.put(targets ? logp : nullptr, 1, N, N, 4, true);
-  o.put(entropy, 1, N, N, 4, true);
-  o.put(peak, 1, N, N, 4, true);
-  o.put(log_sum, 1, N, N, 4, true);
-  o.put(top_logp, 1, N * top, N * top, 4, true);
-  o.put(top_ids, 1, N * top, N * top, 4, true);
-  o.put(dev_err, 1, 1, 1, 4, true);
-  o.put(need ? ws : nullptr, 1, static_cast<int64_t>(need), static_cast<int64_t>(need), 1, true);
-  o.put(logits, N, V, ld, element_size(dtype), false);
-  o.put(targets, 1, N, N, idtype == LM_I64 ? 8 : 4, false);
+  o.vector(targets ? logp : nullptr, N, 4, true);
+  o.vector(entropy, N, 4, true);
+  o.vector(peak, N, 4, true);
+  o.vector(log_sum, N, 4, true);
+  o.vector(top_logp, N * top, 4, true);
+  o.vector(top_ids, N * top, 4, true);
+  o.vector(dev_err, 1, 4, true);
+  o.vector(need ? ws : nullptr, static_cast<int64_t>(need), 1, true);
+  o.matrix(logits, N, V, ld, element_size(dtype), false);
+  o.vector(targets, N, idtype == LM_I64 ? 8 : 4, false);
   if (const int rc = o.check()) return rc;
   return logp_run(logits, ld, N, V, dtype, targets, idtype, ignore, scale, top, logp, entropy,
                   peak, log_sum, top_logp, top_ids, dev_err, ws, static_cast<hipStream_t>(stream));
@@ -776,14 +781,14 @@ int lm_token_logprobs_grad(const void* logits, int64_t ld, int64_t N, int64_t V,
   if (logp_grad_blocks(N, V, dtype) > INT32_MAX) return LM_E_UNSUPPORTED;
   Operands o;
   const int size = element_size(dtype);
-  o.put(out, N, V, ld_out, size, true);
-  o.put(logits, N, V, ld, size, false);
-  o.put(dlogp ? targets : nullptr, 1, N, N, idtype == LM_I64 ? 8 : 4, false);
-  o.put(peak, 1, N, N, 4, false);
-  o.put(log_sum, 1, N, N, 4, false);
-  o.put(dlogp, 1, N, N, 4, false);
-  o.put(dentropy ? entropy : nullptr, 1, N, N, 4, false);
-  o.put(dentropy, 1, N, N, 4, false);
+  o.matrix(out, N, V, ld_out, size, true);
+  o.matrix(logits, N, V, ld, size, false);
+  o.vector(dlogp ? targets : nullptr, N, idtype == LM_I64 ? 8 : 4, false);
+  o.vector(peak, N, 4, false);
+  o.vector(log_sum, N, 4, false);
+  o.vector(dlogp, N, 4, false);
+  o.vector(dentropy ? entropy : nullptr, N, 4, false);
+  o.vector(dentropy, N, 4, false);
   if (const int rc = o.check()) return rc;
   return logp_grad_run(logits, ld, N, V, dtype, targets, idtype, ignore, scale, peak, log_sum,
                        dlogp, entropy, dentropy, out, ld_out, static_cast<hipStream_t>(stream));

@@ -218,6 +218,46 @@ def test_layer_norm_grad(lz, rows, D, gap, off, dtype):
             assert r.dx is r.dh
 
 
+# Rows enough for a wave of their own each, and for every workgroup to have several turns
+MANY = [(70_001, 40), (8300, 300), (4200, 517), (2100, 1025), (2100, 2048), (1100, 4100),
+        (1030, 8191), (1026, 16384)]
+
+
+@pytest.mark.parametrize("rows,D", MANY)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_layer_norm_of_many_rows(lz, rows, D, dtype):
+    gen = gen_of("many", rows, D, dtype)
+    x, add = rows_of(gen, rows, D, dtype, 1.5, 0.7), rows_of(gen, rows, D, dtype, 2.0, -1.0)
+    w, b = params(gen, D)
+    r = lz.layer_norm(x, w, b, add=add, p=0.2, seed=9)
+    ref = A.norm(wide(x), wide(w), wide(b), 1e-5, 0.2, 9, wide(add))
+    for name, dt in (("mean", None), ("rstd", None), ("y", dtype), ("h", dtype)):
+        close(getattr(r, name), *ref[name], name, dt)
+    g = lz.layer_norm_grad(add, r.h, r.mean, r.rstd, w, add=x, p=0.2, seed=9)
+    ref = A.norm_grad(wide(add), wide(r.h), wide(r.mean), wide(r.rstd), wide(w), wide(x), 0.2, 9)
+    for name, dt in (("dh", dtype), ("dx", dtype), ("dweight", None), ("dbias", None)):
+        close(getattr(g, name), *ref[name], name, dt)
+
+
+def test_results_of_tens_of_megabytes(lz):
+    """Results that are written through the caches (32 to 256 MiB): the same numbers."""
+    rows, D = 8300, 1025
+    gen = gen_of("cached")
+    x, dy = rows_of(gen, rows, D, F32), rows_of(gen, rows, D, F32)
+    ref, tol = A.dropout(wide(x), 0.3, 2)
+    close(lz.dropout(x, 0.3, 2), ref, tol, "dropout")
+    r = lz.layer_norm(x)
+    ref = A.norm(wide(x), None, None, 1e-5)
+    close(r.y, *ref["y"], "y")
+    g = lz.layer_norm_grad(dy, x, r.mean, r.rstd)
+    close(g.dh, *A.norm_grad(wide(dy), wide(x), wide(r.mean), wide(r.rstd), None)["dh"], "dh")
+    t = torch.randint(0, D, (rows,), generator=gen, device=DEV)
+    s = lz.token_logprobs(x, t)
+    ref, tol = A.logprobs_grad(wide(x), t.cpu().numpy(), wide(s.peak), wide(s.log_sum), 1.0,
+                               wide(s.logp))
+    close(lz.token_logprobs_grad(x, t, s.peak, s.log_sum, s.logp), ref, tol, "dlogits")
+
+
 def test_layer_norm_grad_against_autograd_and_differences(lz):
     """fp32 against torch's autograd of the definition in 64 bits, and against differences of
     it: both through dropout, the residual sum and the norm."""
