@@ -31,7 +31,6 @@ struct DropArgs {
   uint64_t word;     // of the first row
   uint32_t vectors;  // of the launch
   Divide per_row;
-  bool cached;
 };
 
 template <typename T, bool ADD, bool NARROW>
@@ -67,7 +66,7 @@ __global__ __launch_bounds__(kDropThreads) void k_dropout(const T* x, const T* a
 #pragma unroll
       for (int e = 0; e < P; ++e) y[e] += z[e];
     }
-    s.store(out + row[u] * a.ld_out, y, a.cached);
+    s.store(out + row[u] * a.ld_out, y);
   }
 }
 
@@ -86,8 +85,7 @@ static int dropout_launch(const T* x, int64_t ld_x, const T* add, int64_t ld_add
   for (int64_t r = 0; r < rows; r += most) {
     const int64_t n = rows - r < most ? rows - r : most;
     const DropArgs a{D, ld_x, ld_add, ld_out, static_cast<uint64_t>(r) * pairs,
-                     static_cast<uint32_t>(n * per_row), Divide(static_cast<uint32_t>(per_row)),
-                     cached_bytes(rows, D * static_cast<int64_t>(sizeof(T)))};
+                     static_cast<uint32_t>(n * per_row), Divide(static_cast<uint32_t>(per_row))};
     const uint32_t blocks = static_cast<uint32_t>((n * per_row + kBlock - 1) / kBlock);
     kernel<<<blocks, kDropThreads, 0, st>>>(x + r * ld_x, add ? add + r * ld_add : nullptr,
                                             out + r * ld_out, a, k);

@@ -593,7 +593,6 @@ struct LogpGradArgs {
   const float *peak, *log_sum, *dlogp, *entropy, *dentropy;
   void* out;
   int64_t ld_out;
-  bool cached;
 };
 
 // A workgroup: kGradThreads / LANES rows, of each a tile of LANES * kGradVectors vectors.
@@ -663,7 +662,7 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
       d += v * P + e == target ? dlogp : 0.f;
       y[e] = none ? 0.f : d;
     }
-    s.store(out, y, a.cached);
+    s.store(out, y);
   }
 }
 
@@ -788,7 +787,7 @@ int logp_grad_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtyp
   if (N == 0) return LM_OK;
   const LogpGradArgs a{logits, ld, N, static_cast<int>(V), 0, targets, ignore, idtype == LM_I64,
                        scale, peak, log_sum, targets ? dlogp : nullptr, entropy, dentropy, out,
-                       ld_out, cached_bytes(N, V * (dtype == LM_BF16 ? 2 : 4))};
+                       ld_out};
   return dtype == LM_BF16 ? grad_lanes<bf16_t>(a, st) : grad_lanes<float>(a, st);
 }
 

@@ -17,7 +17,6 @@ struct NormArgs {
   int D;
   float eps, inv_d;
   KeepArgs keep;
-  bool cached;
 };
 
 // Rows of a group, all of their loads under way at once. 200,000 rows of 128 bf16: 21 us, one
@@ -68,7 +67,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm(NormArgs a, uint32_t first
       }
 #pragma unroll
       for (int e = 0; e < P; ++e) sum[r] += h[r][v][e];
-      if (a.h && live) s.store(static_cast<T*>(a.h) + row * a.ld_h, h[r][v], a.cached);
+      if (a.h && live) s.store(static_cast<T*>(a.h) + row * a.ld_h, h[r][v]);
     }
   }
   group_sums<S>(sum, part[0]);
@@ -104,7 +103,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm(NormArgs a, uint32_t first
         h[r][v][e] = __builtin_fmaf(h[r][v][e] * square[r], a.weight ? w[e] : 1.f,
                                     a.bias ? b[e] : 0.f);
       if (i0 + r < a.rows)
-        s.store(static_cast<T*>(a.y) + (i0 + r) * a.ld_y, h[r][v], a.cached);
+        s.store(static_cast<T*>(a.y) + (i0 + r) * a.ld_y, h[r][v]);
     }
   }
 #pragma unroll
@@ -166,8 +165,7 @@ int norm_run(const void* x, int64_t ld_x, const void* add, int64_t ld_add, int64
   if (rows == 0) return LM_OK;
   const NormArgs a{x, add, weight, bias, y, h, mean, rstd, ld_x, ld_add, ld_y, ld_h, rows,
                    static_cast<int>(D), eps, static_cast<float>(1.0 / static_cast<double>(D)),
-                   make_keep(p, seed, seed_at),
-                   cached_bytes(rows, D * (dtype == LM_BF16 ? 2 : 4) * (h ? 2 : 1))};
+                   make_keep(p, seed, seed_at)};
   return dtype == LM_BF16 ? norm_launch<bf16_t>(a, st) : norm_launch<float>(a, st);
 }
 

@@ -19,7 +19,6 @@ struct NormGradArgs {
   int D;
   float inv_d;
   KeepArgs keep;
-  bool cached;
 };
 
 // Rows of a group, all of their loads under way at once.
@@ -130,10 +129,10 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
           const float d = (y[e] * w[v][e] - e0) - n[e] * e1;
           y[e] = __builtin_fmaf(rstd[r], d, ADD ? z[e] : 0.f);
         }
-        s.store(static_cast<T*>(a.dh) + row * a.ld_dh, y, a.cached);
+        s.store(static_cast<T*>(a.dh) + row * a.ld_dh, y);
         if (a.dx) {
           keep.apply<P>(static_cast<uint64_t>(row) * pairs + (lane + v * S::kGroup) * (P / 2), y);
-          s.store(static_cast<T*>(a.dx) + row * a.ld_dx, y, a.cached);
+          s.store(static_cast<T*>(a.dx) + row * a.ld_dx, y);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -278,8 +277,7 @@ int norm_grad_run(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, co
                          sums ? static_cast<float*>(ws) : nullptr, ld_dy, ld_h, ld_add, ld_dh,
                          ld_dx, rows, static_cast<int>(D),
                          static_cast<float>(1.0 / static_cast<double>(D)),
-                         make_keep(p, seed, seed_at),
-                         cached_bytes(rows, D * (dtype == LM_BF16 ? 2 : 4) * (dx ? 2 : 1))};
+                         make_keep(p, seed, seed_at)};
     const int rc = dtype == LM_BF16 ? norm_grad_launch<bf16_t>(a, blocks, st)
                                     : norm_grad_launch<float>(a, blocks, st);
     if (rc != LM_OK) return rc;

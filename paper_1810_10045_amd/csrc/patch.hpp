@@ -35,10 +35,6 @@ struct Patch<float> {
   static __device__ __forceinline__ void store(float* p, const float* x) {
     __builtin_nontemporal_store(f32x4e{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4e*>(p));
   }
-  // The same through the caches.
-  static __device__ __forceinline__ void keep(float* p, const float* x) {
-    *reinterpret_cast<f32x4e*>(p) = f32x4e{x[0], x[1], x[2], x[3]};
-  }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
   static __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 };
@@ -76,26 +72,11 @@ struct Patch<bf16_t> {
     const raw_t w = pack(x);
     __builtin_nontemporal_store(u32x4e{w.x, w.y, w.z, w.w}, reinterpret_cast<u32x4e*>(p));
   }
-  static __device__ __forceinline__ void keep(bf16_t* p, const float* x) {
-    const raw_t w = pack(x);
-    *reinterpret_cast<u32x4e*>(p) = u32x4e{w.x, w.y, w.z, w.w};
-  }
   static __device__ __forceinline__ float one(const bf16_t* p) { return bf16_to_f32(p->bits); }
   static __device__ __forceinline__ void put(bf16_t* p, float x) {
     p->bits = static_cast<uint16_t>(bits(x));
   }
 };
-
-// Whether results of rows of so many bytes are written through the caches (others past them). The
-// memory-side cache holds 256 MiB: what fits in it is still there for the next call that
-// reads it. Dropout on 2048 bf16 columns, its output the next call's input, 256 MiB each: 6.6
-// TB/s, past the caches 6.1; 64 MiB: 6.1 and 5.6; 384 MiB: 5.7 and 6.2. What fits in the
-// L2 caches would stay there until they are written back at the kernel's end: 16 MiB 4.1 and
-// 4.6. (Where nothing reads the outputs again, 256 MiB: 5.9 and 6.1.)
-static inline bool cached_bytes(int64_t rows, int64_t bytes) {
-  const double n = static_cast<double>(rows) * static_cast<double>(bytes);
-  return n > 32 << 20 && n <= 256 << 20;
-}
 
 // How rows end: every one in whole vectors of P values, in a part of one, or they hold fewer
 // than P (and are loaded one value at a time).
@@ -145,16 +126,9 @@ struct Span {
     }
     Patch<T>::widen(r, x);
   }
-  __device__ __forceinline__ void store(T* row, const float* x, bool cached) const {
+  __device__ __forceinline__ void store(T* row, const float* x) const {
     if (have == P) {
-      // (the empty statements keep the two apart: made one store, they would lose the hint)
-      if (cached) {
-        asm volatile("");
-        Patch<T>::keep(at(row, from), x);
-        asm volatile("");
-      } else {
-        Patch<T>::store(at(row, from), x);
-      }
+      Patch<T>::store(at(row, from), x);
     } else if (ENDS != Ends::WHOLE) {
       T* p = at(row, NARROW ? 0 : from + by);
 #pragma unroll
