@@ -33,6 +33,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 # The current device's number, of a process whose device is in use: a third of the public call's time.
 _this_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
+# The current stream's handle on a device.
+_stream_of = _raw_stream or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "liblmzipf.so")
 
@@ -146,6 +149,24 @@ _lib = _load()
 
 def lib():
     return _lib
+
+
+def _load_calls():
+    """The plain calls of dropout, layer norm and the token log probabilities without Python
+    between the checks, the results' allocation and the library (``csrc/calls.cpp``): of a call
+    of few rows that is more than half."""
+    try:
+        from . import _lmzipf_calls as calls
+    except ImportError as e:
+        raise ImportError(f"{e}: build it with `python -c 'import __graft_entry__ as g; g.build()'`") from e
+    names = ("lm_dropout", "lm_layer_norm", "lm_layer_norm_grad_workspace_bytes",
+             "lm_layer_norm_grad", "lm_token_logprobs_workspace_bytes", "lm_token_logprobs",
+             "lm_token_logprobs_grad", "lm_status_string")
+    calls.bind(LmError, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names))
+    return calls
+
+
+_calls = _load_calls()
 
 
 def status_string(rc: int) -> str:
@@ -1038,6 +1059,11 @@ def dropout(x: torch.Tensor, p: float, seed, add: Optional[torch.Tensor] = None,
     `dropout(dout, p, seed)`. seed: a number, or an int64 tensor of one element
     on the device, which a captured call reads with every replay. `out` may be x
     or `add`. Not recorded by autograd, as ``rel_bias``."""
+    if out is None and stream is None and x.is_cuda:
+        here = _this_device()
+        r = _calls.dropout(here, _stream_of(here), x, p, seed, add)
+        if r is not None:
+            return r[0]
     _no_graph("dropout", x, add, out, gradient="its gradient is dropout with the same seed")
     _dev(x, "x")
     device = x.device
@@ -1082,6 +1108,11 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
     where nothing is added or dropped, else `sum_out` (which may be `add`: the
     residual stream) or a new tensor; y goes to `out` (which may be x) or a new
     one. p and seed as ``dropout``'s. Not recorded by autograd, as ``rel_bias``."""
+    if out is None and sum_out is None and stream is None and x.is_cuda:
+        here = _this_device()
+        r = _calls.layer_norm(here, _stream_of(here), x, weight, bias, eps, add, p, seed)
+        if r is not None:
+            return NormResult(*r)
     _no_graph("layer_norm", x, weight, bias, add, out, sum_out, gradient=_NORM_GRADIENT)
     _dev(x, "x")
     device = x.device
@@ -1138,6 +1169,13 @@ def layer_norm_grad(dy: torch.Tensor, h: torch.Tensor, mean: torch.Tensor, rstd:
     `accumulate` added to; new where not given, dweight where there is a weight,
     dbias as `bias` says (None: as the weight). Without `ws` the call takes its
     workspace from torch's allocator. Not recorded by autograd, as ``rel_bias``."""
+    if (out is None and dx is None and dweight is None and dbias is None and not accumulate and
+            ws is None and stream is None and dy.is_cuda):
+        here = _this_device()
+        r = _calls.layer_norm_grad(here, _stream_of(here), dy, h, mean, rstd, weight, add, p, seed,
+                                   bias)
+        if r is not None:
+            return NormGrad(*r)
     _no_graph("layer_norm_grad", dy, h, weight, add, out, dx, dweight, dbias,
               gradient=_NORM_GRADIENT)
     _dev(dy, "dy")
@@ -1220,6 +1258,12 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None,
     tells of targets outside the vocabulary (their logp is NaN). Without `ws` the
     call takes its workspace from torch's allocator. Not recorded by autograd, as
     ``rel_bias``."""
+    if ws is None and stream is None and logits.is_cuda:
+        here = _this_device()
+        r = _calls.token_logprobs(here, _stream_of(here), logits, targets, scale, top, ignore,
+                                  dev_err)
+        if r is not None:
+            return TokenLogprobs(*r)
     _no_graph("token_logprobs", logits, gradient=_LOGP_GRADIENT)
     _dev(logits, "logits")
     device = logits.device
@@ -1260,6 +1304,12 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor],
     of logp (dlogp) and of the entropy (dentropy, with the entropy itself), and
     what ``token_logprobs`` returned. `out` may be the logits. Not recorded by
     autograd, as ``rel_bias``."""
+    if out is None and stream is None and logits.is_cuda:
+        here = _this_device()
+        r = _calls.token_logprobs_grad(here, _stream_of(here), logits, targets, peak, log_sum, dlogp,
+                                       entropy, dentropy, scale, ignore)
+        if r is not None:
+            return r[0]
     _no_graph("token_logprobs_grad", logits, dlogp, dentropy, out, gradient=_LOGP_GRADIENT)
     _dev(logits, "logits")
     device = logits.device
