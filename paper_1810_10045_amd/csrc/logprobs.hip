@@ -505,7 +505,7 @@ constexpr int kJoinThreads = 256;
 
 template <typename T, bool TOP>
 __global__ __launch_bounds__(kJoinThreads) void k_logp_join(LogpArgs a, uint32_t first) {
-  constexpr int P = Patch<T>::P;
+  constexpr int P = Patch<T>::P, U = 4;
   __shared__ Sums lds[kJoinThreads / kWave];
   __shared__ std::conditional_t<TOP, TopSpace<kJoinThreads>, NoSpace> space;
   const int64_t row = first + static_cast<int64_t>(blockIdx.x);
@@ -539,11 +539,13 @@ __global__ __launch_bounds__(kJoinThreads) void k_logp_join(LogpArgs a, uint32_t
   if constexpr (TOP) {
     const T* x = static_cast<const T*>(a.logits) + row * a.ld;
     const int vectors = (a.V + P - 1) / P;
-    auto look = [&](int v, int end, auto f) {
-      if (v >= end) return;
-      const Span<T, Ends::PART> s(static_cast<int64_t>(v) * P, a.V);
+    auto span = [&](int v) {
+      return Span<T, Ends::PART>(static_cast<int64_t>(v) * P, a.V, v < vectors);
+    };
+    auto look = [&](int v, const typename Patch<T>::raw_t& r, auto f) {
+      const auto s = span(v);
       float y[P];
-      s.widen(s.load(x), y);
+      s.widen(r, y);
 #pragma unroll
       for (int e = 0; e < P; ++e)
         if (e < s.have) f(y[e], static_cast<uint32_t>(v * P + e));
@@ -565,15 +567,26 @@ __global__ __launch_bounds__(kJoinThreads) void k_logp_join(LogpArgs a, uint32_t
             return;
           }
           const int turns = (a.part_vectors + kPartThreads - 1) / kPartThreads;
-          for (int i = threadIdx.x; i < groups * turns * 4; i += kJoinThreads) {
-            const int g = space.list[i / (turns * 4)], j = i % (turns * 4);
-            const int v0 = g / kMaxima * a.part_vectors;
-            const int v1 = a.part_vectors < vectors - v0 ? v0 + a.part_vectors : vectors;
-            look(v0 + g % kMaxima * 4 + j % 4 + j / 4 * kPartThreads, v1, f);
+          const int each = turns * 4, all = groups * each;
+          for (int i0 = threadIdx.x; i0 - mine_at < all; i0 += kJoinThreads * U) {
+            typename Patch<T>::raw_t r[U];
+            int v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const int i = i0 + u * kJoinThreads;
+              const int at = i < all ? i / each : 0, j = i - at * each;
+              const int g = space.list[at], part = g / kMaxima;
+              const int in = g % kMaxima * 4 + j % 4 + j / 4 * kPartThreads;
+              v[u] = i < all && in < a.part_vectors ? part * a.part_vectors + in : vectors;
+              r[u] = span(v[u]).load(x);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if (v[u] < vectors) look(v[u], r[u], f);
           }
         },
         [&](auto f) {
-          for (int v = threadIdx.x; v < vectors; v += kJoinThreads) look(v, vectors, f);
+          for (int v = threadIdx.x; v < vectors; v += kJoinThreads) look(v, span(v).load(x), f);
         });
   }
   finish_row(a, row, t, target, space.top, threadIdx.x, kJoinThreads);
