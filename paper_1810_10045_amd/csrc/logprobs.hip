@@ -309,8 +309,10 @@ __global__ __launch_bounds__(kPartThreads) void k_logp_rows(LogpArgs a, uint32_t
   const int vectors = (a.V + P - 1) / P;
   raw_t r[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+  for (int u = 0; u < U; ++u) {
+    if (u * LANES >= vectors) break;
     r[u] = Span<T, ENDS, uint32_t>((lane + u * LANES) * P, a.V).load(x);
+  }
   const Target target = target_of<T>(a, row);
   float y[U * P];
   Sums t{-kInf, 0.f, 0.f};
@@ -630,6 +632,7 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int v = v0 + u * LANES;
+    if ((tile * U + u) * LANES >= vectors) break;
     r[u] = Span<T, NARROW ? Ends::NARROW : Ends::PART>(static_cast<int64_t>(v) * P, a.V, v < vectors).load(x);
   }
   float dlogp = 0.f;
