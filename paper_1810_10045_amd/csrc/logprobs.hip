@@ -31,16 +31,24 @@ __device__ __forceinline__ float larger(float a, float b) {
 // A row's sums so far: its maximum m (NaN for good once it met one) and, with c = scale log2 e,
 //     s = sum 2^(c x - b),  e = sum 2^(c x - b) (c x - b)
 // relative to b, the fp32 number next to c m: then each exponent is one fma, and b's rounding
-// is known (slip) where the sums are used. Where c m is no number to subtract (masks of the
-// type's lowest value), they are relative to m itself: exponents c (x - m). s and e are 0
-// while m is -infinity.
+// (slip, at most 2^-5) is known where the sums are used. From |c m| = 2^20 on (masks of the
+// type's lowest value among them) that rounding may be as large as the exponents, and they are
+// relative to c m itself: c (x - m). s and e are 0 while m is -infinity.
 struct Sums {
   float m, s, e;
-  static __device__ __forceinline__ bool plain(float b) { return __builtin_fabsf(b) < 1e38f; }
+  static __device__ __forceinline__ bool plain(float b) { return __builtin_fabsf(b) < 0x1p20f; }
+  // c m - b.
+  static __device__ __forceinline__ float slip(float m, float c) {
+    const float b = m * c;
+    return plain(b) ? __builtin_fmaf(m, c, -b) : 0.f;
+  }
   // The sums relative to `to`, which is no less than m.
   __device__ __forceinline__ void rebase(float to, float c) {
 #pragma clang fp contract(off)  // the b of both are rounded numbers
-    float by = __builtin_fmaxf(m * c - to * c, kFarBelow);  // (infinity less itself: far below)
+    float by = m * c - to * c;
+    const bool ok = plain(m * c) && plain(to * c);
+    if (ballot(!ok && m > -kInf)) by = ok ? by : (m - to) * c - slip(m, c) + slip(to, c);
+    by = __builtin_fmaxf(by, kFarBelow);  // (NaN, of infinity less itself, too)
     by = m == to || m == -kInf ? 0.f : by;
     const float f = __builtin_amdgcn_exp2f(by);
     e = f * __builtin_fmaf(s, by, e);
@@ -53,11 +61,6 @@ struct Sums {
     o.rebase(to, c);
     s += o.s;
     e += o.e;
-  }
-  // c m - b.
-  __device__ __forceinline__ float slip(float c) const {
-    const float b = m * c;
-    return plain(b) ? __builtin_fmaf(m, c, -b) : 0.f;
   }
 };
 
@@ -244,7 +247,7 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const
                                            int threads) {
   const bool bad = !(t.m < kInf);  // a NaN or +infinity among the logits
   const float nan = __builtin_nanf("");
-  const float slip = t.slip(a.c), mean = t.e / t.s;
+  const float slip = Sums::slip(t.m, a.c), mean = t.e / t.s;
   // s = 2^slip sum 2^(c (x - m)); c's own rounding moves its logarithm by the mean exponent.
   const float log_sum = logf(t.s) - kLn2 * (slip + a.c_off * (mean - slip));
   if (tid == 0) {

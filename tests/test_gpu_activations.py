@@ -507,6 +507,30 @@ def test_token_logprobs_far_from_zero(lz, dtype):
     close(got, ref, tol, "dlogits", dtype)
 
 
+@pytest.mark.parametrize("power", [0, 31, 100])
+@pytest.mark.parametrize("size", [15, 19, 20, 22, 25, 31, 60])
+@pytest.mark.parametrize("N,V", [(3, 500), (4, 9000), (2, 40_000)])
+def test_token_logprobs_of_any_size(lz, power, size, N, V):
+    """Rows around plus and minus 2^power whose exponents are around 2^size, and rows that hold
+    both: neighbouring fp32 numbers count for what their difference is."""
+    gen = gen_of("size", power, size, V)
+    step = 2.0 ** (power - 23)
+    x = torch.randint(-20, 21, (N, V), generator=gen, device=DEV) * step + 2.0 ** power
+    x[1] *= -1
+    if N > 2:
+        x[2, ::2] *= -1
+    x[0, : V // 2] -= 2.0 ** (power - 1)  # the first half is less, or nothing, beside the second
+    t = torch.randint(V // 2, V, (N,), generator=gen, device=DEV)
+    scale = 2.0 ** (size - power)
+    r, _ = check_logprobs(lz, x, t, scale, 5)
+    check_logprobs(lz, x, t, scale, 0)
+    a = torch.ones(N, device=DEV)
+    ref, tol = A.logprobs_grad(wide(x), t.cpu().numpy(), wide(r.peak), wide(r.log_sum), scale, wide(a),
+                               wide(r.entropy), wide(a))
+    close(lz.token_logprobs_grad(x, t, r.peak, r.log_sum, a, r.entropy, a, scale=scale), ref, tol,
+          "dlogits")
+
+
 def test_token_logprobs_ties(lz):
     """Equal logits: the lowest ids, also where more are equal than are kept as candidates, in
     rows that are cut into parts and rows that are not."""
