@@ -607,7 +607,7 @@ struct LogpGradArgs {
   const void* targets;
   int64_t ignore;
   int wide;
-  float scale;
+  float scale, c;  // c: scale log2 e
   const float *peak, *log_sum, *dlogp, *entropy, *dentropy;
   void* out;
   int64_t ld_out;
@@ -648,7 +648,7 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
       target = id < 0 || id >= a.V ? -1 : static_cast<int>(id);
     }
   }
-  const float peak = a.peak[row], log_sum = a.log_sum[row];
+  const float peak = a.peak[row], log_sum = a.log_sum[row], log2_sum = log_sum * kLog2e;
   float entropy = 0.f, dentropy = 0.f;
   if constexpr (ENTROPY) {
     entropy = a.entropy[row];
@@ -666,20 +666,32 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
     s.widen(r[u], y);
 #pragma unroll
     for (int e = 0; e < P; ++e) {
-      const float l = __builtin_fmaf(y[e] - peak, a.scale, -log_sum);
-      const float z = l * kLog2e;
-      float q = __builtin_amdgcn_exp2f(z);
+      float l, q;
       if constexpr (sizeof(T) == 4) {
-        // fp32 gradients: z's rounding and the rest of log2 e, to first order
+        // fp32 gradients: the exponent's rounding and the rest of log2 e, to first order
         constexpr float kRest = 1.925963033e-8f;  // log2 e - kLog2e
-        const float rest = __builtin_fmaf(l, kLog2e, -z) + l * kRest;
+        l = __builtin_fmaf(y[e] - peak, a.scale, -log_sum);
+        const float z = l * kLog2e, rest = __builtin_fmaf(l, kLog2e, -z) + l * kRest;
+        q = __builtin_amdgcn_exp2f(z);
         q = l > kFarBelow ? __builtin_fmaf(q, rest * kLn2, q) : q;
+      } else {
+        const float z = __builtin_fmaf(y[e] - peak, a.c, -log2_sum);
+        q = __builtin_amdgcn_exp2f(z);
+        l = z * kLn2;
       }
       float d = -dlogp * q;
       if constexpr (ENTROPY)
         d = __builtin_fmaf(-dentropy * q, __builtin_fmaxf(l, kFarBelow) + entropy, d);
-      d += v * P + e == target ? dlogp : 0.f;
-      y[e] = none ? 0.f : d;
+      y[e] = d;
+    }
+    const int hit = target - v * P;
+    if (hit >= 0 && hit < P) {
+#pragma unroll
+      for (int e = 0; e < P; ++e) y[e] += e == hit ? dlogp : 0.f;
+    }
+    if (none) {
+#pragma unroll
+      for (int e = 0; e < P; ++e) y[e] = 0.f;
     }
     s.store(out, y);
   }
@@ -805,7 +817,8 @@ int logp_grad_run(const void* logits, int64_t ld, int64_t N, int64_t V, int dtyp
                   const float* dentropy, void* out, int64_t ld_out, hipStream_t st) {
   if (N == 0) return LM_OK;
   const LogpGradArgs a{logits, ld, N, static_cast<int>(V), 0, targets, ignore, idtype == LM_I64,
-                       scale, peak, log_sum, targets ? dlogp : nullptr, entropy, dentropy, out,
+                       scale, static_cast<float>(1.4426950408889634 * static_cast<double>(scale)),
+                       peak, log_sum, targets ? dlogp : nullptr, entropy, dentropy, out,
                        ld_out};
   return dtype == LM_BF16 ? grad_lanes<bf16_t>(a, st) : grad_lanes<float>(a, st);
 }
