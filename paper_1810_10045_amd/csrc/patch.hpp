@@ -86,11 +86,13 @@ static inline Ends ends_of(int64_t D, int P) {
   return D < P ? Ends::NARROW : D % P ? Ends::PART : Ends::WHOLE;
 }
 
-// Where a lane's vector of P values at column `col` lies in a row of D. Every load is a whole vector inside the row, so
-// that none stands under a condition: at the row's end it starts at D - P, and the values
-// are moved `by` places down to their own. `have`: how many of them exist. OFF: what holds
-// a column's distance from the row's start in bytes (with uint32_t and a row that the wave
-// shares, an address is that distance in one register beside the row's in scalar ones).
+// Where a lane's vector of P values at column `col` lies in a row of D. Every load (but of
+// NARROW rows) is a whole vector inside the row, so that none stands under a condition: at
+// the row's end it starts at D - P, and the values are moved `by` places down to their own;
+// what else it read is not used, so a row may be written in place by others meanwhile.
+// `have`: how many of the lane's values exist. OFF: what holds a column's distance from the
+// row's start in bytes (with uint32_t and a row that the wave shares, an address is that
+// distance in one register beside the row's in scalar ones).
 template <typename T, Ends ENDS, typename OFF = int64_t>
 struct Span {
   static constexpr int P = Patch<T>::P;
@@ -108,7 +110,8 @@ struct Span {
   template <typename Q>  // T or const T
   static __device__ __forceinline__ Q* at(Q* row, index_t col) {
     using byte_t = std::conditional_t<std::is_const<Q>::value, const char, char>;
-    return reinterpret_cast<Q*>(reinterpret_cast<byte_t*>(row) + static_cast<OFF>(col * static_cast<index_t>(sizeof(T))));
+    return reinterpret_cast<Q*>(reinterpret_cast<byte_t*>(row) +
+                                static_cast<OFF>(col * static_cast<index_t>(sizeof(T))));
   }
   __device__ __forceinline__ raw_t load(const T* row) const {
     if constexpr (!NARROW) return Patch<T>::load(at(row, from));

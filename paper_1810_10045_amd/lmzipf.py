@@ -30,7 +30,7 @@ import torch
 
 # The current stream's handle (not a public name of torch: the public call where it is absent).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-# The current device's number, of a process whose device is in use: a third of the public call's time.
+# The current device's number, where the device is in use already: a third of the public call's time.
 _this_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 # The current stream's handle on a device.
@@ -158,7 +158,8 @@ def _load_calls():
     try:
         from . import _lmzipf_calls as calls
     except ImportError as e:
-        raise ImportError(f"{e}: build it with `python -c 'import __graft_entry__ as g; g.build()'`") from e
+        raise ImportError(
+            f"{e}: build it with `python -c 'import __graft_entry__ as g; g.build()'`") from e
     names = ("lm_dropout", "lm_layer_norm", "lm_layer_norm_grad_workspace_bytes",
              "lm_layer_norm_grad", "lm_token_logprobs_workspace_bytes", "lm_token_logprobs",
              "lm_token_logprobs_grad", "lm_status_string")
@@ -1306,8 +1307,8 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor],
     autograd, as ``rel_bias``."""
     if out is None and stream is None and logits.is_cuda:
         here = _this_device()
-        r = _calls.token_logprobs_grad(here, _stream_of(here), logits, targets, peak, log_sum, dlogp,
-                                       entropy, dentropy, scale, ignore)
+        r = _calls.token_logprobs_grad(here, _stream_of(here), logits, targets, peak, log_sum,
+                                       dlogp, entropy, dentropy, scale, ignore)
         if r is not None:
             return r[0]
     _no_graph("token_logprobs_grad", logits, dlogp, dentropy, out, gradient=_LOGP_GRADIENT)

@@ -233,6 +233,52 @@ def test_memory_of_a_side_streams_results(lz):
     assert all(bool((t == 7.0).all()) for t in new)
 
 
+def test_plain_calls_are_the_other_calls(lz):
+    """Calls that go through the extension module and the same calls that do not (an output, a
+    workspace or a stream of the caller's): the same results, of the same shapes."""
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    here = torch.cuda.current_stream()
+    ws = lz.Workspace(DEV)
+    seed = torch.tensor([77], device=DEV)
+    for dtype in (F32, BF16):
+        x, add, dy = (torch.randn(2, 9, 130, generator=gen, device=DEV).to(dtype) for _ in range(3))
+        w, b = torch.randn(2, 130, generator=gen, device=DEV).unbind()
+        for s in (77, seed):
+            for a in (None, add):
+                got, want = lz.dropout(x, 0.3, s, add=a), torch.empty_like(x)
+                lz.dropout(x, 0.3, 77, add=a, out=want)
+                assert torch.equal(got, want)
+                for p in (0.0, 0.3):
+                    f = lz.layer_norm(x, w, b, add=a, p=p, seed=s)
+                    g = lz.layer_norm(x, w, b, add=a, p=p, seed=s, stream=here)
+                    assert all(torch.equal(u, v) and u.shape == v.shape for u, v in zip(f, g))
+                    assert (f.h is x) == (g.h is x)
+                    for bias in (None, True, False):
+                        f2 = lz.layer_norm_grad(dy, f.h, f.mean, f.rstd, w, a, p, s, bias=bias)
+                        g2 = lz.layer_norm_grad(dy, f.h, f.mean, f.rstd, w, a, p, s, bias=bias, ws=ws)
+                        assert (f2.dbias is None) == (bias is False) == (g2.dbias is None)
+                        for u, v in zip(f2, g2):
+                            assert u is v is None or torch.equal(u, v)
+                        assert (f2.dx is f2.dh) == (p == 0)
+        for V in (130, 9000):
+            z = torch.randn(3, V, generator=gen, device=DEV).to(dtype)
+            t = torch.tensor([1, -100, V - 1], device=DEV)
+            for targets in (None, t, t.int()):
+                for top in (0, 4):
+                    f = lz.token_logprobs(z, targets, 0.5, top)
+                    g = lz.token_logprobs(z, targets, 0.5, top, stream=here)
+                    for u, v in zip(f, g):
+                        assert u is v is None or (torch.equal(u, v) and u.dtype == v.dtype)
+            dl = torch.randn(3, generator=gen, device=DEV)
+            f = lz.token_logprobs_grad(z, t, g.peak, g.log_sum, dl, g.entropy, dl, 0.5)
+            assert torch.equal(f, lz.token_logprobs_grad(z, t, g.peak, g.log_sum, dl, g.entropy, dl,
+                                                         0.5, out=torch.empty_like(z)))
+    p = torch.nn.Parameter(torch.randn(4, 8, device=DEV))
+    with torch.no_grad():
+        assert not lz.dropout(p, 0.5, 1).requires_grad
+        assert torch.equal(lz.layer_norm(p).y, lz.layer_norm(p.detach()).y)
+
+
 # ---------------------------------------------------------------------------
 # Autograd
 # ---------------------------------------------------------------------------
