@@ -642,7 +642,7 @@ int lm_dropout(const void* x, int64_t ld_x, const void* add, int64_t ld_add, voi
  * dweight, dbias  every value written (accumulate 0) or added to (1), or NULL.
  * ws         device workspace of lm_layer_norm_grad_workspace_bytes(...) bytes
  *            where dweight or dbias is given, 4-byte aligned, no initial
- *            contents required (0 rows: NULL). */
+ *            contents required (0 bytes for few rows: NULL). */
 #define LM_NORM_MAX_WIDTH 16384
 int lm_layer_norm(const void* x, int64_t ld_x, const void* add, int64_t ld_add, int64_t rows,
                   int64_t D, int32_t dtype, const float* weight, const float* bias, float eps,

@@ -21,18 +21,12 @@ struct NormArgs {
   KeepArgs keep;
 };
 
-// Rows of a group, all of their loads under way at once. 200,000 rows of 128 bf16: 21 us, one
-// row a group 24; with several vectors a lane there is no difference, and 256 rows of 2048 take
-// 5.8 us, one row a group 4.3.
-template <typename S>
-constexpr int kNormBatch = S::NV == 1 && S::WAVES == 1 ? 2 : 1;
-
 template <typename T, typename S, bool ADD, Ends ENDS>
 __global__ __launch_bounds__(S::kThreads) void k_norm(NormArgs a, uint32_t first) {
-  constexpr int P = Patch<T>::P, NV = S::NV, R = kNormBatch<S>;
+  constexpr int P = Patch<T>::P, NV = S::NV, R = S::ROWS;
   using raw_t = typename Patch<T>::raw_t;
   __shared__ float part[2][S::kThreads / kWave][R];
-  const int64_t i0 = ((first + static_cast<int64_t>(blockIdx.x)) * S::kRows + S::group()) * R;
+  const int64_t i0 = (first + static_cast<int64_t>(blockIdx.x)) * S::kRows + S::group() * R;
   const int lane = threadIdx.x % S::kGroup;
   raw_t rx[R][NV], ra[R][NV];
 #pragma unroll
@@ -118,23 +112,28 @@ __global__ __launch_bounds__(S::kThreads) void k_norm(NormArgs a, uint32_t first
 
 // Calls f with the shape for rows of D values of type T. Waves of their own, which wait for
 // no other, where there are rows enough to fill the device (65,536 x 2048 bf16: 190 us, 206
-// with four waves a row; 4099 x 517 fp32 6.2 and 8.9); rows that are few are spread over
-// more waves (1 x 2048 bf16: 2.3 us with four waves, 3.7 with one; 256 rows 2.9 and 4.3; at 2048
-// rows both take 8.5).
+// with four waves a row; 4099 x 517 fp32 6.2 and 8.9), short rows two at a time (200,000 x 128
+// bf16: 21 us, one at a time 24). Rows that are few are spread over more waves (1 x 2048 bf16:
+// 2.3 us with four waves, 3.7 with one; 256 rows 2.9 and 4.3; at 2048 rows both take 8.5), one
+// at a time (700 x 128 bf16: 2.6 us, two at a time 3.0; 1000 x 500 4.0 and 4.6).
 template <typename T, typename F>
 static inline int norm_shape(int64_t rows, int64_t D, F f) {
   constexpr int64_t most = LM_NORM_MAX_WIDTH / Patch<T>::P;
   const int64_t vectors = (D + Patch<T>::P - 1) / Patch<T>::P;
-  if (vectors <= 8) return f(NormShape<8, 1, 1>{});
-  if (vectors <= 16) return f(NormShape<16, 1, 1>{});
-  if (vectors <= 32) return f(NormShape<32, 1, 1>{});
-  if (vectors <= 64) return f(NormShape<64, 1, 1>{});
   if (rows <= 1024) {
+    if (vectors <= 8) return f(NormShape<8, 1, 1>{});
+    if (vectors <= 16) return f(NormShape<16, 1, 1>{});
+    if (vectors <= 32) return f(NormShape<32, 1, 1>{});
+    if (vectors <= 64) return f(NormShape<64, 1, 1>{});
     if (vectors <= 128) return f(NormShape<64, 2, 1>{});
     if (vectors <= 256) return f(NormShape<64, 4, 1>{});
     if (vectors <= 512) return f(NormShape<64, 8, 1>{});
     if (vectors <= 1024) return f(NormShape<64, 16, 1>{});
   }
+  if (vectors <= 8) return f(NormShape<8, 1, 1, 2>{});
+  if (vectors <= 16) return f(NormShape<16, 1, 1, 2>{});
+  if (vectors <= 32) return f(NormShape<32, 1, 1, 2>{});
+  if (vectors <= 64) return f(NormShape<64, 1, 1, 2>{});
   if (vectors <= 128) return f(NormShape<64, 1, 2>{});
   if (vectors <= 192) return f(NormShape<64, 1, 3>{});
   if (vectors <= 256) return f(NormShape<64, 1, 4>{});
@@ -152,8 +151,7 @@ static int norm_launch(const NormArgs& a, hipStream_t st) {
       constexpr Ends kEnds = decltype(ends)::value;
       return a.add ? k_norm<T, S, true, kEnds> : k_norm<T, S, false, kEnds>;
     });
-    constexpr int kRows = S::kRows * kNormBatch<S>;
-    return launch_parts((a.rows + kRows - 1) / kRows, S::kThreads,
+    return launch_parts((a.rows + S::kRows - 1) / S::kRows, S::kThreads,
                         [&](uint32_t first, uint32_t n) {
                           kernel<<<n, S::kThreads, 0, st>>>(a, first);
                           return launch_status(hipGetLastError());

@@ -17,16 +17,16 @@ struct NormGradArgs {
   const void *dy, *h, *add;
   const float *mean, *rstd, *weight;
   void *dh, *dx;
-  float* sums;  // [workgroups][2][D]: dweight, dbias; or nullptr
+  // Where the first workgroup's sums go, the others' lying `pitch` behind one another. A
+  // workgroup without others writes the results.
+  float *dweight, *dbias;
+  int64_t pitch;
+  int accumulate;
   int64_t ld_dy, ld_h, ld_add, ld_dh, ld_dx, rows;
   int D;
   float inv_d;
   KeepArgs keep;
 };
-
-// Rows of a group, all of their loads under way at once.
-template <typename T, typename S>
-constexpr int kBatch = S::NV * Patch<T>::P > 8 ? 1 : 2;
 
 // The value of an operand that is kept as it was loaded, and not widened, between its uses.
 __device__ __forceinline__ f32x4 kept(f32x4 x) {
@@ -40,7 +40,7 @@ __device__ __forceinline__ u32x4 kept(u32x4 x) {
 
 template <typename T, typename S, bool ADD, Ends ENDS>
 __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
-  constexpr int P = Patch<T>::P, NV = S::NV, R = kBatch<T, S>;
+  constexpr int P = Patch<T>::P, NV = S::NV, R = S::ROWS;
   constexpr int kWaves = S::kThreads / kWave;
   using raw_t = typename Patch<T>::raw_t;
   __shared__ float part[2][kWaves][2 * R];
@@ -51,16 +51,18 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const NormSpan<T, ENDS> s((lane + v * S::kGroup) * P, a.D);
-    if (a.weight) load_params(a.weight, s, w[v]);
+    if (a.weight) {
+      load_params(a.weight, s, w[v]);  // under way until the first turn uses them
+    } else {
 #pragma unroll
-    for (int e = 0; e < P; ++e) {
-      w[v][e] = a.weight ? w[v][e] : 1.f;
-      dw[v][e] = db[v][e] = 0.f;
+      for (int e = 0; e < P; ++e) w[v][e] = 1.f;
     }
+#pragma unroll
+    for (int e = 0; e < P; ++e) dw[v][e] = db[v][e] = 0.f;
   }
   int turn = 0;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows * R;
-  for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * S::kRows * R; i0 < a.rows; i0 += step) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * S::kRows;
+  for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * S::kRows; i0 < a.rows; i0 += step) {
     raw_t ry[R][NV], rh[R][NV], ra[R][NV];
     float mean[R], rstd[R];
 #pragma unroll
@@ -141,12 +143,17 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
       }
     }
   }
-  if (!a.sums) return;
+  if (!a.dweight && !a.dbias) return;
   // The groups' sums, added in their order: of a wave by their lanes, of the waves in LDS.
   constexpr int kGroups = S::kThreads / (S::kGroup > kWave ? S::kGroup : kWave);
   constexpr int kCols = S::kGroup * NV * P;
   __shared__ float joined[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kCols : 1];
-  float* mine = a.sums + static_cast<int64_t>(blockIdx.x) * 2 * a.D;
+  auto put = [&](int k, int col, float x) {
+    if (float* out = k ? a.dbias : a.dweight) {
+      out += blockIdx.x * a.pitch + col;
+      *out = a.accumulate ? *out + x : x;
+    }
+  };
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     if (k && kGroups > 1) __syncthreads();
@@ -162,7 +169,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
         if constexpr (kGroups > 1) {
           joined[threadIdx.x / (kGroups > 1 ? S::kThreads / kGroups : 1)][col] = x;
         } else if (e < s.have) {
-          mine[k * a.D + col] = x;
+          put(k, col, x);
         }
       }
     }
@@ -172,7 +179,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
         float x = joined[0][c];
 #pragma unroll
         for (int g = 1; g < kGroups; ++g) x += joined[g][c];
-        mine[k * a.D + c] = x;
+        put(k, c, x);
       }
     }
   }
@@ -208,43 +215,52 @@ __global__ __launch_bounds__(kJoinThreads) void k_norm_join(const float* sums, i
   *out = accumulate ? *out + y : y;
 }
 
-// Calls f with the shape for rows of D values of type T, in workgroups of THREADS.
-template <typename T, int THREADS, typename F>
+// Calls f with the shape for rows of D values of type T, in workgroups of THREADS that take up
+// to MOST rows a group at once.
+template <typename T, int THREADS, int MOST, typename F>
 static inline int grad_shape(int64_t D, F f) {
   constexpr int P = Patch<T>::P;
   const int64_t vectors = (D + P - 1) / P;
-  if (vectors <= 8) return f(NormShape<8, 1, 1, THREADS>{});
-  if (vectors <= 16) return f(NormShape<16, 1, 1, THREADS>{});
-  if (vectors <= 32) return f(NormShape<32, 1, 1, THREADS>{});
-  if (vectors <= 64) return f(NormShape<64, 1, 1, THREADS>{});
-  if (D <= 512) return f(NormShape<64, 1, 8 / P, THREADS>{});
-  if (D <= 1024) return f(NormShape<64, 2, 8 / P, THREADS>{});
-  if (D <= 2048) return f(NormShape<64, 4, 8 / P, THREADS>{});
-  if (D <= 4096) return f(NormShape<64, 4, 16 / P, THREADS>{});
-  if (D <= 8192) return f(NormShape<64, 8, 16 / P, THREADS>{});
+  if (vectors <= 8) return f(NormShape<8, 1, 1, MOST, THREADS>{});
+  if (vectors <= 16) return f(NormShape<16, 1, 1, MOST, THREADS>{});
+  if (vectors <= 32) return f(NormShape<32, 1, 1, MOST, THREADS>{});
+  if (vectors <= 64) return f(NormShape<64, 1, 1, MOST, THREADS>{});
+  if (D <= 512) return f(NormShape<64, 1, 8 / P, MOST, THREADS>{});
+  if (D <= 1024) return f(NormShape<64, 2, 8 / P, MOST, THREADS>{});
+  if (D <= 2048) return f(NormShape<64, 4, 8 / P, MOST, THREADS>{});
+  if (D <= 4096) return f(NormShape<64, 4, 16 / P, 1, THREADS>{});
+  if (D <= 8192) return f(NormShape<64, 8, 16 / P, 1, THREADS>{});
   static_assert(LM_NORM_MAX_WIDTH == 16384, "the widest shape");
-  return f(NormShape<64, 16, 16 / P, THREADS>{});
+  return f(NormShape<64, 16, 16 / P, 1, THREADS>{});
 }
 
-// Workgroups of the pass, at most kGradBlocks: each leaves 2 D sums behind, so that fewer and
-// larger ones cost less where every one has but a turn or two: 1280 x 1792 fp32 takes 12.4 us
+// Workgroups of the pass, at most kGradBlocks. Each leaves 2 D sums behind, so that fewer and
+// larger ones cost less where every one has but a turn or two: 1280 x 1792 fp32 takes 12.9 us
 // with 160 of 1024 threads, 14.4 with 320 of 512 (16,384 x 1000 fp32 44 and 41).
 constexpr int64_t kGradBlocks = 512;
 
+// Rows that up to this many workgroups of one wave a SIMD hold, a row a group, go to these, as
+// the instructions of the four waves of a larger one follow each other: 27 x 459 bf16 takes 6.4
+// us, 11.0 otherwise, 700 x 480 6.9 and 9.5, 200 x 650 fp32 7.6 and 12.8. More sums than
+// kGradSums cost what that saves (2000 x 480 bf16: 9.9 and 9.8; 256 x 2048 11.1 and 10.3).
+constexpr int64_t kGradSmall = 384, kGradSums = int64_t(1) << 19;
+
 template <typename T, typename F>
 static inline int norm_grad_shape(int64_t rows, int64_t D, F f) {
-  const bool few = grad_shape<T, 512>(D, [&](auto shape) {
-    using S = decltype(shape);
-    return rows <= kGradBlocks * S::kRows * kBatch<T, S> ? 1 : 0;
-  });
-  return few ? grad_shape<T, 1024>(D, f) : grad_shape<T, 512>(D, f);
+  const int64_t few = kGradSums / (2 * D) < kGradSmall ? kGradSums / (2 * D) : kGradSmall;
+  const auto fit = [rows](int64_t blocks) {
+    return [rows, blocks](auto shape) { return rows <= blocks * decltype(shape)::kRows ? 1 : 0; };
+  };
+  if (grad_shape<T, 256, 1>(D, fit(few))) return grad_shape<T, 256, 1>(D, f);
+  return grad_shape<T, 512, 2>(D, fit(kGradBlocks)) ? grad_shape<T, 1024, 2>(D, f)
+                                                    : grad_shape<T, 512, 2>(D, f);
 }
 
 template <typename T>
 static int64_t grad_blocks(int64_t rows, int64_t D) {
   return norm_grad_shape<T>(rows, D, [&](auto shape) {
     using S = decltype(shape);
-    const int64_t n = (rows + S::kRows * kBatch<T, S> - 1) / (S::kRows * kBatch<T, S>);
+    const int64_t n = (rows + S::kRows - 1) / S::kRows;  // turns
     return static_cast<int>(n < kGradBlocks ? n : kGradBlocks);
   });
 }
@@ -253,7 +269,8 @@ static int64_t norm_grad_blocks(int64_t rows, int64_t D, int dtype) {
 }
 
 size_t norm_grad_workspace_bytes(int64_t rows, int64_t D, int dtype) {
-  return static_cast<size_t>(norm_grad_blocks(rows, D, dtype)) * 2 * D * sizeof(float);
+  const int64_t blocks = norm_grad_blocks(rows, D, dtype);
+  return blocks <= 1 ? 0 : static_cast<size_t>(blocks) * 2 * D * sizeof(float);
 }
 
 template <typename T>
@@ -274,22 +291,24 @@ int norm_grad_run(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, co
                   const float* rstd, const float* weight, float p, uint64_t seed,
                   const int64_t* seed_at, void* dh, int64_t ld_dh, void* dx, int64_t ld_dx,
                   float* dweight, float* dbias, int accumulate, void* ws, hipStream_t st) {
-  const bool sums = dweight || dbias;
   const int blocks = static_cast<int>(norm_grad_blocks(rows, D, dtype));
+  const bool join = (dweight || dbias) && blocks != 1;
+  float* sums = static_cast<float*>(ws);
   if (rows > 0) {
     const NormGradArgs a{dy, h, add, mean, rstd, weight, dh, dx,
-                         sums ? static_cast<float*>(ws) : nullptr, ld_dy, ld_h, ld_add, ld_dh,
-                         ld_dx, rows, static_cast<int>(D),
+                         join ? sums : dweight, join ? sums + D : dbias, 2 * D,
+                         !join && accumulate, ld_dy, ld_h, ld_add, ld_dh, ld_dx, rows,
+                         static_cast<int>(D),
                          static_cast<float>(1.0 / static_cast<double>(D)),
                          make_keep(p, seed, dx ? seed_at : nullptr)};
     const int rc = dtype == LM_BF16 ? norm_grad_launch<bf16_t>(a, blocks, st)
                                     : norm_grad_launch<float>(a, blocks, st);
     if (rc != LM_OK) return rc;
   }
-  if (!sums) return LM_OK;
+  if (!join) return LM_OK;
   const int cols = static_cast<int>(2 * D);
   k_norm_join<<<(cols + kJoinCols - 1) / kJoinCols, kJoinThreads, 0, st>>>(
-      static_cast<const float*>(ws), blocks, static_cast<int>(D), dweight, dbias, accumulate);
+      sums, blocks, static_cast<int>(D), dweight, dbias, accumulate);
   return launch_status(hipGetLastError());
 }
 

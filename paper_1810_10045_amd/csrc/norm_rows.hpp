@@ -1,7 +1,7 @@
 // Layer norm: how a row is shared out among lanes, for the forward and the backward pass.
 // A row stays in the registers of its group: LANES lanes of a wave, or WAVES whole waves,
 // NV vectors of 16 bytes a lane, vector v of lane l being number l + v * lanes (a wave's
-// lanes load neighbouring vectors).
+// lanes load neighbouring vectors). A group takes ROWS rows at once, all of their loads under way.
 #pragma once
 
 #include "keep.hpp"
@@ -11,16 +11,17 @@ namespace lmz {
 
 constexpr int kNormThreads = 256;  // of a workgroup, where a row's group is no larger
 
-template <int LANES_, int WAVES_, int NV_, int THREADS_ = kNormThreads>
+template <int LANES_, int WAVES_, int NV_, int ROWS_ = 1, int THREADS_ = kNormThreads>
 struct NormShape {
-  static constexpr int LANES = LANES_, WAVES = WAVES_, NV = NV_;
+  static constexpr int LANES = LANES_, WAVES = WAVES_, NV = NV_, ROWS = ROWS_;
   static constexpr int kGroup = WAVES > 1 ? WAVES * kWave : LANES;  // lanes of a row
   static constexpr int kThreads = kGroup > THREADS_ ? kGroup : THREADS_;
-  static constexpr int kRows = kThreads / kGroup;  // rows of a workgroup at once
+  static constexpr int kGroups = kThreads / kGroup;  // of a workgroup
+  static constexpr int kRows = kGroups * ROWS;       // of a workgroup at once
   static_assert(WAVES == 1 || LANES == kWave, "whole waves");
   // The thread's group in its workgroup, in a scalar register where a wave has but one.
   static __device__ __forceinline__ int group() {
-    if constexpr (kRows == 1) return 0;
+    if constexpr (kGroups == 1) return 0;
     const int g = threadIdx.x / kGroup;
     return kGroup >= kWave ? first_lane(g) : g;
   }

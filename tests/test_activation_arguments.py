@@ -44,7 +44,7 @@ class Calls:
         return self.lib.lm_layer_norm(x, ld_x, add, ld_add, rows, D, dtype, weight, bias, eps, p, 1,
                                       seed_at, y, ld_y, h, ld_h, mean, rstd, None)
 
-    def norm_grad(self, dy=1 * FAR, ld_dy=8, h=2 * FAR, ld_h=8, add=None, ld_add=0, rows=4, D=8,
+    def norm_grad(self, dy=1 * FAR, ld_dy=8, h=2 * FAR, ld_h=8, add=None, ld_add=0, rows=4000, D=8,
                   dtype=F32, mean=3 * FAR, rstd=4 * FAR, weight=5 * FAR, p=0.0, dh=6 * FAR, ld_dh=8,
                   dx=None, ld_dx=0, dw=7 * FAR, db=8 * FAR, ws=9 * FAR, ws_bytes=1 << 18):
         return self.lib.lm_layer_norm_grad(dy, ld_dy, h, ld_h, add, ld_add, rows, D, dtype, mean,
@@ -115,10 +115,16 @@ def test_layer_norm_refusals(c, kw, code):
     (dict(ws=9 * FAR + 2), INVAL), (dict(ld_dy=7), INVAL), (dict(ld_dh=7), INVAL),
     (dict(dx=6 * FAR, ld_dx=8), INVAL),             # dx and dh in one place
     (dict(dx=2 * FAR, ld_dx=9), INVAL),             # over h, at other rows
-    (dict(dw=8 * FAR - 4), INVAL), (dict(dw=5 * FAR), INVAL), (dict(dw=3 * FAR, D=4), INVAL), (dict(ws=7 * FAR - 60), INVAL),
+    (dict(dw=8 * FAR - 4), INVAL), (dict(dw=5 * FAR), INVAL), (dict(dw=3 * FAR), INVAL), (dict(ws=7 * FAR - 60), INVAL),
     (dict(dh=3 * FAR - 4), INVAL), (dict(add=6 * FAR + 4, ld_add=8), INVAL)])
 def test_layer_norm_grad_refusals(c, kw, code):
     assert c.norm_grad(**kw) == code
+
+
+def test_layer_norm_grad_of_few_rows_needs_no_workspace(c):
+    """(refused for another reason, so that nothing is launched)"""
+    assert c.norm_grad(rows=4, ws=None, ws_bytes=0, dw=5 * FAR) == INVAL
+    assert c.norm_grad(rows=4, ws=None, ws_bytes=0, dw=8 * FAR - 4) == INVAL
 
 
 def test_layer_norm_grad_workspace(lz):
@@ -128,8 +134,9 @@ def test_layer_norm_grad_workspace(lz):
     for rows in (1, 100, 5000, 1 << 20):
         for D in (1, 8, 517, 2048, 16384):
             for t in (F32, BF16):
-                assert 8 * D <= f(rows, D, t) <= 512 * 8 * D
-    assert f(1 << 20, 2048, BF16) >= f(100, 2048, BF16)
+                assert f(rows, D, t) % (8 * D) == 0 and f(rows, D, t) <= 512 * 8 * D
+    assert f(1 << 20, 2048, BF16) >= f(100, 2048, BF16) > 0
+    assert f(1, 2048, BF16) == 0  # one workgroup writes the results itself
 
 
 @pytest.mark.parametrize("kw,code", [

@@ -341,9 +341,10 @@ def test_layer_norm_in_place(lz, dtype, D):
         assert torch.equal(got, ref)
 
 
-def test_layer_norm_grad_accumulates(lz):
-    gen = gen_of("accumulate")
-    h, dy = (rows_of(gen, 300, 77, BF16) for _ in range(2))
+@pytest.mark.parametrize("rows", [1, 5, 130, 300, 5000])
+def test_layer_norm_grad_accumulates(lz, rows):
+    gen = gen_of("accumulate", rows)
+    h, dy = (rows_of(gen, rows, 77, BF16) for _ in range(2))
     w, _ = params(gen, 77)
     s = lz.layer_norm(h)
     one = lz.layer_norm_grad(dy, h, s.mean, s.rstd, w)
