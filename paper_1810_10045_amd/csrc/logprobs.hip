@@ -134,6 +134,19 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t x) {
   return x;
 }
 
+// Of n different keys the k largest to their places in `top`, by THREADS threads.
+template <int THREADS>
+__device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int k, uint64_t* top,
+                                          int tid) {
+  for (int i = tid; i < n; i += THREADS) {
+    const uint64_t key = keys[i];
+    int rank = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) rank += keys[j] > key ? 1 : 0;
+    if (rank < k) top[rank] = key;
+  }
+}
+
 // The largest number of groups of LANES lanes, in all of them; NaN if one is.
 template <int LANES>
 __device__ __forceinline__ float lanes_larger(float x) {
@@ -178,13 +191,7 @@ __device__ __forceinline__ void select_top(float mine, int k, TopSpace<THREADS>&
   __syncthreads();
   const int n = t.n;
   if (n <= kTopKeys) {
-    for (int i = tid; i < n; i += THREADS) {
-      const uint64_t key = t.keys[i];
-      int rank = 0;
-#pragma unroll 4
-      for (int j = 0; j < n; ++j) rank += t.keys[j] > key ? 1 : 0;
-      if (rank < k) t.top[rank] = key;
-    }
+    rank_keys<THREADS>(t.keys, n, k, t.top, tid);
     __syncthreads();
     return;
   }
@@ -368,12 +375,7 @@ __global__ __launch_bounds__(kPartThreads) void k_logp_rows(LogpArgs a, uint32_t
     }
     wave_order();
     if (n <= kRowKeys) {
-      for (int j = lane; j < n; j += kWave) {
-        const uint64_t k = key[j];
-        int rank = 0;
-        for (int l = 0; l < n; ++l) rank += key[l] > k ? 1 : 0;
-        if (rank < a.k) best[rank] = k;
-      }
+      rank_keys<kWave>(key, n, a.k, best, lane);
     } else {
       uint64_t last = ~uint64_t(0);
       for (int rank = 0; rank < a.k; ++rank) {
