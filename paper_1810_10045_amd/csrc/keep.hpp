@@ -7,7 +7,7 @@
 // round(65536 p), and multiplied by 1 over the share that is kept: the expectation is
 // exact for the p that is drawn, which is within 2^-17 of the caller's. Two values to a
 // word: the hash's two 32-bit products take a quarter of the vector rate, and a word for
-// each value would cost as much as a large call's memory. Over 2^22 values, kept values correlate
+// each value would cost as much as a large call's memory. Over 2^23 words kept values correlate
 // by 0.001 with their neighbours' and by 0.014 at most where word numbers differ by a power of
 // two (128: 0.014; 65,536: 0.013), and seeds that follow each other not at all.
 #pragma once

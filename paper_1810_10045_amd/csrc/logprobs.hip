@@ -618,7 +618,7 @@ struct LogpGradArgs {
 };
 
 // A workgroup: kGradThreads / LANES rows, of each a tile of LANES * kGradVectors vectors.
-constexpr int kGradThreads = 256, kGradVectors = 4;
+constexpr int kGradThreads = 256, kGradVectors = 2;
 
 template <typename T, int LANES, bool ENTROPY, Ends ENDS>
 __global__ __launch_bounds__(kGradThreads) void k_logp_grad(LogpGradArgs a, uint32_t first) {
