@@ -17,16 +17,16 @@ struct NormGradArgs {
   const void *dy, *h, *add;
   const float *mean, *rstd, *weight;
   void *dh, *dx;
-  // Where the first workgroup's sums go, the others' lying `pitch` behind one another. A
-  // workgroup without others writes the results.
-  float *dweight, *dbias;
-  int64_t pitch;
+  float* sums;  // [workgroups][2][D]: dweight, dbias; or nullptr
+  float *dweight, *dbias;  // of a workgroup without others, which writes the results itself
   int accumulate;
   int64_t ld_dy, ld_h, ld_add, ld_dh, ld_dx, rows;
   int D;
   float inv_d;
   KeepArgs keep;
 };
+
+constexpr int kSmallThreads = 256;  // of a workgroup of few rows
 
 // The value of an operand that is kept as it was loaded, and not widened, between its uses.
 __device__ __forceinline__ f32x4 kept(f32x4 x) {
@@ -143,15 +143,17 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
       }
     }
   }
-  if (!a.dweight && !a.dbias) return;
+  constexpr bool kAlone = S::THREADS == kSmallThreads;  // may have the call to itself
+  if (!a.sums && (!kAlone || (!a.dweight && !a.dbias))) return;
   // The groups' sums, added in their order: of a wave by their lanes, of the waves in LDS.
   constexpr int kGroups = S::kThreads / (S::kGroup > kWave ? S::kGroup : kWave);
   constexpr int kCols = S::kGroup * NV * P;
   __shared__ float joined[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kCols : 1];
   auto put = [&](int k, int col, float x) {
-    if (float* out = k ? a.dbias : a.dweight) {
-      out += blockIdx.x * a.pitch + col;
-      *out = a.accumulate ? *out + x : x;
+    if (!kAlone || a.sums) {
+      a.sums[(static_cast<int64_t>(blockIdx.x) * 2 + k) * a.D + col] = x;
+    } else if (float* out = k ? a.dbias : a.dweight) {
+      out[col] = a.accumulate ? out[col] + x : x;
     }
   };
 #pragma unroll
@@ -235,7 +237,7 @@ static inline int grad_shape(int64_t D, F f) {
 }
 
 // Workgroups of the pass, at most kGradBlocks. Each leaves 2 D sums behind, so that fewer and
-// larger ones cost less where every one has but a turn or two: 1280 x 1792 fp32 takes 12.9 us
+// larger ones cost less where every one has but a turn or two: 1280 x 1792 fp32 takes 12.5 us
 // with 160 of 1024 threads, 14.4 with 320 of 512 (16,384 x 1000 fp32 44 and 41).
 constexpr int64_t kGradBlocks = 512;
 
@@ -244,6 +246,8 @@ constexpr int64_t kGradBlocks = 512;
 // us, 11.0 otherwise, 700 x 480 6.9 and 9.5, 200 x 650 fp32 7.6 and 12.8. More sums than
 // kGradSums cost what that saves (2000 x 480 bf16: 9.9 and 9.8; 256 x 2048 11.1 and 10.3).
 constexpr int64_t kGradSmall = 384, kGradSums = int64_t(1) << 19;
+// Rows of one of the larger workgroups, at most eight times a small one's, always fit.
+static_assert(kGradSums / (2 * LM_NORM_MAX_WIDTH) >= 8 && kSmallThreads * 8 == 1024 * 2, "");
 
 template <typename T, typename F>
 static inline int norm_grad_shape(int64_t rows, int64_t D, F f) {
@@ -251,7 +255,7 @@ static inline int norm_grad_shape(int64_t rows, int64_t D, F f) {
   const auto fit = [rows](int64_t blocks) {
     return [rows, blocks](auto shape) { return rows <= blocks * decltype(shape)::kRows ? 1 : 0; };
   };
-  if (grad_shape<T, 256, 1>(D, fit(few))) return grad_shape<T, 256, 1>(D, f);
+  if (grad_shape<T, kSmallThreads, 1>(D, fit(few))) return grad_shape<T, kSmallThreads, 1>(D, f);
   return grad_shape<T, 512, 2>(D, fit(kGradBlocks)) ? grad_shape<T, 1024, 2>(D, f)
                                                     : grad_shape<T, 512, 2>(D, f);
 }
@@ -296,9 +300,8 @@ int norm_grad_run(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, co
   float* sums = static_cast<float*>(ws);
   if (rows > 0) {
     const NormGradArgs a{dy, h, add, mean, rstd, weight, dh, dx,
-                         join ? sums : dweight, join ? sums + D : dbias, 2 * D,
-                         !join && accumulate, ld_dy, ld_h, ld_add, ld_dh, ld_dx, rows,
-                         static_cast<int>(D),
+                         join ? sums : nullptr, dweight, dbias, accumulate, ld_dy, ld_h, ld_add,
+                         ld_dh, ld_dx, rows, static_cast<int>(D),
                          static_cast<float>(1.0 / static_cast<double>(D)),
                          make_keep(p, seed, dx ? seed_at : nullptr)};
     const int rc = dtype == LM_BF16 ? norm_grad_launch<bf16_t>(a, blocks, st)

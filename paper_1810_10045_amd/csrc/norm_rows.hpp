@@ -13,7 +13,7 @@ constexpr int kNormThreads = 256;  // of a workgroup, where a row's group is no 
 
 template <int LANES_, int WAVES_, int NV_, int ROWS_ = 1, int THREADS_ = kNormThreads>
 struct NormShape {
-  static constexpr int LANES = LANES_, WAVES = WAVES_, NV = NV_, ROWS = ROWS_;
+  static constexpr int LANES = LANES_, WAVES = WAVES_, NV = NV_, ROWS = ROWS_, THREADS = THREADS_;
   static constexpr int kGroup = WAVES > 1 ? WAVES * kWave : LANES;  // lanes of a row
   static constexpr int kThreads = kGroup > THREADS_ ? kGroup : THREADS_;
   static constexpr int kGroups = kThreads / kGroup;  // of a workgroup
