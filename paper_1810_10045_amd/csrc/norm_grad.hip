@@ -241,11 +241,12 @@ static inline int grad_shape(int64_t D, F f) {
 // with 160 of 1024 threads, 14.4 with 320 of 512 (16,384 x 1000 fp32 44 and 41).
 constexpr int64_t kGradBlocks = 512;
 
-// Rows that up to this many workgroups of one wave a SIMD hold, a row a group, go to these, as
+// Rows that up to kGradSmall workgroups of one wave a SIMD hold, a row a group, go to these, as
 // the instructions of the four waves of a larger one follow each other: 27 x 459 bf16 takes 6.4
-// us, 11.0 otherwise, 700 x 480 6.9 and 9.5, 200 x 650 fp32 7.6 and 12.8. More sums than
-// kGradSums cost what that saves (2000 x 480 bf16: 9.9 and 9.8; 256 x 2048 11.1 and 10.3).
-constexpr int64_t kGradSmall = 384, kGradSums = int64_t(1) << 19;
+// us, 11.0 otherwise, 700 x 480 6.9 and 9.5, 22,882 x 35 9.7 and 12.5, 200 x 650 fp32 7.6 and
+// 12.8. More sums than kGradSums cost what that saves (2000 x 480 bf16: 9.9 and 9.8; 256 x 2048
+// 11.1 and 10.3).
+constexpr int64_t kGradSmall = 1024, kGradSums = int64_t(1) << 19;
 // Rows of one of the larger workgroups, at most eight times a small one's, always fit.
 static_assert(kGradSums / (2 * LM_NORM_MAX_WIDTH) >= 8 && kSmallThreads * 8 == 1024 * 2, "");
 
