@@ -221,9 +221,14 @@ def test_layer_norm_grad(lz, rows, D, gap, off, dtype):
 # Rows enough for a wave of their own each, and for every workgroup to have several turns
 MANY = [(70_001, 40), (8300, 300), (4200, 517), (2100, 1025), (2100, 2048), (1100, 4100),
         (1030, 8191), (1026, 16384)]
+# Rows between few and many: on both sides of where the forms of both passes change
+BETWEEN = [(1024, 30), (1025, 30), (20_000, 3), (33_000, 3), (70_001, 3), (1024, 300), (3492, 300),
+           (3493, 300), (1014, 517), (1015, 517), (255, 1025), (256, 1025), (1024, 1025),
+           (128, 2048), (129, 2048), (1, 2048), (63, 4100), (64, 4100), (33, 8191), (16, 16384),
+           (17, 16384), (600, 16384)]
 
 
-@pytest.mark.parametrize("rows,D", MANY)
+@pytest.mark.parametrize("rows,D", MANY + BETWEEN)
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_layer_norm_of_many_rows(lz, rows, D, dtype):
     gen = gen_of("many", rows, D, dtype)
@@ -240,7 +245,7 @@ def test_layer_norm_of_many_rows(lz, rows, D, dtype):
 
 
 def test_results_of_tens_of_megabytes(lz):
-    """Results that are written through the caches (32 to 256 MiB): the same numbers."""
+    """Results that the caches hold in part (32 to 256 MiB): the same numbers."""
     rows, D = 8300, 1025
     gen = gen_of("cached")
     x, dy = rows_of(gen, rows, D, F32), rows_of(gen, rows, D, F32)
@@ -341,19 +346,20 @@ def test_layer_norm_in_place(lz, dtype, D):
         assert torch.equal(got, ref)
 
 
-@pytest.mark.parametrize("rows", [1, 5, 130, 300, 5000])
-def test_layer_norm_grad_accumulates(lz, rows):
+@pytest.mark.parametrize("rows,D", [(1, 77), (5, 77), (130, 77), (300, 77), (5000, 77), (3, 5),
+                                    (1, 2048), (2, 1025), (1, 9001), (40, 9001)])
+def test_layer_norm_grad_accumulates(lz, rows, D):
     gen = gen_of("accumulate", rows)
-    h, dy = (rows_of(gen, rows, 77, BF16) for _ in range(2))
-    w, _ = params(gen, 77)
+    h, dy = (rows_of(gen, rows, D, BF16) for _ in range(2))
+    w, _ = params(gen, D)
     s = lz.layer_norm(h)
     one = lz.layer_norm_grad(dy, h, s.mean, s.rstd, w)
-    dw, db = torch.full((77,), 2.0, device=DEV), torch.full((77,), -1.0, device=DEV)
+    dw, db = torch.full((D,), 2.0, device=DEV), torch.full((D,), -1.0, device=DEV)
     two = lz.layer_norm_grad(dy, h, s.mean, s.rstd, w, dweight=dw, dbias=db, accumulate=True)
     assert two.dweight is dw and torch.equal(dw, one.dweight + 2.0)
     assert torch.equal(db, one.dbias - 1.0)
     none = lz.layer_norm_grad(dy[:0], h[:0], s.mean[:0], s.rstd[:0], w, dweight=dw, dbias=db)
-    assert not dw.any() and not db.any() and none.dh.shape == (0, 77)
+    assert not dw.any() and not db.any() and none.dh.shape == (0, D)
     only = lz.layer_norm_grad(dy, h, s.mean, s.rstd, w, bias=False)
     assert only.dbias is None and torch.equal(only.dweight, one.dweight)
 
