@@ -148,7 +148,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
   // The groups' sums, added in their order: of a wave by their lanes, of the waves in LDS.
   constexpr int kGroups = S::kThreads / (S::kGroup > kWave ? S::kGroup : kWave);
   constexpr int kCols = S::kGroup * NV * P;
-  __shared__ float joined[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kCols : 1];
+  alignas(16) __shared__ float joined[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kCols : 1];
   auto put = [&](int k, int col, float x) {
     if (!kAlone || a.sums) {
       a.sums[(static_cast<int64_t>(blockIdx.x) * 2 + k) * a.D + col] = x;
@@ -162,17 +162,28 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const NormSpan<T, ENDS> s((lane + v * S::kGroup) * P, a.D);
+      const int col = (lane + v * S::kGroup) * P;
+      float x[P];
 #pragma unroll
       for (int e = 0; e < P; ++e) {
-        float x = k ? db[v][e] : dw[v][e];
+        x[e] = k ? db[v][e] : dw[v][e];
 #pragma unroll
-        for (int off = S::kGroup; off < kWave; off *= 2) x += __shfl_xor(x, off, kWave);
-        const int col = (lane + v * S::kGroup) * P + e;
-        if constexpr (kGroups > 1) {
-          joined[threadIdx.x / (kGroups > 1 ? S::kThreads / kGroups : 1)][col] = x;
-        } else if (e < s.have) {
-          put(k, col, x);
-        }
+        for (int off = S::kGroup; off < kWave; off *= 2) x[e] += __shfl_xor(x[e], off, kWave);
+      }
+      if constexpr (kGroups > 1) {
+#pragma unroll
+        for (int e = 0; e < P; ++e)
+          joined[threadIdx.x / (kGroups > 1 ? S::kThreads / kGroups : 1)][col + e] = x[e];
+      } else if (a.sums && s.have == P) {
+        // whole vectors: 100 x 16,384 bf16 22.7 us, 33.4 a value at a time
+        float* out = a.sums + (static_cast<int64_t>(blockIdx.x) * 2 + k) * a.D + col;
+#pragma unroll
+        for (int e = 0; e < P; e += 4)
+          *reinterpret_cast<f32x4e*>(out + e) = f32x4e{x[e], x[e + 1], x[e + 2], x[e + 3]};
+      } else {
+#pragma unroll
+        for (int e = 0; e < P; ++e)
+          if (e < s.have) put(k, col + e, x[e]);
       }
     }
     if constexpr (kGroups > 1) {
@@ -189,25 +200,25 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
 
 // dweight and dbias (+)= the workgroups' sums, kJoinCols columns of the two a workgroup:
 // kJoinRows threads share a column's parts, their sums are added in a fixed order.
-constexpr int kJoinThreads = 1024, kJoinCols = 16, kJoinRows = kJoinThreads / kJoinCols;
-constexpr int kJoinWaves = kJoinThreads / kWave;
+constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / kWave;
 
+template <int COLS>
 __global__ __launch_bounds__(kJoinThreads) void k_norm_join(const float* sums, int parts, int D,
                                                             float* dweight, float* dbias,
                                                             int accumulate) {
-  __shared__ float lds[kJoinWaves][kJoinCols];
-  const int col = threadIdx.x % kJoinCols, wave = threadIdx.x / kWave;
-  const int c = blockIdx.x * kJoinCols + col;
+  __shared__ float lds[kJoinWaves][COLS];
+  const int col = threadIdx.x % COLS, wave = threadIdx.x / kWave;
+  const int c = blockIdx.x * COLS + col;
   const float* at = sums + (c < 2 * D ? c : 0);
   float x = 0.f;
 #pragma unroll 8
-  for (int g = threadIdx.x / kJoinCols; g < parts; g += kJoinRows)
+  for (int g = threadIdx.x / COLS; g < parts; g += kJoinThreads / COLS)
     x += at[static_cast<int64_t>(g) * 2 * D];
 #pragma unroll
-  for (int off = kJoinCols; off < kWave; off *= 2) x += __shfl_xor(x, off, kWave);
-  if (threadIdx.x % kWave < kJoinCols) lds[wave][col] = x;
+  for (int off = COLS; off < kWave; off *= 2) x += __shfl_xor(x, off, kWave);
+  if (threadIdx.x % kWave < COLS) lds[wave][col] = x;
   __syncthreads();
-  if (threadIdx.x >= kJoinCols || c >= 2 * D) return;
+  if (threadIdx.x >= COLS || c >= 2 * D) return;
   float y = 0.f;
 #pragma unroll
   for (int w = 0; w < kJoinWaves; ++w) y += lds[w][col];
@@ -244,19 +255,22 @@ constexpr int64_t kGradBlocks = 512;
 // Rows that up to kGradSmall workgroups of one wave a SIMD hold, a row a group, go to these, as
 // the instructions of the four waves of a larger one follow each other: 27 x 459 bf16 takes 6.4
 // us, 11.0 otherwise, 700 x 480 6.9 and 9.5, 22,882 x 35 9.7 and 12.5, 200 x 650 fp32 7.6 and
-// 12.8. More sums than kGradSums cost what that saves (2000 x 480 bf16: 9.9 and 9.8; 256 x 2048
-// 11.1 and 10.3).
-constexpr int64_t kGradSmall = 1024, kGradSums = int64_t(1) << 19;
+// 12.8, 200 x 2048 8.6 and 10.3. More sums than kGradSums cost what that saves, or half as many
+// where several rows' are added first (900 x 1000 bf16: 11.5 and 9.7).
+constexpr int64_t kGradSmall = 1024, kGradSums = int64_t(1) << 20;
 // Rows of one of the larger workgroups, at most eight times a small one's, always fit.
-static_assert(kGradSums / (2 * LM_NORM_MAX_WIDTH) >= 8 && kSmallThreads * 8 == 1024 * 2, "");
+static_assert(kGradSums / 2 / (2 * LM_NORM_MAX_WIDTH) >= 8 && kSmallThreads * 8 == 1024 * 2, "");
 
 template <typename T, typename F>
 static inline int norm_grad_shape(int64_t rows, int64_t D, F f) {
-  const int64_t few = kGradSums / (2 * D) < kGradSmall ? kGradSums / (2 * D) : kGradSmall;
   const auto fit = [rows](int64_t blocks) {
     return [rows, blocks](auto shape) { return rows <= blocks * decltype(shape)::kRows ? 1 : 0; };
   };
-  if (grad_shape<T, kSmallThreads, 1>(D, fit(few))) return grad_shape<T, kSmallThreads, 1>(D, f);
+  const bool small = grad_shape<T, kSmallThreads, 1>(D, [&](auto shape) {
+    const int64_t most = (decltype(shape)::kGroups > 1 ? kGradSums / 2 : kGradSums) / (2 * D);
+    return fit(most < kGradSmall ? most : kGradSmall)(shape);
+  });
+  if (small) return grad_shape<T, kSmallThreads, 1>(D, f);
   return grad_shape<T, 512, 2>(D, fit(kGradBlocks)) ? grad_shape<T, 1024, 2>(D, f)
                                                     : grad_shape<T, 512, 2>(D, f);
 }
@@ -266,7 +280,9 @@ static int64_t grad_blocks(int64_t rows, int64_t D) {
   return norm_grad_shape<T>(rows, D, [&](auto shape) {
     using S = decltype(shape);
     const int64_t n = (rows + S::kRows - 1) / S::kRows;  // turns
-    return static_cast<int>(n < kGradBlocks ? n : kGradBlocks);
+    // Of 16 waves a compute unit has but one: 2000 x 16,384 bf16 82 us, with 512 of them 109.
+    constexpr int64_t most = S::kGroup == 1024 ? kGradBlocks / 2 : kGradBlocks;
+    return static_cast<int>(n < most ? n : most);
   });
 }
 static int64_t norm_grad_blocks(int64_t rows, int64_t D, int dtype) {
@@ -310,8 +326,12 @@ int norm_grad_run(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, co
     if (rc != LM_OK) return rc;
   }
   if (!join) return LM_OK;
-  const int cols = static_cast<int>(2 * D);
-  k_norm_join<<<(cols + kJoinCols - 1) / kJoinCols, kJoinThreads, 0, st>>>(
+  // Columns of a workgroup: few where there would be no workgroup for each compute unit (900 x
+  // 1000 bf16: 9.7 us with 16, 9.9 with 32), else whole cache lines (2048 x 2048 14.1 with 32,
+  // 15.6 with 16; 100 x 16,384 16.7 with 64, 18.0 with 32, 22.5 with 16).
+  const int cols = static_cast<int>(2 * D), each = D <= 1024 ? 16 : D <= 4096 ? 32 : 64;
+  auto kernel = each == 16 ? k_norm_join<16> : each == 32 ? k_norm_join<32> : k_norm_join<64>;
+  kernel<<<(cols + each - 1) / each, kJoinThreads, 0, st>>>(
       sums, blocks, static_cast<int>(D), dweight, dbias, accumulate);
   return launch_status(hipGetLastError());
 }

@@ -225,7 +225,8 @@ MANY = [(70_001, 40), (8300, 300), (4200, 517), (2100, 1025), (2100, 2048), (110
 BETWEEN = [(1024, 30), (1025, 30), (20_000, 3), (33_000, 3), (70_001, 3), (1024, 300), (3492, 300),
            (3493, 300), (1014, 517), (1015, 517), (255, 1025), (256, 1025), (1024, 1025),
            (128, 2048), (129, 2048), (1, 2048), (63, 4100), (64, 4100), (33, 8191), (16, 16384),
-           (17, 16384), (600, 16384)]
+           (17, 16384), (600, 16384), (257, 2048), (511, 1025), (128, 4096), (32, 16384),
+           (33, 16384), (260, 9001)]
 
 
 @pytest.mark.parametrize("rows,D", MANY + BETWEEN)
