@@ -665,6 +665,8 @@ int lm_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int64_t ld_
  * their log probabilities. A logit of -infinity is masked: no word, no
  * alternative. Where a row has fewer than `top` words left, the places behind
  * the last hold id -1 and -infinity.
+ * log_sum and entropy are no less than 0, log probabilities no more, however
+ * they round.
  * A row with nothing left: peak, log_sum and logp -infinity, entropy 0. A row
  * with a NaN or +infinity: NaN, ids -1.
  * targets    device, N ids of dtype `idtype`, or NULL (logp is not written).

@@ -260,7 +260,10 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const
   const float nan = __builtin_nanf("");
   const float slip = Sums::slip(t.m, a.c), mean = t.e / t.s;
   // s = 2^slip sum 2^(c (x - m)); c's own rounding moves its logarithm by the mean exponent.
-  const float log_sum = logf(t.s) - kLn2 * (slip + a.c_off * (mean - slip));
+  // The sum holds its maximum's own 1, so its logarithm is no less than 0: what comes out below is
+  // the rounding of 2^slip (one word left at 6.0: -4.6e-8), and would be a probability above 1.
+  const float log_sum =
+      __builtin_fmaxf(logf(t.s) - kLn2 * (slip + a.c_off * (mean - slip)), 0.f);
   if (tid == 0) {
     if (a.logp) {
       const float x = target.in ? target.x : nan;
