@@ -5,12 +5,14 @@
 // Each function takes the arguments of its namesake in lmzipf.py, allocates the results and
 // calls the C ABI. It returns None, and has done nothing, where a call is not plain: all
 // tensors torch's own, contiguous, of the right types and sizes, on the current device,
-// none that autograd would record, all results to be allocated. lmzipf.py then goes through
-// its own checks, which name what is wrong or take the call.
+// none that autograd would record or that has a forward-mode tangent, all results to be
+// allocated. lmzipf.py then goes through its own checks, which name what is wrong or take the
+// call.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 
 #include "../../include/lmzipf.h"
@@ -37,6 +39,7 @@ class Plain {
     device_ = PyLong_AsLong(args[0]);
     stream = PyLong_AsVoidPtr(args[1]);
     records_ = c10::GradMode::is_enabled();
+    tangents_ = c10::AutogradState::get_tls_state().get_fw_grad_mode();
     ok = !PyErr_Occurred();
     PyErr_Clear();
   }
@@ -46,7 +49,8 @@ class Plain {
     if (!(ok = THPVariable_CheckExact(args_[i]))) return {};
     const at::Tensor& t = THPVariable_Unpack(args_[i]);
     ok = t.is_cuda() && t.device().index() == device_ && t.layout() == at::kStrided &&
-         t.is_contiguous() && !(records_ && t.requires_grad()) && !t.is_conj() && !t.is_neg();
+         t.is_contiguous() && !(records_ && t.requires_grad()) && !t.is_conj() && !t.is_neg() &&
+         !(tangents_ && t._fw_grad(0).defined());  // torch has the one level
     return t;
   }
   // The matrix that a call is about: its rows, columns and dtype.
@@ -113,7 +117,7 @@ class Plain {
  private:
   PyObject* const* args_;
   long device_ = -1;
-  bool records_ = true;
+  bool records_ = true, tangents_ = true;
 
  public:
   bool ok;

@@ -27,6 +27,7 @@ import os
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 # The current stream's handle (not a public name of torch: the public call where it is absent).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -906,6 +907,20 @@ def _no_graph(what: str, *tensors, gradient="rel_bias_grad is the gradient of re
         if t is not None and t.requires_grad and torch.is_grad_enabled():
             raise LmError(f"{what} is not recorded by autograd: call it under torch.no_grad() or"
                           f" in an autograd.Function ({gradient})")
+    _no_tangent(what, *tensors)
+
+
+def _no_tangent(what: str, *tensors):
+    """A tensor with a forward-mode tangent would come out of the call without it, under
+    torch.no_grad() too, which is of reverse mode only."""
+    # the level that is entered, -1 for none (not a public name: 0 where it is absent)
+    if getattr(forward_ad, "_current_level", 0) < 0:
+        return
+    for t in tensors:
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            raise LmError(f"{what} has no forward-mode derivative and would drop a tensor's tangent:"
+                          " call it on forward_ad.unpack_dual(tensor).primal or in an"
+                          " autograd.Function with a jvp")
 
 
 _Strides = ctypes.c_int64 * 3
@@ -926,7 +941,7 @@ def rel_bias(table: torch.Tensor, buckets: RelBuckets, Lq: int, Lk: int, q_start
     and key j, as an H x Lq x Lk tensor of `dtype`; with `add` (B x H x Lq x Lk
     attention scores) the scores plus the bias, of their shape and dtype. `out`
     may be `add` itself. Not recorded by autograd: tensors that require grad are
-    refused while grad mode is on."""
+    refused while grad mode is on, and tensors with a forward-mode tangent."""
     _no_graph("rel_bias", table, add, out)
     _dev(table, "table")
     size = table.shape
@@ -1179,6 +1194,7 @@ def layer_norm_grad(dy: torch.Tensor, h: torch.Tensor, mean: torch.Tensor, rstd:
             return NormGrad(*r)
     _no_graph("layer_norm_grad", dy, h, weight, add, out, dx, dweight, dbias,
               gradient=_NORM_GRADIENT)
+    _no_tangent("layer_norm_grad", mean, rstd)
     _dev(dy, "dy")
     device = dy.device
     rows, D, ld = _matrix(dy, "dy")
@@ -1312,6 +1328,7 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor],
         if r is not None:
             return r[0]
     _no_graph("token_logprobs_grad", logits, dlogp, dentropy, out, gradient=_LOGP_GRADIENT)
+    _no_tangent("token_logprobs_grad", peak, log_sum, entropy)
     _dev(logits, "logits")
     device = logits.device
     N, V, ld = _matrix(logits, "logits")
