@@ -64,11 +64,11 @@ def build(verbose: bool = False) -> str:
     with ThreadPoolExecutor(max(1, min(len(srcs) + 1, os.cpu_count() or 1))) as ex:
         calls = ex.submit(build_calls, verbose)
         objs = list(ex.map(compile_one, srcs))
-        calls.result()
     tmp = LIB_PATH + f".tmp{os.getpid()}"
     subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs],
                    check=True)
     os.replace(tmp, LIB_PATH)
+    calls.result()  # raises where it failed; the library does not need it
     return LIB_PATH
 
 

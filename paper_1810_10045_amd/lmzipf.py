@@ -24,6 +24,7 @@ from __future__ import annotations
 import ctypes
 import operator
 import os
+import warnings
 from typing import NamedTuple, Optional
 
 import torch
@@ -155,12 +156,15 @@ def lib():
 def _load_calls():
     """The plain calls of dropout, layer norm and the token log probabilities without Python
     between the checks, the results' allocation and the library (``csrc/calls.cpp``): of a call
-    of few rows that is more than half."""
+    of few rows that is more than half. It is built against one Python and one torch; where it is
+    absent or cannot be loaded (None, and a warning) these calls take ctypes as all others do, to
+    the same kernels."""
     try:
         from . import _lmzipf_calls as calls
     except ImportError as e:
-        raise ImportError(
-            f"{e}: build it with `python -c 'import __graft_entry__ as g; g.build()'`") from e
+        warnings.warn(f"short calls take longer without _lmzipf_calls ({e}): build it with"
+                      " `python -c 'import __graft_entry__ as g; g.build()'`", RuntimeWarning)
+        return None
     names = ("lm_dropout", "lm_layer_norm", "lm_layer_norm_grad_workspace_bytes",
              "lm_layer_norm_grad", "lm_token_logprobs_workspace_bytes", "lm_token_logprobs",
              "lm_token_logprobs_grad", "lm_status_string")
@@ -1075,7 +1079,7 @@ def dropout(x: torch.Tensor, p: float, seed, add: Optional[torch.Tensor] = None,
     `dropout(dout, p, seed)`. seed: a number, or an int64 tensor of one element
     on the device, which a captured call reads with every replay. `out` may be x
     or `add`. Not recorded by autograd, as ``rel_bias``."""
-    if out is None and stream is None and x.is_cuda:
+    if _calls and out is None and stream is None and x.is_cuda:
         here = _this_device()
         r = _calls.dropout(here, _stream_of(here), x, p, seed, add)
         if r is not None:
@@ -1124,7 +1128,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
     where nothing is added or dropped, else `sum_out` (which may be `add`: the
     residual stream) or a new tensor; y goes to `out` (which may be x) or a new
     one. p and seed as ``dropout``'s. Not recorded by autograd, as ``rel_bias``."""
-    if out is None and sum_out is None and stream is None and x.is_cuda:
+    if _calls and out is None and sum_out is None and stream is None and x.is_cuda:
         here = _this_device()
         r = _calls.layer_norm(here, _stream_of(here), x, weight, bias, eps, add, p, seed)
         if r is not None:
@@ -1185,8 +1189,8 @@ def layer_norm_grad(dy: torch.Tensor, h: torch.Tensor, mean: torch.Tensor, rstd:
     `accumulate` added to; new where not given, dweight where there is a weight,
     dbias as `bias` says (None: as the weight). Without `ws` the call takes its
     workspace from torch's allocator. Not recorded by autograd, as ``rel_bias``."""
-    if (out is None and dx is None and dweight is None and dbias is None and not accumulate and
-            ws is None and stream is None and dy.is_cuda):
+    if (_calls and out is None and dx is None and dweight is None and dbias is None and
+            not accumulate and ws is None and stream is None and dy.is_cuda):
         here = _this_device()
         r = _calls.layer_norm_grad(here, _stream_of(here), dy, h, mean, rstd, weight, add, p, seed,
                                    bias)
@@ -1275,7 +1279,7 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None,
     tells of targets outside the vocabulary (their logp is NaN). Without `ws` the
     call takes its workspace from torch's allocator. Not recorded by autograd, as
     ``rel_bias``."""
-    if ws is None and stream is None and logits.is_cuda:
+    if _calls and ws is None and stream is None and logits.is_cuda:
         here = _this_device()
         r = _calls.token_logprobs(here, _stream_of(here), logits, targets, scale, top, ignore,
                                   dev_err)
@@ -1321,7 +1325,7 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor],
     of logp (dlogp) and of the entropy (dentropy, with the entropy itself), and
     what ``token_logprobs`` returned. `out` may be the logits. Not recorded by
     autograd, as ``rel_bias``."""
-    if out is None and stream is None and logits.is_cuda:
+    if _calls and out is None and stream is None and logits.is_cuda:
         here = _this_device()
         r = _calls.token_logprobs_grad(here, _stream_of(here), logits, targets, peak, log_sum,
                                        dlogp, entropy, dentropy, scale, ignore)
