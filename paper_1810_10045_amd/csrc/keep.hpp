@@ -7,9 +7,12 @@
 // round(65536 p), and multiplied by 1 over the share that is kept: the expectation is
 // exact for the p that is drawn, which is within 2^-17 of the caller's. Two values to a
 // word: the hash's two 32-bit products take a quarter of the vector rate, and a word for
-// each value would cost as much as a large call's memory. Over 2^23 words kept values correlate
-// by 0.001 with their neighbours' and by 0.014 at most where word numbers differ by a power of
-// two (128: 0.014; 65,536: 0.013), and seeds that follow each other not at all.
+// each value would cost as much as a large call's memory. What is kept correlates by 0.001 with
+// its neighbours, seeds that follow each other not at all. The hash has one product
+// left in which high bits of a word's number can spread, so certain far words do correlate: most
+// where numbers differ by powers of two and their sums and differences, by up to 0.02 within 2^16
+// words, 0.04 within 2^20, 0.08 within 2^24, 0.2 within 2^28, 0.4 within 2^32 and 0.95 beyond,
+// where the number's upper half only adds a constant to the word before that product.
 #pragma once
 
 #include <math.h>

@@ -57,7 +57,9 @@ __host__ __device__ static inline StepKeys step_keys(uint64_t seed) {
 // The random word of value number e: two rounds of multiply and xor-shift. The
 // multipliers here and above are published ones, known to mix well: three primes of Y.
 // Collet's 32-bit hash (2012), 2^64 over the golden ratio (Knuth) and that of a published
-// 64-bit mixer (0xD6E8FEB86659FD93); the rounds are this file's.
+// 64-bit mixer (0xD6E8FEB86659FD93); the rounds are this file's. Neighbouring words are
+// independent to 0.001, words whose numbers differ by a large power of two are not (keep.hpp):
+// for a rounding each value's own word counts, which is uniform.
 constexpr uint32_t kHighWord = 0x85EBCA77u;
 
 __device__ __forceinline__ uint32_t value_word(uint64_t e, const StepKeys& k) {

@@ -1077,8 +1077,10 @@ def dropout(x: torch.Tensor, p: float, seed, add: Optional[torch.Tensor] = None,
     its last dimension the columns. The mask is a function of `seed`, the
     element's row and column and the number of columns: the gradient is
     `dropout(dout, p, seed)`. seed: a number, or an int64 tensor of one element
-    on the device, which a captured call reads with every replay. `out` may be x
-    or `add`. Not recorded by autograd, as ``rel_bias``."""
+    on the device, which a captured call reads with every replay. Far values' masks
+    correlate (lm_dropout says how much): a matrix of more than 2^33 elements goes
+    into several calls, each with its own seed. `out` may be x or `add`. Not
+    recorded by autograd, as ``rel_bias``."""
     if _calls and out is None and stream is None and x.is_cuda:
         here = _this_device()
         r = _calls.dropout(here, _stream_of(here), x, p, seed, add)
