@@ -686,8 +686,14 @@ int lm_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int64_t ld_
  * dev_err    device int32 or NULL.
  * ws         device workspace of lm_token_logprobs_workspace_bytes(...), 16-byte
  *            aligned, no initial contents required (0 bytes where rows are many
- *            or short: NULL). More than 1024 equal logits at the border of the
- *            alternatives cost `top` further passes over their row.
+ *            or short: NULL).
+ * The alternatives are ranked among the logits that reach the `top`-th largest of
+ * the maxima of 64 parts of a row. More than 256 such logits in rows of up to
+ * 2048 bf16 or 1024 fp32, or more than 1024 in longer ones, cost `top` further
+ * passes over the row (short rows: over registers). Many equal logits do so, and
+ * logits that few of the parts have (masks, rows of fewer than 512 bf16 with
+ * `top` above an eighth of them); in short rows with `top` from 62 on, any do:
+ * about half of the rows with 64, a few in a hundred with 62.
  *
  * lm_token_logprobs_grad: the logits' gradient from those of logp and entropy,
  * l = log q:
