@@ -99,3 +99,139 @@ def test_alternatives_in_a_few_parts_of_a_row(lz, V, live, dtype):
         got = r.top_logp[rows].double().cpu().numpy()
         with np.errstate(invalid="ignore"):
             assert ((got == want) | (np.abs(got - want) <= tol + A.TINY)).all()
+
+
+# ---------------------------------------------------------------------------
+# Memory around a result that has gaps
+# ---------------------------------------------------------------------------
+class Framed:
+    """rows x D values to be written, `gap` elements between rows, in memory of NaN."""
+
+    def __init__(self, rows, D, dtype, values=None, gap=5, off=3):
+        ld = D + gap
+        self.flat = torch.full((off + rows * ld + 64,), NAN, dtype=dtype, device=DEV)
+        self.t = self.flat[off:off + rows * ld].view(rows, ld)[:, :D]
+        self.around = torch.ones_like(self.flat, dtype=torch.bool)
+        self.around[off:off + rows * ld].view(rows, ld)[:, :D] = False
+        if values is not None:
+            self.t.copy_(values)
+
+    def check(self, what):
+        assert bool(torch.isfinite(self.t).all()), f"{what}: not every value is written"
+        n = int((~torch.isnan(self.flat[self.around])).sum())
+        assert n == 0, f"{what}: {n} elements around the rows are written"
+
+
+# On both sides of a vector's width (4 fp32, 8 bf16), of a wave's and of a workgroup's, one row,
+# rows that fill a workgroup's groups and rows that do not
+@pytest.mark.parametrize("rows", [1, 3, 41, 1100])
+@pytest.mark.parametrize("D", [1, 3, 4, 5, 7, 8, 9, 63, 64, 65, 255, 257, 512, 517, 2047, 2049])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_nothing_around_the_rows_is_written(lz, dtype, D, rows):
+    gen = torch.Generator(device=DEV).manual_seed(rows * 10_000 + D)
+    x, add, dy = (torch.randn(rows, D, generator=gen, device=DEV).to(dtype) for _ in range(3))
+    new = lambda values=None: Framed(rows, D, dtype, values)  # noqa: E731
+
+    def same(frame, want, what):
+        frame.check(what)
+        assert torch.equal(frame.t, want), what
+    want = lz.dropout(x, 0.3, 5, add=add)
+    a, b, c = new(), new(x), new(add)
+    lz.dropout(x, 0.3, 5, add=add, out=a.t)
+    same(a, want, "dropout")
+    lz.dropout(b.t, 0.3, 5, add=c.t, out=b.t)
+    same(b, want, "dropout in place")
+    same(c, add, "dropout's addend")
+    f = lz.layer_norm(x, add=add, p=0.2, seed=4)
+    y, h, s = new(), new(), new(add)
+    lz.layer_norm(x, add=add, p=0.2, seed=4, out=y.t, sum_out=h.t)
+    same(y, f.y, "norm")
+    same(h, f.h, "norm's sum")
+    lz.layer_norm(x, add=s.t, p=0.2, seed=4, sum_out=s.t)
+    same(s, f.h, "norm's sum in place")
+    g = lz.layer_norm_grad(dy, f.h, f.mean, f.rstd, add=add, p=0.2, seed=4, bias=True)
+    dh, dx, past = new(), new(), new(add)
+    db = Framed(1, D, F32, gap=0)
+    lz.layer_norm_grad(dy, f.h, f.mean, f.rstd, add=add, p=0.2, seed=4, out=dh.t, dx=dx.t,
+                       dbias=db.t[0])
+    same(dh, g.dh, "norm's gradient")
+    same(dx, g.dx, "norm's gradient through dropout")
+    same(db, g.dbias[None], "the bias's gradient")
+    lz.layer_norm_grad(dy, f.h, f.mean, f.rstd, add=past.t, p=0.2, seed=4, out=past.t)
+    same(past, g.dh, "norm's gradient in place")
+    t = torch.randint(0, D, (rows,), generator=gen, device=DEV)
+    r = lz.token_logprobs(x, t)
+    want = lz.token_logprobs_grad(x, t, r.peak, r.log_sum, r.entropy + 1, r.entropy, r.entropy + 1)
+    out, z = new(), new(x)
+    for where, source in ((out, x), (z, z.t)):
+        lz.token_logprobs_grad(source, t, r.peak, r.log_sum, r.entropy + 1, r.entropy, r.entropy + 1,
+                               out=where.t)
+        same(where, want, "the logits' gradient")
+
+
+# ---------------------------------------------------------------------------
+# A workspace that two graphs share
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,D", [(900, 300), (4000, 40), (2000, 517), (100, 4100)])
+def test_weights_gradients_of_two_graphs_with_one_workspace(lz, rows, D):
+    """The results that pass through the workspace, whatever it holds before a replay."""
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    h, dy = ([torch.randn(rows, D, generator=gen, device=DEV) for _ in range(2)] for _ in range(2))
+    w = torch.randn(D, generator=gen, device=DEV)
+    m, r = torch.zeros(rows, device=DEV), torch.ones(rows, device=DEV)
+    need = lz.lib().lm_layer_norm_grad_workspace_bytes(rows, D, lz.F32)
+    assert need > 0
+    ws = lz.Workspace(DEV)
+    ws.get(need)
+
+    def run(i):
+        return [*lz.layer_norm_grad(dy[i], h[i], m, r, w, ws=ws)]
+    want = [run(i) for i in range(2)]
+    for i in range(2):
+        ref = A.norm_grad(*(t.double().cpu().numpy() for t in (dy[i], h[i], m, r, w)))
+        for name in ("dweight", "dbias"):
+            got = dict(zip(("dh", "dx", "dweight", "dbias"), want[i]))[name].double().cpu().numpy()
+            assert (np.abs(got - ref[name][0]) <= ref[name][1] + A.TINY).all(), name
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for i, g in enumerate(graphs):
+        with torch.cuda.graph(g, stream=side):
+            outs.append(run(i))
+    for n in range(4):
+        [t.zero_() for out in outs for t in out]
+        ws.buf.view(torch.uint8).fill_(0xff)  # NaN
+        for g in graphs if n % 2 else reversed(graphs):
+            g.replay()
+        torch.cuda.synchronize()
+        run(n % 2)  # the program's own call with the same workspace
+        for a, b in zip(outs, want):
+            assert all(torch.equal(p, q) for p, q in zip(a, b)), n
+
+
+# ---------------------------------------------------------------------------
+# The gradient of the longest rows
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("V", [(1 << 29) + 3, 1 << 30])
+def test_gradient_of_the_longest_rows(lz, V):
+    """Every word's gradient, to the rounding of bf16 and what log_sum may be off."""
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GiB")
+    x = torch.full((1, V), -4.0, dtype=BF16, device=DEV)
+    at = [V - 1, V // 2, 7, V - 2]
+    x[0, at] = torch.tensor([9.0, 8.5, 8.0, 7.5], dtype=BF16, device=DEV)
+    t = torch.tensor([V // 2], device=DEV)
+    r = lz.token_logprobs(x, t)
+    S = (V - 4) * np.exp(-13.0) + 1 + np.exp(-0.5) + np.exp(-1.0) + np.exp(-1.5)
+    # a thread sums V / 2^15 logits in batches of 32, parts are joined
+    off = (V // (1 << 15) // 32 + 200) * A.U
+    g = lz.token_logprobs_grad(x, t, r.peak, r.log_sum, torch.full((1,), 3.0, device=DEV), out=x)
+    q = np.exp(np.array([0.0, -0.5, -1.0, -1.5, -13.0])) / S
+    want = 3 * (np.array([0, 1.0, 0, 0, 0]) - q)
+    got = g[0, [*at, 0]].double().cpu().numpy()
+    # an exponent of up to 13 + log S is off by 16 of its half steps at most
+    tol = 1.01 * A.HALF[BF16] * np.abs(want) + 3 * q * (1.01 * off + 16 * (13 + np.log(S)) * A.U)
+    assert (np.abs(got - want) <= tol).all(), (got, want, tol)
+    assert int((g == g[0, 0]).sum()) == V - 4
