@@ -175,7 +175,7 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
         for (int e = 0; e < P; ++e)
           joined[threadIdx.x / (kGroups > 1 ? S::kThreads / kGroups : 1)][col + e] = x[e];
       } else if (a.sums && s.have == P) {
-        // whole vectors: 100 x 16,384 bf16 22.7 us, 33.4 a value at a time
+        // whole vectors: 100 x 16,384 bf16 15.9 us, 26.9 a value at a time
         float* out = a.sums + (static_cast<int64_t>(blockIdx.x) * 2 + k) * a.D + col;
 #pragma unroll
         for (int e = 0; e < P; e += 4)
@@ -198,8 +198,8 @@ __global__ __launch_bounds__(S::kThreads) void k_norm_grad(NormGradArgs a) {
   }
 }
 
-// dweight and dbias (+)= the workgroups' sums, kJoinCols columns of the two a workgroup:
-// kJoinRows threads share a column's parts, their sums are added in a fixed order.
+// dweight and dbias (+)= the workgroups' sums, COLS columns of the two a workgroup:
+// kJoinThreads / COLS threads share a column's parts, their sums are added in a fixed order.
 constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / kWave;
 
 template <int COLS>
@@ -248,15 +248,19 @@ static inline int grad_shape(int64_t D, F f) {
 }
 
 // Workgroups of the pass, at most kGradBlocks. Each leaves 2 D sums behind, so that fewer and
-// larger ones cost less where every one has but a turn or two: 1280 x 1792 fp32 takes 12.5 us
-// with 160 of 1024 threads, 14.4 with 320 of 512 (16,384 x 1000 fp32 44 and 41).
+// larger ones cost less where every one has but a turn or two: 1280 x 1792 fp32 takes 11.3 us
+// with 160 of 1024 threads, 13.4 with 320 of 512 (2048 x 2048 bf16 14.5 and 16.3). Where every
+// one has many turns the smaller ones do: 16,384 x 1000 fp32 40.3 us with them, 42.4 with 1024.
 constexpr int64_t kGradBlocks = 512;
 
-// Rows that up to kGradSmall workgroups of one wave a SIMD hold, a row a group, go to these, as
-// the instructions of the four waves of a larger one follow each other: 27 x 459 bf16 takes 6.4
-// us, 11.0 otherwise, 700 x 480 6.9 and 9.5, 22,882 x 35 9.7 and 12.5, 200 x 650 fp32 7.6 and
-// 12.8, 200 x 2048 8.6 and 10.3. More sums than kGradSums cost what that saves, or half as many
-// where several rows' are added first (900 x 1000 bf16: 11.5 and 9.7).
+// Rows that kGradSmall workgroups of one wave a SIMD would hold, a row a group, go to such small
+// ones, as the instructions of the four waves of a larger one follow each other: 700 x 480 bf16
+// takes 6.2 us, 7.0 otherwise, 16,384 x 35 8.5 and 10.7, 200 x 650 fp32 7.1 and 9.7, 200 x 2048
+// bf16 8.1 and 8.4. These too are kGradBlocks at most: twice as many rows have two turns, as each
+// workgroup's sums cost the join more than a turn takes (30,000 x 35 bf16: 10.0 us, with up to
+// kGradSmall workgroups 12.3, with larger ones 11.5; 22,882 x 35 9.3, 10.1 and 10.9). More sums
+// than kGradSums cost what small workgroups save, or half as many where several rows' are added
+// first (900 x 1000 bf16: 11.8 and 9.7).
 constexpr int64_t kGradSmall = 1024, kGradSums = int64_t(1) << 20;
 // Rows of one of the larger workgroups, at most eight times a small one's, always fit.
 static_assert(kGradSums / 2 / (2 * LM_NORM_MAX_WIDTH) >= 8 && kSmallThreads * 8 == 1024 * 2, "");
@@ -280,7 +284,7 @@ static int64_t grad_blocks(int64_t rows, int64_t D) {
   return norm_grad_shape<T>(rows, D, [&](auto shape) {
     using S = decltype(shape);
     const int64_t n = (rows + S::kRows - 1) / S::kRows;  // turns
-    // Of 16 waves a compute unit has but one: 2000 x 16,384 bf16 82 us, with 512 of them 109.
+    // Of 16 waves a compute unit has but one: 2000 x 16,384 bf16 66 us, with 512 of them 77.
     constexpr int64_t most = S::kGroup == 1024 ? kGradBlocks / 2 : kGradBlocks;
     return static_cast<int>(n < most ? n : most);
   });
@@ -326,9 +330,9 @@ int norm_grad_run(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, co
     if (rc != LM_OK) return rc;
   }
   if (!join) return LM_OK;
-  // Columns of a workgroup: few where there would be no workgroup for each compute unit (900 x
-  // 1000 bf16: 9.7 us with 16, 9.9 with 32), else whole cache lines (2048 x 2048 14.1 with 32,
-  // 15.6 with 16; 100 x 16,384 16.7 with 64, 18.0 with 32, 22.5 with 16).
+  // Columns of a workgroup: few where there would be no workgroup for each compute unit (200 x
+  // 650 fp32: 7.1 us with 16, 7.5 with 32; 900 x 1000 bf16 9.7 and 9.9), else whole cache lines
+  // (2048 x 2048 14.5 with 32, 16.1 with 16; 100 x 16,384 15.8 with 64, 16.8 with 32, 21.9 with 16).
   const int cols = static_cast<int>(2 * D), each = D <= 1024 ? 16 : D <= 4096 ? 32 : 64;
   auto kernel = each == 16 ? k_norm_join<16> : each == 32 ? k_norm_join<32> : k_norm_join<64>;
   kernel<<<(cols + each - 1) / each, kJoinThreads, 0, st>>>(
